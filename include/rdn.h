@@ -374,6 +374,179 @@ rdn_status_t rdn_fwd_workspace_size(const rdn_fwd_args *args, size_t *bytes);
 rdn_status_t rla_bwd_workspace_size(const rdn_bwd_args *args, size_t *bytes);
 rdn_status_t rdn_bwd_workspace_size(const rdn_bwd_args *args, size_t *bytes);
 
+/* ---- Operators around the recurrence ------------------------------------
+ * What a layer has next to its recurrence: the short causal convolution in
+ * front of it, a selective state space scan (per-channel, per-state decays,
+ * where the recurrences above have one decay per head), and the norms around
+ * the block with its gate and residual scale.  The conventions above hold,
+ * with these differences:
+ *  - Token rows may be strided: a field *_ld is the distance, in elements,
+ *    between consecutive token rows of that tensor (0 = contiguous; at least
+ *    the row's length; batch row b, token t is row b * T + t), so that an
+ *    operand can be a slice of a wider projection's rows.
+ *  - Data pointers with row lengths and strides of whole 16-byte groups take
+ *    16-byte accesses; others must be aligned to their element and take
+ *    single-element accesses.  Parameters and states in fp32 need 4 bytes.
+ *  - cu_seqlens / num_seqs as in rdn_fwd_args (B = 1; empty sequences pass
+ *    their states through).
+ *  - Sums over tokens (parameter gradients) and over channels (dB, dC) are
+ *    made of partial sums in the workspace, joined in a fixed order: the same
+ *    call gives the same bits. */
+
+/* Short causal convolution, depthwise (one filter of W taps per channel):
+ *     p_t = bias + sum_{j<W} w[:,j] x_{t-W+1+j},   y_t = p_t or SiLU(p_t)
+ * where x before a sequence's start comes from state0 (its last W-1 inputs,
+ * oldest first) or is zero.
+ *   B, T, C, W        B >= 1, T >= 0, C >= 1, W in {2, 3, 4}.
+ *   dtype             of x, y, states and their gradients.
+ *   silu              1: y = SiLU(p); 0: y = p.
+ *   x, y              [B,T,C] with row strides x_ld, y_ld.
+ *   w [C,W], bias [C] fp32; bias may be NULL (= 0).
+ *   state0, stateT    [num_seqs or B, W-1, C] or NULL: inputs before the
+ *                     start, and the last W-1 inputs (output).
+ * Backward (rdn_conv_bwd; recomputes p): dy [B,T,C], dstateT like stateT or
+ * NULL -> dx [B,T,C], dw [C,W] and dbias [C] fp32 (dbias may be NULL),
+ * dstate0 like state0 or NULL. */
+typedef struct {
+  int B, T, C, W;
+  int dtype, silu;
+  long long x_ld, y_ld, dy_ld, dx_ld;
+  const void *x;
+  const float *w, *bias;
+  const void *state0;
+  void *y, *stateT;
+  const int *cu_seqlens;
+  int num_seqs;
+  const void *dy, *dstateT;
+  void *dx;
+  float *dw, *dbias;
+  void *dstate0;
+  void *workspace;
+  size_t workspace_bytes;
+} rdn_conv_args;
+rdn_status_t rdn_conv_fwd(const rdn_conv_args *args, rdn_stream_t stream);
+rdn_status_t rdn_conv_bwd(const rdn_conv_args *args, rdn_stream_t stream);
+rdn_status_t rdn_conv_bwd_workspace_size(const rdn_conv_args *args, size_t *bytes);
+
+/* One token for N requests: x, y [N,C]; state [num_slots, W-1, C] updated in
+ * place.  slots [N] int32 (device): the state of each row, distinct; a row
+ * whose slot lies outside [0, num_slots) is idle (y = 0, no state touched).
+ * NULL: row n uses state n (num_slots >= N). */
+typedef struct {
+  int N, C, W;
+  int dtype, silu;
+  int num_slots;
+  long long x_ld, y_ld;
+  const void *x;
+  const float *w, *bias;
+  void *state;
+  const int *slots;
+  void *y;
+} rdn_conv_step_args;
+rdn_status_t rdn_conv_step(const rdn_conv_step_args *args, rdn_stream_t stream);
+
+/* Selective state space scan: D channels with S states each, group g of the
+ * G groups of D / G channels sharing its rows of B and C:
+ *     dl_t = softplus(dt_t + dt_bias)          (dt_softplus = 0: dt_t + dt_bias)
+ *     h_t[d,n] = exp(dl_t[d] A[d,n]) h_{t-1}[d,n] + dl_t[d] x_t[d] B_t[g(d),n]
+ *     y_t[d] = sum_n C_t[g(d),n] h_t[d,n] + Dskip[d] x_t[d]
+ *     out_t = y_t  or, with z,  y_t SiLU(z_t)
+ *   B, T              as above;  D >= 1;  1 <= S <= 64;  G divides D.
+ *   dtype             of x, dt, z, out, Bm, Cm, dout and their gradients.
+ *   x, dt, z, out     [B,T,D] with row strides; z may be NULL (no gate).
+ *   Bm, Cm            [B,T,G,S] with row strides (G * S contiguous).
+ *   A [D,S], Dskip [D], dt_bias [D]  fp32; Dskip and dt_bias may be NULL.
+ *   h0, hT            [num_seqs or B, D, S] fp32 or NULL.
+ *   h_chunks          NULL, or [rdn_scan_chunk_slots][D][S] fp32: the states
+ *                     at the start of every 16 tokens of each sequence, in
+ *                     the order of the sequences (written by the forward, read
+ *                     by the backward, which computes them itself if NULL).
+ * Backward: dout [B,T,D], dhT like hT or NULL -> dx, ddt, dz [B,T,D], dB, dC
+ * [B,T,G,S] contiguous, dA [D,S], dD [D], ddt_bias [D] fp32, dh0 like h0.
+ * dz is required with z; dD, ddt_bias and dh0 may be NULL. */
+#define RDN_SCAN_CHUNK 16
+typedef struct {
+  int B, T, D, S, G;
+  int dtype, dt_softplus;
+  long long x_ld, dt_ld, z_ld, b_ld, c_ld, out_ld;
+  const void *x, *dt, *z, *Bm, *Cm;
+  const float *A, *Dskip, *dt_bias, *h0;
+  void *out;
+  float *hT, *h_chunks;
+  const int *cu_seqlens;
+  int num_seqs;
+  long long dout_ld, dx_ld, ddt_ld, dz_ld;
+  const void *dout;
+  const float *dhT;
+  void *dx, *ddt, *dz, *dB, *dC;
+  float *dA, *dD, *ddt_bias, *dh0;
+  void *workspace;
+  size_t workspace_bytes;
+} rdn_scan_args;
+rdn_status_t rdn_scan_fwd(const rdn_scan_args *args, rdn_stream_t stream);
+rdn_status_t rdn_scan_bwd(const rdn_scan_args *args, rdn_stream_t stream);
+rdn_status_t rdn_scan_fwd_workspace_size(const rdn_scan_args *args, size_t *bytes);
+rdn_status_t rdn_scan_bwd_workspace_size(const rdn_scan_args *args, size_t *bytes);
+/* D x S blocks of h_chunks: B * ceil(T/16), or the bound num_seqs +
+ * ceil(T/16) with cu_seqlens. */
+rdn_status_t rdn_scan_chunk_slots(const rdn_scan_args *args, long long *slots);
+
+/* One token of the scan for N requests: x, dt, z, out [N,D]; Bm, Cm [N,G,S];
+ * h [num_slots,D,S] fp32 updated in place; slots as in rdn_conv_step_args. */
+typedef struct {
+  int N, D, S, G;
+  int dtype, dt_softplus;
+  int num_slots;
+  long long x_ld, dt_ld, z_ld, b_ld, c_ld, out_ld;
+  const void *x, *dt, *z, *Bm, *Cm;
+  const float *A, *Dskip, *dt_bias;
+  float *h;
+  const int *slots;
+  void *out;
+} rdn_scan_step_args;
+rdn_status_t rdn_scan_step(const rdn_scan_step_args *args, rdn_stream_t stream);
+
+/* The norms after and before a block, with the block's gate and its scaled
+ * residual, per row of D elements (RMS norms: no mean is taken out):
+ *     u = f / rms(f) * w * act(z),   rms(t) = sqrt(mean(t^2) + eps)
+ *     r = x + scale * u,             h = r / rms(r) * w_next
+ * Parts may be left out:
+ *   f = NULL          r = x (only the norm before a block): needs x and
+ *                     w_next; w, z, scale, r_out unused.
+ *   z = NULL          no gate.
+ *   x = NULL          no residual: r_out = u, scale unused.
+ *   w_next = NULL     no h.
+ *   rows, D           rows >= 1, 2 <= D <= 16384 (of a row of one element the
+ *                     norm keeps the sign alone, and the gradient is a
+ *                     difference of nearly equal numbers: refused).
+ *   heads             rows of w: row i takes w[i % heads] (rows % heads == 0;
+ *                     heads > 1 only without x and w_next).
+ *   dtype             of f, z, h and their gradients.
+ *   x_dtype           of x, r_out and their gradients (u: dtype).
+ *   gate              0: act = SiLU, 1: act = sigmoid.
+ *   scale [D] fp32 or NULL with scale_const; w [heads,D], w_next [D] fp32.
+ * Backward: dr (gradient of r_out, or NULL = 0), dh (of h, with w_next) -> dx,
+ * df, dz, dw [heads,D], dw_next [D], dscale [D] fp32 (each required if its
+ * operand is given; dscale only with scale). */
+typedef struct {
+  long long rows;
+  int D, heads;
+  int dtype, x_dtype, gate;
+  float eps, scale_const;
+  long long f_ld, z_ld, x_ld;
+  const void *f, *z, *x;
+  const float *w, *scale, *w_next;
+  void *r_out, *h;
+  const void *dr, *dh;
+  void *df, *dz, *dx;
+  float *dw, *dscale, *dw_next;
+  void *workspace;
+  size_t workspace_bytes;
+} rdn_norm_args;
+rdn_status_t rdn_norm_fwd(const rdn_norm_args *args, rdn_stream_t stream);
+rdn_status_t rdn_norm_bwd(const rdn_norm_args *args, rdn_stream_t stream);
+rdn_status_t rdn_norm_bwd_workspace_size(const rdn_norm_args *args, size_t *bytes);
+
 /* Message describing the last non-OK status returned on this thread
  * ("" if none).  The pointer stays valid until the next call on the
  * thread. */

@@ -30,8 +30,13 @@ from ._abi import (RDN_FLAG_DECAYED_RESIDUAL as DECAYED_RESIDUAL,  # noqa: F401
                    RDN_FLAG_STATELESS_AUX as STATELESS_AUX,
                    RDN_FLAG_TANH_RESIDUAL as TANH_RESIDUAL)
 
+from .layer_ops import (block_norm_bwd, block_norm_fwd, causal_conv_bwd, causal_conv_fwd,
+                        causal_conv_step, selective_scan_bwd, selective_scan_fwd,
+                        selective_scan_step)
+
 __all__ = ["rla_fwd", "rdn_fwd", "rla_bwd", "rdn_bwd", "qk_prologue", "qk_prologue_bwd", "rdn_decode_step", "RdnError", "library",
-           "CHUNK"]
+           "CHUNK", "causal_conv_fwd", "causal_conv_bwd", "causal_conv_step", "selective_scan_fwd",
+           "selective_scan_bwd", "selective_scan_step", "block_norm_fwd", "block_norm_bwd"]
 
 CHUNK = 64
 

@@ -29,7 +29,13 @@ STATUS = {0: "RDN_OK", 1: "RDN_ERR_INVALID_ARG", 2: "RDN_ERR_UNSUPPORTED", 3: "R
 EXPORTS = ["rla_fwd", "rdn_fwd", "rla_bwd", "rdn_bwd", "rdn_decode_step", "rla_fwd_workspace_size",
            "rdn_fwd_workspace_size", "rla_bwd_workspace_size", "rdn_bwd_workspace_size",
            "rdn_last_error", "rdn_version", "rdn_prof_start", "rdn_prof_stop", "rdn_fwd_noalloc",
-           "rdn_qk_prologue", "rdn_qk_prologue_bwd", "rdn_chunk_slots", "rdn_device_status"]
+           "rdn_qk_prologue", "rdn_qk_prologue_bwd", "rdn_chunk_slots", "rdn_device_status",
+           "rdn_conv_fwd", "rdn_conv_bwd", "rdn_conv_bwd_workspace_size", "rdn_conv_step",
+           "rdn_scan_fwd", "rdn_scan_bwd", "rdn_scan_fwd_workspace_size",
+           "rdn_scan_bwd_workspace_size", "rdn_scan_chunk_slots", "rdn_scan_step", "rdn_norm_fwd",
+           "rdn_norm_bwd", "rdn_norm_bwd_workspace_size"]
+
+SCAN_CHUNK = 16  # RDN_SCAN_CHUNK
 
 
 class ProfRecord(ctypes.Structure):
@@ -74,8 +80,54 @@ class PrologueArgs(ctypes.Structure):
                 ("dx", P * 2)]
 
 
+# ctypes type of each field-type letter of the structs below, and the letter of
+# struct.pack: i int, q long long, f float, n size_t, P pointer (0 = NULL)
+_CT = {"i": ctypes.c_int, "q": ctypes.c_longlong, "f": ctypes.c_float, "n": ctypes.c_size_t, "P": P}
+
+
+def _layout(name, fields):
+    """A ctypes struct and the packer of its bytes (values in field order) from
+    "type name name ...; type ..." -- one packing call costs a few hundred
+    nanoseconds where setting thirty fields one by one costs microseconds."""
+    decl = [(f, t) for part in fields.split(";") for t, *names in [part.split()] for f in names]
+    cls = type(name, (ctypes.Structure,), {"_fields_": [(f, _CT[t]) for f, t in decl]})
+    # tail padding to 8 bytes, as the C compiler lays the struct out
+    lay = struct.Struct("@" + "".join(t if t != "n" else "N" for _, t in decl) + "0q")
+    assert lay.size == ctypes.sizeof(cls), name
+    return cls, lay.pack
+
+
+ConvArgs, CONV_PACK = _layout(
+    "ConvArgs", "i B T C W dtype silu; q x_ld y_ld dy_ld dx_ld; P x w bias state0 y stateT"
+    " cu_seqlens; i num_seqs; P dy dstateT dx dw dbias dstate0 workspace; n workspace_bytes")
+ConvStepArgs, CONV_STEP_PACK = _layout(
+    "ConvStepArgs", "i N C W dtype silu num_slots; q x_ld y_ld; P x w bias state slots y")
+ScanArgs, SCAN_PACK = _layout(
+    "ScanArgs", "i B T D S G dtype dt_softplus; q x_ld dt_ld z_ld b_ld c_ld out_ld; P x dt z Bm Cm"
+    " A Dskip dt_bias h0 out hT h_chunks cu_seqlens; i num_seqs; q dout_ld dx_ld ddt_ld dz_ld;"
+    " P dout dhT dx ddt dz dB dC dA dD ddt_bias dh0 workspace; n workspace_bytes")
+ScanStepArgs, SCAN_STEP_PACK = _layout(
+    "ScanStepArgs", "i N D S G dtype dt_softplus num_slots; q x_ld dt_ld z_ld b_ld c_ld out_ld;"
+    " P x dt z Bm Cm A Dskip dt_bias h slots out")
+NormArgs, NORM_PACK = _layout(
+    "NormArgs", "q rows; i D heads dtype x_dtype gate; f eps scale_const; q f_ld z_ld x_ld;"
+    " P f z x w scale w_next r_out h dr dh df dz dx dw dscale dw_next workspace; n workspace_bytes")
+
 _lib = None
 _decode_step = None
+_packed = {}
+
+
+def packed(name):
+    """The entry point `name` taking its argument struct as packed bytes, and a
+    stream or, for the size queries, a pointer to the answer."""
+    fn = _packed.get(name)
+    if fn is None:
+        fn = load()[name]  # (a function object of its own)
+        fn.argtypes = [ctypes.c_char_p, ctypes.c_void_p]
+        fn.restype = ctypes.c_int
+        _packed[name] = fn
+    return fn
 
 
 def decode_step():
@@ -117,6 +169,19 @@ def load(build_if_missing: bool = True):
                        ("rdn_fwd_workspace_size", [ctypes.POINTER(FwdArgs), ctypes.POINTER(ctypes.c_size_t)]),
                        ("rla_bwd_workspace_size", [ctypes.POINTER(BwdArgs), ctypes.POINTER(ctypes.c_size_t)]),
                        ("rdn_bwd_workspace_size", [ctypes.POINTER(BwdArgs), ctypes.POINTER(ctypes.c_size_t)]),
+                       ("rdn_conv_fwd", [ctypes.POINTER(ConvArgs), P]),
+                       ("rdn_conv_bwd", [ctypes.POINTER(ConvArgs), P]),
+                       ("rdn_conv_bwd_workspace_size", [ctypes.POINTER(ConvArgs), ctypes.POINTER(ctypes.c_size_t)]),
+                       ("rdn_conv_step", [ctypes.POINTER(ConvStepArgs), P]),
+                       ("rdn_scan_fwd", [ctypes.POINTER(ScanArgs), P]),
+                       ("rdn_scan_bwd", [ctypes.POINTER(ScanArgs), P]),
+                       ("rdn_scan_fwd_workspace_size", [ctypes.POINTER(ScanArgs), ctypes.POINTER(ctypes.c_size_t)]),
+                       ("rdn_scan_bwd_workspace_size", [ctypes.POINTER(ScanArgs), ctypes.POINTER(ctypes.c_size_t)]),
+                       ("rdn_scan_chunk_slots", [ctypes.POINTER(ScanArgs), ctypes.POINTER(ctypes.c_longlong)]),
+                       ("rdn_scan_step", [ctypes.POINTER(ScanStepArgs), P]),
+                       ("rdn_norm_fwd", [ctypes.POINTER(NormArgs), P]),
+                       ("rdn_norm_bwd", [ctypes.POINTER(NormArgs), P]),
+                       ("rdn_norm_bwd_workspace_size", [ctypes.POINTER(NormArgs), ctypes.POINTER(ctypes.c_size_t)]),
                        ("rdn_chunk_slots", [ctypes.POINTER(FwdArgs), ctypes.POINTER(ctypes.c_longlong)])]:
         fn = getattr(lib, name)
         fn.argtypes = argt

@@ -10,9 +10,8 @@
 #include <mutex>
 #include <vector>
 
-#include <nvtx3/nvToolsExt.h>
-
 #include "common.cuh"
+#include "entry.cuh"
 #include "status.cuh"
 
 namespace rdn {
@@ -168,12 +167,7 @@ rdn_status_t cuda_status(const char *fn, cudaError_t e) {
   return fail(RDN_ERR_CUDA, "%s: CUDA error %d (%s)", fn, (int)e, cudaGetErrorString(e));
 }
 
-// An NVTX range named after the entry point for the duration of the call
-// (host side: validation and enqueueing), seen by profilers and free without one.
-struct CallRange {
-  explicit CallRange(const char *fn) { nvtxRangePushA(fn); }
-  ~CallRange() { nvtxRangePop(); }
-};
+using rdn::CallRange;
 
 rdn_status_t fwd_common(const char *fn, const rdn_fwd_args *a0, int variant, cudaStream_t s) {
   CallRange range(fn);
@@ -195,6 +189,19 @@ rdn_status_t fwd_common(const char *fn, const rdn_fwd_args *a0, int variant, cud
 }
 
 }  // namespace
+
+namespace rdn {
+rdn_status_t entry_fail(rdn_status_t st, const char *fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_err, sizeof g_err, fmt, ap);
+  va_end(ap);
+  return st;
+}
+rdn_status_t entry_ok() { return ok(); }
+rdn_status_t entry_injected(const char *fn) { return injected(fn); }
+rdn_status_t entry_cuda(const char *fn, cudaError_t e) { return cuda_status(fn, e); }
+}  // namespace rdn
 
 extern "C" {
 

@@ -1,0 +1,473 @@
+// conv.cu -- the short causal convolution in front of a recurrence: depthwise,
+// W = 2..4 taps per channel, optional SiLU,
+//     p_t = bias + sum_{k<W} w[W-1-k] x_{t-k},        y_t = act(p_t)
+// and its backward
+//     dp_t = dy_t act'(p_t),   dx_t = sum_k w[W-1-k] dp_{t+k},
+//     dw[W-1-k] = sum_t dp_t x_{t-k},   dbias = sum_t dp_t
+// (p recomputed from x), and its step of one token.
+//
+// Memory-bound: x in and y out, or x and dy in and dx out.  A thread owns a few
+// consecutive channels (one vector access) over a run of tokens and slides the
+// W-1 older inputs -- in the backward, which walks down, the W-1 later dp --
+// through registers, so x is read once but for the W-1 rows above a run.  The
+// loads of a group of tokens are issued together.  A sequence's start within a
+// run (packed sequences) is a rare branch that takes the taps from state0.
+#include <initializer_list>
+#include <utility>
+
+#include "rows.cuh"
+
+namespace rdn {
+namespace {
+
+constexpr int kConvThreads = 128;
+constexpr int kFwdGroup = 8;  // tokens whose loads a thread issues together
+constexpr int kBwdGroup = 4;
+
+struct ConvP {
+  int B, T, C, ns, run;  // run: tokens per thread
+  int runs;              // runs per batch row
+  int silu;
+  long long x_ld, y_ld, dy_ld, dx_ld;
+  const void *x, *state0, *dy, *dstateT;
+  void *y, *stateT, *dx, *dstate0;
+  const float *w, *bias;
+  const int *cu;
+  float *part;  // backward: [row groups of the grid][C][W + 1]
+};
+
+// the taps w[W-1-k] of V channels (tap[k]) and their biases
+template <int W, int V>
+__device__ __forceinline__ void load_taps(const ConvP &p, int c0, float (&tap)[W][V], float (&bias)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+#pragma unroll
+    for (int k = 0; k < W; ++k) tap[k][e] = __ldg(p.w + (size_t)(c0 + e) * W + W - 1 - k);
+    bias[e] = p.bias ? __ldg(p.bias + c0 + e) : 0.f;
+  }
+}
+
+// Sequences without tokens pass their state (or its gradient) through.
+template <typename T, int W, int V>
+__device__ __forceinline__ void pass_empty(const ConvP &p, long long unit, long long units, int c0,
+                                           const void *from, void *to) {
+  using K = Pack<T, V>;
+  if (!to || (!p.cu && p.T > 0)) return;
+  for (long long s = unit; s < p.ns; s += units) {
+    if (p.cu && cu_at(p.cu, p.ns, p.T, (int)s) < cu_at(p.cu, p.ns, p.T, (int)s + 1)) continue;
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) {
+      const size_t at = ((size_t)s * (W - 1) + i) * p.C + c0;
+      K::st((T *)to + at, from ? K::ld((const T *)from + at) : K::zero());
+    }
+  }
+}
+
+// x before a sequence's start: row i of its state0, or zero
+template <typename T, int W, int V>
+__device__ __forceinline__ void from_state(const ConvP &p, int s, int i, int c0, float (&v)[V]) {
+  using K = Pack<T, V>;
+  K::get(p.state0 ? K::ld((const T *)p.state0 + ((size_t)s * (W - 1) + i) * p.C + c0) : K::zero(), v);
+}
+
+template <typename T, int W, int V>
+__global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(ConvP p) {
+  using K = Pack<T, V>;
+  const int c0 = (blockIdx.y * blockDim.x + threadIdx.x) * V;
+  const long long unit = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+  const long long units = (long long)p.B * p.runs;
+  if (c0 >= p.C || unit >= units) return;
+  pass_empty<T, W, V>(p, unit, units, c0, p.state0, p.stateT);
+  const int b = (int)(unit / p.runs), t0 = (int)(unit % p.runs) * p.run;
+  if (t0 >= p.T) return;
+  const long long r0 = (long long)b * p.T + t0;
+  const long long r1 = r0 + min(p.run, p.T - t0);
+  float tap[W][V], bias[V];
+  load_taps<W, V>(p, c0, tap, bias);
+  const T *X = (const T *)p.x + c0;
+  T *Y = (T *)p.y + c0;
+  SeqSpan q = find_seq(p.cu, p.ns, p.T, b, t0);
+  float win[W - 1][V];  // win[k] = x_{t-1-k}
+#pragma unroll
+  for (int k = 0; k < W - 1; ++k) {
+    const long long r = r0 - 1 - k;
+    if (r >= q.begin) K::get(K::ld(X + r * p.x_ld), win[k]);
+    else from_state<T, W, V>(p, q.s, (int)(W - 1 + r - q.begin), c0, win[k]);
+  }
+  for (long long g = r0; g < r1; g += kFwdGroup) {
+    typename K::Raw raw[kFwdGroup];
+#pragma unroll
+    for (int u = 0; u < kFwdGroup; ++u) raw[u] = g + u < r1 ? K::ld(X + (g + u) * p.x_ld) : K::zero();
+#pragma unroll
+    for (int u = 0; u < kFwdGroup; ++u) {
+      const long long r = g + u;
+      if (r >= r1) break;
+      if (r >= q.end) {  // the next sequence that has tokens (packed rows only)
+        while (q.s < p.ns - 1 && r >= q.end) {
+          ++q.s;
+          q.begin = q.end;
+          q.end = cu_at(p.cu, p.ns, p.T, q.s + 1);
+        }
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k) from_state<T, W, V>(p, q.s, W - 2 - k, c0, win[k]);
+      }
+      float x[V], y[V];
+      K::get(raw[u], x);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float a = fmaf(tap[0][e], x[e], bias[e]);
+#pragma unroll
+        for (int k = 1; k < W; ++k) a = fmaf(tap[k][e], win[k - 1][e], a);
+        y[e] = p.silu ? siluf(a) : a;
+#pragma unroll
+        for (int k = W - 2; k > 0; --k) win[k][e] = win[k - 1][e];
+        win[0][e] = x[e];
+      }
+      K::st(Y + r * p.y_ld, K::put(y));
+      if (r == q.end - 1 && p.stateT) {
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k)
+          K::st((T *)p.stateT + ((size_t)q.s * (W - 1) + W - 2 - k) * p.C + c0, K::put(win[k]));
+      }
+    }
+  }
+}
+
+template <typename T, int W, int V>
+__global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
+  using K = Pack<T, V>;
+  constexpr int U = kBwdGroup;
+  extern __shared__ float sh[];  // [blockDim.y][blockDim.x][V][W + 1]
+  const int c0 = (blockIdx.y * blockDim.x + threadIdx.x) * V;
+  const long long unit = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+  const long long units = (long long)p.B * p.runs;
+  const bool live = c0 < p.C && unit < units;
+  float dw[W + 1][V];  // dw[k] of tap[k]; dw[W]: the bias
+#pragma unroll
+  for (int k = 0; k <= W; ++k)
+#pragma unroll
+    for (int e = 0; e < V; ++e) dw[k][e] = 0.f;
+  if (live) pass_empty<T, W, V>(p, unit, units, c0, p.dstateT, p.dstate0);
+  const int b = live ? (int)(unit / p.runs) : 0, t0 = live ? (int)(unit % p.runs) * p.run : p.T;
+  if (live && t0 < p.T) {
+    const long long rb0 = (long long)b * p.T, rb1 = rb0 + p.T;
+    const long long r0 = rb0 + t0, r1 = r0 + min(p.run, p.T - t0);
+    const long long top = min(r1 + W - 2, rb1 - 1);  // dx of the last row takes dp of the W-1 rows after it
+    float tap[W][V], bias[V];
+    load_taps<W, V>(p, c0, tap, bias);
+    const T *X = (const T *)p.x + c0, *DY = (const T *)p.dy + c0;
+    T *DX = (T *)p.dx + c0;
+    SeqSpan q = find_seq(p.cu, p.ns, p.T, b, (int)(top - rb0));
+    float dpw[W - 1][V];  // dpw[k] = dp_{t+1+k} of the same sequence
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k)
+#pragma unroll
+      for (int e = 0; e < V; ++e) dpw[k][e] = 0.f;
+    // groups [g, g + U) from the top down; xr[i] = x row g - (W-1) + i
+    typename K::Raw xr[U + W - 1];
+    long long g = r0 + (top - r0) / U * U;
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) {
+      const long long r = g + U - (W - 1) + i;
+      xr[i] = r >= rb0 && r <= top ? K::ld(X + r * p.x_ld) : K::zero();
+    }
+    for (; g >= r0; g -= U) {
+      typename K::Raw dyr[U];
+#pragma unroll
+      for (int i = W - 2; i >= 0; --i) xr[U + i] = xr[i];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const long long r = g - (W - 1) + i;
+        xr[i] = r >= rb0 && r <= top ? K::ld(X + r * p.x_ld) : K::zero();
+        dyr[i] = g + i <= top ? K::ld(DY + (g + i) * p.dy_ld) : K::zero();
+      }
+#pragma unroll
+      for (int u = U - 1; u >= 0; --u) {
+        const long long r = g + u;
+        if (r > top) continue;
+        if (r < q.begin) {  // the sequence before, past empty ones
+          while (q.s > 0 && r < q.begin) {
+            --q.s;
+            q.end = q.begin;
+            q.begin = cu_at(p.cu, p.ns, p.T, q.s);
+          }
+#pragma unroll
+          for (int k = 0; k < W - 1; ++k)
+#pragma unroll
+            for (int e = 0; e < V; ++e) dpw[k][e] = 0.f;
+        }
+        float x[W][V], dp[V];
+#pragma unroll
+        for (int k = 0; k < W; ++k) K::get(xr[u + W - 1 - k], x[k]);
+        if (r - (W - 1) < q.begin) {
+#pragma unroll
+          for (int k = 1; k < W; ++k)
+            if (r - k < q.begin) from_state<T, W, V>(p, q.s, (int)(W - 1 + r - k - q.begin), c0, x[k]);
+        }
+        K::get(dyr[u], dp);
+        if (p.silu) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            float a = bias[e];
+#pragma unroll
+            for (int k = 0; k < W; ++k) a = fmaf(tap[k][e], x[k][e], a);
+            dp[e] *= silu_grad(a, sigmoidf(a));
+          }
+        }
+        if (r < r1) {
+          float dx[V];
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            float a = tap[0][e] * dp[e];
+#pragma unroll
+            for (int k = 1; k < W; ++k) a = fmaf(tap[k][e], dpw[k - 1][e], a);
+            dx[e] = a;
+#pragma unroll
+            for (int k = 0; k < W; ++k) dw[k][e] = fmaf(dp[e], x[k][e], dw[k][e]);
+            dw[W][e] += dp[e];
+          }
+          if (p.dstateT && q.end - r <= W - 1) {
+            float d[V];
+            K::get(K::ld((const T *)p.dstateT + ((size_t)q.s * (W - 1) + W - 1 - (q.end - r)) * p.C + c0), d);
+#pragma unroll
+            for (int e = 0; e < V; ++e) dx[e] += d[e];
+          }
+          K::st(DX + r * p.dx_ld, K::put(dx));
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+#pragma unroll
+          for (int k = W - 2; k > 0; --k) dpw[k][e] = dpw[k - 1][e];
+          dpw[0][e] = dp[e];
+        }
+        if (r == q.begin && r < r1 && p.dstate0) {
+          const long long len = q.end - q.begin;
+#pragma unroll
+          for (int v = 1; v < W; ++v) {  // the input v rows before the start: state row W-1-v
+            float d[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              d[e] = 0.f;
+#pragma unroll
+              for (int k = v; k < W; ++k) d[e] = fmaf(tap[k][e], dpw[k - v][e], d[e]);
+            }
+            const int i = W - 1 - v;
+            if (p.dstateT && i >= len) {  // a sequence shorter than the state hands part of it on
+              float t[V];
+              K::get(K::ld((const T *)p.dstateT + ((size_t)q.s * (W - 1) + i - len) * p.C + c0), t);
+#pragma unroll
+              for (int e = 0; e < V; ++e) d[e] += t[e];
+            }
+            K::st((T *)p.dstate0 + ((size_t)q.s * (W - 1) + i) * p.C + c0, K::put(d));
+          }
+        }
+      }
+    }
+  }
+  // the CTA's sums over its runs, in order
+  const int row = blockDim.x * V * (W + 1);
+  float *mine = sh + threadIdx.y * row + threadIdx.x * V * (W + 1);
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+#pragma unroll
+    for (int k = 0; k < W; ++k) mine[e * (W + 1) + W - 1 - k] = dw[k][e];
+    mine[e * (W + 1) + W] = dw[W][e];
+  }
+  __syncthreads();
+  const int cbase = blockIdx.y * blockDim.x * V;
+  const int tid = threadIdx.y * blockDim.x + threadIdx.x;
+  for (int i = tid; i < row; i += blockDim.x * blockDim.y) {
+    if (cbase + i / (W + 1) >= p.C) continue;
+    float a = 0.f;
+    for (int y = 0; y < (int)blockDim.y; ++y) a += sh[y * row + i];
+    p.part[((size_t)blockIdx.x * p.C + cbase) * (W + 1) + i] = a;
+  }
+}
+
+// dw [C][W] and dbias [C] from the partials [parts][C][W + 1], in order
+template <int W>
+__global__ void __launch_bounds__(512) conv_grad_kernel(const float *__restrict__ part, int C, int parts,
+                                                        float *__restrict__ dw, float *__restrict__ dbias) {
+  __shared__ float sh[16][32];
+  const long long n = (long long)C * (W + 1), i = (long long)blockIdx.x * 32 + threadIdx.x;
+  float a = 0.f;
+  if (i < n)
+    for (int q = threadIdx.y; q < parts; q += 16) a += part[(size_t)q * n + i];
+  sh[threadIdx.y][threadIdx.x] = a;
+  __syncthreads();
+  if (threadIdx.y || i >= n) return;
+#pragma unroll
+  for (int y = 1; y < 16; ++y) a += sh[y][threadIdx.x];
+  const int c = (int)(i / (W + 1)), k = (int)(i % (W + 1));
+  if (k < W) dw[(size_t)c * W + k] = a;
+  else if (dbias) dbias[c] = a;
+}
+
+struct ConvStepP {
+  int N, C, num_slots, silu;
+  long long x_ld, y_ld;
+  const void *x;
+  const float *w, *bias;
+  void *state, *y;
+  const int *slots;
+};
+
+template <typename T, int W, int V>
+__global__ void __launch_bounds__(kConvThreads) conv_step_kernel(ConvStepP p) {
+  using K = Pack<T, V>;
+  const int c0 = (blockIdx.y * blockDim.x + threadIdx.x) * V;
+  const int n = blockIdx.x * blockDim.y + threadIdx.y;
+  if (c0 >= p.C || n >= p.N) return;
+  const int slot = p.slots ? __ldg(p.slots + n) : n;
+  T *Y = (T *)p.y + (size_t)n * p.y_ld + c0;
+  if (slot < 0 || slot >= p.num_slots) {
+    K::st(Y, K::zero());
+    return;
+  }
+  T *S = (T *)p.state + (size_t)slot * (W - 1) * p.C + c0;
+  typename K::Raw raw[W];  // x_{t-W+1} .. x_t
+#pragma unroll
+  for (int i = 0; i < W - 1; ++i) raw[i] = K::ld(S + (size_t)i * p.C);
+  raw[W - 1] = K::ld((const T *)p.x + (size_t)n * p.x_ld + c0);
+  float y[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) y[e] = p.bias ? __ldg(p.bias + c0 + e) : 0.f;
+#pragma unroll
+  for (int j = 0; j < W; ++j) {
+    float x[V];
+    K::get(raw[j], x);
+#pragma unroll
+    for (int e = 0; e < V; ++e) y[e] = fmaf(__ldg(p.w + (size_t)(c0 + e) * W + j), x[e], y[e]);
+  }
+#pragma unroll
+  for (int i = 0; i < W - 1; ++i) K::st(S + (size_t)i * p.C, raw[i + 1]);
+  if (p.silu) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) y[e] = siluf(y[e]);
+  }
+  K::st(Y, K::put(y));
+}
+
+// Whether every row of the tensors that are given starts on a multiple of
+// `bytes` (pointers and strides in elements of `size` bytes).
+bool rows_on(size_t bytes, size_t size, std::initializer_list<std::pair<const void *, long long>> rows) {
+  for (const auto &r : rows)
+    if (r.first && (((uintptr_t)r.first | ((size_t)r.second * size)) & (bytes - 1))) return false;
+  return true;
+}
+
+struct ConvPlan {
+  int run, runs;      // tokens per thread, runs per batch row
+  unsigned bx, by;    // CTA: channel vectors, runs
+  unsigned gx, gy;    // grid: CTAs over the runs, over the channels
+};
+// Threads want long runs (the backward repeats W-1 rows of x and dy per run),
+// the GPU wants about 1,500 threads per SM: the longest run in [group, most]
+// that still gives them.
+ConvPlan conv_plan(const rdn_conv_args &a, int V, int group, int most) {
+  ConvPlan pl;
+  const long long nvec = (a.C + V - 1) / V, tokens = (long long)a.B * a.T;
+  long long run = tokens * nvec / (152ll * 1536) / group * group;
+  pl.run = (int)(run < group ? group : run > most ? most : run);
+  pl.runs = a.T > 0 ? (a.T + pl.run - 1) / pl.run : 1;
+  pl.bx = 32;
+  while (pl.bx > 1 && pl.bx / 2 >= nvec) pl.bx /= 2;
+  pl.by = kConvThreads / pl.bx;
+  pl.gx = (unsigned)(((long long)a.B * pl.runs + pl.by - 1) / pl.by);
+  pl.gy = (unsigned)((nvec + pl.bx - 1) / pl.bx);
+  return pl;
+}
+constexpr int kFwdMost = 16, kBwdMost = 64;
+
+// Channels per thread: 4 in the sequence kernels, whose registers hold up to
+// 4 W + 1 values per channel; single ones where a row is not on their bytes.
+bool conv_vec(const rdn_conv_args &a, bool bwd) {
+  const size_t size = a.dtype == RDN_BF16 ? 2 : 4, bytes = 4 * size;
+  if (a.C % 4) return false;
+  return bwd ? rows_on(bytes, size, {{a.x, a.x_ld}, {a.dy, a.dy_ld}, {a.dx, a.dx_ld}, {a.state0, 0},
+                                     {a.dstateT, 0}, {a.dstate0, 0}})
+             : rows_on(bytes, size, {{a.x, a.x_ld}, {a.y, a.y_ld}, {a.state0, 0}, {a.stateT, 0}});
+}
+
+ConvP conv_params(const rdn_conv_args &a, const ConvPlan &pl) {
+  ConvP p{};
+  p.B = a.B; p.T = a.T; p.C = a.C;
+  p.ns = a.cu_seqlens ? a.num_seqs : a.B;
+  p.run = pl.run; p.runs = pl.runs; p.silu = a.silu;
+  p.x_ld = a.x_ld; p.y_ld = a.y_ld; p.dy_ld = a.dy_ld; p.dx_ld = a.dx_ld;
+  p.x = a.x; p.state0 = a.state0; p.dy = a.dy; p.dstateT = a.dstateT;
+  p.y = a.y; p.stateT = a.stateT; p.dx = a.dx; p.dstate0 = a.dstate0;
+  p.w = a.w; p.bias = a.bias; p.cu = a.cu_seqlens;
+  p.part = static_cast<float *>(a.workspace);
+  return p;
+}
+
+template <typename T, int W, int V>
+cudaError_t fwd_t(const rdn_conv_args &a, cudaStream_t s) {
+  const ConvPlan pl = conv_plan(a, V, kFwdGroup, kFwdMost);
+  const ConvP p = conv_params(a, pl);
+  RDN_LAUNCH("conv_fwd", s,
+             (conv_fwd_kernel<T, W, V><<<dim3(pl.gx, pl.gy), dim3(pl.bx, pl.by), 0, s>>>(p)));
+  return cudaGetLastError();
+}
+template <typename T, int W, int V>
+cudaError_t bwd_t(const rdn_conv_args &a, cudaStream_t s) {
+  const ConvPlan pl = conv_plan(a, V, kBwdGroup, kBwdMost);
+  const ConvP p = conv_params(a, pl);
+  const size_t smem = sizeof(float) * kConvThreads * V * (W + 1);
+  RDN_LAUNCH("conv_bwd", s,
+             (conv_bwd_kernel<T, W, V><<<dim3(pl.gx, pl.gy), dim3(pl.bx, pl.by), smem, s>>>(p)));
+  const unsigned grid = (unsigned)(((long long)a.C * (W + 1) + 31) / 32);
+  RDN_LAUNCH("conv_grad", s,
+             (conv_grad_kernel<W><<<grid, dim3(32, 16), 0, s>>>(p.part, a.C, (int)pl.gx, a.dw, a.dbias)));
+  return cudaGetLastError();
+}
+template <typename T, int W>
+cudaError_t conv_w(const rdn_conv_args &a, bool bwd, cudaStream_t s) {
+  const bool vec = conv_vec(a, bwd);
+  if (bwd) return vec ? bwd_t<T, W, 4>(a, s) : bwd_t<T, W, 1>(a, s);
+  return vec ? fwd_t<T, W, 4>(a, s) : fwd_t<T, W, 1>(a, s);
+}
+template <typename T>
+cudaError_t conv_d(const rdn_conv_args &a, bool bwd, cudaStream_t s) {
+  return a.W == 2 ? conv_w<T, 2>(a, bwd, s) : a.W == 3 ? conv_w<T, 3>(a, bwd, s) : conv_w<T, 4>(a, bwd, s);
+}
+
+template <typename T, int W, int V>
+cudaError_t step_t(const ConvStepP &p, cudaStream_t s) {
+  const int nvec = (p.C + V - 1) / V;
+  unsigned bx = kConvThreads;
+  while (bx > 32 && bx / 2 >= (unsigned)nvec) bx /= 2;
+  const unsigned by = kConvThreads / bx;
+  RDN_LAUNCH("conv_step", s,
+             (conv_step_kernel<T, W, V><<<dim3((p.N + by - 1) / by, (nvec + bx - 1) / bx), dim3(bx, by), 0, s>>>(p)));
+  return cudaGetLastError();
+}
+template <typename T, int V>
+cudaError_t step_w(const ConvStepP &p, int W, cudaStream_t s) {
+  return W == 2 ? step_t<T, 2, V>(p, s) : W == 3 ? step_t<T, 3, V>(p, s) : step_t<T, 4, V>(p, s);
+}
+
+}  // namespace
+
+size_t conv_bwd_bytes(const rdn_conv_args &a) {
+  // (the larger of the two accesses' plans: the query sees no pointers)
+  const ConvPlan v = conv_plan(a, 4, kBwdGroup, kBwdMost), e = conv_plan(a, 1, kBwdGroup, kBwdMost);
+  const size_t parts = v.gx > e.gx ? v.gx : e.gx;
+  return round256(sizeof(float) * parts * a.C * (a.W + 1));
+}
+
+cudaError_t launch_conv(const rdn_conv_args &a, bool bwd, cudaStream_t s) {
+  return a.dtype == RDN_BF16 ? conv_d<__nv_bfloat16>(a, bwd, s) : conv_d<float>(a, bwd, s);
+}
+
+cudaError_t launch_conv_step(const rdn_conv_step_args &a, cudaStream_t s) {
+  ConvStepP p{a.N, a.C, a.num_slots, a.silu, a.x_ld, a.y_ld, a.x, a.w, a.bias, a.state, a.y, a.slots};
+  const size_t size = a.dtype == RDN_BF16 ? 2 : 4;
+  const bool vec = a.C % (16 / size) == 0 && rows_on(16, size, {{a.x, a.x_ld}, {a.y, a.y_ld}, {a.state, 0}});
+  if (a.dtype == RDN_BF16)
+    return vec ? step_w<__nv_bfloat16, 8>(p, a.W, s) : step_w<__nv_bfloat16, 1>(p, a.W, s);
+  return vec ? step_w<float, 4>(p, a.W, s) : step_w<float, 1>(p, a.W, s);
+}
+
+}  // namespace rdn

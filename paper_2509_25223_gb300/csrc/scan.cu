@@ -1,0 +1,349 @@
+// scan.cu -- the selective state space scan, forward, and its step of one token:
+//     h_t = exp(dl_t A) h_{t-1} + dl_t x_t B_t,  y_t = C_t . h_t + Dskip x_t,
+//     out_t = y_t SiLU(z_t),  dl_t = softplus(dt_t + dt_bias)
+// (layout and units: scan.cuh).
+//
+// A CTA owns 256 / L channels of one unit.  Per tile of 16 tokens its threads
+// turn the loaded dt and x into (dl, dl x) in shared memory, widen B and C to
+// fp32 there, then run the 16 steps from registers and shared memory alone; the
+// sums over the states come back through shared memory to the threads that
+// hold x and z of the same elements, which finish and store them.  The next
+// tile's global loads are in flight during the steps.
+#include "scan.cuh"
+
+namespace rdn {
+namespace {
+
+// FIRST: the first pass over the units (end state from a zero start, sum of dl).
+template <typename T, int L, bool VEC, bool FIRST>
+__global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(ScanP p) {
+  using Sh = ScanShape<T, L, VEC>;
+  using Rows = TileRows<T, L, VEC>;
+  using K = typename Rows::K;
+  __shared__ __align__(16) float2 s_dx[kScanTile][Sh::CT];  // (dl, dl x)
+  __shared__ __align__(16) float s_B[kScanTile][Sh::SP], s_C[kScanTile][Sh::SP];
+  __shared__ __align__(16) float s_y[kScanTile][Sh::CT];
+  const Unit w = find_unit(p, blockIdx.x);
+  if (!w.ok || (FIRST && w.j == w.n - 1)) return;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int sl = lane % L, cl = lane / L, n0 = sl * 4;
+  const int g = blockIdx.y / p.tiles_g, Dg = p.D / p.G;
+  const int c0 = g * Dg + blockIdx.y % p.tiles_g * Sh::CT;  // the tile's first channel
+  const int nch = min(Sh::CT, (g + 1) * Dg - c0);
+  int ch[2];  // this lane's channels within the tile: the one its sums end at first
+#pragma unroll
+  for (int j = 0; j < 2; ++j) ch[j] = warp * Sh::CW + cl * 2 + (j ^ (sl & 1));
+  float A2[2][4], h[2][4], sumd[2] = {0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const size_t d = c0 + ch[j];
+    const bool on = ch[j] < nch;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) A2[j][i] = h[j][i] = 0.f;
+    if (!on) continue;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n0 + i < p.S) A2[j][i] = __ldg(p.A + d * p.S + n0 + i) * kLog2e;
+    if (FIRST) continue;
+    if (p.h0) load_states(p.h0 + ((size_t)w.s * p.D + d) * p.S, p.S, n0, h[j]);
+    for (int k = 0; k < w.j; ++k) {  // over the units before this one
+      const size_t u = blockIdx.x - w.j + k;
+      const float sd = p.sumd[u * p.D + d];
+      const float4 e = *reinterpret_cast<const float4 *>(p.carry + (u * p.D + d) * Sh::SP + n0);
+      const float ee[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[j][i] = fmaf(decay(sd, A2[j][i]), h[j][i], ee[i]);
+    }
+  }
+  const long long r0 = w.begin + (long long)w.j * p.seg;
+  const long long r1 = min(r0 + p.seg, w.end);
+  const T *X = (const T *)p.x + c0, *DT = (const T *)p.dt + c0;
+  const T *Z = p.z ? (const T *)p.z + c0 : nullptr;
+  const T *Bm = (const T *)p.Bm + (size_t)g * p.S, *Cm = (const T *)p.Cm + (size_t)g * p.S;
+  Rows x, dt, z;
+  TileBC<T, L> tb, tc;
+  auto load = [&](long long r) {
+    const int ntok = (int)max(0ll, min((long long)kScanTile, r1 - r));
+    x.load(X + r * p.x_ld, p.x_ld, ntok, nch);
+    dt.load(DT + r * p.dt_ld, p.dt_ld, ntok, nch);
+    tb.load(Bm + r * p.b_ld, p.b_ld, ntok, p.S);
+    if (!FIRST && p.out) {
+      z.load(Z ? Z + r * p.z_ld : nullptr, p.z_ld, ntok, nch);
+      tc.load(Cm + r * p.c_ld, p.c_ld, ntok, p.S);
+    }
+  };
+  load(r0);
+  for (long long r = r0; r < r1; r += kScanTile) {
+    const int ntok = (int)min((long long)kScanTile, r1 - r);
+    const Rows xc = x, zc = z;
+#pragma unroll
+    for (int i = 0; i < Sh::NV; ++i) {
+      const int id = i * kScanThreads + tid, t = id / Sh::COLS, c = id % Sh::COLS * Sh::V;
+      if (t >= kScanTile) break;
+      float xv[Sh::V], dv[Sh::V];
+      x.get(i, xv);
+      dt.get(i, dv);
+#pragma unroll
+      for (int e = 0; e < Sh::V; ++e) {
+        float v = dv[e];
+        if (p.dt_bias && c + e < nch) v += __ldg(p.dt_bias + c0 + c + e);
+        const float dl = p.softplus ? softplusf(v) : v;
+        s_dx[t][c + e] = make_float2(dl, dl * xv[e]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < Sh::NB; ++i) {
+      const int id = i * kScanThreads + tid;
+      s_B[id / Sh::SP][id % Sh::SP] = to_f32<T>(tb.raw[i]);
+      if (!FIRST) s_C[id / Sh::SP][id % Sh::SP] = p.out ? to_f32<T>(tc.raw[i]) : 0.f;
+    }
+    __syncthreads();
+    load(r + kScanTile);
+    if (!FIRST && p.chunks) {
+      const long long slot = w.chunk0 + (r - w.begin) / kScanTile;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (ch[j] < nch && slot < p.slots) store_states(p.chunks + ((size_t)slot * p.D + c0 + ch[j]) * p.S, p.S, n0, h[j]);
+    }
+#pragma unroll 1
+    for (int t4 = 0; t4 < ntok; t4 += 4) {
+      float y[4][2];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int t = t4 + u;
+        y[u][0] = y[u][1] = 0.f;
+        if (t >= ntok) continue;
+        const float4 b4 = *reinterpret_cast<const float4 *>(&s_B[t][n0]);
+        const float bb[4] = {b4.x, b4.y, b4.z, b4.w};
+        float cc[4];
+        if (!FIRST) {
+          const float4 c4 = *reinterpret_cast<const float4 *>(&s_C[t][n0]);
+          cc[0] = c4.x; cc[1] = c4.y; cc[2] = c4.z; cc[3] = c4.w;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float2 d = s_dx[t][ch[j]];
+          if (FIRST) sumd[j] += d.x;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            h[j][i] = fmaf(decay(d.x, A2[j][i]), h[j][i], d.y * bb[i]);
+            if (!FIRST) y[u][j] = fmaf(cc[i], h[j][i], y[u][j]);
+          }
+        }
+      }
+      if (!FIRST && p.out) sum_states<L>(y, &s_y[t4][0], Sh::CT, ch[0], sl);
+    }
+    __syncthreads();
+    if (FIRST || !p.out) continue;
+    T *O = (T *)p.out + r * p.out_ld + c0;
+#pragma unroll
+    for (int i = 0; i < Sh::NV; ++i) {
+      const int id = i * kScanThreads + tid, t = id / Sh::COLS, c = id % Sh::COLS * Sh::V;
+      if (t >= ntok || c >= nch) continue;
+      float xv[Sh::V], zv[Sh::V], o[Sh::V];
+      xc.get(i, xv);
+      zc.get(i, zv);
+#pragma unroll
+      for (int e = 0; e < Sh::V; ++e) {
+        o[e] = s_y[t][c + e];
+        if (p.Dskip) o[e] = fmaf(__ldg(p.Dskip + c0 + c + e), xv[e], o[e]);
+        if (p.z) o[e] *= siluf(zv[e]);
+      }
+      K::st(O + t * p.out_ld + c, K::put(o));
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if (ch[j] >= nch) continue;
+    const size_t d = c0 + ch[j];
+    if (FIRST) {
+      const size_t u = blockIdx.x;
+      if (sl == 0) p.sumd[u * p.D + d] = sumd[j];
+      *reinterpret_cast<float4 *>(p.carry + (u * p.D + d) * Sh::SP + n0) =
+          make_float4(h[j][0], h[j][1], h[j][2], h[j][3]);
+    } else if (p.hT && w.j == w.n - 1) {
+      store_states(p.hT + ((size_t)w.s * p.D + d) * p.S, p.S, n0, h[j]);
+    }
+  }
+}
+
+template <typename T, int L, bool VEC>
+cudaError_t fwd_l(const ScanP &p, const ScanPlan &pl, cudaStream_t s) {
+  const dim3 grid(pl.units, pl.tiles);
+  if (pl.split)
+    RDN_LAUNCH("scan_carry", s, (scan_fwd_kernel<T, L, VEC, true><<<grid, kScanThreads, 0, s>>>(p)));
+  RDN_LAUNCH("scan_fwd", s, (scan_fwd_kernel<T, L, VEC, false><<<grid, kScanThreads, 0, s>>>(p)));
+  return cudaGetLastError();
+}
+template <typename T, bool VEC>
+cudaError_t fwd_v(const ScanP &p, const ScanPlan &pl, cudaStream_t s) {
+  switch (pl.L) {
+    case 2: return fwd_l<T, 2, VEC>(p, pl, s);
+    case 4: return fwd_l<T, 4, VEC>(p, pl, s);
+    case 8: return fwd_l<T, 8, VEC>(p, pl, s);
+    default: return fwd_l<T, 16, VEC>(p, pl, s);
+  }
+}
+
+struct StepP {
+  int N, D, S, G, num_slots, softplus;
+  long long x_ld, dt_ld, z_ld, b_ld, c_ld, out_ld;
+  const void *x, *dt, *z, *Bm, *Cm;
+  const float *A, *Dskip, *dt_bias;
+  float *h;
+  const int *slots;
+  void *out;
+};
+
+// One token: L lanes per channel, 4 states each; the state streams through
+// once (memory-bound: 8 bytes per state).
+template <typename T, int L>
+__global__ void __launch_bounds__(kScanThreads) scan_step_kernel(StepP p) {
+  constexpr int CH = kScanThreads / L;
+  const int sl = threadIdx.x % L, n0 = sl * 4, n = blockIdx.x;
+  const int d = blockIdx.y * CH + threadIdx.x / L;
+  const int slot = p.slots ? __ldg(p.slots + n) : n;
+  const bool on = d < p.D, idle = slot < 0 || slot >= p.num_slots;
+  float y = 0.f, xv = 0.f;
+  if (on && !idle) {
+    float *row = p.h + ((size_t)slot * p.D + d) * p.S;
+    float h[4], bb[4], cc[4], A2[4];
+    load_states(row, p.S, n0, h);
+    const int g = d / (p.D / p.G);
+    const T *Bm = (const T *)p.Bm + (size_t)n * p.b_ld + (size_t)g * p.S;
+    const T *Cm = (const T *)p.Cm + (size_t)n * p.c_ld + (size_t)g * p.S;
+    xv = to_f32<T>(((const T *)p.x)[(size_t)n * p.x_ld + d]);
+    float v = to_f32<T>(((const T *)p.dt)[(size_t)n * p.dt_ld + d]);
+    load_states(p.A + (size_t)d * p.S, p.S, n0, A2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bb[i] = n0 + i < p.S ? to_f32<T>(Bm[n0 + i]) : 0.f;
+      cc[i] = n0 + i < p.S ? to_f32<T>(Cm[n0 + i]) : 0.f;
+    }
+    if (p.dt_bias) v += __ldg(p.dt_bias + d);
+    const float dl = p.softplus ? softplusf(v) : v, dx = dl * xv;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h[i] = fmaf(decay(dl, A2[i] * kLog2e), h[i], dx * bb[i]);
+      y = fmaf(cc[i], h[i], y);
+    }
+    store_states(row, p.S, n0, h);
+  }
+#pragma unroll
+  for (int o = L / 2; o; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
+  if (!on || sl) return;
+  if (!idle) {
+    if (p.Dskip) y = fmaf(__ldg(p.Dskip + d), xv, y);
+    if (p.z) y *= siluf(to_f32<T>(((const T *)p.z)[(size_t)n * p.z_ld + d]));
+  }
+  ((T *)p.out)[(size_t)n * p.out_ld + d] = from_f32<T>(idle ? 0.f : y);
+}
+
+template <typename T>
+cudaError_t step_d(const StepP &p, cudaStream_t s) {
+  const int L = p.S <= 8 ? 2 : p.S <= 16 ? 4 : p.S <= 32 ? 8 : 16;
+  const dim3 grid(p.N, (p.D + kScanThreads / L - 1) / (kScanThreads / L));
+  switch (L) {
+    case 2: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 2><<<grid, kScanThreads, 0, s>>>(p))); break;
+    case 4: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 4><<<grid, kScanThreads, 0, s>>>(p))); break;
+    case 8: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 8><<<grid, kScanThreads, 0, s>>>(p))); break;
+    default: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 16><<<grid, kScanThreads, 0, s>>>(p))); break;
+  }
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+long long scan_slots(const rdn_scan_args &a) {
+  const long long nc = ((long long)a.T + kScanTile - 1) / kScanTile;
+  return a.cu_seqlens ? a.num_seqs + nc : a.B * nc;
+}
+
+// Units: enough CTAs of 4 warps for about four per SM, in units of at least 64
+// tokens; one unit per sequence where that is enough already.
+ScanPlan scan_plan(const rdn_scan_args &a) {
+  ScanPlan pl;
+  pl.L = a.S <= 8 ? 2 : a.S <= 16 ? 4 : a.S <= 32 ? 8 : 16;
+  pl.CT = 256 / pl.L;
+  const int Dg = a.D / a.G;
+  pl.tiles_g = (Dg + pl.CT - 1) / pl.CT;
+  pl.tiles = pl.tiles_g * a.G;
+  const long long want = 152ll * 4;
+  const long long ns = a.cu_seqlens ? 1 : a.B;
+  const long long per_seq = (want + ns * pl.tiles - 1) / (ns * pl.tiles);  // units wanted per sequence
+  const long long len = a.T;
+  long long seg = per_seq <= 1 ? len : (len + per_seq - 1) / per_seq;
+  seg = (seg + kScanTile - 1) / kScanTile * kScanTile;
+  if (seg < 64) seg = 64;
+  pl.seg = (int)seg;
+  pl.units_row = a.T > 0 ? (int)((a.T + seg - 1) / seg) : 1;
+  pl.units = a.cu_seqlens ? a.num_seqs + (int)((a.T + seg - 1) / seg) : a.B * pl.units_row;
+  pl.split = a.T > seg;
+  return pl;
+}
+
+ScanP scan_params(const rdn_scan_args &a, const ScanPlan &pl) {
+  ScanP p{};
+  p.B = a.B; p.T = a.T; p.D = a.D; p.S = a.S; p.G = a.G;
+  p.ns = a.cu_seqlens ? a.num_seqs : a.B;
+  p.softplus = a.dt_softplus;
+  p.seg = pl.seg; p.units = pl.units; p.units_row = pl.units_row; p.tiles_g = pl.tiles_g;
+  p.x_ld = a.x_ld; p.dt_ld = a.dt_ld; p.z_ld = a.z_ld; p.b_ld = a.b_ld; p.c_ld = a.c_ld;
+  p.out_ld = a.out_ld; p.dout_ld = a.dout_ld; p.dx_ld = a.dx_ld; p.ddt_ld = a.ddt_ld; p.dz_ld = a.dz_ld;
+  p.x = a.x; p.dt = a.dt; p.z = a.z; p.Bm = a.Bm; p.Cm = a.Cm; p.dout = a.dout;
+  p.A = a.A; p.Dskip = a.Dskip; p.dt_bias = a.dt_bias; p.h0 = a.h0; p.dhT = a.dhT;
+  p.out = a.out; p.dx = a.dx; p.ddt = a.ddt; p.dz = a.dz;
+  p.slots = scan_slots(a);
+  p.hT = a.hT; p.chunks = a.h_chunks; p.dh0 = a.dh0; p.cu = a.cu_seqlens;
+  return p;
+}
+
+// 16-byte accesses: every row of every operand and every channel tile on 16 bytes
+bool scan_vec(const rdn_scan_args &a, bool bwd) {
+  const size_t size = a.dtype == RDN_BF16 ? 2 : 4;
+  if ((a.D / a.G) % (16 / size)) return false;
+  auto on = [&](const void *p, long long ld) { return !p || (((uintptr_t)p | (size_t)ld * size) & 15) == 0; };
+  if (!on(a.x, a.x_ld) || !on(a.dt, a.dt_ld) || !on(a.z, a.z_ld)) return false;
+  if (!bwd) return on(a.out, a.out_ld);
+  return on(a.dout, a.dout_ld) && on(a.dx, a.dx_ld) && on(a.ddt, a.ddt_ld) && on(a.dz, a.dz_ld);
+}
+
+size_t scan_fwd_bytes(const rdn_scan_args &a) {
+  const ScanPlan pl = scan_plan(a);
+  if (!pl.split) return 0;
+  return round256(sizeof(float) * (size_t)pl.units * a.D * 4 * pl.L) +
+         round256(sizeof(float) * (size_t)pl.units * a.D);
+}
+
+namespace {
+cudaError_t scan_run(const rdn_scan_args &a, const ScanP &p, const ScanPlan &pl, cudaStream_t s) {
+  const bool vec = scan_vec(a, false);
+  if (a.dtype == RDN_BF16)
+    return vec ? fwd_v<__nv_bfloat16, true>(p, pl, s) : fwd_v<__nv_bfloat16, false>(p, pl, s);
+  return vec ? fwd_v<float, true>(p, pl, s) : fwd_v<float, false>(p, pl, s);
+}
+}  // namespace
+
+cudaError_t launch_scan_fwd(const rdn_scan_args &a, cudaStream_t s) {
+  const ScanPlan pl = scan_plan(a);
+  ScanP p = scan_params(a, pl);
+  if (pl.split) {
+    p.carry = static_cast<float *>(a.workspace);
+    p.sumd = p.carry + round256(sizeof(float) * (size_t)pl.units * a.D * 4 * pl.L) / sizeof(float);
+  }
+  return scan_run(a, p, pl, s);
+}
+
+cudaError_t scan_states(const rdn_scan_args &a, ScanP p, const ScanPlan &pl, cudaStream_t s) {
+  p.out = nullptr;
+  p.hT = nullptr;
+  return scan_run(a, p, pl, s);
+}
+
+cudaError_t launch_scan_step(const rdn_scan_step_args &a, cudaStream_t s) {
+  const StepP p{a.N, a.D, a.S, a.G, a.num_slots, a.dt_softplus, a.x_ld, a.dt_ld, a.z_ld, a.b_ld,
+                a.c_ld, a.out_ld, a.x, a.dt, a.z, a.Bm, a.Cm, a.A, a.Dskip, a.dt_bias, a.h, a.slots, a.out};
+  return a.dtype == RDN_BF16 ? step_d<__nv_bfloat16>(p, s) : step_d<float>(p, s);
+}
+
+}  // namespace rdn
