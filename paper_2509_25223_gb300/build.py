@@ -1,6 +1,6 @@
 """Build librdn.so (the C-ABI library of include/rdn.h) for sm_103a.
 
-Each .cu under csrc/ is compiled by nvcc in parallel, then linked into
+Each .cu under csrc/ (and csrc/layer/, the operators around the recurrence) is compiled by nvcc in parallel, then linked into
 paper_2509_25223_gb300/_build/librdn.so.  Rebuilds only when a source, a
 header or this file is newer than the library.
 """
@@ -32,11 +32,12 @@ def _nvcc():
 
 
 def sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
+    return sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "layer", "*.cu")))
 
 
 def _deps():
     return sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + \
+        glob.glob(os.path.join(CSRC, "layer", "*.cuh")) + \
         glob.glob(os.path.join(INCLUDE, "*.h")) + [os.path.abspath(__file__)]
 
 

@@ -1,4 +1,4 @@
-// api_ops.cu -- the C ABI of the operators around the recurrence (convolution,
+// api_layer.cu -- the C ABI of the operators around the recurrence (convolution,
 // selective scan, norms; include/rdn.h): argument validation and dispatch to
 // the launchers.  No exception or abort crosses this boundary.
 #include <math.h>
