@@ -184,7 +184,7 @@ rdn_status_t scan_common(const char *fn, const rdn_scan_args *args, bool bwd, cu
   TRY(check_ptr(fn, "dA", a->dA, 4, true));
   TRY(check_ptr(fn, "dD", a->dD, 4, false));
   TRY(check_ptr(fn, "ddt_bias", a->ddt_bias, 4, false));
-  TRY(check_ptr(fn, "dh0", a->dh0, 4, false));
+  TRY(check_ptr16(fn, "dh0", a->dh0, false));
   TRY(check_ws(fn, a->workspace, a->workspace_bytes, rdn::scan_bwd_bytes(*a)));
   TRY(entry_injected(fn));
   return entry_cuda(fn, rdn::launch_scan_bwd(*a, s));

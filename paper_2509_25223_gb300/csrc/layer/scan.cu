@@ -14,15 +14,24 @@
 namespace rdn {
 namespace {
 
+template <typename T, int L, bool VEC>
+struct FwdSmem {
+  using Sh = ScanShape<T, L, VEC>;
+  float4 dx[kScanTile][Sh::CT / 2];                       // (dl, dl', dl x, dl' x') of a pair, at spread16
+  float y[kScanTile][Sh::CT];
+  typename Sh::Raw raw[2][3][Sh::NV][kScanThreads];       // each thread's x, dt, z: this tile's and the next's
+  T B[2][kScanTile][Sh::SP], C[2][kScanTile][Sh::SP];
+  float bias[Sh::CT], D[Sh::CT];
+};
+
 // FIRST: the first pass over the units (end state from a zero start, sum of dl).
 template <typename T, int L, bool VEC, bool FIRST>
-__global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(ScanP p) {
+__global__ void __launch_bounds__(kScanThreads, 7) scan_fwd_kernel(ScanP p) {
   using Sh = ScanShape<T, L, VEC>;
-  using Rows = TileRows<T, L, VEC>;
-  using K = typename Rows::K;
-  __shared__ __align__(16) float2 s_dx[kScanTile][Sh::CT];  // (dl, dl x)
-  __shared__ __align__(16) float s_B[kScanTile][Sh::SP], s_C[kScanTile][Sh::SP];
-  __shared__ __align__(16) float s_y[kScanTile][Sh::CT];
+  using K = typename Sh::K;
+  constexpr int V = Sh::V;
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  FwdSmem<T, L, VEC> &sm = *reinterpret_cast<FwdSmem<T, L, VEC> *>(smem_raw);
   const Unit w = find_unit(p, blockIdx.x);
   if (!w.ok || (FIRST && w.j == w.n - 1)) return;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -30,139 +39,145 @@ __global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(ScanP p) {
   const int g = blockIdx.y / p.tiles_g, Dg = p.D / p.G;
   const int c0 = g * Dg + blockIdx.y % p.tiles_g * Sh::CT;  // the tile's first channel
   const int nch = min(Sh::CT, (g + 1) * Dg - c0);
-  int ch[2];  // this lane's channels within the tile: the one its sums end at first
+  const int first = warp * Sh::CW + cl * 4;                 // this lane's first channel in the tile
+  int at[2];                                                // entries of its pairs
 #pragma unroll
-  for (int j = 0; j < 2; ++j) ch[j] = warp * Sh::CW + cl * 2 + (j ^ (sl & 1));
-  float A2[2][4], h[2][4], sumd[2] = {0.f, 0.f};
+  for (int j = 0; j < 2; ++j) at[j] = spread16(first / 2 + (j ^ (sl & 1)));
+  for (int c = tid; c < Sh::CT; c += kScanThreads) {
+    sm.bias[c] = p.dt_bias && c < nch ? p.dt_bias[c0 + c] : 0.f;
+    sm.D[c] = p.Dskip && c < nch ? p.Dskip[c0 + c] : 0.f;
+  }
+  // channel pair j, state n0 + i
+  f2 A2[2][4], h[2][4], sumd[2];
+  const f2 shift = pack2(kExpShift, kExpShift);
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const size_t d = c0 + ch[j];
-    const bool on = ch[j] < nch;
+    float a[2][4], v[2][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) A2[j][i] = h[j][i] = 0.f;
-    if (!on) continue;
+    for (int e = 0; e < 2; ++e) {
+      const int ch = first + 2 * (j ^ (sl & 1)) + e;
+      const size_t d = c0 + ch;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (n0 + i < p.S) A2[j][i] = __ldg(p.A + d * p.S + n0 + i) * kLog2e;
-    if (FIRST) continue;
-    if (p.h0) load_states(p.h0 + ((size_t)w.s * p.D + d) * p.S, p.S, n0, h[j]);
-    for (int k = 0; k < w.j; ++k) {  // over the units before this one
-      const size_t u = blockIdx.x - w.j + k;
-      const float sd = p.sumd[u * p.D + d];
-      const float4 e = *reinterpret_cast<const float4 *>(p.carry + (u * p.D + d) * Sh::SP + n0);
-      const float ee[4] = {e.x, e.y, e.z, e.w};
+      for (int i = 0; i < 4; ++i) a[e][i] = v[e][i] = 0.f;
+      if (ch >= nch) continue;
+      load_states(p.A + d * p.S, p.S, n0, a[e]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) h[j][i] = fmaf(decay(sd, A2[j][i]), h[j][i], ee[i]);
+      for (int i = 0; i < 4; ++i) a[e][i] *= kLog2e;
+      if (FIRST) continue;
+      if (p.h0) load_states(p.h0 + ((size_t)w.s * p.D + d) * p.S, p.S, n0, v[e]);
+      for (int k = 0; k < w.j; ++k) {  // over the units before this one
+        const size_t u = blockIdx.x - w.j + k;
+        const float sd = p.sumd[u * p.D + d];
+        const float4 x = *reinterpret_cast<const float4 *>(p.carry + (u * p.D + d) * Sh::SP + n0);
+        const float xx[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[e][i] = fmaf(decay(sd, a[e][i]), v[e][i], xx[i]);
+      }
+    }
+    sumd[j] = pack2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      A2[j][i] = pack2(a[0][i], a[1][i]);
+      h[j][i] = pack2(v[0][i], v[1][i]);
     }
   }
   const long long r0 = w.begin + (long long)w.j * p.seg;
   const long long r1 = min(r0 + p.seg, w.end);
-  const T *X = (const T *)p.x + c0, *DT = (const T *)p.dt + c0;
-  const T *Z = p.z ? (const T *)p.z + c0 : nullptr;
+  const bool out = !FIRST && p.out;
+  const T *X = (const T *)p.x + c0, *DT = (const T *)p.dt + c0, *Z = p.z ? (const T *)p.z + c0 : nullptr;
   const T *Bm = (const T *)p.Bm + (size_t)g * p.S, *Cm = (const T *)p.Cm + (size_t)g * p.S;
-  Rows x, dt, z;
-  TileBC<T, L> tb, tc;
-  auto load = [&](long long r) {
+  auto load = [&](long long r, int b) {
     const int ntok = (int)max(0ll, min((long long)kScanTile, r1 - r));
-    x.load(X + r * p.x_ld, p.x_ld, ntok, nch);
-    dt.load(DT + r * p.dt_ld, p.dt_ld, ntok, nch);
-    tb.load(Bm + r * p.b_ld, p.b_ld, ntok, p.S);
-    if (!FIRST && p.out) {
-      z.load(Z ? Z + r * p.z_ld : nullptr, p.z_ld, ntok, nch);
-      tc.load(Cm + r * p.c_ld, p.c_ld, ntok, p.S);
+    fetch_rows<Sh>(sm.raw[b][0], X + r * p.x_ld, p.x_ld, ntok, nch);
+    fetch_rows<Sh>(sm.raw[b][1], DT + r * p.dt_ld, p.dt_ld, ntok, nch);
+    fetch_states(sm.B[b], Bm + r * p.b_ld, p.b_ld, ntok, p.S, p.bc_vec);
+    if (out) {
+      if (Z) fetch_rows<Sh>(sm.raw[b][2], Z + r * p.z_ld, p.z_ld, ntok, nch);
+      fetch_states(sm.C[b], Cm + r * p.c_ld, p.c_ld, ntok, p.S, p.bc_vec);
     }
   };
-  load(r0);
-  for (long long r = r0; r < r1; r += kScanTile) {
+  if (r0 < r1) load(r0, 0);
+  __syncthreads();  // bias, D
+  int b = 0;
+  for (long long r = r0; r < r1; r += kScanTile, b ^= 1) {
     const int ntok = (int)min((long long)kScanTile, r1 - r);
-    const Rows xc = x, zc = z;
+    fetched();
 #pragma unroll
     for (int i = 0; i < Sh::NV; ++i) {
-      const int id = i * kScanThreads + tid, t = id / Sh::COLS, c = id % Sh::COLS * Sh::V;
+      const int t = Sh::tok(i), c = Sh::chan(i);
       if (t >= kScanTile) break;
-      float xv[Sh::V], dv[Sh::V];
-      x.get(i, xv);
-      dt.get(i, dv);
-#pragma unroll
-      for (int e = 0; e < Sh::V; ++e) {
-        float v = dv[e];
-        if (p.dt_bias && c + e < nch) v += __ldg(p.dt_bias + c0 + c + e);
-        const float dl = p.softplus ? softplusf(v) : v;
-        s_dx[t][c + e] = make_float2(dl, dl * xv[e]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < Sh::NB; ++i) {
-      const int id = i * kScanThreads + tid;
-      s_B[id / Sh::SP][id % Sh::SP] = to_f32<T>(tb.raw[i]);
-      if (!FIRST) s_C[id / Sh::SP][id % Sh::SP] = p.out ? to_f32<T>(tc.raw[i]) : 0.f;
+      float xv[V], dl[V];
+      K::get(sm.raw[b][0][i][tid], xv);
+      K::get(sm.raw[b][1][i][tid], dl);
+      step_sizes<V>(p, sm.bias + c, t < ntok, dl);
+      store_steps<V>(sm.dx[t], c, dl, xv);
     }
     __syncthreads();
-    load(r + kScanTile);
+    load(r + kScanTile, b ^ 1);
     if (!FIRST && p.chunks) {
       const long long slot = w.chunk0 + (r - w.begin) / kScanTile;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        if (ch[j] < nch && slot < p.slots) store_states(p.chunks + ((size_t)slot * p.D + c0 + ch[j]) * p.S, p.S, n0, h[j]);
+      for (int j = 0; j < 2; ++j) store_pairs(p.chunks, slot, slot < p.slots, p, c0, first + 2 * (j ^ (sl & 1)), nch, n0, h[j]);
     }
-#pragma unroll 1
-    for (int t4 = 0; t4 < ntok; t4 += 4) {
-      float y[4][2];
+#pragma unroll 2
+    for (int t = 0; t < ntok; ++t) {
+      f2 bb[4], cc[4], y[2];
+      states4(&sm.B[b][t][n0], 0, bb);
+      if (!FIRST) states4(&sm.C[b][t][n0], 0, cc);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int t = t4 + u;
-        y[u][0] = y[u][1] = 0.f;
-        if (t >= ntok) continue;
-        const float4 b4 = *reinterpret_cast<const float4 *>(&s_B[t][n0]);
-        const float bb[4] = {b4.x, b4.y, b4.z, b4.w};
-        float cc[4];
-        if (!FIRST) {
-          const float4 c4 = *reinterpret_cast<const float4 *>(&s_C[t][n0]);
-          cc[0] = c4.x; cc[1] = c4.y; cc[2] = c4.z; cc[3] = c4.w;
-        }
+      for (int j = 0; j < 2; ++j) {
+        const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dx[t][at[j]]);
+        if (FIRST) sumd[j] = add2(sumd[j], d.x);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float2 d = s_dx[t][ch[j]];
-          if (FIRST) sumd[j] += d.x;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            h[j][i] = fmaf(decay(d.x, A2[j][i]), h[j][i], d.y * bb[i]);
-            if (!FIRST) y[u][j] = fmaf(cc[i], h[j][i], y[u][j]);
-          }
+        for (int i = 0; i < 4; ++i) {
+          h[j][i] = fma2(decay2(d.x, A2[j][i], shift), h[j][i], mul2(d.y, bb[i]));
+          if (!FIRST) y[j] = i ? fma2(cc[i], h[j][i], y[j]) : mul2(cc[i], h[j][i]);
         }
       }
-      if (!FIRST && p.out) sum_states<L>(y, &s_y[t4][0], Sh::CT, ch[0], sl);
+      if (out) sum_states<L>(y, sm.y[t], first, sl);
     }
     __syncthreads();
-    if (FIRST || !p.out) continue;
+    if (!out) continue;
     T *O = (T *)p.out + r * p.out_ld + c0;
 #pragma unroll
     for (int i = 0; i < Sh::NV; ++i) {
-      const int id = i * kScanThreads + tid, t = id / Sh::COLS, c = id % Sh::COLS * Sh::V;
+      const int t = Sh::tok(i), c = Sh::chan(i);
       if (t >= ntok || c >= nch) continue;
-      float xv[Sh::V], zv[Sh::V], o[Sh::V];
-      xc.get(i, xv);
-      zc.get(i, zv);
+      float o[V], v[V];
 #pragma unroll
-      for (int e = 0; e < Sh::V; ++e) {
-        o[e] = s_y[t][c + e];
-        if (p.Dskip) o[e] = fmaf(__ldg(p.Dskip + c0 + c + e), xv[e], o[e]);
-        if (p.z) o[e] *= siluf(zv[e]);
+      for (int e = 0; e < V; ++e) o[e] = sm.y[t][c + e];
+      if (p.Dskip) {
+        K::get(sm.raw[b][0][i][tid], v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = fmaf(sm.D[c + e], v[e], o[e]);
+      }
+      if (p.z) {
+        K::get(sm.raw[b][2][i][tid], v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] *= siluf(v[e]);
       }
       K::st(O + t * p.out_ld + c, K::put(o));
     }
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    if (ch[j] >= nch) continue;
-    const size_t d = c0 + ch[j];
+    const int pair = first + 2 * (j ^ (sl & 1));
     if (FIRST) {
       const size_t u = blockIdx.x;
-      if (sl == 0) p.sumd[u * p.D + d] = sumd[j];
-      *reinterpret_cast<float4 *>(p.carry + (u * p.D + d) * Sh::SP + n0) =
-          make_float4(h[j][0], h[j][1], h[j][2], h[j][3]);
+      float s[2], v[2][4];
+      unpack2(sumd[j], s[0], s[1]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) unpack2(h[j][i], v[0][i], v[1][i]);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (pair + e >= nch) continue;
+        const size_t d = c0 + pair + e;
+        if (sl == 0) p.sumd[u * p.D + d] = s[e];
+        *reinterpret_cast<float4 *>(p.carry + (u * p.D + d) * Sh::SP + n0) =
+            make_float4(v[e][0], v[e][1], v[e][2], v[e][3]);
+      }
     } else if (p.hT && w.j == w.n - 1) {
-      store_states(p.hT + ((size_t)w.s * p.D + d) * p.S, p.S, n0, h[j]);
+      store_pairs(p.hT, w.s, true, p, c0, pair, nch, n0, h[j]);
     }
   }
 }
@@ -170,9 +185,13 @@ __global__ void __launch_bounds__(kScanThreads) scan_fwd_kernel(ScanP p) {
 template <typename T, int L, bool VEC>
 cudaError_t fwd_l(const ScanP &p, const ScanPlan &pl, cudaStream_t s) {
   const dim3 grid(pl.units, pl.tiles);
+  const int smem = (int)sizeof(FwdSmem<T, L, VEC>);
+  cudaError_t e;
+  if ((e = allow_smem(scan_fwd_kernel<T, L, VEC, true>, smem)) != cudaSuccess) return e;
+  if ((e = allow_smem(scan_fwd_kernel<T, L, VEC, false>, smem)) != cudaSuccess) return e;
   if (pl.split)
-    RDN_LAUNCH("scan_carry", s, (scan_fwd_kernel<T, L, VEC, true><<<grid, kScanThreads, 0, s>>>(p)));
-  RDN_LAUNCH("scan_fwd", s, (scan_fwd_kernel<T, L, VEC, false><<<grid, kScanThreads, 0, s>>>(p)));
+    RDN_LAUNCH("scan_carry", s, (scan_fwd_kernel<T, L, VEC, true><<<grid, kScanThreads, smem, s>>>(p)));
+  RDN_LAUNCH("scan_fwd", s, (scan_fwd_kernel<T, L, VEC, false><<<grid, kScanThreads, smem, s>>>(p)));
   return cudaGetLastError();
 }
 template <typename T, bool VEC>
@@ -197,9 +216,10 @@ struct StepP {
 
 // One token: L lanes per channel, 4 states each; the state streams through
 // once (memory-bound: 8 bytes per state).
+constexpr int kStepThreads = 128;
 template <typename T, int L>
-__global__ void __launch_bounds__(kScanThreads) scan_step_kernel(StepP p) {
-  constexpr int CH = kScanThreads / L;
+__global__ void __launch_bounds__(kStepThreads) scan_step_kernel(StepP p) {
+  constexpr int CH = kStepThreads / L;
   const int sl = threadIdx.x % L, n0 = sl * 4, n = blockIdx.x;
   const int d = blockIdx.y * CH + threadIdx.x / L;
   const int slot = p.slots ? __ldg(p.slots + n) : n;
@@ -242,12 +262,12 @@ __global__ void __launch_bounds__(kScanThreads) scan_step_kernel(StepP p) {
 template <typename T>
 cudaError_t step_d(const StepP &p, cudaStream_t s) {
   const int L = p.S <= 8 ? 2 : p.S <= 16 ? 4 : p.S <= 32 ? 8 : 16;
-  const dim3 grid(p.N, (p.D + kScanThreads / L - 1) / (kScanThreads / L));
+  const dim3 grid(p.N, (p.D + kStepThreads / L - 1) / (kStepThreads / L));
   switch (L) {
-    case 2: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 2><<<grid, kScanThreads, 0, s>>>(p))); break;
-    case 4: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 4><<<grid, kScanThreads, 0, s>>>(p))); break;
-    case 8: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 8><<<grid, kScanThreads, 0, s>>>(p))); break;
-    default: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 16><<<grid, kScanThreads, 0, s>>>(p))); break;
+    case 2: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 2><<<grid, kStepThreads, 0, s>>>(p))); break;
+    case 4: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 4><<<grid, kStepThreads, 0, s>>>(p))); break;
+    case 8: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 8><<<grid, kStepThreads, 0, s>>>(p))); break;
+    default: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 16><<<grid, kStepThreads, 0, s>>>(p))); break;
   }
   return cudaGetLastError();
 }
@@ -261,16 +281,16 @@ long long scan_slots(const rdn_scan_args &a) {
 
 // Units: enough CTAs of 4 warps for about four per SM, in units of at least 64
 // tokens; one unit per sequence where that is enough already.
-ScanPlan scan_plan(const rdn_scan_args &a) {
+ScanPlan scan_plan(const rdn_scan_args &a, bool bwd) {
   ScanPlan pl;
   pl.L = a.S <= 8 ? 2 : a.S <= 16 ? 4 : a.S <= 32 ? 8 : 16;
   pl.CT = 256 / pl.L;
   const int Dg = a.D / a.G;
   pl.tiles_g = (Dg + pl.CT - 1) / pl.CT;
   pl.tiles = pl.tiles_g * a.G;
-  const long long want = 152ll * 4;
+  const long long want = 152ll * (bwd ? 4 : 8);
   const long long ns = a.cu_seqlens ? 1 : a.B;
-  const long long per_seq = (want + ns * pl.tiles - 1) / (ns * pl.tiles);  // units wanted per sequence
+  const long long per_seq = want / (ns * pl.tiles);  // units per sequence: all CTAs resident at once
   const long long len = a.T;
   long long seg = per_seq <= 1 ? len : (len + per_seq - 1) / per_seq;
   seg = (seg + kScanTile - 1) / kScanTile * kScanTile;
@@ -288,6 +308,9 @@ ScanP scan_params(const rdn_scan_args &a, const ScanPlan &pl) {
   p.ns = a.cu_seqlens ? a.num_seqs : a.B;
   p.softplus = a.dt_softplus;
   p.seg = pl.seg; p.units = pl.units; p.units_row = pl.units_row; p.tiles_g = pl.tiles_g;
+  const size_t esz = a.dtype == RDN_BF16 ? 2 : 4;
+  p.bc_vec = a.S % (16 / esz) == 0 &&
+             (((uintptr_t)a.Bm | (uintptr_t)a.Cm | (size_t)a.b_ld * esz | (size_t)a.c_ld * esz) & 15) == 0;
   p.x_ld = a.x_ld; p.dt_ld = a.dt_ld; p.z_ld = a.z_ld; p.b_ld = a.b_ld; p.c_ld = a.c_ld;
   p.out_ld = a.out_ld; p.dout_ld = a.dout_ld; p.dx_ld = a.dx_ld; p.ddt_ld = a.ddt_ld; p.dz_ld = a.dz_ld;
   p.x = a.x; p.dt = a.dt; p.z = a.z; p.Bm = a.Bm; p.Cm = a.Cm; p.dout = a.dout;
@@ -309,7 +332,7 @@ bool scan_vec(const rdn_scan_args &a, bool bwd) {
 }
 
 size_t scan_fwd_bytes(const rdn_scan_args &a) {
-  const ScanPlan pl = scan_plan(a);
+  const ScanPlan pl = scan_plan(a, false);
   if (!pl.split) return 0;
   return round256(sizeof(float) * (size_t)pl.units * a.D * 4 * pl.L) +
          round256(sizeof(float) * (size_t)pl.units * a.D);
@@ -325,7 +348,7 @@ cudaError_t scan_run(const rdn_scan_args &a, const ScanP &p, const ScanPlan &pl,
 }  // namespace
 
 cudaError_t launch_scan_fwd(const rdn_scan_args &a, cudaStream_t s) {
-  const ScanPlan pl = scan_plan(a);
+  const ScanPlan pl = scan_plan(a, false);
   ScanP p = scan_params(a, pl);
   if (pl.split) {
     p.carry = static_cast<float *>(a.workspace);

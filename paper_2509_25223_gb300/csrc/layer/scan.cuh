@@ -9,11 +9,13 @@
 // registers from one end of a run of tokens to the other and touch HBM once.
 //
 // A warp's lanes are L state lanes (4 states each, L = 2 .. 16) times 32 / L
-// channel lanes (2 channels each): 8 (channel, state) pairs per lane.  B and C
-// are read once per 2 channels, and a sum over the states takes log2(L)
-// exchanges, where a thread per channel would read all of B and C for each of
-// its channels (twice the shared-memory reads) and sums over the channels
-// (backward: dB, dC) would exchange every state.
+// channel lanes (4 channels each): 16 (channel, state) pairs per lane, worked
+// on as packed pairs of channels.  What limits the loop beside the FMA pipe and
+// the exponentials is what shared memory hands out (128 bytes per clock and SM,
+// to the lanes, equal addresses or not): per token a lane takes 4 states of B
+// and C and 4 channels' (dl, dl x), 12 to 16 words for 16 pairs.  A lane per
+// channel takes 34 for as many, 2 channels by 4 states 24 (measured 1.5 times
+// as long).  A sum over the states takes 3 exchanges for 4 channels.
 //
 // A sequence is cut into units of `seg` tokens where there are too few
 // channels and sequences to fill the GPU: a first pass finds each unit's end
@@ -25,7 +27,7 @@
 
 namespace rdn {
 
-constexpr int kScanThreads = 128, kScanWarps = 4;
+constexpr int kScanThreads = 64, kScanWarps = 2;  // small CTAs: their number divides over the SMs finely
 constexpr int kScanTile = RDN_SCAN_CHUNK;  // tokens staged at a time, and between kept states
 
 // exp2 of the decay's exponent.  ex2.approx comes out low by about 2e-8 on
@@ -36,14 +38,84 @@ constexpr int kScanTile = RDN_SCAN_CHUNK;  // tokens staged at a time, and betwe
 // 1.5e-8 there.
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kExpShift = 2.5e-8f;
-__device__ __forceinline__ float decay(float dl, float A2) {
+__device__ __forceinline__ float ex2(float x) {
   float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaf(dl, A2, kExpShift)));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float decay(float dl, float A2) { return ex2(fmaf(dl, A2, kExpShift)); }
 
-// softplus, and its derivative from its argument
-__device__ __forceinline__ float softplusf(float v) { return v > 20.f ? v : log1pf(__expf(v)); }
+// Pairs of fp32 values in one register pair: one issue slot for two operations
+// (the FMA pipe's rate is the same; the slots go to the exponentials and loads).
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pack2(float lo, float hi) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(f2 v, float &lo, float &hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float sum2(f2 v) {
+  float lo, hi;
+  unpack2(v, lo, hi);
+  return lo + hi;
+}
+// decay() of a pair
+__device__ __forceinline__ f2 decay2(f2 dl, f2 A2, f2 shift) {
+  float lo, hi;
+  unpack2(fma2(dl, A2, shift), lo, hi);
+  return pack2(ex2(lo), ex2(hi));
+}
+
+// softplus(v) = max(v, 0) + log1p(u), u = exp(-|v|); log1p(u) = 2 atanh(t), t = u / (2 + u) <= 1/3,
+// with atanh(t) / t as a polynomial in t^2 fitted to 4e-9 on [0, 1/9].  About 14 instructions, two
+// units in the last place at every size of the result (the library's log1p takes three times as
+// many, and log2 of 1 + u would lose a small u).
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float softplusf(float v) {
+  const float u = ex2(fabsf(v) * -kLog2e);
+  const float t = u * rcp_approx(2.f + u), q = t * t;
+  float a = fmaf(0.28178335f, q, 0.27960603f);
+  a = fmaf(a, q, 0.40024910f);
+  a = fmaf(a, q, 0.66666315f);
+  a = fmaf(a, q, 2.f);
+  return fmaf(t, a, fmaxf(v, 0.f));
+}
+// of a pair
+__device__ __forceinline__ f2 softplus2(f2 v) {
+  float x, y;
+  unpack2(v, x, y);
+  const float u0 = ex2(fabsf(x) * -kLog2e), u1 = ex2(fabsf(y) * -kLog2e);
+  const f2 u = pack2(u0, u1);
+  float w0, w1;
+  unpack2(add2(u, pack2(2.f, 2.f)), w0, w1);
+  const f2 t = mul2(u, pack2(rcp_approx(w0), rcp_approx(w1))), q = mul2(t, t);
+  f2 a = fma2(pack2(0.28178335f, 0.28178335f), q, pack2(0.27960603f, 0.27960603f));
+  a = fma2(a, q, pack2(0.40024910f, 0.40024910f));
+  a = fma2(a, q, pack2(0.66666315f, 0.66666315f));
+  a = fma2(a, q, pack2(2.f, 2.f));
+  return fma2(t, a, pack2(fmaxf(x, 0.f), fmaxf(y, 0.f)));
+}
 
 struct ScanP {
   int B, T, D, S, G, ns;
@@ -51,6 +123,7 @@ struct ScanP {
   int seg;          // tokens per unit (a multiple of kScanTile)
   int units, units_row;  // units of the call (packed: a bound); without cu: per sequence
   int tiles_g;      // channel tiles per group
+  bool bc_vec;      // rows of B and C on 16 bytes
   long long x_ld, dt_ld, z_ld, b_ld, c_ld, out_ld, dout_ld, dx_ld, ddt_ld, dz_ld;
   const void *x, *dt, *z, *Bm, *Cm, *dout;
   const float *A, *Dskip, *dt_bias, *h0, *dhT;
@@ -128,75 +201,122 @@ __device__ __forceinline__ Unit find_unit(const ScanP &p, int u) {
 // The shape of a CTA's work for L state lanes.
 template <typename T, int L, bool VEC>
 struct ScanShape {
-  static constexpr int CW = 64 / L;                // channels of a warp
+  static constexpr int CL = 32 / L;                // channel lanes
+  static constexpr int CW = 4 * CL;                // channels of a warp
   static constexpr int CT = kScanWarps * CW;       // and of a CTA
   static constexpr int SP = 4 * L;                 // states, padded
   static constexpr int V = VEC ? kVec<T> : 1;      // channels per global access
   static constexpr int COLS = CT / V;              // accesses per token
   static constexpr int NV = (kScanTile * COLS + kScanThreads - 1) / kScanThreads;  // per thread
-  static constexpr int NB = kScanTile * SP / kScanThreads;  // B (or C) elements per thread
+  static constexpr int TOK = kScanThreads / COLS > 0 ? kScanThreads / COLS : 1;    // tokens between a thread's accesses
+  using K = Pack<T, V>;
+  using Raw = typename K::Raw;
+  // access i of this thread: its token and its first channel in the tile
+  __device__ static int tok(int i) { return (i * kScanThreads + (int)threadIdx.x) / COLS; }
+  __device__ static int chan(int i) { return (i * kScanThreads + (int)threadIdx.x) % COLS * V; }
 };
 
-// A thread's part of one operand's tile (kScanTile tokens x CT channels), as loaded.
-template <typename T, int L, bool VEC>
-struct TileRows {
-  using Sh = ScanShape<T, L, VEC>;
-  using K = Pack<T, Sh::V>;
-  typename K::Raw raw[Sh::NV];
-  // tokens [0, ntok) at base + t * ld, channels [0, nch) of the tile
-  __device__ void load(const T *base, long long ld, int ntok, int nch) {
-#pragma unroll
-    for (int i = 0; i < Sh::NV; ++i) {
-      const int id = i * kScanThreads + threadIdx.x, t = id / Sh::COLS, c = id % Sh::COLS * Sh::V;
-      raw[i] = base && t < ntok && c < nch ? K::ld(base + t * ld + c) : K::zero();
+// A slot of shared memory filled from global memory (zero if src is NULL),
+// 16-byte ones without a register in between (fetched() waits for them).
+template <typename Raw>
+__device__ __forceinline__ void fetch(Raw *slot, const void *src) {
+  if constexpr (sizeof(Raw) == 16) {
+    if (src) {
+      const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot);
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src) : "memory");
+      return;
     }
   }
-  __device__ void get(int i, float (&v)[Sh::V]) const { K::get(raw[i], v); }
-};
+  Raw v{};
+  if (src) v = *static_cast<const Raw *>(src);
+  *slot = v;
+}
+__device__ __forceinline__ void fetched() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// A thread's part of B or C: kScanTile tokens x SP states (zero past S).
-template <typename T, int L>
-struct TileBC {
-  static constexpr int SP = 4 * L, NB = kScanTile * SP / kScanThreads;
-  T raw[NB];
-  __device__ void load(const T *base, long long ld, int ntok, int S) {
+// One operand's tile into the threads' own slots: tokens [0, ntok) from `base`
+// (channel column included), channels [0, nch).
+template <typename Sh, typename T>
+__device__ __forceinline__ void fetch_rows(typename Sh::Raw (*slot)[kScanThreads], const T *base, long long ld, int ntok,
+                                           int nch) {
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const int id = i * kScanThreads + threadIdx.x, t = id / SP, n = id % SP;
-      raw[i] = t < ntok && n < S ? base[t * ld + n] : from_f32<T>(0.f);
+  for (int i = 0; i < Sh::NV; ++i) {
+    const int t = Sh::tok(i), c = Sh::chan(i);
+    fetch(&slot[i][threadIdx.x], base && t < ntok && c < nch ? base + t * ld + c : nullptr);
+  }
+}
+// B or C of a tile, in the inputs' type (zero past S and ntok)
+template <int SP, typename T>
+__device__ __forceinline__ void fetch_states(T (*dst)[SP], const T *base, long long ld, int ntok, int S, bool vec) {
+  constexpr int V = kVec<T>;
+  if (vec) {
+    for (int id = threadIdx.x; id < kScanTile * SP / V; id += kScanThreads) {
+      const int t = id / (SP / V), n = id % (SP / V) * V;
+      fetch(reinterpret_cast<uint4 *>(&dst[t][n]), t < ntok && n < S ? base + t * ld + n : nullptr);
+    }
+  } else {
+    for (int id = threadIdx.x; id < kScanTile * SP; id += kScanThreads) {
+      const int t = id / SP, n = id % SP;
+      dst[t][n] = t < ntok && n < S ? base[t * ld + n] : from_f32<T>(0.f);
     }
   }
-};
+}
 
-// y[t] over 4 tokens, each a lane's part of two channels' sums over the states
-// (v[t][0]: the channel cl * 2 + (sl & 1), v[t][1]: the other one), summed over
-// the L state lanes and written to dst[token][channel] (row pitch `pitch`).
-// The order of the channels differs between the lanes that exchange, so the
-// first exchange needs no selects; the next two split the tokens.
+// 4 consecutive states of B or C from shared memory, each in both halves of a
+// pair; in the order n ^ perm (perm < 4, the lane's own).
+__device__ __forceinline__ void states4(const __nv_bfloat16 *row, int perm, f2 (&v)[4]) {
+  const uint2 w = *reinterpret_cast<const uint2 *>(row);
+  const uint32_t lo = perm & 2 ? w.y : w.x, hi = perm & 2 ? w.x : w.y;
+  const uint32_t even = perm & 1 ? 0x3244u : 0x1044u, odd = perm & 1 ? 0x1044u : 0x3244u;  // bytes (x y 0 0)
+  const uint32_t a[4] = {__byte_perm(lo, 0u, even), __byte_perm(lo, 0u, odd), __byte_perm(hi, 0u, even),
+                         __byte_perm(hi, 0u, odd)};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = pack2(__uint_as_float(a[i]), __uint_as_float(a[i]));
+}
+// out[i] = v[i ^ perm]
+__device__ __forceinline__ void permute(const float (&v)[4], int perm, float (&out)[4]) {
+  const bool b0 = perm & 1, b1 = perm & 2;
+  float a[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] = b0 ? v[i ^ 1] : v[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out[i] = b1 ? a[i ^ 2] : a[i];
+}
+__device__ __forceinline__ void states4(const float *row, int perm, f2 (&v)[4]) {
+  const float4 w = *reinterpret_cast<const float4 *>(row);
+  const float a[4] = {w.x, w.y, w.z, w.w};
+  float b[4];
+  permute(a, perm, b);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = pack2(b[i], b[i]);
+}
+
+// Where the 16-byte entry of channel pair c lies in a row of them: the threads
+// of a phase, which write the same entry of consecutive groups of 4 or 2 pairs,
+// then write 8 different ones of the 8 that a 128-byte line of banks holds.
+__device__ __forceinline__ int spread16(int c) { return c ^ ((c >> 3) & 3); }
+
+// A lane's part (pairs v[0], v[1] of channels) of the sums over the states,
+// summed over the L state lanes into row[channel].  v[0] holds the pair
+// 2 cl + (sl & 1) of the warp, v[1] the other: the lanes that exchange hold
+// them in opposite orders, so the first exchange needs no selects.
 template <int L>
-__device__ __forceinline__ void sum_states(float (&v)[4][2], float *dst, int pitch, int ch, int sl) {
-  float r[4];
-#pragma unroll
-  for (int t = 0; t < 4; ++t) r[t] = v[t][0] + __shfl_xor_sync(0xffffffffu, v[t][1], 1);
+__device__ __forceinline__ void sum_states(const f2 (&v)[2], float *row, int first, int sl) {
+  constexpr unsigned all = 0xffffffffu;
+  float a, b, c, d;
+  unpack2(v[0], a, b);
+  unpack2(v[1], c, d);
+  a += __shfl_xor_sync(all, c, 1);
+  b += __shfl_xor_sync(all, d, 1);
+  const int pair = first + 2 * (sl & 1);  // (first: channel of the lane's first pair in the tile)
   if (L == 2) {
-#pragma unroll
-    for (int t = 0; t < 4; ++t) dst[t * pitch + ch] = r[t];
+    *reinterpret_cast<float2 *>(row + pair) = make_float2(a, b);
     return;
   }
-  float r2[2];
-  const bool b1 = sl & 2;
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-    r2[t] = (b1 ? r[2 * t + 1] : r[2 * t]) + __shfl_xor_sync(0xffffffffu, b1 ? r[2 * t] : r[2 * t + 1], 2);
-  if (L == 4) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) dst[(2 * t + (b1 ? 1 : 0)) * pitch + ch] = r2[t];
-    return;
-  }
-  const bool b2 = sl & 4;
-  float r1 = (b2 ? r2[1] : r2[0]) + __shfl_xor_sync(0xffffffffu, b2 ? r2[0] : r2[1], 4);
-  if (L == 16) r1 += __shfl_xor_sync(0xffffffffu, r1, 8);
-  if (L == 8 || !(sl & 8)) dst[((b2 ? 2 : 0) + (b1 ? 1 : 0)) * pitch + ch] = r1;
+  const bool hi = sl & 2;
+  float r = (hi ? b : a) + __shfl_xor_sync(all, hi ? a : b, 2);
+  if (L >= 8) r += __shfl_xor_sync(all, r, 4);
+  if (L >= 16) r += __shfl_xor_sync(all, r, 8);
+  if (sl < 4) row[pair + (hi ? 1 : 0)] = r;
 }
 
 // 4 consecutive states n0 .. n0 + 3 of a row of S (zero past S), and their store
@@ -219,6 +339,66 @@ __device__ __forceinline__ void store_states(float *row, int S, int n0, const fl
   }
 }
 
+// V channels' step sizes from dt: bias, softplus; none for a token past the
+// end (dl = 0: a decay of exactly 1, nothing added).
+template <int V>
+__device__ __forceinline__ void step_sizes(const ScanP &p, const float *bias, bool live, float (&dl)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) dl[e] += bias[e];
+  if (p.softplus) {
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+      for (int e = 0; e < V; e += 2) unpack2(softplus2(pack2(dl[e], dl[e + 1])), dl[e], dl[e + 1]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) dl[e] = softplusf(dl[e]);
+    }
+  }
+  if (!live) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) dl[e] = 0.f;
+  }
+}
+// Two values of each of V channels from channel c on into a token's row of
+// entries (a, a', b, b') of channel pairs.
+template <int V>
+__device__ __forceinline__ void store_two(float4 *row, int c, const float (&a)[V], const float (&b)[V]) {
+  if constexpr (V % 2 == 0) {
+#pragma unroll
+    for (int e = 0; e < V; e += 2) row[spread16((c + e) / 2)] = make_float4(a[e], a[e + 1], b[e], b[e + 1]);
+  } else {
+    float *at = reinterpret_cast<float *>(row + spread16(c / 2)) + (c & 1);
+    at[0] = a[0];
+    at[2] = b[0];
+  }
+}
+// (dl, dl x) of V channels
+template <int V>
+__device__ __forceinline__ void store_steps(float4 *row, int c, const float (&dl)[V], const float (&x)[V]) {
+  float dx[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) dx[e] = dl[e] * x[e];
+  store_two<V>(row, c, dl, dx);
+}
+// States n0 .. n0 + 3 of the channel pair `pair` of the tile into block `block`
+// of to[..][D][S].
+__device__ __forceinline__ void store_pairs(float *to, long long block, bool on, const ScanP &p, int c0, int pair,
+                                            int nch, int n0, const f2 (&h)[4]) {
+  float v[2][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) unpack2(h[i], v[0][i], v[1][i]);
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (on && pair + e < nch) store_states(to + ((size_t)block * p.D + c0 + pair + e) * p.S, p.S, n0, v[e]);
+}
+
+// Dynamic shared memory beyond 48 KB has to be asked for.
+template <typename F>
+inline cudaError_t allow_smem(F kernel, int bytes) {
+  return bytes <= 48 * 1024 ? cudaSuccess
+                            : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
 struct ScanPlan {
   int L, CT, tiles_g, tiles;
   int seg, units, units_row;
@@ -227,7 +407,7 @@ struct ScanPlan {
 long long scan_slots(const rdn_scan_args &a);
 // The forward without out (and hT): the kept states alone, into p.chunks.
 cudaError_t scan_states(const rdn_scan_args &a, ScanP p, const ScanPlan &pl, cudaStream_t s);
-ScanPlan scan_plan(const rdn_scan_args &a);
+ScanPlan scan_plan(const rdn_scan_args &a, bool bwd);
 ScanP scan_params(const rdn_scan_args &a, const ScanPlan &pl);
 bool scan_vec(const rdn_scan_args &a, bool bwd);
 

@@ -23,14 +23,24 @@ namespace {
 
 constexpr int kSub = 8;  // tokens whose states are in registers together
 
+template <typename T, int L, bool VEC>
+struct CarrySmem {
+  using Sh = ScanShape<T, L, VEC>;
+  float4 dg[kScanTile][Sh::CT / 2];                  // (dl, dl', gy, gy') of a pair, at spread16
+  typename Sh::Raw raw[3][Sh::NV][kScanThreads];     // each thread's dt, z, dout of the next tile
+  T C[2][kScanTile][Sh::SP];
+  float bias[Sh::CT];
+};
+
 // The first pass: each unit's q at its first token from q = 0 past its end,
 // and the sum of its dl (units but the first of a sequence).
 template <typename T, int L, bool VEC>
-__global__ void __launch_bounds__(kScanThreads) scan_bwd_carry_kernel(ScanP p) {
+__global__ void __launch_bounds__(kScanThreads, 7) scan_bwd_carry_kernel(ScanP p) {
   using Sh = ScanShape<T, L, VEC>;
-  using Rows = TileRows<T, L, VEC>;
-  __shared__ __align__(16) float2 s_dg[kScanTile][Sh::CT];  // (dl, gy)
-  __shared__ __align__(16) float s_C[kScanTile][Sh::SP];
+  using K = typename Sh::K;
+  constexpr int V = Sh::V;
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  CarrySmem<T, L, VEC> &sm = *reinterpret_cast<CarrySmem<T, L, VEC> *>(smem_raw);
   const Unit w = find_unit(p, blockIdx.x);
   if (!w.ok || w.j == 0) return;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -38,87 +48,94 @@ __global__ void __launch_bounds__(kScanThreads) scan_bwd_carry_kernel(ScanP p) {
   const int g = blockIdx.y / p.tiles_g, Dg = p.D / p.G;
   const int c0 = g * Dg + blockIdx.y % p.tiles_g * Sh::CT;
   const int nch = min(Sh::CT, (g + 1) * Dg - c0);
-  float A2[2][4], q[2][4], sumd[2] = {0.f, 0.f};
-  const int ch0 = warp * Sh::CW + cl * 2;
+  const int first = warp * Sh::CW + cl * 4;
+  const int at[2] = {spread16(first / 2), spread16(first / 2 + 1)};
+  for (int c = tid; c < Sh::CT; c += kScanThreads) sm.bias[c] = p.dt_bias && c < nch ? p.dt_bias[c0 + c] : 0.f;
+  f2 A2[2][4], q[2][4], sumd[2];
+  const f2 shift = pack2(kExpShift, kExpShift), zero2 = pack2(0.f, 0.f);
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+  for (int j = 0; j < 2; ++j) {
+    float a[2][4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[e][i] = 0.f;
+      if (first + 2 * j + e < nch) load_states(p.A + (size_t)(c0 + first + 2 * j + e) * p.S, p.S, n0, a[e]);
+    }
+    sumd[j] = zero2;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      q[j][i] = 0.f;
-      A2[j][i] = ch0 + j < nch && n0 + i < p.S ? __ldg(p.A + (size_t)(c0 + ch0 + j) * p.S + n0 + i) * kLog2e : 0.f;
+      A2[j][i] = pack2(a[0][i] * kLog2e, a[1][i] * kLog2e);
+      q[j][i] = zero2;
     }
+  }
   const long long r0 = w.begin + (long long)w.j * p.seg;
   const long long r1 = min(r0 + p.seg, w.end);
-  const T *DT = (const T *)p.dt + c0, *DO = (const T *)p.dout + c0;
-  const T *Z = p.z ? (const T *)p.z + c0 : nullptr;
-  const T *Cm = (const T *)p.Cm + (size_t)g * p.S;
-  Rows dt, z, dout;
-  TileBC<T, L> tc;
-  auto load = [&](long long r) {
-    const int ntok = r < r0 ? 0 : (int)min((long long)kScanTile, r1 - r);
-    dt.load(DT + r * p.dt_ld, p.dt_ld, ntok, nch);
-    dout.load(DO + r * p.dout_ld, p.dout_ld, ntok, nch);
-    z.load(Z ? Z + r * p.z_ld : nullptr, p.z_ld, ntok, nch);
-    tc.load(Cm + r * p.c_ld, p.c_ld, ntok, p.S);
-  };
   const long long last = r0 + (r1 - 1 - r0) / kScanTile * kScanTile;
-  load(last);
-  for (long long r = last; r >= r0; r -= kScanTile) {
+  const T *Cm = (const T *)p.Cm + (size_t)g * p.S;
+  auto load = [&](long long r, int b) {
+    const int ntok = r < r0 ? 0 : (int)min((long long)kScanTile, r1 - r);
+    fetch_rows<Sh>(sm.raw[0], (const T *)p.dt + c0 + r * p.dt_ld, p.dt_ld, ntok, nch);
+    if (p.z) fetch_rows<Sh>(sm.raw[1], (const T *)p.z + c0 + r * p.z_ld, p.z_ld, ntok, nch);
+    fetch_rows<Sh>(sm.raw[2], (const T *)p.dout + c0 + r * p.dout_ld, p.dout_ld, ntok, nch);
+    fetch_states(sm.C[b], Cm + r * p.c_ld, p.c_ld, ntok, p.S, p.bc_vec);
+  };
+  load(last, 0);
+  __syncthreads();  // bias
+  int b = 0;
+  for (long long r = last; r >= r0; r -= kScanTile, b ^= 1) {
     const int ntok = (int)min((long long)kScanTile, r1 - r);
+    fetched();
 #pragma unroll
     for (int i = 0; i < Sh::NV; ++i) {
-      const int id = i * kScanThreads + tid, t = id / Sh::COLS, c = id % Sh::COLS * Sh::V;
+      const int t = Sh::tok(i), c = Sh::chan(i);
       if (t >= kScanTile) break;
-      float dv[Sh::V], zv[Sh::V], gv[Sh::V];
-      dt.get(i, dv);
-      z.get(i, zv);
-      dout.get(i, gv);
+      float dl[V], gv[V], zv[V];
+      K::get(sm.raw[0][i][tid], dl);
+      K::get(sm.raw[2][i][tid], gv);
+      step_sizes<V>(p, sm.bias + c, t < ntok, dl);
+      if (p.z) {
+        K::get(sm.raw[1][i][tid], zv);
 #pragma unroll
-      for (int e = 0; e < Sh::V; ++e) {
-        float v = dv[e];
-        if (p.dt_bias && c + e < nch) v += __ldg(p.dt_bias + c0 + c + e);
-        s_dg[t][c + e] = make_float2(p.softplus ? softplusf(v) : v, p.z ? gv[e] * siluf(zv[e]) : gv[e]);
+        for (int e = 0; e < V; ++e) gv[e] *= siluf(zv[e]);
       }
-    }
-#pragma unroll
-    for (int i = 0; i < Sh::NB; ++i) {
-      const int id = i * kScanThreads + tid;
-      s_C[id / Sh::SP][id % Sh::SP] = to_f32<T>(tc.raw[i]);
+      store_two<V>(sm.dg[t], c, dl, gv);
     }
     __syncthreads();
-    load(r - kScanTile);
-#pragma unroll 4
+    load(r - kScanTile, b ^ 1);
+#pragma unroll 2
     for (int t = ntok - 1; t >= 0; --t) {
-      const float4 c4 = *reinterpret_cast<const float4 *>(&s_C[t][n0]);
-      const float cc[4] = {c4.x, c4.y, c4.z, c4.w};
+      f2 cc[4];
+      states4(&sm.C[b][t][n0], 0, cc);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const float2 d = s_dg[t][ch0 + j];
-        sumd[j] += d.x;
+        const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dg[t][at[j]]);
+        sumd[j] = add2(sumd[j], d.x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[j][i] = decay(d.x, A2[j][i]) * fmaf(cc[i], d.y, q[j][i]);
+        for (int i = 0; i < 4; ++i) q[j][i] = mul2(decay2(d.x, A2[j][i], shift), fma2(cc[i], d.y, q[j][i]));
       }
     }
     __syncthreads();
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    if (ch0 + j >= nch) continue;
-    const size_t u = blockIdx.x, d = c0 + ch0 + j;
-    if (sl == 0) p.sumd[u * p.D + d] = sumd[j];
-    *reinterpret_cast<float4 *>(p.carry + (u * p.D + d) * Sh::SP + n0) =
-        make_float4(q[j][0], q[j][1], q[j][2], q[j][3]);
+    const size_t u = blockIdx.x;
+    float s[2], v[2][4];
+    unpack2(sumd[j], s[0], s[1]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(q[j][i], v[0][i], v[1][i]);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      if (first + 2 * j + e >= nch) continue;
+      const size_t d = c0 + first + 2 * j + e;
+      if (sl == 0) p.sumd[u * p.D + d] = s[e];
+      *reinterpret_cast<float4 *>(p.carry + (u * p.D + d) * Sh::SP + n0) = make_float4(v[e][0], v[e][1], v[e][2], v[e][3]);
+    }
   }
 }
 
-template <int L>
-struct BwdShape {
-  static constexpr int CL = 32 / L;                // channel lanes
-  static constexpr int PB = CL < 4 ? CL : 4;       // orders of a lane's four states (n ^ (cl % PB))
-};
-
 // The sums over a warp's channel lanes of db[i] and dc[i] (i-th state in this
-// lane's order), written to red[0 .. 4 L) (dB) and red[4 L .. 8 L) (dC).
+// lane's order, i ^ (cl & 3)), written to red[0 .. 4 L) (dB) and red[4 L .. 8 L) (dC).
 template <int L>
 __device__ __forceinline__ void sum_channels(const float (&db)[4], const float (&dc)[4], int sl, int cl,
                                              float *red) {
@@ -147,232 +164,250 @@ __device__ __forceinline__ void sum_channels(const float (&db)[4], const float (
   if (L == 4 || !(cl & 8)) r[hi ? 4 * L : 0] = v;
 }
 
-// out[i] = v[i ^ perm]
-__device__ __forceinline__ void permute(const float (&v)[4], int perm, float (&out)[4]) {
-  const bool b0 = perm & 1, b1 = perm & 2;
-  float a[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) a[i] = b0 ? v[i ^ 1] : v[i];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) out[i] = b1 ? a[i ^ 2] : a[i];
-}
-
 template <typename T, int L, bool VEC>
 struct BwdSmem {
   using Sh = ScanShape<T, L, VEC>;
-  static constexpr int PB = BwdShape<L>::PB;
-  float2 dx[kScanTile][Sh::CT];                    // (dl, dl x)
-  float gy[kScanTile][Sh::CT];
-  float B[kScanTile][PB][Sh::SP], C[kScanTile][PB][Sh::SP];  // in each of the PB orders
-  float sums[3][kScanTile][Sh::CT];                // sum_n g B, sum_n A2 q h, y
-  float red[kScanWarps][kScanTile][2 * Sh::SP];    // dB, dC of each warp's channels
-  float acc[2][Sh::V][kScanThreads];               // dD and ddt_bias of a thread's elements
+  float4 dx[kScanTile][Sh::CT / 2];                  // (dl, dl', dl x, dl' x') of a pair, at spread16
+  float2 gy[kScanTile][Sh::CT / 2];
+  float sums[3][kScanTile][Sh::CT];                  // sum_n g B, sum_n A2 q h, y
+  float red[kScanWarps][kScanTile][2 * Sh::SP];      // dB, dC of each warp's channels
+  static constexpr int AC = Sh::COLS > kScanThreads ? Sh::COLS / kScanThreads : 1;  // columns of a thread
+  float acc[2][AC * Sh::V][kScanThreads];            // dD and ddt_bias of a thread's elements
+  float4 kept[4][kScanThreads];                      // each lane's states before the tile
+  typename Sh::Raw raw[2][4][Sh::NV][kScanThreads];  // each thread's x, dt, z, dout: this tile's and the next's
+  T B[2][kScanTile][Sh::SP], C[2][kScanTile][Sh::SP];
+  float bias[Sh::CT], D[Sh::CT];
 };
 
 template <typename T, int L, bool VEC>
-__global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(ScanP p) {
+__global__ void __launch_bounds__(kScanThreads, 4) scan_bwd_kernel(ScanP p) {
   using Sh = ScanShape<T, L, VEC>;
-  using Rows = TileRows<T, L, VEC>;
-  using K = typename Rows::K;
-  using Sm = BwdSmem<T, L, VEC>;
+  using K = typename Sh::K;
+  constexpr int V = Sh::V;
   extern __shared__ __align__(16) unsigned char smem_raw[];
+  using Sm = BwdSmem<T, L, VEC>;
   Sm &sm = *reinterpret_cast<Sm *>(smem_raw);
   const Unit w = find_unit(p, blockIdx.x);
   const size_t u = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int sl = lane % L, cl = lane / L, n0 = sl * 4, perm = cl % Sm::PB;
+  const int sl = lane % L, cl = lane / L, n0 = sl * 4, perm = cl & (Sh::CL < 4 ? Sh::CL - 1 : 3);
   const int g = blockIdx.y / p.tiles_g, Dg = p.D / p.G;
   const int c0 = g * Dg + blockIdx.y % p.tiles_g * Sh::CT;
   const int nch = min(Sh::CT, (g + 1) * Dg - c0);
-  int ch[2];
+  const int first = warp * Sh::CW + cl * 4;
+  int pair[2], at[2];  // this lane's channel pairs in the tile (opposite orders in the lanes that exchange)
 #pragma unroll
-  for (int j = 0; j < 2; ++j) ch[j] = warp * Sh::CW + cl * 2 + (j ^ (sl & 1));
-  float A2[2][4], q[2][4], dA[2][4];
+  for (int j = 0; j < 2; ++j) {
+    pair[j] = first / 2 + (j ^ (sl & 1));
+    at[j] = spread16(pair[j]);
+  }
+  for (int c = tid; c < Sh::CT; c += kScanThreads) {
+    sm.bias[c] = p.dt_bias && c < nch ? p.dt_bias[c0 + c] : 0.f;
+    sm.D[c] = p.Dskip && c < nch ? p.Dskip[c0 + c] : 0.f;
+  }
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+  for (int e = 0; e < Sm::AC * V; ++e) sm.acc[0][e][tid] = sm.acc[1][e][tid] = 0.f;
+  const f2 shift = pack2(kExpShift, kExpShift), zero2 = pack2(0.f, 0.f);
+  f2 A2[2][4], q[2][4], dA[2][4];  // [channel pair][state n0 + (i ^ perm)]
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    float a[2][4], v[2][4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int ch = 2 * pair[j] + e;
+      const size_t d = c0 + ch;
+      float ta[4] = {0.f, 0.f, 0.f, 0.f}, tv[4] = {0.f, 0.f, 0.f, 0.f};
+      if (ch < nch) {
+        load_states(p.A + d * p.S, p.S, n0, ta);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ta[i] *= kLog2e;
+        if (w.ok) {  // q past the unit's end, over the units after it
+          if (p.dhT) load_states(p.dhT + ((size_t)w.s * p.D + d) * p.S, p.S, n0, tv);
+          for (int k = w.n - 1; k > w.j; --k) {
+            const size_t o = u - w.j + k;
+            const float sd = p.sumd[o * p.D + d];
+            const float4 x = *reinterpret_cast<const float4 *>(p.carry + (o * p.D + d) * Sh::SP + n0);
+            const float xx[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tv[i] = fmaf(decay(sd, ta[i]), tv[i], xx[i]);
+          }
+        }
+      }
+      permute(ta, perm, a[e]);
+      permute(tv, perm, v[e]);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int n = n0 + (i ^ perm);
-      q[j][i] = dA[j][i] = 0.f;
-      A2[j][i] = ch[j] < nch && n < p.S ? __ldg(p.A + (size_t)(c0 + ch[j]) * p.S + n) * kLog2e : 0.f;
-    }
-#pragma unroll
-  for (int e = 0; e < Sh::V; ++e) sm.acc[0][e][tid] = sm.acc[1][e][tid] = 0.f;
-  const long long r0 = w.ok ? w.begin + (long long)w.j * p.seg : 0;
-  const long long r1 = w.ok ? min(r0 + p.seg, w.end) : 0;
-  if (w.ok) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {  // q past the unit's end
-      if (ch[j] >= nch) continue;
-      const size_t d = c0 + ch[j];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int n = n0 + (i ^ perm);
-        if (p.dhT && n < p.S) q[j][i] = p.dhT[((size_t)w.s * p.D + d) * p.S + n];
-      }
-      for (int k = w.n - 1; k > w.j; --k) {
-        const size_t v = u - w.j + k;
-        const float sd = p.sumd[v * p.D + d];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          q[j][i] = fmaf(decay(sd, A2[j][i]), q[j][i], p.carry[(v * p.D + d) * Sh::SP + n0 + (i ^ perm)]);
-      }
+      A2[j][i] = pack2(a[0][i], a[1][i]);
+      q[j][i] = pack2(v[0][i], v[1][i]);
+      dA[j][i] = zero2;
     }
   }
+  const long long r0 = w.ok ? w.begin + (long long)w.j * p.seg : 0;
+  const long long r1 = w.ok ? min(r0 + p.seg, w.end) : 0;
+  const long long last = r1 > r0 ? r0 + (r1 - 1 - r0) / kScanTile * kScanTile : r0 - kScanTile;
   const T *X = (const T *)p.x + c0, *DT = (const T *)p.dt + c0, *DO = (const T *)p.dout + c0;
-  const T *Z = p.z ? (const T *)p.z + c0 : nullptr;
   const T *Bm = (const T *)p.Bm + (size_t)g * p.S, *Cm = (const T *)p.Cm + (size_t)g * p.S;
-  Rows x, dt, z, dout;
-  TileBC<T, L> tb, tc;
-  float hn[2][4];  // the state before the tile, in this lane's order
-  auto load = [&](long long r) {
+  auto load = [&](long long r, int b) {
     const int ntok = r < r0 ? 0 : (int)min((long long)kScanTile, r1 - r);
+    fetch_rows<Sh>(sm.raw[b][0], X + r * p.x_ld, p.x_ld, ntok, nch);
+    fetch_rows<Sh>(sm.raw[b][1], DT + r * p.dt_ld, p.dt_ld, ntok, nch);
+    if (p.z) fetch_rows<Sh>(sm.raw[b][2], (const T *)p.z + c0 + r * p.z_ld, p.z_ld, ntok, nch);
+    fetch_rows<Sh>(sm.raw[b][3], DO + r * p.dout_ld, p.dout_ld, ntok, nch);
+    fetch_states(sm.B[b], Bm + r * p.b_ld, p.b_ld, ntok, p.S, p.bc_vec);
+    fetch_states(sm.C[b], Cm + r * p.c_ld, p.c_ld, ntok, p.S, p.bc_vec);
+  };
+  // the kept states before the tile at r: read by this lane alone
+  auto load_kept = [&](long long r) {
     const long long slot = w.chunk0 + (r - w.begin) / kScanTile;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      float v[4] = {0.f, 0.f, 0.f, 0.f};
-      if (ntok && ch[j] < nch && slot < p.slots)
-        load_states(p.chunks + ((size_t)slot * p.D + c0 + ch[j]) * p.S, p.S, n0, v);
-      permute(v, perm, hn[j]);
+    for (int k = 0; k < 4; ++k) {
+      const int ch = 2 * pair[k >> 1] + (k & 1);
+      const bool on = r >= r0 && ch < nch && slot < p.slots;
+      const float *row = p.chunks + ((size_t)slot * p.D + c0 + ch) * p.S;
+      if (p.S % 4 == 0) {
+        fetch(&sm.kept[k][tid], on && n0 < p.S ? row + n0 : nullptr);
+      } else {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (on) load_states(row, p.S, n0, v);
+        sm.kept[k][tid] = make_float4(v[0], v[1], v[2], v[3]);
+      }
     }
-    x.load(X + r * p.x_ld, p.x_ld, ntok, nch);
-    dt.load(DT + r * p.dt_ld, p.dt_ld, ntok, nch);
-    dout.load(DO + r * p.dout_ld, p.dout_ld, ntok, nch);
-    z.load(Z ? Z + r * p.z_ld : nullptr, p.z_ld, ntok, nch);
-    tb.load(Bm + r * p.b_ld, p.b_ld, ntok, p.S);
-    tc.load(Cm + r * p.c_ld, p.c_ld, ntok, p.S);
   };
-  const long long last = r1 > r0 ? r0 + (r1 - 1 - r0) / kScanTile * kScanTile : r0 - kScanTile;
-  if (last >= r0) load(last);
-  for (long long r = last; r >= r0; r -= kScanTile) {
+  if (last >= r0) {
+    load(last, 0);
+    load_kept(last);
+  }
+  __syncthreads();  // bias, D
+  int b = 0;
+  for (long long r = last; r >= r0; r -= kScanTile, b ^= 1) {
     const int ntok = (int)min((long long)kScanTile, r1 - r);
+    fetched();
     // the tile's operands into shared memory
 #pragma unroll
     for (int i = 0; i < Sh::NV; ++i) {
-      const int id = i * kScanThreads + tid, t = id / Sh::COLS, c = id % Sh::COLS * Sh::V;
+      const int t = Sh::tok(i), c = Sh::chan(i);
       if (t >= kScanTile) break;
-      float xv[Sh::V], dv[Sh::V], zv[Sh::V], gv[Sh::V];
-      x.get(i, xv);
-      dt.get(i, dv);
-      z.get(i, zv);
-      dout.get(i, gv);
+      float xv[V], dl[V], gv[V], zv[V];
+      K::get(sm.raw[b][0][i][tid], xv);
+      K::get(sm.raw[b][1][i][tid], dl);
+      K::get(sm.raw[b][3][i][tid], gv);
+      step_sizes<V>(p, sm.bias + c, t < ntok, dl);
+      if (p.z) {
+        K::get(sm.raw[b][2][i][tid], zv);
 #pragma unroll
-      for (int e = 0; e < Sh::V; ++e) {
-        float v = dv[e];
-        if (p.dt_bias && c + e < nch) v += __ldg(p.dt_bias + c0 + c + e);
-        const float dl = p.softplus ? softplusf(v) : v;
-        sm.dx[t][c + e] = make_float2(dl, dl * xv[e]);
-        sm.gy[t][c + e] = p.z ? gv[e] * siluf(zv[e]) : gv[e];
+        for (int e = 0; e < V; ++e) gv[e] *= siluf(zv[e]);
       }
+      store_steps<V>(sm.dx[t], c, dl, xv);
+      float *gy = &sm.gy[t][0].x + c;
+#pragma unroll
+      for (int e = 0; e < V; ++e) gy[e] = gv[e];
     }
-#pragma unroll
-    for (int i = 0; i < Sh::NB; ++i) {
-      const int id = i * kScanThreads + tid, t = id / Sh::SP, n = id % Sh::SP;
-      const float b = to_f32<T>(tb.raw[i]), c = to_f32<T>(tc.raw[i]);
-#pragma unroll
-      for (int k = 0; k < Sm::PB; ++k) {
-        sm.B[t][k][n ^ k] = b;
-        sm.C[t][k][n ^ k] = c;
-      }
-    }
-    float hs[2][4];
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) hs[j][i] = hn[j][i];
-    const Rows xc = x, zc = z, doc = dout, dtc = dt;
     __syncthreads();
-    load(r - kScanTile);
+    load(r - kScanTile, b ^ 1);
 #pragma unroll 1
     for (int half = ntok > kSub ? 1 : 0; half >= 0; --half) {
-      float h0[2][4], hist[kSub][2][4];
+      f2 h0[2][4], hist[kSub][2][4];
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < 2; ++j) {
+        float v[2][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h0[j][i] = hs[j][i];
-      auto step = [&](int t, const float (&from)[2][4], float (&to)[2][4]) {
-        const float4 b4 = *reinterpret_cast<const float4 *>(&sm.B[t][perm][n0]);
-        const float bb[4] = {b4.x, b4.y, b4.z, b4.w};
+        for (int e = 0; e < 2; ++e) {
+          const float4 k = sm.kept[2 * j + e][tid];
+          const float x[4] = {k.x, k.y, k.z, k.w};
+          permute(x, perm, v[e]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h0[j][i] = pack2(v[0][i], v[1][i]);
+      }
+      if (!half) load_kept(r - kScanTile);
+      auto step = [&](int t, const f2 (&from)[2][4], f2 (&to)[2][4]) {
+        f2 bb[4];
+        states4(&sm.B[b][t][n0], perm, bb);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const float2 d = sm.dx[t][ch[j]];
+          const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dx[t][at[j]]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) to[j][i] = fmaf(decay(d.x, A2[j][i]), from[j][i], d.y * bb[i]);
+          for (int i = 0; i < 4; ++i) to[j][i] = fma2(decay2(d.x, A2[j][i], shift), from[j][i], mul2(d.y, bb[i]));
         }
       };
       if (half) {
-#pragma unroll
+#pragma unroll 2
         for (int t = 0; t < kSub; ++t) step(t, h0, h0);
       }
 #pragma unroll
       for (int t = 0; t < kSub; ++t) step(half * kSub + t, t ? hist[t - 1] : h0, hist[t]);
 #pragma unroll
-      for (int t4 = kSub - 4; t4 >= 0; t4 -= 4) {
-        float gB[4][2], Aq[4][2], y[4][2];
+      for (int tl = kSub - 1; tl >= 0; --tl) {
+        const int t = half * kSub + tl;
+        f2 bb[4], cc[4], db[4], dc[4], gB[2], Aq[2], y[2];
+        states4(&sm.B[b][t][n0], perm, bb);
+        states4(&sm.C[b][t][n0], perm, cc);
 #pragma unroll
-        for (int k = 3; k >= 0; --k) {
-          const int tl = t4 + k, t = half * kSub + tl;
+        for (int j = 0; j < 2; ++j) {
+          const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dx[t][at[j]]);
+          const f2 gy = *reinterpret_cast<const f2 *>(&sm.gy[t][pair[j]]);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) gB[k][j] = Aq[k][j] = y[k][j] = 0.f;
-          if (t >= ntok) continue;
-          const float4 b4 = *reinterpret_cast<const float4 *>(&sm.B[t][perm][n0]);
-          const float4 c4 = *reinterpret_cast<const float4 *>(&sm.C[t][perm][n0]);
-          const float bb[4] = {b4.x, b4.y, b4.z, b4.w}, cc[4] = {c4.x, c4.y, c4.z, c4.w};
-          float db[4] = {0.f, 0.f, 0.f, 0.f}, dc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float2 d = sm.dx[t][ch[j]];
-            const float gy = sm.gy[t][ch[j]];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float h = hist[tl][j][i], hp = tl ? hist[tl - 1][j][i] : h0[j][i];
-              const float gg = fmaf(cc[i], gy, q[j][i]);
-              y[k][j] = fmaf(cc[i], h, y[k][j]);
-              gB[k][j] = fmaf(gg, bb[i], gB[k][j]);
-              dc[i] = fmaf(gy, h, dc[i]);
-              db[i] = fmaf(gg, d.y, db[i]);
-              q[j][i] = decay(d.x, A2[j][i]) * gg;
-              const float qh = q[j][i] * hp;
-              dA[j][i] = fmaf(d.x, qh, dA[j][i]);
-              Aq[k][j] = fmaf(A2[j][i], qh, Aq[k][j]);
-            }
+          for (int i = 0; i < 4; ++i) {
+            const f2 h = hist[tl][j][i], hp = tl ? hist[tl > 0 ? tl - 1 : 0][j][i] : h0[j][i];
+            const f2 gr = fma2(cc[i], gy, q[j][i]);
+            y[j] = i ? fma2(cc[i], h, y[j]) : mul2(cc[i], h);
+            gB[j] = i ? fma2(gr, bb[i], gB[j]) : mul2(gr, bb[i]);
+            dc[i] = j ? fma2(gy, h, dc[i]) : mul2(gy, h);
+            db[i] = j ? fma2(gr, d.y, db[i]) : mul2(gr, d.y);
+            q[j][i] = mul2(decay2(d.x, A2[j][i], shift), gr);
+            const f2 qh = mul2(q[j][i], hp);
+            dA[j][i] = fma2(d.x, qh, dA[j][i]);
+            Aq[j] = i ? fma2(A2[j][i], qh, Aq[j]) : mul2(A2[j][i], qh);
           }
-          sum_channels<L>(db, dc, sl, cl, &sm.red[warp][t][0]);
         }
-        const int tb4 = half * kSub + t4;
-        sum_states<L>(gB, &sm.sums[0][tb4][0], Sh::CT, ch[0], sl);
-        sum_states<L>(Aq, &sm.sums[1][tb4][0], Sh::CT, ch[0], sl);
-        sum_states<L>(y, &sm.sums[2][tb4][0], Sh::CT, ch[0], sl);
+        float dbv[4], dcv[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          dbv[i] = sum2(db[i]);
+          dcv[i] = sum2(dc[i]);
+        }
+        sum_channels<L>(dbv, dcv, sl, cl, &sm.red[warp][t][0]);
+        sum_states<L>(gB, sm.sums[0][t], first, sl);
+        sum_states<L>(Aq, sm.sums[1][t], first, sl);
+        if (p.z) sum_states<L>(y, sm.sums[2][t], first, sl);
       }
     }
     __syncthreads();
-    // results of the tile's elements
 #pragma unroll
     for (int i = 0; i < Sh::NV; ++i) {
-      const int id = i * kScanThreads + tid, t = id / Sh::COLS, c = id % Sh::COLS * Sh::V;
+      const int t = Sh::tok(i), c = Sh::chan(i);
       if (t >= ntok || c >= nch) continue;
-      float xv[Sh::V], dv[Sh::V], zv[Sh::V], gv[Sh::V], dx[Sh::V], ddt[Sh::V], dz[Sh::V];
-      xc.get(i, xv);
-      dtc.get(i, dv);
-      zc.get(i, zv);
-      doc.get(i, gv);
-#pragma unroll
-      for (int e = 0; e < Sh::V; ++e) {
-        const float dl = sm.dx[t][c + e].x, gy = sm.gy[t][c + e], gB = sm.sums[0][t][c + e];
-        const float Dk = p.Dskip ? __ldg(p.Dskip + c0 + c + e) : 0.f;
-        float v = dv[e];
-        if (p.dt_bias) v += __ldg(p.dt_bias + c0 + c + e);
-        dx[e] = fmaf(dl, gB, Dk * gy);
-        const float ddl = fmaf(sm.sums[1][t][c + e], kLn2, gB * xv[e]);
-        ddt[e] = p.softplus ? ddl * sigmoidf(v) : ddl;
-        if (p.z) dz[e] = gv[e] * fmaf(Dk, xv[e], sm.sums[2][t][c + e]) * silu_grad(zv[e], sigmoidf(zv[e]));
-        sm.acc[0][e][tid] = fmaf(gy, xv[e], sm.acc[0][e][tid]);
-        sm.acc[1][e][tid] += ddt[e];
-      }
+      float xv[V], dv[V], dx[V], ddt[V];
+      K::get(sm.raw[b][0][i][tid], xv);
+      K::get(sm.raw[b][1][i][tid], dv);
       const long long row = r + t;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float dl = (&sm.dx[t][spread16((c + e) / 2)].x)[(c + e) & 1], gy = (&sm.gy[t][0].x)[c + e];
+        const float gB = sm.sums[0][t][c + e];
+        dx[e] = dl * gB;
+        if (p.Dskip) dx[e] = fmaf(sm.D[c + e], gy, dx[e]);
+        ddt[e] = fmaf(sm.sums[1][t][c + e], kLn2, gB * xv[e]);
+        if (p.softplus) ddt[e] *= sigmoidf(dv[e] + sm.bias[c + e]);
+        float &aD = sm.acc[0][i % Sm::AC * V + e][tid], &ab = sm.acc[1][i % Sm::AC * V + e][tid];
+        aD = fmaf(gy, xv[e], aD);
+        ab += ddt[e];
+      }
       K::st((T *)p.dx + c0 + row * p.dx_ld + c, K::put(dx));
       K::st((T *)p.ddt + c0 + row * p.ddt_ld + c, K::put(ddt));
-      if (p.z) K::st((T *)p.dz + c0 + row * p.dz_ld + c, K::put(dz));
+      if (p.z) {
+        float zv[V], gv[V], dz[V];
+        K::get(sm.raw[b][2][i][tid], zv);
+        K::get(sm.raw[b][3][i][tid], gv);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          float y = sm.sums[2][t][c + e];
+          if (p.Dskip) y = fmaf(sm.D[c + e], xv[e], y);
+          dz[e] = gv[e] * y * silu_grad(zv[e], sigmoidf(zv[e]));
+        }
+        K::st((T *)p.dz + c0 + row * p.dz_ld + c, K::put(dz));
+      }
     }
     for (int i = tid; i < ntok * 2 * Sh::SP; i += kScanThreads) {
       const int t = i / (2 * Sh::SP), n = i % (2 * Sh::SP);
@@ -386,22 +421,30 @@ __global__ void __launch_bounds__(kScanThreads) scan_bwd_kernel(ScanP p) {
   // parameter gradients of the unit (zero where it has no tokens), dh0
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    if (ch[j] >= nch) continue;
-    const size_t d = c0 + ch[j];
+    float x[2][4], v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = n0 + (i ^ perm);
-      if (n >= p.S) continue;
-      p.part_A[(u * p.D + d) * p.S + n] = dA[j][i];
-      if (p.dh0 && w.ok && w.j == 0) p.dh0[((size_t)w.s * p.D + d) * p.S + n] = q[j][i];
+    for (int i = 0; i < 4; ++i) unpack2(dA[j][i], x[0][i], x[1][i]);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      permute(x[e], perm, v);  // (its own inverse)
+      if (2 * pair[j] + e < nch) store_states(p.part_A + (u * p.D + c0 + 2 * pair[j] + e) * p.S, p.S, n0, v);
+    }
+    if (!p.dh0 || !w.ok || w.j) continue;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(q[j][i], x[0][i], x[1][i]);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      permute(x[e], perm, v);
+      if (2 * pair[j] + e < nch) store_states(p.dh0 + ((size_t)w.s * p.D + c0 + 2 * pair[j] + e) * p.S, p.S, n0, v);
     }
   }
   __syncthreads();
   for (int i = tid; i < 2 * Sh::CT; i += kScanThreads) {
-    const int which = i / Sh::CT, c = i % Sh::CT;
+    const int which = i / Sh::CT, c = i % Sh::CT, col = c / V;
     if (c >= nch) continue;
-    float a = 0.f;  // the threads that hold channel c: columns c / V of every row of threads
-    for (int k = c / Sh::V; k < kScanThreads; k += Sh::COLS) a += sm.acc[which][c % Sh::V][k];
+    float a = 0.f;  // the threads whose accesses are of column col
+    for (int k = col % kScanThreads; k < kScanThreads; k += Sh::COLS)
+      a += sm.acc[which][col / kScanThreads * V + c % V][k];
     p.part_D[(u * 2 + which) * p.D + c0 + c] = a;
   }
 }
@@ -450,7 +493,7 @@ __global__ void __launch_bounds__(512) scan_grad_kernel(ScanP p, int units, floa
 struct BwdWs {
   size_t carry, sumd, bc, A, D, states, total;  // byte offsets
 };
-BwdWs bwd_ws(const rdn_scan_args &a, const ScanPlan &pl) {
+BwdWs bwd_ws(const rdn_scan_args &a, const ScanPlan &pl, const ScanPlan &fwd) {
   BwdWs w{};
   size_t at = 0;
   auto take = [&](size_t n) {
@@ -459,8 +502,11 @@ BwdWs bwd_ws(const rdn_scan_args &a, const ScanPlan &pl) {
     return o;
   };
   const size_t SP = 4 * pl.L, units = pl.units, M = (size_t)a.B * a.T;
-  w.carry = take(pl.split ? units * a.D * SP : 0);
-  w.sumd = take(pl.split ? units * a.D : 0);
+  // (shared with the forward that computes the kept states, where none are given)
+  size_t first = pl.split ? pl.units : 0;
+  if (!a.h_chunks && fwd.split && (size_t)fwd.units > first) first = fwd.units;
+  w.carry = take(first * a.D * SP);
+  w.sumd = take(first * a.D);
   w.bc = take((size_t)pl.tiles * M * 2 * SP);
   w.A = take(units * a.D * a.S);
   w.D = take(units * 2 * a.D);
@@ -472,11 +518,12 @@ BwdWs bwd_ws(const rdn_scan_args &a, const ScanPlan &pl) {
 template <typename T, int L, bool VEC>
 cudaError_t bwd_l(const ScanP &p, const ScanPlan &pl, cudaStream_t s) {
   const dim3 grid(pl.units, pl.tiles);
+  const int first = (int)sizeof(CarrySmem<T, L, VEC>), smem = (int)sizeof(BwdSmem<T, L, VEC>);
+  cudaError_t e;
+  if ((e = allow_smem(scan_bwd_carry_kernel<T, L, VEC>, first)) != cudaSuccess) return e;
+  if ((e = allow_smem(scan_bwd_kernel<T, L, VEC>, smem)) != cudaSuccess) return e;
   if (pl.split)
-    RDN_LAUNCH("scan_bwd_carry", s, (scan_bwd_carry_kernel<T, L, VEC><<<grid, kScanThreads, 0, s>>>(p)));
-  const int smem = (int)sizeof(BwdSmem<T, L, VEC>);
-  cudaError_t e = cudaFuncSetAttribute(scan_bwd_kernel<T, L, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
+    RDN_LAUNCH("scan_bwd_carry", s, (scan_bwd_carry_kernel<T, L, VEC><<<grid, kScanThreads, first, s>>>(p)));
   RDN_LAUNCH("scan_bwd", s, (scan_bwd_kernel<T, L, VEC><<<grid, kScanThreads, smem, s>>>(p)));
   return cudaGetLastError();
 }
@@ -509,11 +556,11 @@ cudaError_t bwd_t(const rdn_scan_args &a, const ScanP &p, const ScanPlan &pl, cu
 
 }  // namespace
 
-size_t scan_bwd_bytes(const rdn_scan_args &a) { return bwd_ws(a, scan_plan(a)).total; }
+size_t scan_bwd_bytes(const rdn_scan_args &a) { return bwd_ws(a, scan_plan(a, true), scan_plan(a, false)).total; }
 
 cudaError_t launch_scan_bwd(const rdn_scan_args &a, cudaStream_t s) {
-  const ScanPlan pl = scan_plan(a);
-  const BwdWs ws = bwd_ws(a, pl);
+  const ScanPlan pl = scan_plan(a, true), fwd = scan_plan(a, false);
+  const BwdWs ws = bwd_ws(a, pl, fwd);
   ScanP p = scan_params(a, pl);
   char *base = static_cast<char *>(a.workspace);
   p.carry = reinterpret_cast<float *>(base + ws.carry);
@@ -524,7 +571,11 @@ cudaError_t launch_scan_bwd(const rdn_scan_args &a, cudaStream_t s) {
   cudaError_t e;
   if (!a.h_chunks) {  // (the forward's own unit results go where the backward's will)
     p.chunks = reinterpret_cast<float *>(base + ws.states);
-    if ((e = scan_states(a, p, pl, s)) != cudaSuccess) return e;
+    ScanP f = scan_params(a, fwd);
+    f.chunks = p.chunks;
+    f.carry = p.carry;
+    f.sumd = p.sumd;
+    if ((e = scan_states(a, f, fwd, s)) != cudaSuccess) return e;
   }
   return a.dtype == RDN_BF16 ? bwd_t<__nv_bfloat16>(a, p, pl, s) : bwd_t<float>(a, p, pl, s);
 }

@@ -266,3 +266,14 @@ def test_in_a_graph():
     assert torch.equal(out, o2)
     for k in d:
         assert torch.equal(d[k], d2[k]), k
+
+
+def test_steps_of_zero_keep_the_state():
+    """dl = 0 is a decay of exactly one: the state passes through bit by bit, both ways."""
+    x = make(2, 37, 40, 16, dtype="f32", bias=False)
+    x["dt"].zero_()
+    out, hT = call(rdn.selective_scan_fwd, x, dt_softplus=False)
+    assert torch.equal(hT, x["h0"])
+    x["C"].zero_()
+    d = call(rdn.selective_scan_bwd, x, x["dout"], dhT=x["dhT"], dt_softplus=False)
+    assert torch.equal(d["dh0"], x["dhT"])
