@@ -9,6 +9,8 @@
 // sums over the states come back through shared memory to the threads that
 // hold x and z of the same elements, which finish and store them.  The next
 // tile's global loads are in flight during the steps.
+#include <math.h>
+
 #include "scan.cuh"
 
 namespace rdn {
@@ -143,13 +145,13 @@ __global__ void __launch_bounds__(kScanThreads, 7) scan_fwd_kernel(ScanP p) {
     for (int i = 0; i < Sh::NV; ++i) {
       const int t = Sh::tok(i), c = Sh::chan(i);
       if (t >= ntok || c >= nch) continue;
-      float o[V], v[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) o[e] = sm.y[t][c + e];
+      float o[V], v[V], Dk[V];
+      load_vec<V>(&sm.y[t][c], o);
       if (p.Dskip) {
         K::get(sm.raw[b][0][i][tid], v);
+        load_vec<V>(sm.D + c, Dk);
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = fmaf(sm.D[c + e], v[e], o[e]);
+        for (int e = 0; e < V; ++e) o[e] = fmaf(Dk[e], v[e], o[e]);
       }
       if (p.z) {
         K::get(sm.raw[b][2][i][tid], v);
@@ -279,26 +281,58 @@ long long scan_slots(const rdn_scan_args &a) {
   return a.cu_seqlens ? a.num_seqs + nc : a.B * nc;
 }
 
-// Units: enough CTAs of 4 warps for about four per SM, in units of at least 64
-// tokens; one unit per sequence where that is enough already.
+// Time per token of an SM that has r CTAs of a pass to run, of which `resident`
+// fit at a time: up to about half of those it is latency, the same for one as
+// for several, then issue slots.  In us, measured at 4096 channels of 16 states
+// over cuts of 1 to 28 units (prefill of 16384 tokens, training pass of 4 x 2048).
+struct PassTime {
+  int resident;
+  double least, fixed, each;
+  double at(long long r) const {
+    auto wave = [&](long long k) { return fmax(least, fixed + each * k); };
+    return (r / resident) * wave(resident) + (r % resident ? wave(r % resident) : 0.0);
+  }
+};
+constexpr PassTime kFwdTime{8, 0.245, 0.085, 0.040}, kFirstTime{8, 0.140, 0.030, 0.0285};
+constexpr PassTime kBwdTime{4, 0.54, 0.34, 0.10};
+
+// Units: the cut of the sequences that ends first by those times, with each
+// unit's start (its parameters, the states of the units before it) as 16 tokens
+// more and half a token for each of the n units.  Packed sequences, whose
+// lengths are on the device, count as one of T tokens with half a unit more for
+// each.  Units are at least 32 tokens long.
 ScanPlan scan_plan(const rdn_scan_args &a, bool bwd) {
+  constexpr int kSMs = 152;
+  const PassTime &main = bwd ? kBwdTime : kFwdTime;
   ScanPlan pl;
   pl.L = a.S <= 8 ? 2 : a.S <= 16 ? 4 : a.S <= 32 ? 8 : 16;
   pl.CT = 256 / pl.L;
   const int Dg = a.D / a.G;
   pl.tiles_g = (Dg + pl.CT - 1) / pl.CT;
   pl.tiles = pl.tiles_g * a.G;
-  const long long want = 152ll * (bwd ? 4 : 8);
-  const long long ns = a.cu_seqlens ? 1 : a.B;
-  const long long per_seq = want / (ns * pl.tiles);  // units per sequence: all CTAs resident at once
-  const long long len = a.T;
-  long long seg = per_seq <= 1 ? len : (len + per_seq - 1) / per_seq;
-  seg = (seg + kScanTile - 1) / kScanTile * kScanTile;
-  if (seg < 64) seg = 64;
-  pl.seg = (int)seg;
-  pl.units_row = a.T > 0 ? (int)((a.T + seg - 1) / seg) : 1;
-  pl.units = a.cu_seqlens ? a.num_seqs + (int)((a.T + seg - 1) / seg) : a.B * pl.units_row;
-  pl.split = a.T > seg;
+  const long long columns = (a.cu_seqlens ? 1ll : (long long)a.B) * pl.tiles;
+  const long long T16 = ((long long)a.T + kScanTile - 1) / kScanTile;  // tiles of tokens
+  const long long more = a.cu_seqlens ? a.num_seqs / 2 : 0;
+  auto time = [&](long long n, long long len) {
+    const long long ctas = columns * (n + more), first = columns * (n - 1);
+    const double t = main.at((ctas + kSMs - 1) / kSMs) * (len * kScanTile + 16 + 0.5 * n) +
+                     kFirstTime.at((first + kSMs - 1) / kSMs) * (len * kScanTile + 16);
+    return t + (n > 1 ? 2.0 : 0.0);  // (the first pass's launch)
+  };
+  long long best = T16 > 2 ? T16 : 2;  // tiles per unit
+  double cost = time(1, best);
+  for (long long n = 2; n <= 64 && T16 >= 2 * n; ++n) {
+    const long long len = (T16 + n - 1) / n, m = (T16 + len - 1) / len;
+    const double c = time(m, len);
+    if (c < cost) {
+      cost = c;
+      best = len;
+    }
+  }
+  pl.seg = (int)best * kScanTile;
+  pl.units_row = a.T > 0 ? (a.T + pl.seg - 1) / pl.seg : 1;
+  pl.units = a.cu_seqlens ? a.num_seqs + (a.T + pl.seg - 1) / pl.seg : a.B * pl.units_row;
+  pl.split = a.T > pl.seg;
   return pl;
 }
 

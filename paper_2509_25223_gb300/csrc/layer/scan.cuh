@@ -339,12 +339,39 @@ __device__ __forceinline__ void store_states(float *row, int S, int n0, const fl
   }
 }
 
+// V consecutive floats of shared memory (16 bytes at a time where V is a multiple of 4)
+template <int V>
+__device__ __forceinline__ void load_vec(const float *p, float (&v)[V]) {
+  if constexpr (V % 4 == 0) {
+#pragma unroll
+    for (int e = 0; e < V; e += 4) {
+      const float4 a = *reinterpret_cast<const float4 *>(p + e);
+      v[e] = a.x; v[e + 1] = a.y; v[e + 2] = a.z; v[e + 3] = a.w;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = p[e];
+  }
+}
+template <int V>
+__device__ __forceinline__ void store_vec(float *p, const float (&v)[V]) {
+  if constexpr (V % 4 == 0) {
+#pragma unroll
+    for (int e = 0; e < V; e += 4) *reinterpret_cast<float4 *>(p + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) p[e] = v[e];
+  }
+}
+
 // V channels' step sizes from dt: bias, softplus; none for a token past the
 // end (dl = 0: a decay of exactly 1, nothing added).
 template <int V>
 __device__ __forceinline__ void step_sizes(const ScanP &p, const float *bias, bool live, float (&dl)[V]) {
+  float b[V];
+  load_vec<V>(bias, b);
 #pragma unroll
-  for (int e = 0; e < V; ++e) dl[e] += bias[e];
+  for (int e = 0; e < V; ++e) dl[e] += b[e];
   if (p.softplus) {
     if constexpr (V % 2 == 0) {
 #pragma unroll

@@ -172,7 +172,7 @@ struct BwdSmem {
   float sums[3][kScanTile][Sh::CT];                  // sum_n g B, sum_n A2 q h, y
   float red[kScanWarps][kScanTile][2 * Sh::SP];      // dB, dC of each warp's channels
   static constexpr int AC = Sh::COLS > kScanThreads ? Sh::COLS / kScanThreads : 1;  // columns of a thread
-  float acc[2][AC * Sh::V][kScanThreads];            // dD and ddt_bias of a thread's elements
+  float acc[2][AC][kScanThreads][Sh::V];             // dD and ddt_bias of a thread's elements
   float4 kept[4][kScanThreads];                      // each lane's states before the tile
   typename Sh::Raw raw[2][4][Sh::NV][kScanThreads];  // each thread's x, dt, z, dout: this tile's and the next's
   T B[2][kScanTile][Sh::SP], C[2][kScanTile][Sh::SP];
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kScanThreads, 4) scan_bwd_kernel(ScanP p) {
     sm.D[c] = p.Dskip && c < nch ? p.Dskip[c0 + c] : 0.f;
   }
 #pragma unroll
-  for (int e = 0; e < Sm::AC * V; ++e) sm.acc[0][e][tid] = sm.acc[1][e][tid] = 0.f;
+  for (int e = 0; e < Sm::AC * V; ++e) sm.acc[0][e / V][tid][e % V] = sm.acc[1][e / V][tid][e % V] = 0.f;
   const f2 shift = pack2(kExpShift, kExpShift), zero2 = pack2(0.f, 0.f);
   f2 A2[2][4], q[2][4], dA[2][4];  // [channel pair][state n0 + (i ^ perm)]
 #pragma unroll
@@ -299,9 +299,7 @@ __global__ void __launch_bounds__(kScanThreads, 4) scan_bwd_kernel(ScanP p) {
         for (int e = 0; e < V; ++e) gv[e] *= siluf(zv[e]);
       }
       store_steps<V>(sm.dx[t], c, dl, xv);
-      float *gy = &sm.gy[t][0].x + c;
-#pragma unroll
-      for (int e = 0; e < V; ++e) gy[e] = gv[e];
+      store_vec<V>(&sm.gy[t][0].x + c, gv);
     }
     __syncthreads();
     load(r - kScanTile, b ^ 1);
@@ -378,35 +376,51 @@ __global__ void __launch_bounds__(kScanThreads, 4) scan_bwd_kernel(ScanP p) {
     for (int i = 0; i < Sh::NV; ++i) {
       const int t = Sh::tok(i), c = Sh::chan(i);
       if (t >= ntok || c >= nch) continue;
-      float xv[V], dv[V], dx[V], ddt[V];
-      K::get(sm.raw[b][0][i][tid], xv);
-      K::get(sm.raw[b][1][i][tid], dv);
       const long long row = r + t;
+      float xv[V], v[V], gy[V], gB[V], r0v[V], r1v[V], Dk[V], bias[V];
+      K::get(sm.raw[b][0][i][tid], xv);
+      K::get(sm.raw[b][1][i][tid], v);
+      load_vec<V>(&sm.gy[t][0].x + c, gy);
+      load_vec<V>(&sm.sums[0][t][c], gB);
+      load_vec<V>(&sm.sums[1][t][c], r1v);
+      load_vec<V>(sm.D + c, Dk);
+      load_vec<V>(sm.bias + c, bias);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float dl = (&sm.dx[t][spread16((c + e) / 2)].x)[(c + e) & 1], gy = (&sm.gy[t][0].x)[c + e];
-        const float gB = sm.sums[0][t][c + e];
-        dx[e] = dl * gB;
-        if (p.Dskip) dx[e] = fmaf(sm.D[c + e], gy, dx[e]);
-        ddt[e] = fmaf(sm.sums[1][t][c + e], kLn2, gB * xv[e]);
-        if (p.softplus) ddt[e] *= sigmoidf(dv[e] + sm.bias[c + e]);
-        float &aD = sm.acc[0][i % Sm::AC * V + e][tid], &ab = sm.acc[1][i % Sm::AC * V + e][tid];
-        aD = fmaf(gy, xv[e], aD);
-        ab += ddt[e];
+        r0v[e] = (&sm.dx[t][spread16((c + e) / 2)].x)[(c + e) & 1] * gB[e];
+        r1v[e] = fmaf(r1v[e], kLn2, gB[e] * xv[e]);
       }
-      K::st((T *)p.dx + c0 + row * p.dx_ld + c, K::put(dx));
-      K::st((T *)p.ddt + c0 + row * p.ddt_ld + c, K::put(ddt));
-      if (p.z) {
-        float zv[V], gv[V], dz[V];
-        K::get(sm.raw[b][2][i][tid], zv);
-        K::get(sm.raw[b][3][i][tid], gv);
+      if (p.Dskip) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          float y = sm.sums[2][t][c + e];
-          if (p.Dskip) y = fmaf(sm.D[c + e], xv[e], y);
-          dz[e] = gv[e] * y * silu_grad(zv[e], sigmoidf(zv[e]));
+        for (int e = 0; e < V; ++e) r0v[e] = fmaf(Dk[e], gy[e], r0v[e]);
+      }
+      if (p.softplus) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) r1v[e] *= sigmoidf(v[e] + bias[e]);
+      }
+      K::st((T *)p.dx + c0 + row * p.dx_ld + c, K::put(r0v));
+      K::st((T *)p.ddt + c0 + row * p.ddt_ld + c, K::put(r1v));
+      float *aD = sm.acc[0][i % Sm::AC][tid], *ab = sm.acc[1][i % Sm::AC][tid];
+      load_vec<V>(aD, r0v);
+      load_vec<V>(ab, v);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        r0v[e] = fmaf(gy[e], xv[e], r0v[e]);
+        v[e] += r1v[e];
+      }
+      store_vec<V>(aD, r0v);
+      store_vec<V>(ab, v);
+      if (p.z) {
+        K::get(sm.raw[b][2][i][tid], v);
+        K::get(sm.raw[b][3][i][tid], gy);
+        load_vec<V>(&sm.sums[2][t][c], gB);
+        if (p.Dskip) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) gB[e] = fmaf(Dk[e], xv[e], gB[e]);
         }
-        K::st((T *)p.dz + c0 + row * p.dz_ld + c, K::put(dz));
+#pragma unroll
+        for (int e = 0; e < V; ++e) r0v[e] = gy[e] * gB[e] * silu_grad(v[e], sigmoidf(v[e]));
+        K::st((T *)p.dz + c0 + row * p.dz_ld + c, K::put(r0v));
       }
     }
     for (int i = tid; i < ntok * 2 * Sh::SP; i += kScanThreads) {
@@ -444,7 +458,7 @@ __global__ void __launch_bounds__(kScanThreads, 4) scan_bwd_kernel(ScanP p) {
     if (c >= nch) continue;
     float a = 0.f;  // the threads whose accesses are of column col
     for (int k = col % kScanThreads; k < kScanThreads; k += Sh::COLS)
-      a += sm.acc[which][col / kScanThreads * V + c % V][k];
+      a += sm.acc[which][col / kScanThreads][k][c % V];
     p.part_D[(u * 2 + which) * p.D + c0 + c] = a;
   }
 }
