@@ -10,8 +10,11 @@
 // consecutive channels (one vector access) over a run of tokens and slides the
 // W-1 older inputs -- in the backward, which walks down, the W-1 later dp --
 // through registers, so x is read once but for the W-1 rows above a run.  The
-// loads of a group of tokens are issued together.  A sequence's start within a
-// run (packed sequences) is a rare branch that takes the taps from state0.
+// loads of a group of tokens are issued together, a group ahead.
+// Groups within one sequence take a path without per-token checks; what is
+// left per element is about 8 (forward) and 15 (backward) instructions, worked
+// on as pairs of channels.  A sequence's start or end within a group is the
+// rare path, which takes the taps from state0.
 #include <initializer_list>
 #include <utility>
 
@@ -21,8 +24,9 @@ namespace rdn {
 namespace {
 
 constexpr int kConvThreads = 128;
-constexpr int kFwdGroup = 8;  // tokens whose loads a thread issues together
+constexpr int kFwdGroup = 4;  // tokens whose loads a thread issues together
 constexpr int kBwdGroup = 4;
+constexpr int kRunStep = 8, kRunMost = 64;  // tokens of a thread's run
 
 struct ConvP {
   int B, T, C, ns, run;  // run: tokens per thread
@@ -36,15 +40,41 @@ struct ConvP {
   float *part;  // backward: [row groups of the grid][C][W + 1]
 };
 
-// the taps w[W-1-k] of V channels (tap[k]) and their biases
+// The taps w[W-1-k] of V channels (tap[k]) and their biases, through shared
+// memory: a thread's V W taps are consecutive, and read one by one straight
+// from global memory every one of them would take a line per lane.  Called by
+// the whole CTA; sh: blockDim.x * (V W + 1) floats (a row and one: the lanes
+// then read different banks).
 template <int W, int V>
-__device__ __forceinline__ void load_taps(const ConvP &p, int c0, float (&tap)[W][V], float (&bias)[V]) {
+__device__ __forceinline__ void load_taps(const ConvP &p, int c0, float *sh, f2 (&tap)[W][(V + 1) / 2],
+                                          f2 (&bias)[(V + 1) / 2]) {
+  constexpr int R = V * W;
+  const int tid = threadIdx.y * blockDim.x + threadIdx.x;
+  const int base = (c0 - (int)threadIdx.x * V) * W, n = min((int)blockDim.x * R, p.C * W - base);
+  for (int i = tid; i < n; i += kConvThreads) sh[i / R * (R + 1) + i % R] = __ldg(p.w + base + i);
+  __syncthreads();
+  float t[W][V], b[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) {
 #pragma unroll
-    for (int k = 0; k < W; ++k) tap[k][e] = __ldg(p.w + (size_t)(c0 + e) * W + W - 1 - k);
-    bias[e] = p.bias ? __ldg(p.bias + c0 + e) : 0.f;
+    for (int k = 0; k < W; ++k) t[k][e] = sh[threadIdx.x * (R + 1) + e * W + W - 1 - k];
+    b[e] = p.bias && c0 + e < p.C ? __ldg(p.bias + c0 + e) : 0.f;
   }
+#pragma unroll
+  for (int k = 0; k < W; ++k) to_pairs<V>(t[k], tap[k]);
+  to_pairs<V>(b, bias);
+}
+template <typename T, int V>
+__device__ __forceinline__ void get_pairs(const typename Pack<T, V>::Raw &raw, f2 (&p)[(V + 1) / 2]) {
+  float v[V];
+  Pack<T, V>::get(raw, v);
+  to_pairs<V>(v, p);
+}
+template <typename T, int V>
+__device__ __forceinline__ typename Pack<T, V>::Raw put_pairs(const f2 (&p)[(V + 1) / 2]) {
+  float v[V];
+  from_pairs<V>(p, v);
+  return Pack<T, V>::put(v);
 }
 
 // Sequences without tokens pass their state (or its gradient) through.
@@ -65,41 +95,83 @@ __device__ __forceinline__ void pass_empty(const ConvP &p, long long unit, long 
 
 // x before a sequence's start: row i of its state0, or zero
 template <typename T, int W, int V>
-__device__ __forceinline__ void from_state(const ConvP &p, int s, int i, int c0, float (&v)[V]) {
+__device__ __forceinline__ void from_state(const ConvP &p, int s, int i, int c0, f2 (&v)[(V + 1) / 2]) {
   using K = Pack<T, V>;
-  K::get(p.state0 ? K::ld((const T *)p.state0 + ((size_t)s * (W - 1) + i) * p.C + c0) : K::zero(), v);
+  get_pairs<T, V>(p.state0 ? K::ld((const T *)p.state0 + ((size_t)s * (W - 1) + i) * p.C + c0) : K::zero(), v);
 }
 
 template <typename T, int W, int V>
 __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(ConvP p) {
   using K = Pack<T, V>;
+  constexpr int U = kFwdGroup, P = (V + 1) / 2;
   const int c0 = (blockIdx.y * blockDim.x + threadIdx.x) * V;
   const long long unit = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   const long long units = (long long)p.B * p.runs;
+  __shared__ float sh[32 * (V * W + 1)];
+  f2 tap[W][P], bias[P];
+  load_taps<W, V>(p, c0, sh, tap, bias);
   if (c0 >= p.C || unit >= units) return;
   pass_empty<T, W, V>(p, unit, units, c0, p.state0, p.stateT);
   const int b = (int)(unit / p.runs), t0 = (int)(unit % p.runs) * p.run;
   if (t0 >= p.T) return;
   const long long r0 = (long long)b * p.T + t0;
   const long long r1 = r0 + min(p.run, p.T - t0);
-  float tap[W][V], bias[V];
-  load_taps<W, V>(p, c0, tap, bias);
   const T *X = (const T *)p.x + c0;
   T *Y = (T *)p.y + c0;
   SeqSpan q = find_seq(p.cu, p.ns, p.T, b, t0);
-  float win[W - 1][V];  // win[k] = x_{t-1-k}
+  f2 win[W - 1][P];  // win[k] = x_{t-1-k}
 #pragma unroll
   for (int k = 0; k < W - 1; ++k) {
     const long long r = r0 - 1 - k;
-    if (r >= q.begin) K::get(K::ld(X + r * p.x_ld), win[k]);
+    if (r >= q.begin) get_pairs<T, V>(K::ld(X + r * p.x_ld), win[k]);
     else from_state<T, W, V>(p, q.s, (int)(W - 1 + r - q.begin), c0, win[k]);
   }
-  for (long long g = r0; g < r1; g += kFwdGroup) {
-    typename K::Raw raw[kFwdGroup];
+  auto token = [&](const typename K::Raw &raw, T *y) {
+    f2 x[P], o[P];
+    get_pairs<T, V>(raw, x);
 #pragma unroll
-    for (int u = 0; u < kFwdGroup; ++u) raw[u] = g + u < r1 ? K::ld(X + (g + u) * p.x_ld) : K::zero();
+    for (int e = 0; e < P; ++e) {
+      f2 a = fma2(tap[0][e], x[e], bias[e]);
 #pragma unroll
-    for (int u = 0; u < kFwdGroup; ++u) {
+      for (int k = 1; k < W; ++k) a = fma2(tap[k][e], win[k - 1][e], a);
+      o[e] = p.silu ? silu2(a) : a;
+#pragma unroll
+      for (int k = W - 2; k > 0; --k) win[k][e] = win[k - 1][e];
+      win[0][e] = x[e];
+    }
+    K::st(y, put_pairs<T, V>(o));
+  };
+  auto last_state = [&]() {
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k)
+      K::st((T *)p.stateT + ((size_t)q.s * (W - 1) + W - 2 - k) * p.C + c0, put_pairs<T, V>(win[k]));
+  };
+  const T *xr = X + r0 * p.x_ld;
+  T *yr = Y + r0 * p.y_ld;
+  typename K::Raw raw[U], next[U];
+  auto load = [&](long long g) {  // the group from row g on, xr its first
+    if (g + U <= r1) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) next[u] = K::ld(xr + u * p.x_ld);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) next[u] = g + u < r1 ? K::ld(xr + u * p.x_ld) : K::zero();
+    }
+    xr += U * p.x_ld;
+  };
+  load(r0);
+  for (long long g = r0; g < r1; g += U, yr += U * p.y_ld) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = next[u];
+    load(g + U);
+    if (g + U <= r1 && g + U <= q.end) {  // whole, within its sequence
+#pragma unroll
+      for (int u = 0; u < U; ++u) token(raw[u], yr + u * p.y_ld);
+      if (g + U == q.end && p.stateT) last_state();
+      continue;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
       const long long r = g + u;
       if (r >= r1) break;
       if (r >= q.end) {  // the next sequence that has tokens (packed rows only)
@@ -111,24 +183,8 @@ __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(ConvP p) {
 #pragma unroll
         for (int k = 0; k < W - 1; ++k) from_state<T, W, V>(p, q.s, W - 2 - k, c0, win[k]);
       }
-      float x[V], y[V];
-      K::get(raw[u], x);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        float a = fmaf(tap[0][e], x[e], bias[e]);
-#pragma unroll
-        for (int k = 1; k < W; ++k) a = fmaf(tap[k][e], win[k - 1][e], a);
-        y[e] = p.silu ? siluf(a) : a;
-#pragma unroll
-        for (int k = W - 2; k > 0; --k) win[k][e] = win[k - 1][e];
-        win[0][e] = x[e];
-      }
-      K::st(Y + r * p.y_ld, K::put(y));
-      if (r == q.end - 1 && p.stateT) {
-#pragma unroll
-        for (int k = 0; k < W - 1; ++k)
-          K::st((T *)p.stateT + ((size_t)q.s * (W - 1) + W - 2 - k) * p.C + c0, K::put(win[k]));
-      }
+      token(raw[u], yr + u * p.y_ld);
+      if (r == q.end - 1 && p.stateT) last_state();
     }
   }
 }
@@ -136,50 +192,121 @@ __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(ConvP p) {
 template <typename T, int W, int V>
 __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
   using K = Pack<T, V>;
-  constexpr int U = kBwdGroup;
-  extern __shared__ float sh[];  // [blockDim.y][blockDim.x][V][W + 1]
+  constexpr int U = kBwdGroup, P = (V + 1) / 2;
+  extern __shared__ float sh[];  // [blockDim.y][blockDim.x][V][W + 1]; first the taps
   const int c0 = (blockIdx.y * blockDim.x + threadIdx.x) * V;
   const long long unit = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   const long long units = (long long)p.B * p.runs;
   const bool live = c0 < p.C && unit < units;
-  float dw[W + 1][V];  // dw[k] of tap[k]; dw[W]: the bias
+  f2 tap[W][P], bias[P];
+  load_taps<W, V>(p, c0, sh, tap, bias);
+  f2 dw[W + 1][P];  // dw[k] of tap[k]; dw[W]: the bias
 #pragma unroll
   for (int k = 0; k <= W; ++k)
 #pragma unroll
-    for (int e = 0; e < V; ++e) dw[k][e] = 0.f;
+    for (int e = 0; e < P; ++e) dw[k][e] = pack2(0.f, 0.f);
   if (live) pass_empty<T, W, V>(p, unit, units, c0, p.dstateT, p.dstate0);
   const int b = live ? (int)(unit / p.runs) : 0, t0 = live ? (int)(unit % p.runs) * p.run : p.T;
   if (live && t0 < p.T) {
     const long long rb0 = (long long)b * p.T, rb1 = rb0 + p.T;
     const long long r0 = rb0 + t0, r1 = r0 + min(p.run, p.T - t0);
     const long long top = min(r1 + W - 2, rb1 - 1);  // dx of the last row takes dp of the W-1 rows after it
-    float tap[W][V], bias[V];
-    load_taps<W, V>(p, c0, tap, bias);
     const T *X = (const T *)p.x + c0, *DY = (const T *)p.dy + c0;
     T *DX = (T *)p.dx + c0;
     SeqSpan q = find_seq(p.cu, p.ns, p.T, b, (int)(top - rb0));
-    float dpw[W - 1][V];  // dpw[k] = dp_{t+1+k} of the same sequence
+    f2 dpw[W - 1][P];  // dpw[k] = dp_{t+1+k} of the same sequence
 #pragma unroll
     for (int k = 0; k < W - 1; ++k)
 #pragma unroll
-      for (int e = 0; e < V; ++e) dpw[k][e] = 0.f;
+      for (int e = 0; e < P; ++e) dpw[k][e] = pack2(0.f, 0.f);
+    // dp of one row from its taps, its dx if the row is the run's own
+    auto row_dp = [&](const f2 (&x)[W][P], const typename K::Raw &dyr, f2 (&dp)[P]) {
+      get_pairs<T, V>(dyr, dp);
+      if (p.silu) {
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+          f2 a = bias[e];
+#pragma unroll
+          for (int k = 0; k < W; ++k) a = fma2(tap[k][e], x[k][e], a);
+          dp[e] = mul2(dp[e], silu_grad2(a));
+        }
+      }
+    };
+    auto row_dx = [&](const f2 (&x)[W][P], const f2 (&dp)[P], f2 (&dx)[P]) {
+#pragma unroll
+      for (int e = 0; e < P; ++e) {
+        f2 a = mul2(tap[0][e], dp[e]);
+#pragma unroll
+        for (int k = 1; k < W; ++k) a = fma2(tap[k][e], dpw[k - 1][e], a);
+        dx[e] = a;
+#pragma unroll
+        for (int k = 0; k < W; ++k) dw[k][e] = fma2(dp[e], x[k][e], dw[k][e]);
+        dw[W][e] = add2(dw[W][e], dp[e]);
+      }
+    };
+    auto shift = [&](const f2 (&dp)[P]) {
+#pragma unroll
+      for (int e = 0; e < P; ++e) {
+#pragma unroll
+        for (int k = W - 2; k > 0; --k) dpw[k][e] = dpw[k - 1][e];
+        dpw[0][e] = dp[e];
+      }
+    };
     // groups [g, g + U) from the top down; xr[i] = x row g - (W-1) + i
-    typename K::Raw xr[U + W - 1];
+    typename K::Raw xr[U + W - 1], xn[U], dyr[U], dyn[U];
     long long g = r0 + (top - r0) / U * U;
+    const T *xp = X + (g - (W - 1)) * p.x_ld, *dyp = DY + g * p.dy_ld;
+    T *dxp = DX + g * p.dx_ld;
+    auto load = [&](long long at) {  // the rows a group needs beside those of the one above: xp and dyp its first
+      if (at - (W - 1) >= rb0 && at + U - 1 <= top && at >= r0) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          xn[i] = K::ld(xp + i * p.x_ld);
+          dyn[i] = K::ld(dyp + i * p.dy_ld);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const long long r = at - (W - 1) + i;
+          xn[i] = r >= rb0 && r <= top && at >= r0 ? K::ld(xp + i * p.x_ld) : K::zero();
+          dyn[i] = at >= r0 && at + i <= top ? K::ld(dyp + i * p.dy_ld) : K::zero();
+        }
+      }
+      xp -= U * p.x_ld;
+      dyp -= U * p.dy_ld;
+    };
 #pragma unroll
     for (int i = 0; i < W - 1; ++i) {
       const long long r = g + U - (W - 1) + i;
       xr[i] = r >= rb0 && r <= top ? K::ld(X + r * p.x_ld) : K::zero();
     }
-    for (; g >= r0; g -= U) {
-      typename K::Raw dyr[U];
+    load(g);
+    for (; g >= r0; g -= U, dxp -= U * p.dx_ld) {
 #pragma unroll
       for (int i = W - 2; i >= 0; --i) xr[U + i] = xr[i];
 #pragma unroll
       for (int i = 0; i < U; ++i) {
-        const long long r = g - (W - 1) + i;
-        xr[i] = r >= rb0 && r <= top ? K::ld(X + r * p.x_ld) : K::zero();
-        dyr[i] = g + i <= top ? K::ld(DY + (g + i) * p.dy_ld) : K::zero();
+        xr[i] = xn[i];
+        dyr[i] = dyn[i];
+      }
+      load(g - U);
+      if (g + U <= r1 && g - (W - 1) >= q.begin && g + U <= q.end - (p.dstateT ? W - 1 : 0)) {
+        f2 x[U + W - 1][P];  // whole, the run's own, inside its sequence
+#pragma unroll
+        for (int i = 0; i < U + W - 1; ++i) get_pairs<T, V>(xr[i], x[i]);
+#pragma unroll
+        for (int u = U - 1; u >= 0; --u) {
+          f2 taps[W][P], dp[P], dx[P];
+#pragma unroll
+          for (int k = 0; k < W; ++k)
+#pragma unroll
+            for (int e = 0; e < P; ++e) taps[k][e] = x[u + W - 1 - k][e];
+          row_dp(taps, dyr[u], dp);
+          row_dx(taps, dp, dx);
+          K::st(dxp + u * p.dx_ld, put_pairs<T, V>(dx));
+          shift(dp);
+        }
+        continue;
       }
 #pragma unroll
       for (int u = U - 1; u >= 0; --u) {
@@ -194,84 +321,63 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
 #pragma unroll
           for (int k = 0; k < W - 1; ++k)
 #pragma unroll
-            for (int e = 0; e < V; ++e) dpw[k][e] = 0.f;
+            for (int e = 0; e < P; ++e) dpw[k][e] = pack2(0.f, 0.f);
         }
-        float x[W][V], dp[V];
+        f2 x[W][P], dp[P];
 #pragma unroll
-        for (int k = 0; k < W; ++k) K::get(xr[u + W - 1 - k], x[k]);
+        for (int k = 0; k < W; ++k) get_pairs<T, V>(xr[u + W - 1 - k], x[k]);
         if (r - (W - 1) < q.begin) {
 #pragma unroll
           for (int k = 1; k < W; ++k)
             if (r - k < q.begin) from_state<T, W, V>(p, q.s, (int)(W - 1 + r - k - q.begin), c0, x[k]);
         }
-        K::get(dyr[u], dp);
-        if (p.silu) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            float a = bias[e];
-#pragma unroll
-            for (int k = 0; k < W; ++k) a = fmaf(tap[k][e], x[k][e], a);
-            dp[e] *= silu_grad(a, sigmoidf(a));
-          }
-        }
+        row_dp(x, dyr[u], dp);
         if (r < r1) {
-          float dx[V];
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            float a = tap[0][e] * dp[e];
-#pragma unroll
-            for (int k = 1; k < W; ++k) a = fmaf(tap[k][e], dpw[k - 1][e], a);
-            dx[e] = a;
-#pragma unroll
-            for (int k = 0; k < W; ++k) dw[k][e] = fmaf(dp[e], x[k][e], dw[k][e]);
-            dw[W][e] += dp[e];
-          }
+          f2 dx[P];
+          row_dx(x, dp, dx);
           if (p.dstateT && q.end - r <= W - 1) {
-            float d[V];
-            K::get(K::ld((const T *)p.dstateT + ((size_t)q.s * (W - 1) + W - 1 - (q.end - r)) * p.C + c0), d);
+            f2 d[P];
+            get_pairs<T, V>(K::ld((const T *)p.dstateT + ((size_t)q.s * (W - 1) + W - 1 - (q.end - r)) * p.C + c0), d);
 #pragma unroll
-            for (int e = 0; e < V; ++e) dx[e] += d[e];
+            for (int e = 0; e < P; ++e) dx[e] = add2(dx[e], d[e]);
           }
-          K::st(DX + r * p.dx_ld, K::put(dx));
+          K::st(dxp + u * p.dx_ld, put_pairs<T, V>(dx));
         }
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-#pragma unroll
-          for (int k = W - 2; k > 0; --k) dpw[k][e] = dpw[k - 1][e];
-          dpw[0][e] = dp[e];
-        }
+        shift(dp);
         if (r == q.begin && r < r1 && p.dstate0) {
           const long long len = q.end - q.begin;
 #pragma unroll
           for (int v = 1; v < W; ++v) {  // the input v rows before the start: state row W-1-v
-            float d[V];
+            f2 d[P];
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-              d[e] = 0.f;
+            for (int e = 0; e < P; ++e) {
+              d[e] = mul2(tap[v][e], dpw[0][e]);
 #pragma unroll
-              for (int k = v; k < W; ++k) d[e] = fmaf(tap[k][e], dpw[k - v][e], d[e]);
+              for (int k = v + 1; k < W; ++k) d[e] = fma2(tap[k][e], dpw[k - v][e], d[e]);
             }
             const int i = W - 1 - v;
             if (p.dstateT && i >= len) {  // a sequence shorter than the state hands part of it on
-              float t[V];
-              K::get(K::ld((const T *)p.dstateT + ((size_t)q.s * (W - 1) + i - len) * p.C + c0), t);
+              f2 t[P];
+              get_pairs<T, V>(K::ld((const T *)p.dstateT + ((size_t)q.s * (W - 1) + i - len) * p.C + c0), t);
 #pragma unroll
-              for (int e = 0; e < V; ++e) d[e] += t[e];
+              for (int e = 0; e < P; ++e) d[e] = add2(d[e], t[e]);
             }
-            K::st((T *)p.dstate0 + ((size_t)q.s * (W - 1) + i) * p.C + c0, K::put(d));
+            K::st((T *)p.dstate0 + ((size_t)q.s * (W - 1) + i) * p.C + c0, put_pairs<T, V>(d));
           }
         }
       }
     }
   }
+  __syncthreads();  // (sh held the taps)
   // the CTA's sums over its runs, in order
   const int row = blockDim.x * V * (W + 1);
   float *mine = sh + threadIdx.y * row + threadIdx.x * V * (W + 1);
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
+  for (int k = 0; k <= W; ++k) {
+    float v[V];
+    from_pairs<V>(dw[k], v);
 #pragma unroll
-    for (int k = 0; k < W; ++k) mine[e * (W + 1) + W - 1 - k] = dw[k][e];
-    mine[e * (W + 1) + W] = dw[W][e];
+    for (int e = 0; e < V; ++e) mine[e * (W + 1) + (k < W ? W - 1 - k : W)] = v[e];
   }
   __syncthreads();
   const int cbase = blockIdx.y * blockDim.x * V;
@@ -361,14 +467,16 @@ struct ConvPlan {
   unsigned bx, by;    // CTA: channel vectors, runs
   unsigned gx, gy;    // grid: CTAs over the runs, over the channels
 };
-// Threads want long runs (the backward repeats W-1 rows of x and dy per run),
-// the GPU wants about 1,500 threads per SM: the longest run in [group, most]
-// that still gives them.
-ConvPlan conv_plan(const rdn_conv_args &a, int V, int group, int most) {
+// Threads want long runs (each reads W-1 rows above its own again, its taps, and
+// in the backward W-1 rows of dy), the GPU wants threads: runs of 64 tokens where
+// there are 512 threads per SM left, else as many as leave those, 8 at least.
+// (8 x 4096 tokens of 2048 channels: forward 88 us in runs of 8, 69 of 16, 59 of
+// 64, 70 of 256; backward 198, 139, 103, 123.)
+ConvPlan conv_plan(const rdn_conv_args &a, int V) {
   ConvPlan pl;
   const long long nvec = (a.C + V - 1) / V, tokens = (long long)a.B * a.T;
-  long long run = tokens * nvec / (152ll * 1536) / group * group;
-  pl.run = (int)(run < group ? group : run > most ? most : run);
+  long long run = tokens * nvec / (152ll * 512) / kRunStep * kRunStep;
+  pl.run = (int)(run < kRunStep ? kRunStep : run > kRunMost ? kRunMost : run);
   pl.runs = a.T > 0 ? (a.T + pl.run - 1) / pl.run : 1;
   pl.bx = 32;
   while (pl.bx > 1 && pl.bx / 2 >= nvec) pl.bx /= 2;
@@ -377,13 +485,15 @@ ConvPlan conv_plan(const rdn_conv_args &a, int V, int group, int most) {
   pl.gy = (unsigned)((nvec + pl.bx - 1) / pl.bx);
   return pl;
 }
-constexpr int kFwdMost = 16, kBwdMost = 64;
 
-// Channels per thread: 4 in the sequence kernels, whose registers hold up to
-// 4 W + 1 values per channel; single ones where a row is not on their bytes.
+// Channels per thread: a 16-byte access in the forward, 4 in the backward, whose
+// registers hold up to 4 W + 1 values per channel; single ones where the rows do
+// not lie on those bytes.
 bool conv_vec(const rdn_conv_args &a, bool bwd) {
-  const size_t size = a.dtype == RDN_BF16 ? 2 : 4, bytes = 4 * size;
-  if (a.C % 4) return false;
+  const size_t size = a.dtype == RDN_BF16 ? 2 : 4;
+  const int V = bwd ? 4 : (int)(16 / size);
+  const size_t bytes = V * size;
+  if (a.C % V) return false;
   return bwd ? rows_on(bytes, size, {{a.x, a.x_ld}, {a.dy, a.dy_ld}, {a.dx, a.dx_ld}, {a.state0, 0},
                                      {a.dstateT, 0}, {a.dstate0, 0}})
              : rows_on(bytes, size, {{a.x, a.x_ld}, {a.y, a.y_ld}, {a.state0, 0}, {a.stateT, 0}});
@@ -404,7 +514,7 @@ ConvP conv_params(const rdn_conv_args &a, const ConvPlan &pl) {
 
 template <typename T, int W, int V>
 cudaError_t fwd_t(const rdn_conv_args &a, cudaStream_t s) {
-  const ConvPlan pl = conv_plan(a, V, kFwdGroup, kFwdMost);
+  const ConvPlan pl = conv_plan(a, V);
   const ConvP p = conv_params(a, pl);
   RDN_LAUNCH("conv_fwd", s,
              (conv_fwd_kernel<T, W, V><<<dim3(pl.gx, pl.gy), dim3(pl.bx, pl.by), 0, s>>>(p)));
@@ -412,9 +522,9 @@ cudaError_t fwd_t(const rdn_conv_args &a, cudaStream_t s) {
 }
 template <typename T, int W, int V>
 cudaError_t bwd_t(const rdn_conv_args &a, cudaStream_t s) {
-  const ConvPlan pl = conv_plan(a, V, kBwdGroup, kBwdMost);
+  const ConvPlan pl = conv_plan(a, V);
   const ConvP p = conv_params(a, pl);
-  const size_t smem = sizeof(float) * kConvThreads * V * (W + 1);
+  const size_t smem = sizeof(float) * kConvThreads * (V * (W + 1) + 1);
   RDN_LAUNCH("conv_bwd", s,
              (conv_bwd_kernel<T, W, V><<<dim3(pl.gx, pl.gy), dim3(pl.bx, pl.by), smem, s>>>(p)));
   const unsigned grid = (unsigned)(((long long)a.C * (W + 1) + 31) / 32);
@@ -426,7 +536,7 @@ template <typename T, int W>
 cudaError_t conv_w(const rdn_conv_args &a, bool bwd, cudaStream_t s) {
   const bool vec = conv_vec(a, bwd);
   if (bwd) return vec ? bwd_t<T, W, 4>(a, s) : bwd_t<T, W, 1>(a, s);
-  return vec ? fwd_t<T, W, 4>(a, s) : fwd_t<T, W, 1>(a, s);
+  return vec ? fwd_t<T, W, kVec<T>>(a, s) : fwd_t<T, W, 1>(a, s);
 }
 template <typename T>
 cudaError_t conv_d(const rdn_conv_args &a, bool bwd, cudaStream_t s) {
@@ -452,7 +562,7 @@ cudaError_t step_w(const ConvStepP &p, int W, cudaStream_t s) {
 
 size_t conv_bwd_bytes(const rdn_conv_args &a) {
   // (the larger of the two accesses' plans: the query sees no pointers)
-  const ConvPlan v = conv_plan(a, 4, kBwdGroup, kBwdMost), e = conv_plan(a, 1, kBwdGroup, kBwdMost);
+  const ConvPlan v = conv_plan(a, 4), e = conv_plan(a, 1);
   const size_t parts = v.gx > e.gx ? v.gx : e.gx;
   return round256(sizeof(float) * parts * a.C * (a.W + 1));
 }

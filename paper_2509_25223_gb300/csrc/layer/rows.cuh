@@ -75,10 +75,82 @@ struct Pack<T, 1> {
 template <typename T>
 constexpr int kVec = 16 / (int)sizeof(T);
 
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Pairs of fp32 values in one register pair: one issue slot for two operations
+// (the FMA pipe's rate is the same; the slots go to the exponentials and loads).
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pack2(float lo, float hi) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(f2 v, float &lo, float &hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float sum2(f2 v) {
+  float lo, hi;
+  unpack2(v, lo, hi);
+  return lo + hi;
+}
+
 __device__ __forceinline__ float sigmoidf(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 __device__ __forceinline__ float siluf(float x) { return x * sigmoidf(x); }
 // d silu(x) / dx from x and its sigmoid
 __device__ __forceinline__ float silu_grad(float x, float s) { return s * fmaf(x, 1.f - s, 1.f); }
+
+// silu of a pair; and its derivative
+__device__ __forceinline__ f2 sigmoid2(f2 x) {
+  float a, b;
+  unpack2(mul2(x, pack2(-kLog2e, -kLog2e)), a, b);
+  unpack2(add2(pack2(ex2(a), ex2(b)), pack2(1.f, 1.f)), a, b);
+  return pack2(rcp_approx(a), rcp_approx(b));
+}
+__device__ __forceinline__ f2 silu2(f2 x) { return mul2(x, sigmoid2(x)); }
+__device__ __forceinline__ f2 silu_grad2(f2 x) {
+  const f2 s = sigmoid2(x), one = pack2(1.f, 1.f);
+  return mul2(s, fma2(x, fma2(s, pack2(-1.f, -1.f), one), one));
+}
+// V elements as pairs (V = 1: with a zero)
+template <int V>
+__device__ __forceinline__ void to_pairs(const float (&v)[V], f2 (&p)[(V + 1) / 2]) {
+#pragma unroll
+  for (int e = 0; e < V; e += 2) p[e / 2] = pack2(v[e], e + 1 < V ? v[e + 1 < V ? e + 1 : e] : 0.f);
+}
+template <int V>
+__device__ __forceinline__ void from_pairs(const f2 (&p)[(V + 1) / 2], float (&v)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; e += 2) {
+    float lo, hi;
+    unpack2(p[e / 2], lo, hi);
+    v[e] = lo;
+    if (e + 1 < V) v[e + 1 < V ? e + 1 : e] = hi;
+  }
+}
 
 // Packed sequences: token s of the offsets table, clamped into [0, T] (a table
 // that breaks the ordering gives unspecified results, but stays in bounds).

@@ -36,46 +36,10 @@ constexpr int kScanTile = RDN_SCAN_CHUNK;  // tokens staged at a time, and betwe
 // out.  kExpShift (added in the multiply that forms the argument, at no cost)
 // takes the mean below 5e-9 for exponents in [-0.5, 0]; expf has 1e-8 to
 // 1.5e-8 there.
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kExpShift = 2.5e-8f;
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ float decay(float dl, float A2) { return ex2(fmaf(dl, A2, kExpShift)); }
 
-// Pairs of fp32 values in one register pair: one issue slot for two operations
-// (the FMA pipe's rate is the same; the slots go to the exponentials and loads).
-typedef unsigned long long f2;
-__device__ __forceinline__ f2 pack2(float lo, float hi) {
-  f2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack2(f2 v, float &lo, float &hi) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
-  f2 r;
-  asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
-  f2 r;
-  asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f2 add2(f2 a, f2 b) {
-  f2 r;
-  asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ float sum2(f2 v) {
-  float lo, hi;
-  unpack2(v, lo, hi);
-  return lo + hi;
-}
 // decay() of a pair
 __device__ __forceinline__ f2 decay2(f2 dl, f2 A2, f2 shift) {
   float lo, hi;
@@ -87,11 +51,6 @@ __device__ __forceinline__ f2 decay2(f2 dl, f2 A2, f2 shift) {
 // with atanh(t) / t as a polynomial in t^2 fitted to 4e-9 on [0, 1/9].  About 14 instructions, two
 // units in the last place at every size of the result (the library's log1p takes three times as
 // many, and log2 of 1 + u would lose a small u).
-__device__ __forceinline__ float rcp_approx(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ float softplusf(float v) {
   const float u = ex2(fabsf(v) * -kLog2e);
   const float t = u * rcp_approx(2.f + u), q = t * t;
