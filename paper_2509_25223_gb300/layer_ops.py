@@ -29,66 +29,78 @@ _GATES = {"silu": 0, "sigmoid": 1}
 _F32 = torch.float32
 
 
-def _code(t):
-    code = _DTYPES.get(t.dtype)
+def _code(dtype):
+    code = _DTYPES.get(dtype)
     if code is None:
-        raise ValueError(f"rdn: unsupported dtype {t.dtype}")
+        raise ValueError(f"rdn: unsupported dtype {dtype}")
     return code
 
 
-def _rows(name, t, shape, dtype, device):
+# A step of one token is a few microseconds of device time, so the checks below
+# are kept to a few attribute reads per operand (device indexes instead of device
+# objects, dtypes by identity) and the argument structs are packed in one call.
+
+def _bad(name, t, shape, dtype, dev):
+    raise ValueError(f"rdn: {name} must be {tuple(shape)} {dtype} on CUDA device {dev} "
+                     f"(got {tuple(t.shape)} {t.dtype} on {t.device})")
+
+
+def _rows(name, t, shape, dtype, dev):
     """(address, row stride) of rows that lie along t's last axis, evenly spaced."""
-    if t.shape != shape or t.dtype != dtype or t.device != device:
-        raise ValueError(f"rdn: {name} must be {tuple(shape)} {dtype} on {device} "
-                         f"(got {tuple(t.shape)} {t.dtype} on {t.device})")
-    if t.is_contiguous():
-        return t.data_ptr(), 0
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        _bad(name, t, shape, dtype, dev)
+    return t.data_ptr(), 0 if t.is_contiguous() else _stride(name, t)
+
+
+def _stride(name, t):
+    shape = t.shape
     width, lead = 1, len(shape) - 1  # the trailing axes that are contiguous make up a row
-    while lead >= 0 and (t.shape[lead] == 1 or t.stride(lead) == width):
-        width *= t.shape[lead]
+    while lead >= 0 and (shape[lead] == 1 or t.stride(lead) == width):
+        width *= shape[lead]
         lead -= 1
     lead += 1
     if lead == len(shape):
         raise ValueError(f"rdn: the last axis of {name} must be contiguous")
     ld, span = 0, 0
     for a in range(lead - 1, -1, -1):
-        if t.shape[a] == 1:
+        if shape[a] == 1:
             continue
         if ld == 0:
             ld = t.stride(a)
-            span = ld * t.shape[a]
+            span = ld * shape[a]
         elif t.stride(a) != span:
             raise ValueError(f"rdn: the rows of {name} must be evenly spaced")
         else:
-            span *= t.shape[a]
-    return t.data_ptr(), ld
+            span *= shape[a]
+    return ld
 
 
-def _whole(name, t, shape, dtype, device):
+def _whole(name, t, shape, dtype, dev):
     """The address of an optional contiguous tensor (0 = None)."""
     if t is None:
         return 0
-    if t.shape != shape or t.dtype != dtype or t.device != device:
-        raise ValueError(f"rdn: {name} must be {tuple(shape)} {dtype} on {device} "
-                         f"(got {tuple(t.shape)} {t.dtype} on {t.device})")
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        _bad(name, t, shape, dtype, dev)
     if not t.is_contiguous():
         raise ValueError(f"rdn: {name} must be contiguous")
     return t.data_ptr()
 
 
 def _cuda(name, t, dims):
-    if not t.is_cuda:
+    """(device index, shape)"""
+    dev, shape = t.get_device(), t.shape
+    if dev < 0:
         raise ValueError("rdn: tensors must be on a CUDA device")
-    if t.dim() != dims:
-        raise ValueError(f"rdn: {name} must have {dims} axes (got {tuple(t.shape)})")
-    return t.device
+    if len(shape) != dims:
+        raise ValueError(f"rdn: {name} must have {dims} axes (got {tuple(shape)})")
+    return dev, shape
 
 
-def _table(cu, B, device):
+def _table(cu, B, dev):
     """(address, sequences of the table or 0, sequences of the call)"""
     if cu is None:
         return 0, 0, B
-    if cu.dtype != torch.int32 or cu.dim() != 1 or cu.numel() < 2 or cu.device != device:
+    if cu.dtype != torch.int32 or cu.dim() != 1 or cu.numel() < 2 or cu.get_device() != dev:
         raise ValueError("cu_seqlens must be a 1-D int32 device tensor of num_seqs + 1 offsets")
     if not cu.is_contiguous():
         raise ValueError("cu_seqlens must be contiguous")
@@ -100,13 +112,17 @@ def _error(name, st):
     raise RdnError(name, st, _abi.load().rdn_last_error().decode())
 
 
-def _call(name, args, device):
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _call(name, args, dev):
     # the library launches on the current device: make it the operands'
-    if device.index == torch.cuda.current_device():
-        st = _abi.packed(name)(args, torch._C._cuda_getCurrentRawStream(device.index))
+    if dev == _current_device():
+        st = _abi.packed(name)(args, _raw_stream(dev))
     else:
-        with torch.cuda.device(device):
-            st = _abi.packed(name)(args, torch._C._cuda_getCurrentRawStream(device.index))
+        with torch.cuda.device(dev):
+            st = _abi.packed(name)(args, _raw_stream(dev))
     if st:
         _error(name, st)
 
@@ -119,12 +135,12 @@ def _size(name, args):
     return n.value
 
 
-def _workspace(workspace, nbytes, device):
+def _workspace(workspace, nbytes, dev):
     if workspace is not None and workspace.numel() * workspace.element_size() >= nbytes:
-        if workspace.device != device or not workspace.is_contiguous():
+        if workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError("rdn: workspace must be contiguous and on the operands' device")
         return workspace
-    return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=dev)
 
 
 def _silu(activation):
@@ -142,8 +158,8 @@ def causal_conv_fwd(x, weight, bias=None, state=None, activation="silu", cu_seql
     [num_seqs,W-1,C]): the inputs before each sequence's start, oldest first
     (None: zeros).  Returns y [B,T,C], or (y, last state) with return_state.
     cu_seqlens: packed sequences, as for rdn_fwd (B = 1)."""
-    dev = _cuda("x", x, 3)
-    B, T, C = x.shape
+    dev, shape = _cuda("x", x, 3)
+    B, T, C = shape
     W = weight.shape[-1]
     cu, ns, n = _table(cu_seqlens, B, dev)
     y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
@@ -151,7 +167,7 @@ def causal_conv_fwd(x, weight, bias=None, state=None, activation="silu", cu_seql
     px, x_ld = _rows("x", x, (B, T, C), x.dtype, dev)
     py, y_ld = _rows("out", y, (B, T, C), x.dtype, dev)
     args = _abi.CONV_PACK(
-        B, T, C, W, _code(x), _silu(activation), x_ld, y_ld, 0, 0, px,
+        B, T, C, W, _code(x.dtype), _silu(activation), x_ld, y_ld, 0, 0, px,
         _whole("weight", weight, (C, W), _F32, dev), _whole("bias", bias, (C,), _F32, dev),
         _whole("state", state, (n, W - 1, C), x.dtype, dev), py,
         0 if last is None else last.data_ptr(), cu, ns, 0, 0, 0, 0, 0, 0, 0, 0)
@@ -165,8 +181,8 @@ def causal_conv_bwd(x, weight, dy, bias=None, state=None, d_state=None, activati
     dy: gradient of y; d_state: of the returned last state, or None.  Returns a
     dict with dx, dweight [C,W], dbias [C] (fp32; with bias) and dstate (with
     state).  out: tensors to write into, by those names."""
-    dev = _cuda("x", x, 3)
-    B, T, C = x.shape
+    dev, shape = _cuda("x", x, 3)
+    B, T, C = shape
     W = weight.shape[-1]
     cu, ns, n = _table(cu_seqlens, B, dev)
     e = lambda *s, dtype=x.dtype: torch.empty(*s, dtype=dtype, device=dev)  # noqa: E731
@@ -185,7 +201,7 @@ def causal_conv_bwd(x, weight, dy, bias=None, state=None, d_state=None, activati
 
     def pack(ws, nbytes):
         return _abi.CONV_PACK(
-            B, T, C, W, _code(x), _silu(activation), x_ld, 0, dy_ld, dx_ld, px,
+            B, T, C, W, _code(x.dtype), _silu(activation), x_ld, 0, dy_ld, dx_ld, px,
             _whole("weight", weight, (C, W), _F32, dev), _whole("bias", bias, (C,), _F32, dev),
             _whole("state", state, (n, W - 1, C), x.dtype, dev), 0, 0, cu, ns, pdy,
             _whole("d_state", d_state, (n, W - 1, C), x.dtype, dev), pdx,
@@ -202,17 +218,22 @@ def causal_conv_step(x, weight, state, bias=None, activation="silu", slots=None,
     """One token of causal_conv_fwd for N requests: x [N,C]; state
     [num_slots,W-1,C] is updated in place.  slots [N] int32: each request's row
     of state (distinct); a negative one is an idle row (y = 0).  None: row n."""
-    dev = _cuda("x", x, 2)
-    N, C = x.shape
+    dev, shape = _cuda("x", x, 2)
+    N, C = shape
     W = weight.shape[-1]
-    y = torch.empty(N, C, dtype=x.dtype, device=dev) if out is None else out
-    px, x_ld = _rows("x", x, (N, C), x.dtype, dev)
-    py, y_ld = _rows("out", y, (N, C), x.dtype, dev)
+    ty = x.dtype
+    px, x_ld = (x.data_ptr(), 0) if x.is_contiguous() else _rows("x", x, shape, ty, dev)
+    if out is None:
+        y = torch.empty(shape, dtype=ty, device=dev)
+        py, y_ld = y.data_ptr(), 0
+    else:
+        y = out
+        py, y_ld = _rows("out", y, shape, ty, dev)
     num = state.shape[0]
     args = _abi.CONV_STEP_PACK(
-        N, C, W, _code(x), _silu(activation), num, x_ld, y_ld, px,
+        N, C, W, _code(ty), _silu(activation), num, x_ld, y_ld, px,
         _whole("weight", weight, (C, W), _F32, dev), _whole("bias", bias, (C,), _F32, dev),
-        _whole("state", state, (num, W - 1, C), x.dtype, dev),
+        _whole("state", state, (num, W - 1, C), ty, dev),
         _whole("slots", slots, (N,), torch.int32, dev), py)
     _call("rdn_conv_step", args, dev)
     return y
@@ -222,8 +243,9 @@ class _Scan:
     """The operands of a scan, checked, as the leading values of SCAN_PACK."""
 
     def __init__(self, x, dt, A, B, C, D, z, dt_bias, h0, dt_softplus, cu_seqlens):
-        self.dev = dev = _cuda("x", x, 3)
-        b, t, d = x.shape
+        self.dev, shape = _cuda("x", x, 3)
+        dev = self.dev
+        b, t, d = shape
         if B.dim() != 4:
             raise ValueError(f"rdn: B must be [B, T, G, S] (got {tuple(B.shape)})")
         g, s = B.shape[2:]
@@ -233,7 +255,7 @@ class _Scan:
         rows = [_rows("x", x, self.shape, x.dtype, dev), _rows("dt", dt, self.shape, x.dtype, dev),
                 (0, 0) if z is None else _rows("z", z, self.shape, x.dtype, dev),
                 _rows("B", B, self.bc, x.dtype, dev), _rows("C", C, self.bc, x.dtype, dev)]
-        self.head = (b, t, d, s, g, _code(x), 1 if dt_softplus else 0)
+        self.head = (b, t, d, s, g, _code(x.dtype), 1 if dt_softplus else 0)
         self.lds, self.ptrs = [r[1] for r in rows], [r[0] for r in rows]
         self.params = (_whole("A", A, (d, s), _F32, dev), _whole("D", D, (d,), _F32, dev),
                        _whole("dt_bias", dt_bias, (d,), _F32, dev),
@@ -321,22 +343,27 @@ def selective_scan_step(x, dt, A, B, C, h, D=None, z=None, dt_bias=None, dt_soft
     """One token of selective_scan_fwd for N requests: x, dt, z [N,d]; B, C
     [N,G,s]; h [num_slots,d,s] fp32 is updated in place; slots as in
     causal_conv_step.  Returns out [N,d]."""
-    dev = _cuda("x", x, 2)
-    n, d = x.shape
-    if B.dim() != 3:
-        raise ValueError(f"rdn: B must be [N, G, S] (got {tuple(B.shape)})")
-    g, s = B.shape[1:]
+    dev, shape = _cuda("x", x, 2)
+    n, d = shape
+    bshape = B.shape
+    if len(bshape) != 3 or bshape[0] != n:
+        raise ValueError(f"rdn: B must be [N, G, S] (got {tuple(bshape)})")
+    g, s = bshape[1], bshape[2]
     ty = x.dtype
-    y = torch.empty(n, d, dtype=ty, device=dev) if out is None else out
-    px, x_ld = _rows("x", x, (n, d), ty, dev)
-    pdt, dt_ld = _rows("dt", dt, (n, d), ty, dev)
-    pz, z_ld = (0, 0) if z is None else _rows("z", z, (n, d), ty, dev)
-    pB, b_ld = _rows("B", B, (n, g, s), ty, dev)
-    pC, c_ld = _rows("C", C, (n, g, s), ty, dev)
-    py, y_ld = _rows("out", y, (n, d), ty, dev)
+    px, x_ld = (x.data_ptr(), 0) if x.is_contiguous() else _rows("x", x, shape, ty, dev)
+    pdt, dt_ld = _rows("dt", dt, shape, ty, dev)
+    pz, z_ld = (0, 0) if z is None else _rows("z", z, shape, ty, dev)
+    pB, b_ld = _rows("B", B, bshape, ty, dev)
+    pC, c_ld = _rows("C", C, bshape, ty, dev)
+    if out is None:
+        y = torch.empty(shape, dtype=ty, device=dev)
+        py, y_ld = y.data_ptr(), 0
+    else:
+        y = out
+        py, y_ld = _rows("out", y, shape, ty, dev)
     num = h.shape[0]
     args = _abi.SCAN_STEP_PACK(
-        n, d, s, g, _code(x), 1 if dt_softplus else 0, num, x_ld, dt_ld, z_ld, b_ld, c_ld, y_ld, px,
+        n, d, s, g, _code(ty), 1 if dt_softplus else 0, num, x_ld, dt_ld, z_ld, b_ld, c_ld, y_ld, px,
         pdt, pz, pB, pC, _whole("A", A, (d, s), _F32, dev), _whole("D", D, (d,), _F32, dev),
         _whole("dt_bias", dt_bias, (d,), _F32, dev), _whole("h", h, (num, d, s), _F32, dev),
         _whole("slots", slots, (n,), torch.int32, dev), py)
@@ -351,34 +378,35 @@ class _Norm:
         first = f if f is not None else x
         if first is None:
             raise ValueError("rdn: f or x is required")
-        if not first.is_cuda:
+        self.dev = dev = first.get_device()
+        if dev < 0:
             raise ValueError("rdn: tensors must be on a CUDA device")
-        self.dev = dev = first.device
         self.shape = shape = first.shape
         D = shape[-1]
         self.heads, self.wshape = 1, (D,)
         if f is not None:
             if weight is None:
                 raise ValueError("rdn: f needs its weight")
-            self.wshape = tuple(weight.shape)
-            if weight.dim() == 2:
-                self.heads = weight.shape[0]
-            elif weight.dim() != 1:
+            self.wshape = weight.shape
+            if len(self.wshape) == 2:
+                self.heads = self.wshape[0]
+            elif len(self.wshape) != 1:
                 raise ValueError("rdn: weight must be [D] or [heads, D]")
             if self.wshape[-1] != D:
-                raise ValueError(f"rdn: weight must have {D} columns (got {self.wshape})")
+                raise ValueError(f"rdn: weight must have {D} columns (got {tuple(self.wshape)})")
         if gate not in _GATES:
             raise ValueError('rdn: gate must be "silu" or "sigmoid"')
         self.dtype = h_dtype if f is None and h_dtype is not None else first.dtype
         self.xdtype = x.dtype if x is not None else self.dtype
         self.vec = scale if isinstance(scale, torch.Tensor) else None
         const = 1.0 if scale is None or self.vec is not None else float(scale)
-        rows = [(0, 0) if t is None else _rows(k, t, shape, ty, dev)
-                for k, t, ty in (("f", f, self.dtype), ("z", z, self.dtype), ("x", x, self.xdtype))]
+        pf, f_ld = (0, 0) if f is None else _rows("f", f, shape, self.dtype, dev)
+        pz, z_ld = (0, 0) if z is None else _rows("z", z, shape, self.dtype, dev)
+        px, x_ld = (0, 0) if x is None else _rows("x", x, shape, self.xdtype, dev)
         n = first.numel() // D if D else 0
         self.head = (n, D, self.heads, _DTYPES.get(self.dtype, -1), _DTYPES.get(self.xdtype, -1),
-                     _GATES[gate], float(eps), const, rows[0][1], rows[1][1], rows[2][1], rows[0][0], rows[1][0], rows[2][0],
-                     _whole("weight", weight if f is not None else None, self.wshape, _F32, dev),
+                     _GATES[gate], float(eps), const, f_ld, z_ld, x_ld, pf, pz, px,
+                     0 if f is None else _whole("weight", weight, self.wshape, _F32, dev),
                      _whole("scale", self.vec, (D,), _F32, dev),
                      _whole("weight_next", weight_next, (D,), _F32, dev))
 
@@ -398,19 +426,22 @@ def block_norm_fwd(f=None, weight=None, z=None, gate="silu", x=None, scale=None,
     (f=None: h_dtype, or x's).  out: (r, h) to write into."""
     a = _Norm(f, weight, z, gate, x, scale, weight_next, eps, h_dtype)
     r, h = out if out is not None else (None, None)
+    pr = ph = 0
     if f is None:
-        r, pr = x, 0
+        r = x
+    elif r is None:
+        r = torch.empty(a.shape, dtype=a.xdtype, device=a.dev)
+        pr = r.data_ptr()
     else:
-        if r is None:
-            r = torch.empty(a.shape, dtype=a.xdtype, device=a.dev)
         pr = _whole("r", r, a.shape, a.xdtype, a.dev)
     if weight_next is None:
         h = None
     elif h is None:
         h = torch.empty(a.shape, dtype=a.dtype, device=a.dev)
-    args = _abi.NORM_PACK(*a.head, pr, _whole("h", h, a.shape, a.dtype, a.dev),
-                          *(0,) * 10)
-    _call("rdn_norm_fwd", args, a.dev)
+        ph = h.data_ptr()
+    else:
+        ph = _whole("h", h, a.shape, a.dtype, a.dev)
+    _call("rdn_norm_fwd", _abi.NORM_PACK(*a.head, pr, ph, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0), a.dev)
     return r, h
 
 

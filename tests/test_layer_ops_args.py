@@ -189,7 +189,7 @@ def test_size_queries():
 
 
 def test_row_strides():
-    rows = lambda t: layer_ops._rows("t", t, t.shape, t.dtype, t.device)[1]  # noqa: E731
+    rows = lambda t: layer_ops._rows("t", t, t.shape, t.dtype, t.get_device())[1]  # noqa: E731
     t = torch.zeros(3, 5, 40)
     assert rows(t) == 0
     assert rows(t[..., 8:24]) == 40 and rows(t[:, :1, 8:24]) == 200 and rows(t[1:2, :, :4]) == 40
