@@ -42,22 +42,21 @@ struct NormPlan : Launch {
 // CTAs of 256 threads (a row's, if it needs more), as many as are resident, so
 // that they stay for many rows; their slots a multiple of the heads, so that a
 // slot's rows share a row of w.
-cudaError_t norm_plan(const rdn_norm_args &a, bool bwd, NormPlan *pl) {
-  int nsm = 152;
-  const cudaError_t e = sm_count(&nsm);
-  if (e != cudaSuccess) nsm = 152;  // (a size query without a device)
-  pl->elems = a.D <= 8 * 1024 ? 8 : 16;
-  pl->tpr = 8;
-  while (pl->tpr * pl->elems < a.D) pl->tpr *= 2;
-  pl->threads = pl->tpr > 256 ? pl->tpr : 256;
-  const int per = pl->threads / pl->tpr;
+NormPlan norm_plan(const rdn_norm_args &a, bool bwd) {
+  constexpr int kSMs = 152;
+  NormPlan pl;
+  pl.elems = a.D <= 8 * 1024 ? 8 : 16;
+  pl.tpr = 8;
+  while (pl.tpr * pl.elems < a.D) pl.tpr *= 2;
+  pl.threads = pl.tpr > 256 ? pl.tpr : 256;
+  const int per = pl.threads / pl.tpr;
   const int step = a.heads / gcd(a.heads, per);
   const long long need = ((a.rows + per - 1) / per + step - 1) / step * step;
-  const int resident = (bwd ? 512 : 1024) / pl->threads;
-  const long long ctas = ((long long)nsm * (resident > 1 ? resident : 1) + step - 1) / step * step;
-  pl->ctas = (int)(ctas < need ? ctas : need);
-  pl->slots = pl->ctas * per;
-  return e;
+  const int resident = (bwd ? 512 : 1024) / pl.threads;
+  const long long ctas = ((long long)kSMs * (resident > 1 ? resident : 1) + step - 1) / step * step;
+  pl.ctas = (int)(ctas < need ? ctas : need);
+  pl.slots = pl.ctas * per;
+  return pl;
 }
 
 bool norm_vec(const rdn_norm_args &a, bool bwd) {
@@ -73,15 +72,12 @@ bool norm_vec(const rdn_norm_args &a, bool bwd) {
 }  // namespace
 
 size_t norm_bwd_bytes(const rdn_norm_args &a) {
-  NormPlan pl;
-  (void)norm_plan(a, true, &pl);
+  const NormPlan pl = norm_plan(a, true);
   return round256(sizeof(float) * 2 * (size_t)pl.slots * a.D);
 }
 
 cudaError_t launch_norm(const rdn_norm_args &a, bool bwd, cudaStream_t s) {
-  NormPlan pl;
-  cudaError_t e = norm_plan(a, bwd, &pl);
-  if (e != cudaSuccess) return e;
+  NormPlan pl = norm_plan(a, bwd);
   pl.vec = norm_vec(a, bwd);
   NormP p{};
   p.rows = a.rows; p.D = a.D; p.heads = a.heads; p.tpr = pl.tpr;
@@ -94,7 +90,7 @@ cudaError_t launch_norm(const rdn_norm_args &a, bool bwd, cudaStream_t s) {
   p.df = a.df; p.dz = a.dz; p.dx = a.dx;
   p.part = static_cast<float *>(a.workspace);
   const bool xf = a.x_dtype == RDN_F32;
-  e = a.dtype == RDN_BF16 ? norm::run_bf16(p, pl, xf, bwd, s) : norm::run_f32(p, pl, xf, bwd, s);
+  const cudaError_t e = a.dtype == RDN_BF16 ? norm::run_bf16(p, pl, xf, bwd, s) : norm::run_f32(p, pl, xf, bwd, s);
   if (e != cudaSuccess || !bwd) return e;
   const dim3 grid((a.D + 31) / 32, a.heads, 2);
   RDN_LAUNCH("norm_grad", s,

@@ -176,13 +176,6 @@ __device__ __forceinline__ SeqSpan find_seq(const int *cu, int num_seqs, int T, 
   return {lo, cu_at(cu, num_seqs, T, lo), max(cu_at(cu, num_seqs, T, lo + 1), t + 1)};
 }
 
-// SMs of the current device
-inline cudaError_t sm_count(int *n) {
-  int dev = 0;
-  const cudaError_t e = cudaGetDevice(&dev);
-  return e != cudaSuccess ? e : cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
-}
-
 inline size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 }  // namespace rdn

@@ -208,6 +208,8 @@ cudaError_t fwd_v(const ScanP &p, const ScanPlan &pl, cudaStream_t s) {
 
 struct StepP {
   int N, D, S, G, num_slots, softplus;
+  int rows;     // requests per CTA
+  bool bc_vec;  // 4 states of B and C in one access
   long long x_ld, dt_ld, z_ld, b_ld, c_ld, out_ld;
   const void *x, *dt, *z, *Bm, *Cm;
   const float *A, *Dskip, *dt_bias;
@@ -216,62 +218,116 @@ struct StepP {
   void *out;
 };
 
-// One token: L lanes per channel, 4 states each; the state streams through
-// once (memory-bound: 8 bytes per state).
-constexpr int kStepThreads = 128;
+// One token: L = 1 .. 8 lanes per channel, 8 states each (two quads, so that the
+// lanes of a channel read whole sectors); the states stream through once
+// (memory-bound: 8 bytes per state).  A CTA does its channels for up to kStepRows
+// requests, so that A (as many bytes as one request's states) and the channels'
+// parameters are read once for all of them; a request's loads are in flight while
+// the one before is worked on.
+constexpr int kStepThreads = 128, kStepRows = 8;
+// 4 states of B or C from global memory (zero past S)
+template <typename T>
+__device__ __forceinline__ void states_of(const T *row, int S, int n0, bool vec, float (&v)[4]) {
+  using K = Pack<T, 4>;
+  if (vec) {
+    K::get(n0 < S ? K::ld(row + n0) : K::zero(), v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = n0 + i < S ? to_f32<T>(row[n0 + i]) : 0.f;
+  }
+}
 template <typename T, int L>
 __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(StepP p) {
   constexpr int CH = kStepThreads / L;
-  const int sl = threadIdx.x % L, n0 = sl * 4, n = blockIdx.x;
+  __shared__ int s_slot[kStepRows];
+  const int sl = threadIdx.x % L, n0[2] = {sl * 4, 4 * L + sl * 4};
   const int d = blockIdx.y * CH + threadIdx.x / L;
-  const int slot = p.slots ? __ldg(p.slots + n) : n;
-  const bool on = d < p.D, idle = slot < 0 || slot >= p.num_slots;
-  float y = 0.f, xv = 0.f;
-  if (on && !idle) {
-    float *row = p.h + ((size_t)slot * p.D + d) * p.S;
-    float h[4], bb[4], cc[4], A2[4];
-    load_states(row, p.S, n0, h);
-    const int g = d / (p.D / p.G);
-    const T *Bm = (const T *)p.Bm + (size_t)n * p.b_ld + (size_t)g * p.S;
-    const T *Cm = (const T *)p.Cm + (size_t)n * p.c_ld + (size_t)g * p.S;
-    xv = to_f32<T>(((const T *)p.x)[(size_t)n * p.x_ld + d]);
-    float v = to_f32<T>(((const T *)p.dt)[(size_t)n * p.dt_ld + d]);
-    load_states(p.A + (size_t)d * p.S, p.S, n0, A2);
+  const int first = blockIdx.x * p.rows, count = min(p.rows, p.N - first);
+  if (threadIdx.x < count) {
+    const int n = first + threadIdx.x, slot = p.slots ? __ldg(p.slots + n) : n;
+    s_slot[threadIdx.x] = slot < p.num_slots ? slot : -1;
+  }
+  const bool on = d < p.D;
+  const int g = on ? d / (p.D / p.G) : 0;
+  float A2[2][4] = {}, bias = 0.f, Dk = 0.f;
+  if (on) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      bb[i] = n0 + i < p.S ? to_f32<T>(Bm[n0 + i]) : 0.f;
-      cc[i] = n0 + i < p.S ? to_f32<T>(Cm[n0 + i]) : 0.f;
-    }
-    if (p.dt_bias) v += __ldg(p.dt_bias + d);
-    const float dl = p.softplus ? softplusf(v) : v, dx = dl * xv;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      h[i] = fmaf(decay(dl, A2[i] * kLog2e), h[i], dx * bb[i]);
-      y = fmaf(cc[i], h[i], y);
-    }
-    store_states(row, p.S, n0, h);
+    for (int q = 0; q < 2; ++q) load_states(p.A + (size_t)d * p.S, p.S, n0[q], A2[q]);
+    if (p.dt_bias) bias = __ldg(p.dt_bias + d);
+    if (p.Dskip) Dk = __ldg(p.Dskip + d);
   }
 #pragma unroll
-  for (int o = L / 2; o; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
-  if (!on || sl) return;
-  if (!idle) {
-    if (p.Dskip) y = fmaf(__ldg(p.Dskip + d), xv, y);
-    if (p.z) y *= siluf(to_f32<T>(((const T *)p.z)[(size_t)n * p.z_ld + d]));
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) A2[q][i] *= kLog2e;
+  __syncthreads();
+  float hn[2][4] = {}, xn = 0.f, dn = 0.f, zn = 0.f;  // of the next request
+  auto load = [&](int r) {
+    const int slot = r < count ? s_slot[r] : -1;
+    if (!on || slot < 0) return;
+    const float *row = p.h + ((size_t)slot * p.D + d) * p.S;
+    const size_t n = first + r;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) load_states(row, p.S, n0[q], hn[q]);
+    xn = to_f32<T>(((const T *)p.x)[n * p.x_ld + d]);
+    dn = to_f32<T>(((const T *)p.dt)[n * p.dt_ld + d]);
+    if (p.z) zn = to_f32<T>(((const T *)p.z)[n * p.z_ld + d]);
+  };
+  load(0);
+  for (int r = 0; r < count; ++r) {
+    float h[2][4];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[q][i] = hn[q][i];
+    const float x = xn, v = dn + bias, z = zn;
+    load(r + 1);
+    const int slot = s_slot[r];
+    const size_t n = first + r;
+    float y = 0.f;
+    if (slot >= 0) {
+      const T *Bm = (const T *)p.Bm + n * p.b_ld + (size_t)g * p.S;
+      const T *Cm = (const T *)p.Cm + n * p.c_ld + (size_t)g * p.S;
+      const float dl = p.softplus ? softplusf(v) : v, dx = dl * x;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        float bb[4], cc[4];
+        states_of<T>(Bm, p.S, n0[q], p.bc_vec, bb);
+        states_of<T>(Cm, p.S, n0[q], p.bc_vec, cc);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          h[q][i] = fmaf(decay(dl, A2[q][i]), h[q][i], dx * bb[i]);
+          y = fmaf(cc[i], h[q][i], y);
+        }
+        if (on) store_states(p.h + ((size_t)slot * p.D + d) * p.S, p.S, n0[q], h[q]);
+      }
+    }
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
+    if (!on || sl) continue;
+    if (slot >= 0) {
+      if (p.Dskip) y = fmaf(Dk, x, y);
+      if (p.z) y *= siluf(z);
+    }
+    ((T *)p.out)[n * p.out_ld + d] = from_f32<T>(slot >= 0 ? y : 0.f);
   }
-  ((T *)p.out)[(size_t)n * p.out_ld + d] = from_f32<T>(idle ? 0.f : y);
 }
 
+template <typename T, int L>
+cudaError_t step_l(StepP p, cudaStream_t s) {
+  constexpr int CH = kStepThreads / L;
+  const unsigned tiles = (p.D + CH - 1) / CH;
+  // as many requests per CTA as leave about 8 CTAs per SM (4096 x 16 states: 256
+  // requests in 38 us one per CTA, 31 us eight; one request is latency either way)
+  p.rows = kStepRows;
+  while (p.rows > 1 && (long long)tiles * ((p.N + p.rows - 1) / p.rows) < 152 * 8) p.rows /= 2;
+  const dim3 grid((p.N + p.rows - 1) / p.rows, tiles);
+  RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, L><<<grid, kStepThreads, 0, s>>>(p)));
+  return cudaGetLastError();
+}
 template <typename T>
 cudaError_t step_d(const StepP &p, cudaStream_t s) {
-  const int L = p.S <= 8 ? 2 : p.S <= 16 ? 4 : p.S <= 32 ? 8 : 16;
-  const dim3 grid(p.N, (p.D + kStepThreads / L - 1) / (kStepThreads / L));
-  switch (L) {
-    case 2: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 2><<<grid, kStepThreads, 0, s>>>(p))); break;
-    case 4: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 4><<<grid, kStepThreads, 0, s>>>(p))); break;
-    case 8: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 8><<<grid, kStepThreads, 0, s>>>(p))); break;
-    default: RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, 16><<<grid, kStepThreads, 0, s>>>(p))); break;
-  }
-  return cudaGetLastError();
+  return p.S <= 8 ? step_l<T, 1>(p, s) : p.S <= 16 ? step_l<T, 2>(p, s) : p.S <= 32 ? step_l<T, 4>(p, s) : step_l<T, 8>(p, s);
 }
 
 }  // namespace
@@ -292,15 +348,17 @@ struct PassTime {
     auto wave = [&](long long k) { return fmax(least, fixed + each * k); };
     return (r / resident) * wave(resident) + (r % resident ? wave(r % resident) : 0.0);
   }
+  // the same per token-CTA where units of many lengths fill each other's gaps
+  double packed(double sms) const { return (fixed + each * resident) / (resident * sms); }
 };
 constexpr PassTime kFwdTime{8, 0.245, 0.085, 0.040}, kFirstTime{8, 0.140, 0.030, 0.0285};
-constexpr PassTime kBwdTime{4, 0.54, 0.34, 0.10};
+constexpr PassTime kBwdTime{6, 0.54, 0.25, 0.146};
 
 // Units: the cut of the sequences that ends first by those times, with each
 // unit's start (its parameters, the states of the units before it) as 16 tokens
 // more and half a token for each of the n units.  Packed sequences, whose
-// lengths are on the device, count as one of T tokens with half a unit more for
-// each.  Units are at least 32 tokens long.
+// lengths are on the device: their tokens at full occupancy, about half a unit
+// more for each, and one unit's time at the end.  Units are at least 32 tokens.
 ScanPlan scan_plan(const rdn_scan_args &a, bool bwd) {
   constexpr int kSMs = 152;
   const PassTime &main = bwd ? kBwdTime : kFwdTime;
@@ -314,10 +372,16 @@ ScanPlan scan_plan(const rdn_scan_args &a, bool bwd) {
   const long long T16 = ((long long)a.T + kScanTile - 1) / kScanTile;  // tiles of tokens
   const long long more = a.cu_seqlens ? a.num_seqs / 2 : 0;
   auto time = [&](long long n, long long len) {
-    const long long ctas = columns * (n + more), first = columns * (n - 1);
-    const double t = main.at((ctas + kSMs - 1) / kSMs) * (len * kScanTile + 16 + 0.5 * n) +
-                     kFirstTime.at((first + kSMs - 1) / kSMs) * (len * kScanTile + 16);
-    return t + (n > 1 ? 2.0 : 0.0);  // (the first pass's launch)
+    const double tokens = (double)len * kScanTile, start = 16 + 0.5 * n;
+    const double launch = n > 1 ? 2.0 : 0.0;  // of the first pass
+    if (a.cu_seqlens) {
+      const double share = 1.0 - 1.0 / n, units = n + more;
+      return (main.packed(kSMs) + share * kFirstTime.packed(kSMs)) * columns * (a.T + units * start) +
+             (main.least + (n > 1 ? kFirstTime.least : 0.0)) * (tokens + start) + launch;
+    }
+    const long long ctas = columns * n, first = columns * (n - 1);
+    return main.at((ctas + kSMs - 1) / kSMs) * (tokens + start) +
+           kFirstTime.at((first + kSMs - 1) / kSMs) * (tokens + 16) + launch;
   };
   long long best = T16 > 2 ? T16 : 2;  // tiles per unit
   double cost = time(1, best);
@@ -398,7 +462,9 @@ cudaError_t scan_states(const rdn_scan_args &a, ScanP p, const ScanPlan &pl, cud
 }
 
 cudaError_t launch_scan_step(const rdn_scan_step_args &a, cudaStream_t s) {
-  const StepP p{a.N, a.D, a.S, a.G, a.num_slots, a.dt_softplus, a.x_ld, a.dt_ld, a.z_ld, a.b_ld,
+  const size_t esz = a.dtype == RDN_BF16 ? 2 : 4;
+  const bool bc_vec = a.S % 4 == 0 && (((uintptr_t)a.Bm | (uintptr_t)a.Cm | (size_t)a.b_ld * esz | (size_t)a.c_ld * esz) & (4 * esz - 1)) == 0;
+  const StepP p{a.N, a.D, a.S, a.G, a.num_slots, a.dt_softplus, 1, bc_vec, a.x_ld, a.dt_ld, a.z_ld, a.b_ld,
                 a.c_ld, a.out_ld, a.x, a.dt, a.z, a.Bm, a.Cm, a.A, a.Dskip, a.dt_bias, a.h, a.slots, a.out};
   return a.dtype == RDN_BF16 ? step_d<__nv_bfloat16>(p, s) : step_d<float>(p, s);
 }

@@ -190,6 +190,7 @@ __device__ __forceinline__ void fetch(Raw *slot, const void *src) {
   if (src) v = *static_cast<const Raw *>(src);
   *slot = v;
 }
+__device__ __forceinline__ void prefetch(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 __device__ __forceinline__ void fetched() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // One operand's tile into the threads' own slots: tokens [0, ntok) from `base`

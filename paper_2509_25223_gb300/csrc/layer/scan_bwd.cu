@@ -7,21 +7,25 @@
 //     dx_t = dl_t sum_n g_t B_t + Dskip gy_t,   dz_t = dout_t y_t SiLU'(z_t)
 // and dh0 = q of the first token.
 //
-// The states are recomputed from those kept at every 16 tokens: 8 steps at a
-// time stay in registers (8 steps x 8 pairs per lane) while the reverse steps
-// consume them; the later 8 of a tile need the earlier 8 advanced once more.
-// About 15 multiply-adds and 2.5 exponentials per (token, channel, state):
-// FMA-bound.  The sums over channels for dB and dC are exchanged within a warp
-// in an order that needs no selects (the lanes that exchange hold their four
-// states in orders that differ by the bit they exchange over), joined over the
-// CTA's warps in shared memory, and over the channel tiles through the
-// workspace, always in the same order.
+// The states are recomputed from those kept at every 16 tokens: 4 tokens' states
+// at a time stay in registers (4 x 16 pairs per lane) while the reverse steps
+// consume them; the two halves of a tile and the two of a half start from states
+// advanced once more, so that a token is recomputed twice.  Keeping 8 tokens'
+// states takes 255 registers and a loop body beyond the instruction cache: 744 us
+// for 4 x 2048 x 4096 channels where this takes 680.  About 16 multiply-adds and
+// 3 exponentials per (token, channel, state), 26 instructions in all: bound by
+// instruction issue (the FMA pipe is busy a third of the time).  The sums over
+// channels for dB and dC are exchanged within a warp in an order that needs no
+// selects (the lanes that exchange hold their four states in orders that differ by
+// the bit they exchange over), joined over the CTA's warps in shared memory, and
+// over the channel tiles through the workspace, always in the same order.
 #include "scan.cuh"
 
 namespace rdn {
 namespace {
 
-constexpr int kSub = 8;  // tokens whose states are in registers together
+constexpr int kHalf = 8;  // tokens between two joins of the warps' sums
+constexpr int kSub = 4;   // tokens whose states are in registers together
 
 template <typename T, int L, bool VEC>
 struct CarrySmem {
@@ -169,18 +173,17 @@ struct BwdSmem {
   using Sh = ScanShape<T, L, VEC>;
   float4 dx[kScanTile][Sh::CT / 2];                  // (dl, dl', dl x, dl' x') of a pair, at spread16
   float2 gy[kScanTile][Sh::CT / 2];
-  float sums[3][kScanTile][Sh::CT];                  // sum_n g B, sum_n A2 q h, y
-  float red[kScanWarps][kScanTile][2 * Sh::SP];      // dB, dC of each warp's channels
+  float sums[3][kHalf][Sh::CT];                      // sum_n g B, sum_n A2 q h, y
+  float red[kScanWarps][kHalf][2 * Sh::SP];          // dB, dC of each warp's channels
   static constexpr int AC = Sh::COLS > kScanThreads ? Sh::COLS / kScanThreads : 1;  // columns of a thread
   float acc[2][AC][kScanThreads][Sh::V];             // dD and ddt_bias of a thread's elements
-  float4 kept[4][kScanThreads];                      // each lane's states before the tile
-  typename Sh::Raw raw[2][4][Sh::NV][kScanThreads];  // each thread's x, dt, z, dout: this tile's and the next's
+  float4 kept[2][4][kScanThreads];                   // each lane's states before the tile and before its second half
   T B[2][kScanTile][Sh::SP], C[2][kScanTile][Sh::SP];
   float bias[Sh::CT], D[Sh::CT];
 };
 
 template <typename T, int L, bool VEC>
-__global__ void __launch_bounds__(kScanThreads, 4) scan_bwd_kernel(ScanP p) {
+__global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
   using Sh = ScanShape<T, L, VEC>;
   using K = typename Sh::K;
   constexpr int V = Sh::V;
@@ -250,10 +253,15 @@ __global__ void __launch_bounds__(kScanThreads, 4) scan_bwd_kernel(ScanP p) {
   const T *Bm = (const T *)p.Bm + (size_t)g * p.S, *Cm = (const T *)p.Cm + (size_t)g * p.S;
   auto load = [&](long long r, int b) {
     const int ntok = r < r0 ? 0 : (int)min((long long)kScanTile, r1 - r);
-    fetch_rows<Sh>(sm.raw[b][0], X + r * p.x_ld, p.x_ld, ntok, nch);
-    fetch_rows<Sh>(sm.raw[b][1], DT + r * p.dt_ld, p.dt_ld, ntok, nch);
-    if (p.z) fetch_rows<Sh>(sm.raw[b][2], (const T *)p.z + c0 + r * p.z_ld, p.z_ld, ntok, nch);
-    fetch_rows<Sh>(sm.raw[b][3], DO + r * p.dout_ld, p.dout_ld, ntok, nch);
+#pragma unroll
+    for (int i = 0; i < Sh::NV; ++i) {  // the rows come into L2 now, into registers when the tile is begun
+      const int t = Sh::tok(i), c = Sh::chan(i);
+      if (t >= ntok || c >= nch) continue;
+      prefetch(X + (r + t) * p.x_ld + c);
+      prefetch(DT + (r + t) * p.dt_ld + c);
+      prefetch(DO + (r + t) * p.dout_ld + c);
+      if (p.z) prefetch((const T *)p.z + c0 + (r + t) * p.z_ld + c);
+    }
     fetch_states(sm.B[b], Bm + r * p.b_ld, p.b_ld, ntok, p.S, p.bc_vec);
     fetch_states(sm.C[b], Cm + r * p.c_ld, p.c_ld, ntok, p.S, p.bc_vec);
   };
@@ -266,11 +274,11 @@ __global__ void __launch_bounds__(kScanThreads, 4) scan_bwd_kernel(ScanP p) {
       const bool on = r >= r0 && ch < nch && slot < p.slots;
       const float *row = p.chunks + ((size_t)slot * p.D + c0 + ch) * p.S;
       if (p.S % 4 == 0) {
-        fetch(&sm.kept[k][tid], on && n0 < p.S ? row + n0 : nullptr);
+        fetch(&sm.kept[0][k][tid], on && n0 < p.S ? row + n0 : nullptr);
       } else {
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         if (on) load_states(row, p.S, n0, v);
-        sm.kept[k][tid] = make_float4(v[0], v[1], v[2], v[3]);
+        sm.kept[0][k][tid] = make_float4(v[0], v[1], v[2], v[3]);
       }
     }
   };
@@ -284,17 +292,27 @@ __global__ void __launch_bounds__(kScanThreads, 4) scan_bwd_kernel(ScanP p) {
     const int ntok = (int)min((long long)kScanTile, r1 - r);
     fetched();
     // the tile's operands into shared memory
+    typename Sh::Raw raw[4][Sh::NV];
+#pragma unroll
+    for (int i = 0; i < Sh::NV; ++i) {
+      const int t = Sh::tok(i), c = Sh::chan(i);
+      const bool on = t < ntok && c < nch;
+      raw[0][i] = on ? K::ld(X + (r + t) * p.x_ld + c) : K::zero();
+      raw[1][i] = on ? K::ld(DT + (r + t) * p.dt_ld + c) : K::zero();
+      raw[2][i] = on && p.z ? K::ld((const T *)p.z + c0 + (r + t) * p.z_ld + c) : K::zero();
+      raw[3][i] = on ? K::ld(DO + (r + t) * p.dout_ld + c) : K::zero();
+    }
 #pragma unroll
     for (int i = 0; i < Sh::NV; ++i) {
       const int t = Sh::tok(i), c = Sh::chan(i);
       if (t >= kScanTile) break;
       float xv[V], dl[V], gv[V], zv[V];
-      K::get(sm.raw[b][0][i][tid], xv);
-      K::get(sm.raw[b][1][i][tid], dl);
-      K::get(sm.raw[b][3][i][tid], gv);
+      K::get(raw[0][i], xv);
+      K::get(raw[1][i], dl);
+      K::get(raw[3][i], gv);
       step_sizes<V>(p, sm.bias + c, t < ntok, dl);
       if (p.z) {
-        K::get(sm.raw[b][2][i][tid], zv);
+        K::get(raw[2][i], zv);
 #pragma unroll
         for (int e = 0; e < V; ++e) gv[e] *= siluf(zv[e]);
       }
@@ -303,134 +321,173 @@ __global__ void __launch_bounds__(kScanThreads, 4) scan_bwd_kernel(ScanP p) {
     }
     __syncthreads();
     load(r - kScanTile, b ^ 1);
-#pragma unroll 1
-    for (int half = ntok > kSub ? 1 : 0; half >= 0; --half) {
-      f2 h0[2][4], hist[kSub][2][4];
+    auto step = [&](int t, const f2 (&from)[2][4], f2 (&to)[2][4]) {
+      f2 bb[4];
+      states4(&sm.B[b][t][n0], perm, bb);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dx[t][at[j]]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[j][i] = fma2(decay2(d.x, A2[j][i], shift), from[j][i], mul2(d.y, bb[i]));
+      }
+    };
+    auto states = [&](int k, f2 (&h)[2][4]) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         float v[2][4];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float4 k = sm.kept[2 * j + e][tid];
-          const float x[4] = {k.x, k.y, k.z, k.w};
+          const float4 a = sm.kept[k][2 * j + e][tid];
+          const float x[4] = {a.x, a.y, a.z, a.w};
           permute(x, perm, v[e]);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h0[j][i] = pack2(v[0][i], v[1][i]);
+        for (int i = 0; i < 4; ++i) h[j][i] = pack2(v[0][i], v[1][i]);
       }
-      if (!half) load_kept(r - kScanTile);
-      auto step = [&](int t, const f2 (&from)[2][4], f2 (&to)[2][4]) {
-        f2 bb[4];
-        states4(&sm.B[b][t][n0], perm, bb);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dx[t][at[j]]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) to[j][i] = fma2(decay2(d.x, A2[j][i], shift), from[j][i], mul2(d.y, bb[i]));
-        }
-      };
-      if (half) {
+    };
+    if (ntok > kHalf) {
+      f2 h[2][4];
+      states(0, h);
 #pragma unroll 2
-        for (int t = 0; t < kSub; ++t) step(t, h0, h0);
+      for (int t = 0; t < kHalf; ++t) step(t, h, h);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float x[2][4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpack2(h[j][i], x[0][i], x[1][i]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          permute(x[e], perm, v);
+          sm.kept[1][2 * j + e][tid] = make_float4(v[0], v[1], v[2], v[3]);
+        }
       }
+    }
+#pragma unroll 1
+    for (int half = ntok > kHalf ? 1 : 0; half >= 0; --half) {
+      const int th = half * kHalf, nh = min(ntok - th, kHalf);  // tokens [th, th + nh) of the tile
+#pragma unroll 1
+      for (int sub = nh > kSub ? 1 : 0; sub >= 0; --sub) {
+        const int ts = th + sub * kSub;
+        f2 h0[2][4], hist[kSub][2][4];
+        states(half, h0);
+        if (!half && !sub) load_kept(r - kScanTile);
+#pragma unroll 1
+        for (int t = 0; t < sub * kSub; t += 2) {
+          step(th + t, h0, h0);
+          step(th + t + 1, h0, h0);
+        }
 #pragma unroll
-      for (int t = 0; t < kSub; ++t) step(half * kSub + t, t ? hist[t - 1] : h0, hist[t]);
+        for (int t = 0; t < kSub; ++t) step(ts + t, t ? hist[t - 1] : h0, hist[t]);
 #pragma unroll
-      for (int tl = kSub - 1; tl >= 0; --tl) {
-        const int t = half * kSub + tl;
-        f2 bb[4], cc[4], db[4], dc[4], gB[2], Aq[2], y[2];
-        states4(&sm.B[b][t][n0], perm, bb);
-        states4(&sm.C[b][t][n0], perm, cc);
+        for (int tl = kSub - 1; tl >= 0; --tl) {
+          const int t = ts + tl, tr = t - th;
+          f2 bb[4], cc[4], db[4], dc[4], gB[2], Aq[2], y[2];
+          states4(&sm.B[b][t][n0], perm, bb);
+          states4(&sm.C[b][t][n0], perm, cc);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dx[t][at[j]]);
-          const f2 gy = *reinterpret_cast<const f2 *>(&sm.gy[t][pair[j]]);
+          for (int j = 0; j < 2; ++j) {
+            const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dx[t][at[j]]);
+            const f2 gy = *reinterpret_cast<const f2 *>(&sm.gy[t][pair[j]]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const f2 h = hist[tl][j][i], hp = tl ? hist[tl > 0 ? tl - 1 : 0][j][i] : h0[j][i];
+              const f2 gr = fma2(cc[i], gy, q[j][i]);
+              y[j] = i ? fma2(cc[i], h, y[j]) : mul2(cc[i], h);
+              gB[j] = i ? fma2(gr, bb[i], gB[j]) : mul2(gr, bb[i]);
+              dc[i] = j ? fma2(gy, h, dc[i]) : mul2(gy, h);
+              db[i] = j ? fma2(gr, d.y, db[i]) : mul2(gr, d.y);
+              q[j][i] = mul2(decay2(d.x, A2[j][i], shift), gr);
+              const f2 qh = mul2(q[j][i], hp);
+              dA[j][i] = fma2(d.x, qh, dA[j][i]);
+              Aq[j] = i ? fma2(A2[j][i], qh, Aq[j]) : mul2(A2[j][i], qh);
+            }
+          }
+          float dbv[4], dcv[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const f2 h = hist[tl][j][i], hp = tl ? hist[tl > 0 ? tl - 1 : 0][j][i] : h0[j][i];
-            const f2 gr = fma2(cc[i], gy, q[j][i]);
-            y[j] = i ? fma2(cc[i], h, y[j]) : mul2(cc[i], h);
-            gB[j] = i ? fma2(gr, bb[i], gB[j]) : mul2(gr, bb[i]);
-            dc[i] = j ? fma2(gy, h, dc[i]) : mul2(gy, h);
-            db[i] = j ? fma2(gr, d.y, db[i]) : mul2(gr, d.y);
-            q[j][i] = mul2(decay2(d.x, A2[j][i], shift), gr);
-            const f2 qh = mul2(q[j][i], hp);
-            dA[j][i] = fma2(d.x, qh, dA[j][i]);
-            Aq[j] = i ? fma2(A2[j][i], qh, Aq[j]) : mul2(A2[j][i], qh);
+            dbv[i] = sum2(db[i]);
+            dcv[i] = sum2(dc[i]);
           }
+        sum_channels<L>(dbv, dcv, sl, cl, &sm.red[warp][tr][0]);
+          sum_states<L>(gB, sm.sums[0][tr], first, sl);
+          sum_states<L>(Aq, sm.sums[1][tr], first, sl);
+          if (p.z) sum_states<L>(y, sm.sums[2][tr], first, sl);
         }
-        float dbv[4], dcv[4];
+      }
+      // results of the half's elements; its operands once more, from the caches
+      constexpr int NH = (Sh::NV + 1) / 2;
+      typename Sh::Raw own[4][NH];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          dbv[i] = sum2(db[i]);
-          dcv[i] = sum2(dc[i]);
+      for (int i = 0; i < NH; ++i) {
+        const int t = Sh::tok(i), c = Sh::chan(i);
+        const bool on = t < nh && c < nch;
+        const long long row = r + th + t;
+        own[0][i] = on ? K::ld(X + row * p.x_ld + c) : K::zero();
+        own[1][i] = on ? K::ld(DT + row * p.dt_ld + c) : K::zero();
+        own[2][i] = on && p.z ? K::ld((const T *)p.z + c0 + row * p.z_ld + c) : K::zero();
+        own[3][i] = on && p.z ? K::ld(DO + row * p.dout_ld + c) : K::zero();
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < NH; ++i) {
+        const int t = Sh::tok(i), c = Sh::chan(i);
+        if (t >= nh || c >= nch) continue;
+        const long long row = r + th + t;
+        float xv[V], v[V], gy[V], gB[V], r0v[V], r1v[V], Dk[V], bias[V];
+        K::get(own[0][i], xv);
+        K::get(own[1][i], v);
+        load_vec<V>(&sm.gy[th + t][0].x + c, gy);
+        load_vec<V>(&sm.sums[0][t][c], gB);
+        load_vec<V>(&sm.sums[1][t][c], r1v);
+        load_vec<V>(sm.D + c, Dk);
+        load_vec<V>(sm.bias + c, bias);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          r0v[e] = (&sm.dx[th + t][spread16((c + e) / 2)].x)[(c + e) & 1] * gB[e];
+          r1v[e] = fmaf(r1v[e], kLn2, gB[e] * xv[e]);
         }
-        sum_channels<L>(dbv, dcv, sl, cl, &sm.red[warp][t][0]);
-        sum_states<L>(gB, sm.sums[0][t], first, sl);
-        sum_states<L>(Aq, sm.sums[1][t], first, sl);
-        if (p.z) sum_states<L>(y, sm.sums[2][t], first, sl);
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < Sh::NV; ++i) {
-      const int t = Sh::tok(i), c = Sh::chan(i);
-      if (t >= ntok || c >= nch) continue;
-      const long long row = r + t;
-      float xv[V], v[V], gy[V], gB[V], r0v[V], r1v[V], Dk[V], bias[V];
-      K::get(sm.raw[b][0][i][tid], xv);
-      K::get(sm.raw[b][1][i][tid], v);
-      load_vec<V>(&sm.gy[t][0].x + c, gy);
-      load_vec<V>(&sm.sums[0][t][c], gB);
-      load_vec<V>(&sm.sums[1][t][c], r1v);
-      load_vec<V>(sm.D + c, Dk);
-      load_vec<V>(sm.bias + c, bias);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        r0v[e] = (&sm.dx[t][spread16((c + e) / 2)].x)[(c + e) & 1] * gB[e];
-        r1v[e] = fmaf(r1v[e], kLn2, gB[e] * xv[e]);
-      }
-      if (p.Dskip) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) r0v[e] = fmaf(Dk[e], gy[e], r0v[e]);
-      }
-      if (p.softplus) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) r1v[e] *= sigmoidf(v[e] + bias[e]);
-      }
-      K::st((T *)p.dx + c0 + row * p.dx_ld + c, K::put(r0v));
-      K::st((T *)p.ddt + c0 + row * p.ddt_ld + c, K::put(r1v));
-      float *aD = sm.acc[0][i % Sm::AC][tid], *ab = sm.acc[1][i % Sm::AC][tid];
-      load_vec<V>(aD, r0v);
-      load_vec<V>(ab, v);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        r0v[e] = fmaf(gy[e], xv[e], r0v[e]);
-        v[e] += r1v[e];
-      }
-      store_vec<V>(aD, r0v);
-      store_vec<V>(ab, v);
-      if (p.z) {
-        K::get(sm.raw[b][2][i][tid], v);
-        K::get(sm.raw[b][3][i][tid], gy);
-        load_vec<V>(&sm.sums[2][t][c], gB);
         if (p.Dskip) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) gB[e] = fmaf(Dk[e], xv[e], gB[e]);
+          for (int e = 0; e < V; ++e) r0v[e] = fmaf(Dk[e], gy[e], r0v[e]);
         }
+        if (p.softplus) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) r0v[e] = gy[e] * gB[e] * silu_grad(v[e], sigmoidf(v[e]));
-        K::st((T *)p.dz + c0 + row * p.dz_ld + c, K::put(r0v));
+          for (int e = 0; e < V; ++e) r1v[e] *= sigmoidf(v[e] + bias[e]);
+        }
+        K::st((T *)p.dx + c0 + row * p.dx_ld + c, K::put(r0v));
+        K::st((T *)p.ddt + c0 + row * p.ddt_ld + c, K::put(r1v));
+        float *aD = sm.acc[0][i % Sm::AC][tid], *ab = sm.acc[1][i % Sm::AC][tid];
+        load_vec<V>(aD, r0v);
+        load_vec<V>(ab, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          r0v[e] = fmaf(gy[e], xv[e], r0v[e]);
+          v[e] += r1v[e];
+        }
+        store_vec<V>(aD, r0v);
+        store_vec<V>(ab, v);
+        if (p.z) {
+          K::get(own[2][i], v);
+          K::get(own[3][i], gy);
+          load_vec<V>(&sm.sums[2][t][c], gB);
+          if (p.Dskip) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) gB[e] = fmaf(Dk[e], xv[e], gB[e]);
+          }
+#pragma unroll
+          for (int e = 0; e < V; ++e) r0v[e] = gy[e] * gB[e] * silu_grad(v[e], sigmoidf(v[e]));
+          K::st((T *)p.dz + c0 + row * p.dz_ld + c, K::put(r0v));
+        }
       }
-    }
-    for (int i = tid; i < ntok * 2 * Sh::SP; i += kScanThreads) {
-      const int t = i / (2 * Sh::SP), n = i % (2 * Sh::SP);
-      float a = sm.red[0][t][n];
+      for (int i = tid; i < nh * 2 * Sh::SP; i += kScanThreads) {
+        const int t = i / (2 * Sh::SP), n = i % (2 * Sh::SP);
+        float a = sm.red[0][t][n];
 #pragma unroll
-      for (int k = 1; k < kScanWarps; ++k) a += sm.red[k][t][n];
-      p.part_bc[((size_t)blockIdx.y * p.B * p.T + r + t) * (2 * Sh::SP) + n] = a;
+        for (int k = 1; k < kScanWarps; ++k) a += sm.red[k][t][n];
+        p.part_bc[((size_t)blockIdx.y * p.B * p.T + r + th + t) * (2 * Sh::SP) + n] = a;
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
   // parameter gradients of the unit (zero where it has no tokens), dh0
 #pragma unroll
