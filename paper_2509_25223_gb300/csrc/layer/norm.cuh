@@ -44,6 +44,9 @@ struct NormP {
 // the gate (0 none, 1 SiLU, 2 sigmoid), and these bits.
 constexpr int kFwdCtas = 1;
 constexpr int kF = 4, kX = 8, kH = 16, kAny = -1;
+// Rows whose loads a thread has in flight: two where its registers hold them.
+template <int V, int E, int MODE, bool BWD>
+constexpr int kAhead = V == 8 && E == 8 && MODE != kAny && !(BWD && (MODE & (kX | kH))) ? 2 : 1;
 template <int MODE>
 struct Has {
   int m;
@@ -168,7 +171,7 @@ __device__ __forceinline__ void load_c(const NormP &p, bool x, long long slot, i
 
 template <typename T, typename XT, int V, int E, int THREADS, int MODE>
 __global__ void __launch_bounds__(THREADS, THREADS == 512 ? kFwdCtas : 1) fwd_kernel(const NormP p) {
-  constexpr int N = E / 2;
+  constexpr int N = E / 2, R = kAhead<V, E, MODE, false>;
   __shared__ __align__(16) float sh[2][2][32];
   const Has<MODE> has(p);
   const int tpr = p.tpr, t = threadIdx.x % tpr, per = blockDim.x / tpr;
@@ -178,33 +181,36 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? kFwdCtas : 1) fwd_ke
   f2 c[N], wn[N];
   if (has.f()) load_c<V, E>(p, has.x(), slot, t, c);
   if (has.h()) load_param<V, E>(p.w_next, p.D, t, tpr, wn);
-  Part<T, V, E> f, z;
-  Part<XT, V, E> x;
+  Part<T, V, E> f[R], z[R];
+  Part<XT, V, E> x[R];
   const int col = t * V, left = p.D - col;
   // offsets of this thread's elements in the next row (o: of operands with rows of D)
   long long of = slot * p.f_ld + col, oz = slot * p.z_ld + col, ox = slot * p.x_ld + col, o = slot * p.D + col;
-  auto load = [&](long long row) {  // (rows past the end as zeros)
+  auto load = [&](int u, long long row) {  // (rows past the end as zeros)
     const int n = row < p.rows ? left : 0;
-    if (has.f()) f.load((const T *)p.f + of, n, tpr);
-    if (has.gate()) z.load((const T *)p.z + oz, n, tpr);
-    if (has.x()) x.load((const XT *)p.x + ox, n, tpr);
+    if (has.f()) f[u].load((const T *)p.f + of, n, tpr);
+    if (has.gate()) z[u].load((const T *)p.z + oz, n, tpr);
+    if (has.x()) x[u].load((const XT *)p.x + ox, n, tpr);
     of += slots * p.f_ld;
     oz += slots * p.z_ld;
     ox += slots * p.x_ld;
   };
   int calls = 0;
-  load(slot);
-  for (long long base = slot - threadIdx.x / tpr; base < p.rows; base += slots) {
-    const long long row = base + threadIdx.x / tpr;
+#pragma unroll
+  for (int u = 0; u < R; ++u) load(u, slot + u * slots);
+  for (long long base = slot - threadIdx.x / tpr; base < p.rows; base += R * slots) {
+#pragma unroll
+  for (int u = 0; u < R; ++u) {
+    const long long row = base + u * slots + threadIdx.x / tpr;
     const int out = row < p.rows ? left : 0;
     f2 r[N], v[N], zv[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      if (has.f()) v[k] = f.pair(k);
-      if (has.gate()) zv[k] = z.pair(k);
-      if (has.x()) r[k] = x.pair(k);
+      if (has.f()) v[k] = f[u].pair(k);
+      if (has.gate()) zv[k] = z[u].pair(k);
+      if (has.x()) r[k] = x[u].pair(k);
     }
-    load(row + slots);
+    load(u, row + R * slots);
     if (has.f()) {
       f2 ss = pack2(0.f, 0.f);
 #pragma unroll
@@ -236,11 +242,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? kFwdCtas : 1) fwd_ke
     }
     o += slots * p.D;
   }
+  }
 }
 
 template <typename T, typename XT, int V, int E, int THREADS, int MODE>
 __global__ void __launch_bounds__(THREADS, 1) bwd_kernel(const NormP p) {
-  constexpr int N = E / 2;
+  constexpr int N = E / 2, R = kAhead<V, E, MODE, true>;
   __shared__ __align__(16) float sh[2][2][32];
   const Has<MODE> has(p);
   const int tpr = p.tpr, t = threadIdx.x % tpr, per = blockDim.x / tpr;
@@ -248,48 +255,50 @@ __global__ void __launch_bounds__(THREADS, 1) bwd_kernel(const NormP p) {
   const long long slots = (long long)gridDim.x * per;  // (a multiple of heads)
   const float invD = 1.f / (float)p.D;
   const f2 zero2 = pack2(0.f, 0.f);
-  f2 c[N], wn[N], q[N], an[N];
+  f2 c[N], q[N], an[N];
   if (has.f()) load_c<V, E>(p, has.x(), slot, t, c);
-  if (has.h()) load_param<V, E>(p.w_next, p.D, t, tpr, wn);
 #pragma unroll
   for (int k = 0; k < N; ++k) q[k] = an[k] = zero2;
-  Part<T, V, E> f, z, dh, drt;
-  Part<XT, V, E> x, drx;
+  Part<T, V, E> f[R], z[R], dh[R], drt[R];
+  Part<XT, V, E> x[R], drx[R];
   const int col = t * V, left = p.D - col;
   // offsets of this thread's elements in the next row (o: of operands with rows of D)
   long long of = slot * p.f_ld + col, oz = slot * p.z_ld + col, ox = slot * p.x_ld + col, o = slot * p.D + col;
-  auto load = [&](long long row) {  // (rows past the end as zeros)
+  auto load = [&](int u, long long row) {  // (rows past the end as zeros)
     const int n = row < p.rows ? left : 0, nd = p.dr ? n : 0;
-    if (has.f()) f.load((const T *)p.f + of, n, tpr);
-    if (has.gate()) z.load((const T *)p.z + oz, n, tpr);
+    if (has.f()) f[u].load((const T *)p.f + of, n, tpr);
+    if (has.gate()) z[u].load((const T *)p.z + oz, n, tpr);
     if (has.x()) {
-      x.load((const XT *)p.x + ox, n, tpr);
-      drx.load((const XT *)p.dr + o, nd, tpr);
+      x[u].load((const XT *)p.x + ox, n, tpr);
+      drx[u].load((const XT *)p.dr + o, nd, tpr);
     } else {
-      drt.load((const T *)p.dr + o, nd, tpr);
+      drt[u].load((const T *)p.dr + o, nd, tpr);
     }
-    if (has.h()) dh.load((const T *)p.dh + o, n, tpr);
+    if (has.h()) dh[u].load((const T *)p.dh + o, n, tpr);
     of += slots * p.f_ld;
     oz += slots * p.z_ld;
     ox += slots * p.x_ld;
     o += slots * p.D;
   };
   int calls = 0;
-  load(slot);
-  for (long long base = slot - threadIdx.x / tpr; base < p.rows; base += slots) {
-    const long long row = base + threadIdx.x / tpr;
+#pragma unroll
+  for (int u = 0; u < R; ++u) load(u, slot + u * slots);
+  for (long long base = slot - threadIdx.x / tpr; base < p.rows; base += R * slots) {
+#pragma unroll
+  for (int u = 0; u < R; ++u) {
+    const long long row = base + u * slots + threadIdx.x / tpr;
     const int out = row < p.rows ? left : 0;
-    const long long now = o - slots * p.D;  // this row's place (the loads are a row ahead)
+    const long long now = o - R * slots * p.D;  // this row's place (the loads are R rows ahead)
     f2 fi[N], zv[N], act[N], r[N], g[N], d[N];  // f i1; z, then its gradient; act; r; its gradient; dh
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      if (has.f()) fi[k] = f.pair(k);
-      if (has.gate()) zv[k] = z.pair(k);
-      if (has.x()) r[k] = x.pair(k);
-      g[k] = has.x() ? drx.pair(k) : drt.pair(k);
-      if (has.h()) d[k] = dh.pair(k);
+      if (has.f()) fi[k] = f[u].pair(k);
+      if (has.gate()) zv[k] = z[u].pair(k);
+      if (has.x()) r[k] = x[u].pair(k);
+      g[k] = has.x() ? drx[u].pair(k) : drt[u].pair(k);
+      if (has.h()) d[k] = dh[u].pair(k);
     }
-    load(row + slots);
+    load(u, row + R * slots);
     float inv = 0.f;
     if (has.f()) {
       f2 ss = zero2;
@@ -309,7 +318,9 @@ __global__ void __launch_bounds__(THREADS, 1) bwd_kernel(const NormP p) {
       }
     }
     if (has.h()) {  // r, then its gradient
-      f2 s2 = zero2, sd = zero2;
+      // (w_next comes from L1 for every row: with it, too, in registers the kernel spills)
+      f2 s2 = zero2, sd = zero2, wn[N];
+      load_param<V, E>(p.w_next, p.D, t, tpr, wn);
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         if (has.f()) {
@@ -352,6 +363,7 @@ __global__ void __launch_bounds__(THREADS, 1) bwd_kernel(const NormP p) {
       for (int k = 0; k < N; ++k) g[k] = mul2(both(inv), fma2(fi[k], both(m), g[k]));
       store_part<T, V, E>((T *)p.df + now, out, tpr, g);
     }
+  }
   }
   float *mine = p.part + (size_t)slot * 2 * p.D;
   if (has.f()) store_part<float, V, E>(mine + col, left, tpr, q);

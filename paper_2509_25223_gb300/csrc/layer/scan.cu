@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kScanThreads, 7) scan_fwd_kernel(ScanP p) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) store_pairs(p.chunks, slot, slot < p.slots, p, c0, first + 2 * (j ^ (sl & 1)), nch, n0, h[j]);
     }
-#pragma unroll 2
+#pragma unroll 4
     for (int t = 0; t < ntok; ++t) {
       f2 bb[4], cc[4], y[2];
       states4(&sm.B[b][t][n0], 0, bb);
@@ -155,8 +155,7 @@ __global__ void __launch_bounds__(kScanThreads, 7) scan_fwd_kernel(ScanP p) {
       }
       if (p.z) {
         K::get(sm.raw[b][2][i][tid], v);
-#pragma unroll
-        for (int e = 0; e < V; ++e) o[e] *= siluf(v[e]);
+        silu_gate<V>(v, o);
       }
       K::st(O + t * p.out_ld + c, K::put(o));
     }

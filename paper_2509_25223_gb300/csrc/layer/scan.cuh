@@ -324,6 +324,18 @@ __device__ __forceinline__ void store_vec(float *p, const float (&v)[V]) {
   }
 }
 
+// o *= silu(z) of V channels
+template <int V>
+__device__ __forceinline__ void silu_gate(const float (&z)[V], float (&o)[V]) {
+  if constexpr (V % 2 == 0) {
+#pragma unroll
+    for (int e = 0; e < V; e += 2) unpack2(mul2(pack2(o[e], o[e + 1]), silu2(pack2(z[e], z[e + 1]))), o[e], o[e + 1]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] *= siluf(z[e]);
+  }
+}
+
 // V channels' step sizes from dt: bias, softplus; none for a token past the
 // end (dl = 0: a decay of exactly 1, nothing added).
 template <int V>
