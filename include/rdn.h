@@ -384,9 +384,11 @@ rdn_status_t rdn_bwd_workspace_size(const rdn_bwd_args *args, size_t *bytes);
  *    between consecutive token rows of that tensor (0 = contiguous; at least
  *    the row's length; batch row b, token t is row b * T + t), so that an
  *    operand can be a slice of a wider projection's rows.
- *  - Data pointers with row lengths and strides of whole 16-byte groups take
- *    16-byte accesses; others must be aligned to their element and take
- *    single-element accesses.  Parameters and states in fp32 need 4 bytes.
+ *  - Data and parameter pointers need their element's alignment only; rows
+ *    (pointers, lengths and strides) on whole 16-byte groups take 16-byte
+ *    accesses, others single elements.  A and the scan's fp32 states (h0, hT,
+ *    h_chunks, dhT, dh0, h) must be 16-byte aligned.
+ *  - Outputs may not alias inputs.
  *  - cu_seqlens / num_seqs as in rdn_fwd_args (B = 1; empty sequences pass
  *    their states through).
  *  - Sums over tokens (parameter gradients) and over channels (dB, dC) are
@@ -451,7 +453,8 @@ rdn_status_t rdn_conv_step(const rdn_conv_step_args *args, rdn_stream_t stream);
  *     h_t[d,n] = exp(dl_t[d] A[d,n]) h_{t-1}[d,n] + dl_t[d] x_t[d] B_t[g(d),n]
  *     y_t[d] = sum_n C_t[g(d),n] h_t[d,n] + Dskip[d] x_t[d]
  *     out_t = y_t  or, with z,  y_t SiLU(z_t)
- *   B, T              as above;  D >= 1;  1 <= S <= 64;  G divides D.
+ *   B, T              as above;  1 <= D <= 2^19;  1 <= S <= 64;  G divides D,
+ *                     G <= 4096.
  *   dtype             of x, dt, z, out, Bm, Cm, dout and their gradients.
  *   x, dt, z, out     [B,T,D] with row strides; z may be NULL (no gate).
  *   Bm, Cm            [B,T,G,S] with row strides (G * S contiguous).

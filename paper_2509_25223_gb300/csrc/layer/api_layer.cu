@@ -130,8 +130,8 @@ rdn_status_t conv_common(const char *fn, const rdn_conv_args *args, bool bwd, cu
 
 rdn_status_t scan_shapes(const char *fn, rdn_scan_args *a) {
   TRY(check_seqs(fn, a->B, a->T, a->cu_seqlens, a->num_seqs));
-  if (a->D < 1 || a->D > (1 << 20) || a->G < 1 || a->D % a->G)
-    return entry_fail(RDN_ERR_INVALID_ARG, "%s: need 1 <= D <= 2^20 and G dividing D (got D=%d G=%d)", fn, a->D, a->G);
+  if (a->D < 1 || a->D > (1 << 19) || a->G < 1 || a->D % a->G)
+    return entry_fail(RDN_ERR_INVALID_ARG, "%s: need 1 <= D <= 2^19 and G dividing D (got D=%d G=%d)", fn, a->D, a->G);
   if (a->G > 4096) return entry_fail(RDN_ERR_UNSUPPORTED, "%s: at most 4096 groups (got %d)", fn, a->G);
   if (a->S < 1) return entry_fail(RDN_ERR_INVALID_ARG, "%s: need S >= 1 (got %d)", fn, a->S);
   if (a->S > 64) return entry_fail(RDN_ERR_UNSUPPORTED, "%s: at most 64 states (got %d)", fn, a->S);
@@ -335,8 +335,9 @@ rdn_status_t rdn_scan_step(const rdn_scan_step_args *args, rdn_stream_t stream) 
   if (!args) return entry_fail(RDN_ERR_INVALID_ARG, "%s: args is NULL", fn);
   rdn_scan_step_args copy = *args, *a = &copy;
   TRY(check_step(fn, a->N, a->num_slots, a->slots));
-  if (a->D < 1 || a->D > (1 << 20) || a->G < 1 || a->D % a->G)
-    return entry_fail(RDN_ERR_INVALID_ARG, "%s: need 1 <= D <= 2^20 and G dividing D (got D=%d G=%d)", fn, a->D, a->G);
+  if (a->D < 1 || a->D > (1 << 19) || a->G < 1 || a->D % a->G)
+    return entry_fail(RDN_ERR_INVALID_ARG, "%s: need 1 <= D <= 2^19 and G dividing D (got D=%d G=%d)", fn, a->D, a->G);
+  if (a->G > 4096) return entry_fail(RDN_ERR_UNSUPPORTED, "%s: at most 4096 groups (got %d)", fn, a->G);
   if (a->S < 1) return entry_fail(RDN_ERR_INVALID_ARG, "%s: need S >= 1 (got %d)", fn, a->S);
   if (a->S > 64) return entry_fail(RDN_ERR_UNSUPPORTED, "%s: at most 64 states (got %d)", fn, a->S);
   TRY(check_dtype(fn, a->dtype));

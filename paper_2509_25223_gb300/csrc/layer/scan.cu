@@ -52,35 +52,27 @@ __global__ void __launch_bounds__(kScanThreads, 7) scan_fwd_kernel(ScanP p) {
   // channel pair j, state n0 + i
   f2 A2[2][4], h[2][4], sumd[2];
   const f2 shift = pack2(kExpShift, kExpShift);
+  float a[4][4], v[4][4];  // of this lane's 4 channels, pair by pair
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int ch = first + 2 * ((c >> 1) ^ (sl & 1)) + (c & 1);
+    const bool on = ch < nch;
+    const size_t d = c0 + ch;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[c][i] = v[c][i] = 0.f;
+    if (on) load_states(p.A + d * p.S, p.S, n0, a[c]);
+    if (on && !FIRST && p.h0) load_states(p.h0 + ((size_t)w.s * p.D + d) * p.S, p.S, n0, v[c]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[c][i] *= kLog2e;
+  }
+  if (!FIRST) chain<Sh::SP>(p, blockIdx.x - w.j, blockIdx.x, 1, c0 + first, nch - first, sl, a, v);
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    float a[2][4], v[2][4];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int ch = first + 2 * (j ^ (sl & 1)) + e;
-      const size_t d = c0 + ch;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[e][i] = v[e][i] = 0.f;
-      if (ch >= nch) continue;
-      load_states(p.A + d * p.S, p.S, n0, a[e]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[e][i] *= kLog2e;
-      if (FIRST) continue;
-      if (p.h0) load_states(p.h0 + ((size_t)w.s * p.D + d) * p.S, p.S, n0, v[e]);
-      for (int k = 0; k < w.j; ++k) {  // over the units before this one
-        const size_t u = blockIdx.x - w.j + k;
-        const float sd = p.sumd[u * p.D + d];
-        const float4 x = *reinterpret_cast<const float4 *>(p.carry + (u * p.D + d) * Sh::SP + n0);
-        const float xx[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[e][i] = fmaf(decay(sd, a[e][i]), v[e][i], xx[i]);
-      }
-    }
     sumd[j] = pack2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      A2[j][i] = pack2(a[0][i], a[1][i]);
-      h[j][i] = pack2(v[0][i], v[1][i]);
+      A2[j][i] = pack2(a[2 * j][i], a[2 * j + 1][i]);
+      h[j][i] = pack2(v[2 * j][i], v[2 * j + 1][i]);
     }
   }
   const long long r0 = w.begin + (long long)w.j * p.seg;

@@ -299,6 +299,35 @@ __device__ __forceinline__ void store_states(float *row, int S, int n0, const fl
   }
 }
 
+// The states v of a lane's 4 channels (from channel d0 on, `left` of them in the
+// tile; those of the lane's first pair first) over the units from, from + step, ..
+// before `to`: v <- exp(A sum dl) v + the unit's result.  All channels' loads of
+// a few units are in flight together: one channel after the other the chain of a
+// late unit took longer than its tokens.
+template <int SP>
+__device__ __forceinline__ void chain(const ScanP &p, int from, int to, int step, int d0, int left, int sl,
+                                      const float (&a)[4][4], float (&v)[4][4]) {
+#pragma unroll 2
+  for (int u = from; u != to; u += step) {
+    float sd[4];
+    float4 x[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int k = 2 * ((c >> 1) ^ (sl & 1)) + (c & 1);
+      const size_t at = (size_t)u * p.D + d0 + k;
+      sd[c] = k < left ? p.sumd[at] : 0.f;
+      x[c] = k < left ? *reinterpret_cast<const float4 *>(p.carry + at * SP + sl * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      v[c][0] = fmaf(decay(sd[c], a[c][0]), v[c][0], x[c].x);
+      v[c][1] = fmaf(decay(sd[c], a[c][1]), v[c][1], x[c].y);
+      v[c][2] = fmaf(decay(sd[c], a[c][2]), v[c][2], x[c].z);
+      v[c][3] = fmaf(decay(sd[c], a[c][3]), v[c][3], x[c].w);
+    }
+  }
+}
+
 // V consecutive floats of shared memory (16 bytes at a time where V is a multiple of 4)
 template <int V>
 __device__ __forceinline__ void load_vec(const float *p, float (&v)[V]) {

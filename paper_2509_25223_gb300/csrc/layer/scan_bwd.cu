@@ -212,38 +212,36 @@ __global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
   for (int e = 0; e < Sm::AC * V; ++e) sm.acc[0][e / V][tid][e % V] = sm.acc[1][e / V][tid][e % V] = 0.f;
   const f2 shift = pack2(kExpShift, kExpShift), zero2 = pack2(0.f, 0.f);
   f2 A2[2][4], q[2][4], dA[2][4];  // [channel pair][state n0 + (i ^ perm)]
+  {
+    float a[4][4], v[4][4];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    float a[2][4], v[2][4];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int ch = 2 * pair[j] + e;
+    for (int c = 0; c < 4; ++c) {
+      const int ch = 2 * pair[c >> 1] + (c & 1);
+      const bool on = ch < nch;
       const size_t d = c0 + ch;
-      float ta[4] = {0.f, 0.f, 0.f, 0.f}, tv[4] = {0.f, 0.f, 0.f, 0.f};
-      if (ch < nch) {
-        load_states(p.A + d * p.S, p.S, n0, ta);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ta[i] *= kLog2e;
-        if (w.ok) {  // q past the unit's end, over the units after it
-          if (p.dhT) load_states(p.dhT + ((size_t)w.s * p.D + d) * p.S, p.S, n0, tv);
-          for (int k = w.n - 1; k > w.j; --k) {
-            const size_t o = u - w.j + k;
-            const float sd = p.sumd[o * p.D + d];
-            const float4 x = *reinterpret_cast<const float4 *>(p.carry + (o * p.D + d) * Sh::SP + n0);
-            const float xx[4] = {x.x, x.y, x.z, x.w};
+      for (int i = 0; i < 4; ++i) a[c][i] = v[c][i] = 0.f;
+      if (on) load_states(p.A + d * p.S, p.S, n0, a[c]);
+      if (on && w.ok && p.dhT) load_states(p.dhT + ((size_t)w.s * p.D + d) * p.S, p.S, n0, v[c]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) tv[i] = fmaf(decay(sd, ta[i]), tv[i], xx[i]);
-          }
-        }
-      }
-      permute(ta, perm, a[e]);
-      permute(tv, perm, v[e]);
+      for (int i = 0; i < 4; ++i) a[c][i] *= kLog2e;
     }
+    // q past the unit's end, over the units after it
+    if (w.ok) chain<Sh::SP>(p, (int)u - w.j + w.n - 1, (int)u, -1, c0 + first, nch - first, sl, a, v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      A2[j][i] = pack2(a[0][i], a[1][i]);
-      q[j][i] = pack2(v[0][i], v[1][i]);
-      dA[j][i] = zero2;
+    for (int j = 0; j < 2; ++j) {
+      float x[2][4], y[2][4];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        permute(a[2 * j + e], perm, x[e]);
+        permute(v[2 * j + e], perm, y[e]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        A2[j][i] = pack2(x[0][i], x[1][i]);
+        q[j][i] = pack2(y[0][i], y[1][i]);
+        dA[j][i] = zero2;
+      }
     }
   }
   const long long r0 = w.ok ? w.begin + (long long)w.j * p.seg : 0;
