@@ -336,18 +336,18 @@ struct PassTime {
   int resident;
   double least, fixed, each;
   double at(long long r) const {
-    auto wave = [&](long long k) { return fmax(least, fixed + each * k); };
-    return (r / resident) * wave(resident) + (r % resident ? wave(r % resident) : 0.0);
+    auto wave = [&](long long k) { return fmax(least, fixed + each * fmin((double)k, resident)); };
+    return (r / resident) * wave(resident) + (r % resident ? wave(r % resident + 1) : 0.0);
   }
   // the same per token-CTA where units of many lengths fill each other's gaps
   double packed(double sms) const { return (fixed + each * resident) / (resident * sms); }
 };
-constexpr PassTime kFwdTime{8, 0.245, 0.085, 0.040}, kFirstTime{8, 0.140, 0.030, 0.0285};
+constexpr PassTime kFwdTime{8, 0.245, 0.090, 0.037}, kFirstTime{8, 0.150, 0.060, 0.027};
 constexpr PassTime kBwdTime{6, 0.54, 0.25, 0.146};
 
 // Units: the cut of the sequences that ends first by those times, with each
-// unit's start (its parameters, the states of the units before it) as 16 tokens
-// more and half a token for each of the n units.  Packed sequences, whose
+// unit's start (its parameters, the states of the units before it) as 8 tokens
+// more and a quarter of one for each of the n units.  Packed sequences, whose
 // lengths are on the device: their tokens at full occupancy, about half a unit
 // more for each, and one unit's time at the end.  Units are at least 32 tokens.
 ScanPlan scan_plan(const rdn_scan_args &a, bool bwd) {
@@ -363,7 +363,7 @@ ScanPlan scan_plan(const rdn_scan_args &a, bool bwd) {
   const long long T16 = ((long long)a.T + kScanTile - 1) / kScanTile;  // tiles of tokens
   const long long more = a.cu_seqlens ? a.num_seqs / 2 : 0;
   auto time = [&](long long n, long long len) {
-    const double tokens = (double)len * kScanTile, start = 16 + 0.5 * n;
+    const double tokens = (double)len * kScanTile, start = 8 + 0.25 * n;
     const double launch = n > 1 ? 2.0 : 0.0;  // of the first pass
     if (a.cu_seqlens) {
       const double share = 1.0 - 1.0 / n, units = n + more;
@@ -372,17 +372,14 @@ ScanPlan scan_plan(const rdn_scan_args &a, bool bwd) {
     }
     const long long ctas = columns * n, first = columns * (n - 1);
     return main.at((ctas + kSMs - 1) / kSMs) * (tokens + start) +
-           kFirstTime.at((first + kSMs - 1) / kSMs) * (tokens + 16) + launch;
+           kFirstTime.at((first + kSMs - 1) / kSMs) * (tokens + 8) + launch;
   };
   long long best = T16 > 2 ? T16 : 2;  // tiles per unit
   double cost = time(1, best);
   for (long long n = 2; n <= 64 && T16 >= 2 * n; ++n) {
     const long long len = (T16 + n - 1) / n, m = (T16 + len - 1) / len;
     const double c = time(m, len);
-    if (c < cost) {
-      cost = c;
-      best = len;
-    }
+    if (c < cost) { cost = c; best = len; }
   }
   pl.seg = (int)best * kScanTile;
   pl.units_row = a.T > 0 ? (a.T + pl.seg - 1) / pl.seg : 1;
