@@ -24,7 +24,7 @@ namespace rdn {
 namespace {
 
 constexpr int kConvThreads = 128;
-constexpr int kFwdGroup = 4;  // tokens whose loads a thread issues together
+constexpr int kFwdGroup = 8;  // tokens whose loads a thread issues together
 constexpr int kBwdGroup = 4;
 constexpr int kRunStep = 8, kRunMost = 64;  // tokens of a thread's run
 
@@ -108,22 +108,40 @@ __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(ConvP p) {
   const long long unit = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   const long long units = (long long)p.B * p.runs;
   __shared__ float sh[32 * (V * W + 1)];
-  f2 tap[W][P], bias[P];
-  load_taps<W, V>(p, c0, sh, tap, bias);
-  if (c0 >= p.C || unit >= units) return;
-  pass_empty<T, W, V>(p, unit, units, c0, p.state0, p.stateT);
-  const int b = (int)(unit / p.runs), t0 = (int)(unit % p.runs) * p.run;
-  if (t0 >= p.T) return;
+  const bool live = c0 < p.C && unit < units;
+  const int b = live ? (int)(unit / p.runs) : 0, t0 = live ? (int)(unit % p.runs) * p.run : p.T;
   const long long r0 = (long long)b * p.T + t0;
   const long long r1 = r0 + min(p.run, p.T - t0);
-  const T *X = (const T *)p.x + c0;
-  T *Y = (T *)p.y + c0;
-  SeqSpan q = find_seq(p.cu, p.ns, p.T, b, t0);
+  const T *X = (const T *)p.x + c0, *xr = X + r0 * p.x_ld;
+  T *Y = (T *)p.y + c0, *yr = Y + r0 * p.y_ld;
+  typename K::Raw raw[U], next[U];
+  auto load = [&](long long g) {  // the group from row g on, xr its first
+    if (g + U <= r1) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) next[u] = K::ld(xr + u * p.x_ld);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) next[u] = g + u < r1 ? K::ld(xr + u * p.x_ld) : K::zero();
+    }
+    xr += U * p.x_ld;
+  };
+  load(r0);  // (in flight while the taps come)
+  typename K::Raw before[W - 1];
+  SeqSpan q{};
+  if (t0 < p.T) {
+    q = find_seq(p.cu, p.ns, p.T, b, t0);
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k) before[k] = r0 - 1 - k >= q.begin ? K::ld(X + (r0 - 1 - k) * p.x_ld) : K::zero();
+  }
+  f2 tap[W][P], bias[P];
+  load_taps<W, V>(p, c0, sh, tap, bias);
+  if (live) pass_empty<T, W, V>(p, unit, units, c0, p.state0, p.stateT);
+  if (t0 >= p.T) return;
   f2 win[W - 1][P];  // win[k] = x_{t-1-k}
 #pragma unroll
   for (int k = 0; k < W - 1; ++k) {
     const long long r = r0 - 1 - k;
-    if (r >= q.begin) get_pairs<T, V>(K::ld(X + r * p.x_ld), win[k]);
+    if (r >= q.begin) get_pairs<T, V>(before[k], win[k]);
     else from_state<T, W, V>(p, q.s, (int)(W - 1 + r - q.begin), c0, win[k]);
   }
   auto token = [&](const typename K::Raw &raw, T *y) {
@@ -146,20 +164,6 @@ __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(ConvP p) {
     for (int k = 0; k < W - 1; ++k)
       K::st((T *)p.stateT + ((size_t)q.s * (W - 1) + W - 2 - k) * p.C + c0, put_pairs<T, V>(win[k]));
   };
-  const T *xr = X + r0 * p.x_ld;
-  T *yr = Y + r0 * p.y_ld;
-  typename K::Raw raw[U], next[U];
-  auto load = [&](long long g) {  // the group from row g on, xr its first
-    if (g + U <= r1) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) next[u] = K::ld(xr + u * p.x_ld);
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) next[u] = g + u < r1 ? K::ld(xr + u * p.x_ld) : K::zero();
-    }
-    xr += U * p.x_ld;
-  };
-  load(r0);
   for (long long g = r0; g < r1; g += U, yr += U * p.y_ld) {
 #pragma unroll
     for (int u = 0; u < U; ++u) raw[u] = next[u];
@@ -198,6 +202,41 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
   const long long unit = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   const long long units = (long long)p.B * p.runs;
   const bool live = c0 < p.C && unit < units;
+  const int b = live ? (int)(unit / p.runs) : 0, t0 = live ? (int)(unit % p.runs) * p.run : p.T;
+  const long long rb0 = (long long)b * p.T, rb1 = rb0 + p.T;
+  const long long r0 = rb0 + t0, r1 = r0 + min(p.run, p.T - t0);
+  const long long top = min(r1 + W - 2, rb1 - 1);  // dx of the last row takes dp of the W-1 rows after it
+  const T *X = (const T *)p.x + c0, *DY = (const T *)p.dy + c0;
+  T *DX = (T *)p.dx + c0;
+  // groups [g, g + U) from the top down; xr[i] = x row g - (W-1) + i
+  typename K::Raw xr[U + W - 1], xn[U], dyr[U], dyn[U];
+  long long g = r0 + (top - r0) / U * U;
+  const T *xp = X + (g - (W - 1)) * p.x_ld, *dyp = DY + g * p.dy_ld;
+  T *dxp = DX + g * p.dx_ld;
+  auto load = [&](long long at) {  // the rows a group needs beside those of the one above: xp and dyp its first
+    if (at - (W - 1) >= rb0 && at + U - 1 <= top && at >= r0) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        xn[i] = K::ld(xp + i * p.x_ld);
+        dyn[i] = K::ld(dyp + i * p.dy_ld);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const long long r = at - (W - 1) + i;
+        xn[i] = r >= rb0 && r <= top && at >= r0 ? K::ld(xp + i * p.x_ld) : K::zero();
+        dyn[i] = at >= r0 && at + i <= top ? K::ld(dyp + i * p.dy_ld) : K::zero();
+      }
+    }
+    xp -= U * p.x_ld;
+    dyp -= U * p.dy_ld;
+  };
+#pragma unroll
+  for (int i = 0; i < W - 1; ++i) {
+    const long long r = g + U - (W - 1) + i;
+    xr[i] = t0 < p.T && r >= rb0 && r <= top ? K::ld(X + r * p.x_ld) : K::zero();
+  }
+  if (t0 < p.T) load(g);  // (in flight while the taps come)
   f2 tap[W][P], bias[P];
   load_taps<W, V>(p, c0, sh, tap, bias);
   f2 dw[W + 1][P];  // dw[k] of tap[k]; dw[W]: the bias
@@ -206,13 +245,7 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
 #pragma unroll
     for (int e = 0; e < P; ++e) dw[k][e] = pack2(0.f, 0.f);
   if (live) pass_empty<T, W, V>(p, unit, units, c0, p.dstateT, p.dstate0);
-  const int b = live ? (int)(unit / p.runs) : 0, t0 = live ? (int)(unit % p.runs) * p.run : p.T;
-  if (live && t0 < p.T) {
-    const long long rb0 = (long long)b * p.T, rb1 = rb0 + p.T;
-    const long long r0 = rb0 + t0, r1 = r0 + min(p.run, p.T - t0);
-    const long long top = min(r1 + W - 2, rb1 - 1);  // dx of the last row takes dp of the W-1 rows after it
-    const T *X = (const T *)p.x + c0, *DY = (const T *)p.dy + c0;
-    T *DX = (T *)p.dx + c0;
+  if (t0 < p.T) {
     SeqSpan q = find_seq(p.cu, p.ns, p.T, b, (int)(top - rb0));
     f2 dpw[W - 1][P];  // dpw[k] = dp_{t+1+k} of the same sequence
 #pragma unroll
@@ -252,35 +285,6 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
         dpw[0][e] = dp[e];
       }
     };
-    // groups [g, g + U) from the top down; xr[i] = x row g - (W-1) + i
-    typename K::Raw xr[U + W - 1], xn[U], dyr[U], dyn[U];
-    long long g = r0 + (top - r0) / U * U;
-    const T *xp = X + (g - (W - 1)) * p.x_ld, *dyp = DY + g * p.dy_ld;
-    T *dxp = DX + g * p.dx_ld;
-    auto load = [&](long long at) {  // the rows a group needs beside those of the one above: xp and dyp its first
-      if (at - (W - 1) >= rb0 && at + U - 1 <= top && at >= r0) {
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          xn[i] = K::ld(xp + i * p.x_ld);
-          dyn[i] = K::ld(dyp + i * p.dy_ld);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const long long r = at - (W - 1) + i;
-          xn[i] = r >= rb0 && r <= top && at >= r0 ? K::ld(xp + i * p.x_ld) : K::zero();
-          dyn[i] = at >= r0 && at + i <= top ? K::ld(dyp + i * p.dy_ld) : K::zero();
-        }
-      }
-      xp -= U * p.x_ld;
-      dyp -= U * p.dy_ld;
-    };
-#pragma unroll
-    for (int i = 0; i < W - 1; ++i) {
-      const long long r = g + U - (W - 1) + i;
-      xr[i] = r >= rb0 && r <= top ? K::ld(X + r * p.x_ld) : K::zero();
-    }
-    load(g);
     for (; g >= r0; g -= U, dxp -= U * p.dx_ld) {
 #pragma unroll
       for (int i = W - 2; i >= 0; --i) xr[U + i] = xr[i];
@@ -486,12 +490,13 @@ ConvPlan conv_plan(const rdn_conv_args &a, int V) {
   return pl;
 }
 
-// Channels per thread: a 16-byte access in the forward, 4 in the backward, whose
-// registers hold up to 4 W + 1 values per channel; single ones where the rows do
-// not lie on those bytes.
+// Four channels per thread (in the backward the registers hold up to 4 W + 1
+// values per channel; in the forward 8 bf16 channels leave room for the loads of 4
+// tokens instead of 8: 56 us instead of 50 at 8 x 4096 x 2048); single ones where
+// the rows do not lie on that access.
 bool conv_vec(const rdn_conv_args &a, bool bwd) {
   const size_t size = a.dtype == RDN_BF16 ? 2 : 4;
-  const int V = bwd ? 4 : (int)(16 / size);
+  const int V = 4;
   const size_t bytes = V * size;
   if (a.C % V) return false;
   return bwd ? rows_on(bytes, size, {{a.x, a.x_ld}, {a.dy, a.dy_ld}, {a.dx, a.dx_ld}, {a.state0, 0},
@@ -536,7 +541,7 @@ template <typename T, int W>
 cudaError_t conv_w(const rdn_conv_args &a, bool bwd, cudaStream_t s) {
   const bool vec = conv_vec(a, bwd);
   if (bwd) return vec ? bwd_t<T, W, 4>(a, s) : bwd_t<T, W, 1>(a, s);
-  return vec ? fwd_t<T, W, kVec<T>>(a, s) : fwd_t<T, W, 1>(a, s);
+  return vec ? fwd_t<T, W, 4>(a, s) : fwd_t<T, W, 1>(a, s);
 }
 template <typename T>
 cudaError_t conv_d(const rdn_conv_args &a, bool bwd, cudaStream_t s) {

@@ -414,6 +414,7 @@ bool scan_vec(const rdn_scan_args &a, bool bwd) {
   auto on = [&](const void *p, long long ld) { return !p || (((uintptr_t)p | (size_t)ld * size) & 15) == 0; };
   if (!on(a.x, a.x_ld) || !on(a.dt, a.dt_ld) || !on(a.z, a.z_ld)) return false;
   if (!bwd) return on(a.out, a.out_ld);
+  if (!on(a.dt_bias, 0) || !on(a.Dskip, 0)) return false;  // read once per tile
   return on(a.dout, a.dout_ld) && on(a.dx, a.dx_ld) && on(a.ddt, a.ddt_ld) && on(a.dz, a.dz_ld);
 }
 

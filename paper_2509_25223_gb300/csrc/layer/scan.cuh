@@ -353,6 +353,20 @@ __device__ __forceinline__ void store_vec(float *p, const float (&v)[V]) {
   }
 }
 
+// the same as pairs (V = 1: with a zero)
+template <int V>
+__device__ __forceinline__ void get_pairs(const float *p, f2 (&v)[(V + 1) / 2]) {
+  float a[V];
+  load_vec<V>(p, a);
+  to_pairs<V>(a, v);
+}
+template <int V>
+__device__ __forceinline__ void put_pairs(float *p, const f2 (&v)[(V + 1) / 2]) {
+  float a[V];
+  from_pairs<V>(v, a);
+  store_vec<V>(p, a);
+}
+
 // o *= silu(z) of V channels
 template <int V>
 __device__ __forceinline__ void silu_gate(const float (&z)[V], float (&o)[V]) {
@@ -365,14 +379,20 @@ __device__ __forceinline__ void silu_gate(const float (&z)[V], float (&o)[V]) {
   }
 }
 
+// a parameter of V channels from d on (zero where there is none; V > 1: on 16 bytes)
+template <int V>
+__device__ __forceinline__ void param(const float *p, int d, bool on, float (&v)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = 0.f;
+  if (p && on) load_vec<V>(p + d, v);
+}
+
 // V channels' step sizes from dt: bias, softplus; none for a token past the
 // end (dl = 0: a decay of exactly 1, nothing added).
 template <int V>
-__device__ __forceinline__ void step_sizes(const ScanP &p, const float *bias, bool live, float (&dl)[V]) {
-  float b[V];
-  load_vec<V>(bias, b);
+__device__ __forceinline__ void step_sizes(const ScanP &p, const float (&bias)[V], bool live, float (&dl)[V]) {
 #pragma unroll
-  for (int e = 0; e < V; ++e) dl[e] += b[e];
+  for (int e = 0; e < V; ++e) dl[e] += bias[e];
   if (p.softplus) {
     if constexpr (V % 2 == 0) {
 #pragma unroll
@@ -386,6 +406,12 @@ __device__ __forceinline__ void step_sizes(const ScanP &p, const float *bias, bo
 #pragma unroll
     for (int e = 0; e < V; ++e) dl[e] = 0.f;
   }
+}
+template <int V>
+__device__ __forceinline__ void step_sizes(const ScanP &p, const float *bias, bool live, float (&dl)[V]) {
+  float b[V];
+  load_vec<V>(bias, b);
+  step_sizes<V>(p, b, live, dl);
 }
 // Two values of each of V channels from channel c on into a token's row of
 // entries (a, a', b, b') of channel pairs.

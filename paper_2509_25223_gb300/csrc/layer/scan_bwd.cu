@@ -9,11 +9,13 @@
 //
 // The states are recomputed from those kept at every 16 tokens: 4 tokens' states
 // at a time stay in registers (4 x 16 pairs per lane) while the reverse steps
-// consume them; the two halves of a tile and the two of a half start from states
-// advanced once more, so that a token is recomputed twice.  Keeping 8 tokens'
-// states takes 255 registers and a loop body beyond the instruction cache: 744 us
-// for 4 x 2048 x 4096 channels where this takes 680.  About 16 multiply-adds and
-// 3 exponentials per (token, channel, state), 26 instructions in all: bound by
+// consume them, from states advanced once through the tile and left in shared
+// memory at every fourth token, so that three tokens of four are recomputed twice.
+// Keeping 8 tokens' states in registers takes 255 of them and a loop body beyond
+// the instruction cache: 744 us for 4 x 2048 x 4096 channels of 16 states where
+// this takes 660 (0.81e12 (token, channel, state) per second, 14 % of the HBM
+// rate).  About 15 multiply-adds and 2.75 exponentials for each of those, 25
+// instructions in all: bound by
 // instruction issue (the FMA pipe is busy a third of the time).  The sums over
 // channels for dB and dC are exchanged within a warp in an order that needs no
 // selects (the lanes that exchange hold their four states in orders that differ by
@@ -100,8 +102,7 @@ __global__ void __launch_bounds__(kScanThreads, 7) scan_bwd_carry_kernel(ScanP p
       step_sizes<V>(p, sm.bias + c, t < ntok, dl);
       if (p.z) {
         K::get(sm.raw[1][i][tid], zv);
-#pragma unroll
-        for (int e = 0; e < V; ++e) gv[e] *= siluf(zv[e]);
+        silu_gate<V>(zv, gv);
       }
       store_two<V>(sm.dg[t], c, dl, gv);
     }
@@ -177,13 +178,12 @@ struct BwdSmem {
   float red[kScanWarps][kHalf][2 * Sh::SP];          // dB, dC of each warp's channels
   static constexpr int AC = Sh::COLS > kScanThreads ? Sh::COLS / kScanThreads : 1;  // columns of a thread
   float acc[2][AC][kScanThreads][Sh::V];             // dD and ddt_bias of a thread's elements
-  float4 kept[2][4][kScanThreads];                   // each lane's states before the tile and before its second half
-  T B[2][kScanTile][Sh::SP], C[2][kScanTile][Sh::SP];
-  float bias[Sh::CT], D[Sh::CT];
+  float4 kept[3][4][kScanThreads];                   // each lane's states before tokens 0, 4 and 8 of the tile
+  T B[kScanTile][Sh::SP], C[kScanTile][Sh::SP];
 };
 
 template <typename T, int L, bool VEC>
-__global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
+__global__ void __launch_bounds__(kScanThreads, L == 2 ? 4 : 6) scan_bwd_kernel(ScanP p) {
   using Sh = ScanShape<T, L, VEC>;
   using K = typename Sh::K;
   constexpr int V = Sh::V;
@@ -203,10 +203,6 @@ __global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
   for (int j = 0; j < 2; ++j) {
     pair[j] = first / 2 + (j ^ (sl & 1));
     at[j] = spread16(pair[j]);
-  }
-  for (int c = tid; c < Sh::CT; c += kScanThreads) {
-    sm.bias[c] = p.dt_bias && c < nch ? p.dt_bias[c0 + c] : 0.f;
-    sm.D[c] = p.Dskip && c < nch ? p.Dskip[c0 + c] : 0.f;
   }
 #pragma unroll
   for (int e = 0; e < Sm::AC * V; ++e) sm.acc[0][e / V][tid][e % V] = sm.acc[1][e / V][tid][e % V] = 0.f;
@@ -249,10 +245,11 @@ __global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
   const long long last = r1 > r0 ? r0 + (r1 - 1 - r0) / kScanTile * kScanTile : r0 - kScanTile;
   const T *X = (const T *)p.x + c0, *DT = (const T *)p.dt + c0, *DO = (const T *)p.dout + c0;
   const T *Bm = (const T *)p.Bm + (size_t)g * p.S, *Cm = (const T *)p.Cm + (size_t)g * p.S;
-  auto load = [&](long long r, int b) {
+  // the rows of the tile at r into L2 now, into shared memory when it is begun
+  auto ahead = [&](long long r) {
     const int ntok = r < r0 ? 0 : (int)min((long long)kScanTile, r1 - r);
 #pragma unroll
-    for (int i = 0; i < Sh::NV; ++i) {  // the rows come into L2 now, into registers when the tile is begun
+    for (int i = 0; i < Sh::NV; ++i) {
       const int t = Sh::tok(i), c = Sh::chan(i);
       if (t >= ntok || c >= nch) continue;
       prefetch(X + (r + t) * p.x_ld + c);
@@ -260,8 +257,11 @@ __global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
       prefetch(DO + (r + t) * p.dout_ld + c);
       if (p.z) prefetch((const T *)p.z + c0 + (r + t) * p.z_ld + c);
     }
-    fetch_states(sm.B[b], Bm + r * p.b_ld, p.b_ld, ntok, p.S, p.bc_vec);
-    fetch_states(sm.C[b], Cm + r * p.c_ld, p.c_ld, ntok, p.S, p.bc_vec);
+    constexpr int sector = 32 / (int)sizeof(T);
+    if (tid % kScanTile < ntok) {
+      const T *row = tid / kScanTile % 2 ? Cm + (r + tid % kScanTile) * p.c_ld : Bm + (r + tid % kScanTile) * p.b_ld;
+      for (int n = tid / (2 * kScanTile) * sector; n < p.S; n += kScanThreads / (2 * kScanTile) * sector) prefetch(row + n);
+    }
   };
   // the kept states before the tile at r: read by this lane alone
   auto load_kept = [&](long long r) {
@@ -280,16 +280,12 @@ __global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
       }
     }
   };
-  if (last >= r0) {
-    load(last, 0);
-    load_kept(last);
-  }
-  __syncthreads();  // bias, D
-  int b = 0;
-  for (long long r = last; r >= r0; r -= kScanTile, b ^= 1) {
+  if (last >= r0) load_kept(last);
+  for (long long r = last; r >= r0; r -= kScanTile) {
     const int ntok = (int)min((long long)kScanTile, r1 - r);
-    fetched();
     // the tile's operands into shared memory
+    fetch_states(sm.B, Bm + r * p.b_ld, p.b_ld, ntok, p.S, p.bc_vec);
+    fetch_states(sm.C, Cm + r * p.c_ld, p.c_ld, ntok, p.S, p.bc_vec);
     typename Sh::Raw raw[4][Sh::NV];
 #pragma unroll
     for (int i = 0; i < Sh::NV; ++i) {
@@ -308,20 +304,21 @@ __global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
       K::get(raw[0][i], xv);
       K::get(raw[1][i], dl);
       K::get(raw[3][i], gv);
-      step_sizes<V>(p, sm.bias + c, t < ntok, dl);
+      param<V>(p.dt_bias, c0 + c, c < nch, zv);
+      step_sizes<V>(p, zv, t < ntok, dl);
       if (p.z) {
         K::get(raw[2][i], zv);
-#pragma unroll
-        for (int e = 0; e < V; ++e) gv[e] *= siluf(zv[e]);
+        silu_gate<V>(zv, gv);
       }
       store_steps<V>(sm.dx[t], c, dl, xv);
       store_vec<V>(&sm.gy[t][0].x + c, gv);
     }
+    fetched();
     __syncthreads();
-    load(r - kScanTile, b ^ 1);
+    ahead(r - kScanTile);
     auto step = [&](int t, const f2 (&from)[2][4], f2 (&to)[2][4]) {
       f2 bb[4];
-      states4(&sm.B[b][t][n0], perm, bb);
+      states4(&sm.B[t][n0], perm, bb);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dx[t][at[j]]);
@@ -343,20 +340,24 @@ __global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
         for (int i = 0; i < 4; ++i) h[j][i] = pack2(v[0][i], v[1][i]);
       }
     };
-    if (ntok > kHalf) {
-      f2 h[2][4];
-      states(0, h);
+    // the states before the tile's last quarter, those before the others kept on the way
+    f2 h0[2][4];
+    states(0, h0);
+    const int quarter = (ntok - 1) / kSub;
+#pragma unroll 1
+    for (int k = 0; k < quarter; ++k) {
 #pragma unroll 2
-      for (int t = 0; t < kHalf; ++t) step(t, h, h);
+      for (int t = 0; t < kSub; ++t) step(k * kSub + t, h0, h0);
+      if (k == 2) break;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         float x[2][4], v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) unpack2(h[j][i], x[0][i], x[1][i]);
+        for (int i = 0; i < 4; ++i) unpack2(h0[j][i], x[0][i], x[1][i]);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           permute(x[e], perm, v);
-          sm.kept[1][2 * j + e][tid] = make_float4(v[0], v[1], v[2], v[3]);
+          sm.kept[k + 1][2 * j + e][tid] = make_float4(v[0], v[1], v[2], v[3]);
         }
       }
     }
@@ -366,22 +367,17 @@ __global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
 #pragma unroll 1
       for (int sub = nh > kSub ? 1 : 0; sub >= 0; --sub) {
         const int ts = th + sub * kSub;
-        f2 h0[2][4], hist[kSub][2][4];
-        states(half, h0);
-        if (!half && !sub) load_kept(r - kScanTile);
-#pragma unroll 1
-        for (int t = 0; t < sub * kSub; t += 2) {
-          step(th + t, h0, h0);
-          step(th + t + 1, h0, h0);
-        }
+        f2 hist[kSub][2][4];
+        if (ts < quarter * kSub) states(ts / kSub, h0);
+        if (ts == 0) load_kept(r - kScanTile);
 #pragma unroll
         for (int t = 0; t < kSub; ++t) step(ts + t, t ? hist[t - 1] : h0, hist[t]);
 #pragma unroll
         for (int tl = kSub - 1; tl >= 0; --tl) {
           const int t = ts + tl, tr = t - th;
           f2 bb[4], cc[4], db[4], dc[4], gB[2], Aq[2], y[2];
-          states4(&sm.B[b][t][n0], perm, bb);
-          states4(&sm.C[b][t][n0], perm, cc);
+          states4(&sm.B[t][n0], perm, bb);
+          states4(&sm.C[t][n0], perm, cc);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dx[t][at[j]]);
@@ -406,14 +402,14 @@ __global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
             dbv[i] = sum2(db[i]);
             dcv[i] = sum2(dc[i]);
           }
-        sum_channels<L>(dbv, dcv, sl, cl, &sm.red[warp][tr][0]);
+          sum_channels<L>(dbv, dcv, sl, cl, &sm.red[warp][tr][0]);
           sum_states<L>(gB, sm.sums[0][tr], first, sl);
           sum_states<L>(Aq, sm.sums[1][tr], first, sl);
           if (p.z) sum_states<L>(y, sm.sums[2][tr], first, sl);
         }
       }
       // results of the half's elements; its operands once more, from the caches
-      constexpr int NH = (Sh::NV + 1) / 2;
+      constexpr int NH = (Sh::NV + 1) / 2, P = (V + 1) / 2;
       typename Sh::Raw own[4][NH];
 #pragma unroll
       for (int i = 0; i < NH; ++i) {
@@ -431,50 +427,63 @@ __global__ void __launch_bounds__(kScanThreads, 6) scan_bwd_kernel(ScanP p) {
         const int t = Sh::tok(i), c = Sh::chan(i);
         if (t >= nh || c >= nch) continue;
         const long long row = r + th + t;
-        float xv[V], v[V], gy[V], gB[V], r0v[V], r1v[V], Dk[V], bias[V];
-        K::get(own[0][i], xv);
-        K::get(own[1][i], v);
-        load_vec<V>(&sm.gy[th + t][0].x + c, gy);
-        load_vec<V>(&sm.sums[0][t][c], gB);
-        load_vec<V>(&sm.sums[1][t][c], r1v);
-        load_vec<V>(sm.D + c, Dk);
-        load_vec<V>(sm.bias + c, bias);
+        float f[V];  // of one operand or result
+        f2 xv[P], v[P], gy[P], gB[P], Aq[P], Dk[P], o[P];
+        K::get(own[0][i], f);
+        to_pairs<V>(f, xv);
+        K::get(own[1][i], f);
+        to_pairs<V>(f, v);
+        get_pairs<V>(&sm.gy[th + t][0].x + c, gy);
+        get_pairs<V>(&sm.sums[0][t][c], gB);
+        get_pairs<V>(&sm.sums[1][t][c], Aq);
+        param<V>(p.Dskip, c0 + c, true, f);
+        to_pairs<V>(f, Dk);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          r0v[e] = (&sm.dx[th + t][spread16((c + e) / 2)].x)[(c + e) & 1] * gB[e];
-          r1v[e] = fmaf(r1v[e], kLn2, gB[e] * xv[e]);
+        for (int e = 0; e < P; ++e) {
+          const float4 *d = &sm.dx[th + t][spread16(c / 2 + e)];
+          const f2 dl = V > 1 ? *reinterpret_cast<const f2 *>(d) : pack2((&d->x)[c & 1], 0.f);
+          o[e] = mul2(dl, gB[e]);
+          Aq[e] = fma2(Aq[e], pack2(kLn2, kLn2), mul2(gB[e], xv[e]));
         }
         if (p.Dskip) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) r0v[e] = fmaf(Dk[e], gy[e], r0v[e]);
+          for (int e = 0; e < P; ++e) o[e] = fma2(Dk[e], gy[e], o[e]);
         }
         if (p.softplus) {
+          f2 bias[P];
+          param<V>(p.dt_bias, c0 + c, true, f);
+          to_pairs<V>(f, bias);
 #pragma unroll
-          for (int e = 0; e < V; ++e) r1v[e] *= sigmoidf(v[e] + bias[e]);
+          for (int e = 0; e < P; ++e) Aq[e] = mul2(Aq[e], sigmoid2(add2(v[e], bias[e])));
         }
-        K::st((T *)p.dx + c0 + row * p.dx_ld + c, K::put(r0v));
-        K::st((T *)p.ddt + c0 + row * p.ddt_ld + c, K::put(r1v));
+        from_pairs<V>(o, f);
+        K::st((T *)p.dx + c0 + row * p.dx_ld + c, K::put(f));
+        from_pairs<V>(Aq, f);
+        K::st((T *)p.ddt + c0 + row * p.ddt_ld + c, K::put(f));
         float *aD = sm.acc[0][i % Sm::AC][tid], *ab = sm.acc[1][i % Sm::AC][tid];
-        load_vec<V>(aD, r0v);
-        load_vec<V>(ab, v);
+        get_pairs<V>(aD, o);
+        get_pairs<V>(ab, v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          r0v[e] = fmaf(gy[e], xv[e], r0v[e]);
-          v[e] += r1v[e];
+        for (int e = 0; e < P; ++e) {
+          o[e] = fma2(gy[e], xv[e], o[e]);
+          v[e] = add2(v[e], Aq[e]);
         }
-        store_vec<V>(aD, r0v);
-        store_vec<V>(ab, v);
+        put_pairs<V>(aD, o);
+        put_pairs<V>(ab, v);
         if (p.z) {
-          K::get(own[2][i], v);
-          K::get(own[3][i], gy);
-          load_vec<V>(&sm.sums[2][t][c], gB);
+          K::get(own[2][i], f);
+          to_pairs<V>(f, v);
+          K::get(own[3][i], f);
+          to_pairs<V>(f, gy);
+          get_pairs<V>(&sm.sums[2][t][c], o);
           if (p.Dskip) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) gB[e] = fmaf(Dk[e], xv[e], gB[e]);
+            for (int e = 0; e < P; ++e) o[e] = fma2(Dk[e], xv[e], o[e]);
           }
 #pragma unroll
-          for (int e = 0; e < V; ++e) r0v[e] = gy[e] * gB[e] * silu_grad(v[e], sigmoidf(v[e]));
-          K::st((T *)p.dz + c0 + row * p.dz_ld + c, K::put(r0v));
+          for (int e = 0; e < P; ++e) o[e] = mul2(mul2(gy[e], o[e]), silu_grad2(v[e]));
+          from_pairs<V>(o, f);
+          K::st((T *)p.dz + c0 + row * p.dz_ld + c, K::put(f));
         }
       }
       for (int i = tid; i < nh * 2 * Sh::SP; i += kScanThreads) {

@@ -61,6 +61,12 @@ def test_lengths(T, dtype):
     compare(make(2, T, 24, 16, dtype=dtype, seed=T))
 
 
+@pytest.mark.parametrize("T", [3, 5, 8, 9, 12, 13, 25])
+def test_lengths_within_a_tile(T):
+    """(the backward keeps states at every fourth token of sixteen)"""
+    compare(make(2, T, 24, 16, seed=T))
+
+
 @pytest.mark.parametrize("S", [1, 3, 4, 5, 8, 9, 12, 16, 20, 32, 33, 48, 64])
 def test_states(S):
     compare(make(1, 70, 16, S, dtype="f32", seed=S))
@@ -98,6 +104,17 @@ def test_steps_given_directly():
 @pytest.mark.parametrize("pad", [2, 64])
 def test_strided_rows(pad, dtype):
     compare(make(2, 40, 48, 16, dtype=dtype, pad=pad))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_parameters_at_odd_addresses(dtype):
+    x = make(1, 40, 64, 16, dtype=dtype, seed=3)
+    for k in ("D", "dt_bias"):
+        at = torch.empty(65, device="cuda")
+        at[1:] = x[k]
+        x[k] = at[1:]
+        assert x[k].data_ptr() % 16
+    compare(x)
 
 
 def test_operands_of_one_projection():
