@@ -110,12 +110,12 @@ __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(ConvP p) {
   __shared__ float sh[32 * (V * W + 1)];
   const bool live = c0 < p.C && unit < units;
   const int b = live ? (int)(unit / p.runs) : 0, t0 = live ? (int)(unit % p.runs) * p.run : p.T;
-  const long long r0 = (long long)b * p.T + t0;
-  const long long r1 = r0 + min(p.run, p.T - t0);
-  const T *X = (const T *)p.x + c0, *xr = X + r0 * p.x_ld;
-  T *Y = (T *)p.y + c0, *yr = Y + r0 * p.y_ld;
+  const long long rb = (long long)b * p.T;  // (rows below are counted from there)
+  const int r0 = t0, r1 = t0 + min(p.run, p.T - t0);
+  const T *X = (const T *)p.x + c0 + rb * p.x_ld, *xr = X + r0 * p.x_ld;
+  T *yr = (T *)p.y + c0 + (rb + r0) * p.y_ld;
   typename K::Raw raw[U], next[U];
-  auto load = [&](long long g) {  // the group from row g on, xr its first
+  auto load = [&](int g) {  // the group from row g on, xr its first
     if (g + U <= r1) {
 #pragma unroll
       for (int u = 0; u < U; ++u) next[u] = K::ld(xr + u * p.x_ld);
@@ -127,11 +127,14 @@ __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(ConvP p) {
   };
   load(r0);  // (in flight while the taps come)
   typename K::Raw before[W - 1];
-  SeqSpan q{};
+  int qs = 0, qb = 0, qe = 0;  // the sequence, its first row and the one after its last
   if (t0 < p.T) {
-    q = find_seq(p.cu, p.ns, p.T, b, t0);
+    const SeqSpan q = find_seq(p.cu, p.ns, p.T, b, t0);
+    qs = q.s;
+    qb = (int)(q.begin - rb);
+    qe = (int)(q.end - rb);
 #pragma unroll
-    for (int k = 0; k < W - 1; ++k) before[k] = r0 - 1 - k >= q.begin ? K::ld(X + (r0 - 1 - k) * p.x_ld) : K::zero();
+    for (int k = 0; k < W - 1; ++k) before[k] = r0 - 1 - k >= qb ? K::ld(X + (r0 - 1 - k) * p.x_ld) : K::zero();
   }
   f2 tap[W][P], bias[P];
   load_taps<W, V>(p, c0, sh, tap, bias);
@@ -140,9 +143,9 @@ __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(ConvP p) {
   f2 win[W - 1][P];  // win[k] = x_{t-1-k}
 #pragma unroll
   for (int k = 0; k < W - 1; ++k) {
-    const long long r = r0 - 1 - k;
-    if (r >= q.begin) get_pairs<T, V>(before[k], win[k]);
-    else from_state<T, W, V>(p, q.s, (int)(W - 1 + r - q.begin), c0, win[k]);
+    const int r = r0 - 1 - k;
+    if (r >= qb) get_pairs<T, V>(before[k], win[k]);
+    else from_state<T, W, V>(p, qs, W - 1 + r - qb, c0, win[k]);
   }
   auto token = [&](const typename K::Raw &raw, T *y) {
     f2 x[P], o[P];
@@ -162,33 +165,33 @@ __global__ void __launch_bounds__(kConvThreads) conv_fwd_kernel(ConvP p) {
   auto last_state = [&]() {
 #pragma unroll
     for (int k = 0; k < W - 1; ++k)
-      K::st((T *)p.stateT + ((size_t)q.s * (W - 1) + W - 2 - k) * p.C + c0, put_pairs<T, V>(win[k]));
+      K::st((T *)p.stateT + ((size_t)qs * (W - 1) + W - 2 - k) * p.C + c0, put_pairs<T, V>(win[k]));
   };
-  for (long long g = r0; g < r1; g += U, yr += U * p.y_ld) {
+  for (int g = r0; g < r1; g += U, yr += U * p.y_ld) {
 #pragma unroll
     for (int u = 0; u < U; ++u) raw[u] = next[u];
     load(g + U);
-    if (g + U <= r1 && g + U <= q.end) {  // whole, within its sequence
+    if (g + U <= r1 && g + U <= qe) {  // whole, within its sequence
 #pragma unroll
       for (int u = 0; u < U; ++u) token(raw[u], yr + u * p.y_ld);
-      if (g + U == q.end && p.stateT) last_state();
+      if (g + U == qe && p.stateT) last_state();
       continue;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const long long r = g + u;
+      const int r = g + u;
       if (r >= r1) break;
-      if (r >= q.end) {  // the next sequence that has tokens (packed rows only)
-        while (q.s < p.ns - 1 && r >= q.end) {
-          ++q.s;
-          q.begin = q.end;
-          q.end = cu_at(p.cu, p.ns, p.T, q.s + 1);
+      if (r >= qe) {  // the next sequence that has tokens (packed rows only)
+        while (qs < p.ns - 1 && r >= qe) {
+          ++qs;
+          qb = qe;
+          qe = cu_at(p.cu, p.ns, p.T, qs + 1);
         }
 #pragma unroll
-        for (int k = 0; k < W - 1; ++k) from_state<T, W, V>(p, q.s, W - 2 - k, c0, win[k]);
+        for (int k = 0; k < W - 1; ++k) from_state<T, W, V>(p, qs, W - 2 - k, c0, win[k]);
       }
       token(raw[u], yr + u * p.y_ld);
-      if (r == q.end - 1 && p.stateT) last_state();
+      if (r == qe - 1 && p.stateT) last_state();
     }
   }
 }
@@ -203,18 +206,18 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
   const long long units = (long long)p.B * p.runs;
   const bool live = c0 < p.C && unit < units;
   const int b = live ? (int)(unit / p.runs) : 0, t0 = live ? (int)(unit % p.runs) * p.run : p.T;
-  const long long rb0 = (long long)b * p.T, rb1 = rb0 + p.T;
-  const long long r0 = rb0 + t0, r1 = r0 + min(p.run, p.T - t0);
-  const long long top = min(r1 + W - 2, rb1 - 1);  // dx of the last row takes dp of the W-1 rows after it
-  const T *X = (const T *)p.x + c0, *DY = (const T *)p.dy + c0;
-  T *DX = (T *)p.dx + c0;
+  const long long rb = (long long)b * p.T;  // (rows below are counted from there)
+  const int r0 = t0, r1 = t0 + min(p.run, p.T - t0);
+  const int top = min(r1 + W - 2, p.T - 1);  // dx of the last row takes dp of the W-1 rows after it
+  const T *X = (const T *)p.x + c0 + rb * p.x_ld, *DY = (const T *)p.dy + c0 + rb * p.dy_ld;
+  T *DX = (T *)p.dx + c0 + rb * p.dx_ld;
   // groups [g, g + U) from the top down; xr[i] = x row g - (W-1) + i
   typename K::Raw xr[U + W - 1], xn[U], dyr[U], dyn[U];
-  long long g = r0 + (top - r0) / U * U;
+  int g = r0 + (top - r0) / U * U;
   const T *xp = X + (g - (W - 1)) * p.x_ld, *dyp = DY + g * p.dy_ld;
   T *dxp = DX + g * p.dx_ld;
-  auto load = [&](long long at) {  // the rows a group needs beside those of the one above: xp and dyp its first
-    if (at - (W - 1) >= rb0 && at + U - 1 <= top && at >= r0) {
+  auto load = [&](int at) {  // the rows a group needs beside those of the one above: xp and dyp its first
+    if (at >= W - 1 && at + U - 1 <= top && at >= r0) {
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         xn[i] = K::ld(xp + i * p.x_ld);
@@ -223,8 +226,8 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
     } else {
 #pragma unroll
       for (int i = 0; i < U; ++i) {
-        const long long r = at - (W - 1) + i;
-        xn[i] = r >= rb0 && r <= top && at >= r0 ? K::ld(xp + i * p.x_ld) : K::zero();
+        const int r = at - (W - 1) + i;
+        xn[i] = r >= 0 && r <= top && at >= r0 ? K::ld(xp + i * p.x_ld) : K::zero();
         dyn[i] = at >= r0 && at + i <= top ? K::ld(dyp + i * p.dy_ld) : K::zero();
       }
     }
@@ -233,8 +236,8 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
   };
 #pragma unroll
   for (int i = 0; i < W - 1; ++i) {
-    const long long r = g + U - (W - 1) + i;
-    xr[i] = t0 < p.T && r >= rb0 && r <= top ? K::ld(X + r * p.x_ld) : K::zero();
+    const int r = g + U - (W - 1) + i;
+    xr[i] = t0 < p.T && r >= 0 && r <= top ? K::ld(X + r * p.x_ld) : K::zero();
   }
   if (t0 < p.T) load(g);  // (in flight while the taps come)
   f2 tap[W][P], bias[P];
@@ -246,7 +249,8 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
     for (int e = 0; e < P; ++e) dw[k][e] = pack2(0.f, 0.f);
   if (live) pass_empty<T, W, V>(p, unit, units, c0, p.dstateT, p.dstate0);
   if (t0 < p.T) {
-    SeqSpan q = find_seq(p.cu, p.ns, p.T, b, (int)(top - rb0));
+    const SeqSpan q = find_seq(p.cu, p.ns, p.T, b, top);
+    int qs = q.s, qb = (int)(q.begin - rb), qe = (int)(q.end - rb);
     f2 dpw[W - 1][P];  // dpw[k] = dp_{t+1+k} of the same sequence
 #pragma unroll
     for (int k = 0; k < W - 1; ++k)
@@ -294,7 +298,7 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
         dyr[i] = dyn[i];
       }
       load(g - U);
-      if (g + U <= r1 && g - (W - 1) >= q.begin && g + U <= q.end - (p.dstateT ? W - 1 : 0)) {
+      if (g + U <= r1 && g - (W - 1) >= qb && g + U <= qe - (p.dstateT ? W - 1 : 0)) {
         f2 x[U + W - 1][P];  // whole, the run's own, inside its sequence
 #pragma unroll
         for (int i = 0; i < U + W - 1; ++i) get_pairs<T, V>(xr[i], x[i]);
@@ -314,13 +318,13 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
       }
 #pragma unroll
       for (int u = U - 1; u >= 0; --u) {
-        const long long r = g + u;
+        const int r = g + u;
         if (r > top) continue;
-        if (r < q.begin) {  // the sequence before, past empty ones
-          while (q.s > 0 && r < q.begin) {
-            --q.s;
-            q.end = q.begin;
-            q.begin = cu_at(p.cu, p.ns, p.T, q.s);
+        if (r < qb) {  // the sequence before, past empty ones
+          while (qs > 0 && r < qb) {
+            --qs;
+            qe = qb;
+            qb = cu_at(p.cu, p.ns, p.T, qs);
           }
 #pragma unroll
           for (int k = 0; k < W - 1; ++k)
@@ -330,26 +334,26 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
         f2 x[W][P], dp[P];
 #pragma unroll
         for (int k = 0; k < W; ++k) get_pairs<T, V>(xr[u + W - 1 - k], x[k]);
-        if (r - (W - 1) < q.begin) {
+        if (r - (W - 1) < qb) {
 #pragma unroll
           for (int k = 1; k < W; ++k)
-            if (r - k < q.begin) from_state<T, W, V>(p, q.s, (int)(W - 1 + r - k - q.begin), c0, x[k]);
+            if (r - k < qb) from_state<T, W, V>(p, qs, W - 1 + r - k - qb, c0, x[k]);
         }
         row_dp(x, dyr[u], dp);
         if (r < r1) {
           f2 dx[P];
           row_dx(x, dp, dx);
-          if (p.dstateT && q.end - r <= W - 1) {
+          if (p.dstateT && qe - r <= W - 1) {
             f2 d[P];
-            get_pairs<T, V>(K::ld((const T *)p.dstateT + ((size_t)q.s * (W - 1) + W - 1 - (q.end - r)) * p.C + c0), d);
+            get_pairs<T, V>(K::ld((const T *)p.dstateT + ((size_t)qs * (W - 1) + W - 1 - (qe - r)) * p.C + c0), d);
 #pragma unroll
             for (int e = 0; e < P; ++e) dx[e] = add2(dx[e], d[e]);
           }
           K::st(dxp + u * p.dx_ld, put_pairs<T, V>(dx));
         }
         shift(dp);
-        if (r == q.begin && r < r1 && p.dstate0) {
-          const long long len = q.end - q.begin;
+        if (r == qb && r < r1 && p.dstate0) {
+          const int len = qe - qb;
 #pragma unroll
           for (int v = 1; v < W; ++v) {  // the input v rows before the start: state row W-1-v
             f2 d[P];
@@ -362,11 +366,11 @@ __global__ void __launch_bounds__(kConvThreads) conv_bwd_kernel(ConvP p) {
             const int i = W - 1 - v;
             if (p.dstateT && i >= len) {  // a sequence shorter than the state hands part of it on
               f2 t[P];
-              get_pairs<T, V>(K::ld((const T *)p.dstateT + ((size_t)q.s * (W - 1) + i - len) * p.C + c0), t);
+              get_pairs<T, V>(K::ld((const T *)p.dstateT + ((size_t)qs * (W - 1) + i - len) * p.C + c0), t);
 #pragma unroll
               for (int e = 0; e < P; ++e) d[e] = add2(d[e], t[e]);
             }
-            K::st((T *)p.dstate0 + ((size_t)q.s * (W - 1) + i) * p.C + c0, put_pairs<T, V>(d));
+            K::st((T *)p.dstate0 + ((size_t)qs * (W - 1) + i) * p.C + c0, put_pairs<T, V>(d));
           }
         }
       }

@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(kScanThreads, 7) scan_bwd_carry_kernel(ScanP p
     }
     __syncthreads();
     load(r - kScanTile, b ^ 1);
-#pragma unroll 2
+#pragma unroll 4
     for (int t = ntok - 1; t >= 0; --t) {
       f2 cc[4];
       states4(&sm.C[b][t][n0], 0, cc);
