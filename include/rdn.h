@@ -385,7 +385,7 @@ rdn_status_t rdn_bwd_workspace_size(const rdn_bwd_args *args, size_t *bytes);
  *    the row's length; batch row b, token t is row b * T + t), so that an
  *    operand can be a slice of a wider projection's rows.
  *  - Data and parameter pointers need their element's alignment only; rows
- *    (pointers, lengths and strides) on whole 16-byte groups take 16-byte
+ *    (pointers, lengths and strides) on whole 16-byte groups take vector
  *    accesses, others single elements.  A and the scan's fp32 states (h0, hT,
  *    h_chunks, dhT, dh0, h) must be 16-byte aligned.
  *  - Outputs may not alias inputs.

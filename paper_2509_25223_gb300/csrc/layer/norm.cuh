@@ -42,7 +42,6 @@ struct NormP {
 
 // What a call has, fixed at compile time or (MODE = kAny) read from NormP::mode:
 // the gate (0 none, 1 SiLU, 2 sigmoid), and these bits.
-constexpr int kFwdCtas = 1;
 constexpr int kF = 4, kX = 8, kH = 16, kAny = -1;
 // Rows whose loads a thread has in flight: two where its registers hold them.
 template <int V, int E, int MODE, bool BWD>
@@ -170,7 +169,7 @@ __device__ __forceinline__ void load_c(const NormP &p, bool x, long long slot, i
 }
 
 template <typename T, typename XT, int V, int E, int THREADS, int MODE>
-__global__ void __launch_bounds__(THREADS, THREADS == 512 ? kFwdCtas : 1) fwd_kernel(const NormP p) {
+__global__ void __launch_bounds__(THREADS, 1) fwd_kernel(const NormP p) {
   constexpr int N = E / 2, R = kAhead<V, E, MODE, false>;
   __shared__ __align__(16) float sh[2][2][32];
   const Has<MODE> has(p);

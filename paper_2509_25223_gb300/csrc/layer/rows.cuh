@@ -62,30 +62,6 @@ struct Pack<__nv_bfloat16, 4> {
   }
   __device__ static void st(__nv_bfloat16 *p, const Raw &a) { *reinterpret_cast<uint2 *>(p) = a; }
 };
-template <>
-struct Pack<__nv_bfloat16, 2> {
-  using Raw = uint32_t;
-  __device__ static Raw zero() { return 0u; }
-  __device__ static Raw ld(const __nv_bfloat16 *p) { return *reinterpret_cast<const uint32_t *>(p); }
-  __device__ static void get(const Raw &a, float (&v)[2]) {
-    v[0] = __uint_as_float(a << 16);
-    v[1] = __uint_as_float(a & 0xffff0000u);
-  }
-  __device__ static Raw put(const float (&v)[2]) {
-    const __nv_bfloat162 b = __floats2bfloat162_rn(v[0], v[1]);
-    return *reinterpret_cast<const uint32_t *>(&b);
-  }
-  __device__ static void st(__nv_bfloat16 *p, const Raw &a) { *reinterpret_cast<uint32_t *>(p) = a; }
-};
-template <>
-struct Pack<float, 2> {
-  using Raw = float2;
-  __device__ static Raw zero() { return make_float2(0.f, 0.f); }
-  __device__ static Raw ld(const float *p) { return *reinterpret_cast<const float2 *>(p); }
-  __device__ static void get(const Raw &a, float (&v)[2]) { v[0] = a.x; v[1] = a.y; }
-  __device__ static Raw put(const float (&v)[2]) { return make_float2(v[0], v[1]); }
-  __device__ static void st(float *p, const Raw &a) { *reinterpret_cast<float2 *>(p) = a; }
-};
 template <typename T>
 struct Pack<T, 1> {
   using Raw = T;
