@@ -37,25 +37,36 @@ __global__ void __launch_bounds__(512) norm_grad_kernel(const NormP p, int slots
 int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
 
 struct NormPlan : Launch {
-  int tpr, slots;  // threads per row, row slots of the grid
+  int tpr, slots;   // threads per row and CTA, row slots of the grid
+  int split, cols;  // CTAs per row, columns of each
 };
-// CTAs of 256 threads (a row's, if it needs more), as many as are resident, so
-// that they stay for many rows; their slots a multiple of the heads, so that a
-// slot's rows share a row of w.
-NormPlan norm_plan(const rdn_norm_args &a, bool bwd) {
-  constexpr int kSMs = 152;
+// CTAs of up to 256 threads (of 384 where that is the most; a row's, if it needs
+// more), as many as are resident, so that they stay for many rows; their slots a
+// multiple of the heads, so that a slot's rows share a row of w.
+NormPlan norm_plan(const rdn_norm_args &a, bool bwd, bool vec) {
+  constexpr int kSMs = 152, E = 8;
   NormPlan pl;
-  pl.elems = a.D <= 8 * 1024 ? 8 : 16;
-  pl.tpr = 8;
-  while (pl.tpr * pl.elems < a.D) pl.tpr *= 2;
-  pl.threads = pl.tpr > 256 ? pl.tpr : 256;
-  const int per = pl.threads / pl.tpr;
+  pl.vec = vec;
+  const int most = !vec ? norm::kFewThreads : bwd ? norm::kThreads : norm::kMostThreads;
+  pl.split = a.D <= most * E ? 1 : (a.D + norm::kFewThreads * E - 1) / (norm::kFewThreads * E);
+  pl.cols = pl.split == 1 ? a.D : ((a.D + pl.split - 1) / pl.split + 7) / 8 * 8;
+  pl.tpr = (pl.cols + E - 1) / E;
+  pl.tpr = pl.split == 1 && pl.tpr <= 8 ? 8 : pl.split == 1 && pl.tpr <= 16 ? 16 : (pl.tpr + 31) / 32 * 32;
+  const bool any_f32 = a.dtype == RDN_F32 || (a.x && a.x_dtype == RDN_F32);
+  const bool few = pl.split > 1 || norm::few_threads(vec, bwd, any_f32, pl.tpr);
+  // (rows of 5 warps and more have a CTA each)
+  const int per = pl.split > 1 || pl.tpr > 128 ? 1 : (few ? norm::kFewThreads : 256) / pl.tpr;
+  pl.threads = pl.tpr * per;
   const int step = a.heads / gcd(a.heads, per);
   const long long need = ((a.rows + per - 1) / per + step - 1) / step * step;
-  const int resident = (bwd ? 512 : 1024) / pl.threads;
-  const long long ctas = ((long long)kSMs * (resident > 1 ? resident : 1) + step - 1) / step * step;
-  pl.ctas = (int)(ctas < need ? ctas : need);
-  pl.slots = pl.ctas * per;
+  const int threads = few ? norm::kFewThreads : bwd ? norm::kThreads : 2 * norm::kThreads;
+  const int resident = threads / pl.threads > 1 ? threads / pl.threads : 1;
+  // (clusters of more than two leave SMs unused; one more than fits would take as long as all)
+  const long long at_once = pl.split == 1 ? kSMs * resident : pl.split == 2 ? kSMs / 2 : (kSMs - 16) / pl.split;
+  const long long rows = (at_once + step - 1) / step * step;
+  const long long units = (rows < need ? rows : need);
+  pl.ctas = (int)(units * pl.split);
+  pl.slots = (int)(units * per);
   return pl;
 }
 
@@ -72,15 +83,16 @@ bool norm_vec(const rdn_norm_args &a, bool bwd) {
 }  // namespace
 
 size_t norm_bwd_bytes(const rdn_norm_args &a) {
-  const NormPlan pl = norm_plan(a, true);
-  return round256(sizeof(float) * 2 * (size_t)pl.slots * a.D);
+  // (the larger of the two accesses' plans: the query sees no pointers)
+  const int v = norm_plan(a, true, true).slots, e = norm_plan(a, true, false).slots;
+  return round256(sizeof(float) * 2 * (size_t)(v > e ? v : e) * a.D);
 }
 
 cudaError_t launch_norm(const rdn_norm_args &a, bool bwd, cudaStream_t s) {
-  NormPlan pl = norm_plan(a, bwd);
-  pl.vec = norm_vec(a, bwd);
+  const NormPlan pl = norm_plan(a, bwd, norm_vec(a, bwd));
   NormP p{};
   p.rows = a.rows; p.D = a.D; p.heads = a.heads; p.tpr = pl.tpr;
+  p.split = pl.split; p.cols = pl.cols;
   p.mode = (a.f ? norm::kF : 0) | (a.x ? norm::kX : 0) | (a.w_next ? norm::kH : 0) | (a.f && a.z ? 1 + a.gate : 0);
   p.eps = a.eps; p.scale_const = a.scale_const;
   p.f_ld = a.f_ld; p.z_ld = a.z_ld; p.x_ld = a.x_ld;

@@ -13,10 +13,13 @@
 // memory at every fourth token, so that three tokens of four are recomputed twice.
 // Keeping 8 tokens' states in registers takes 255 of them and a loop body beyond
 // the instruction cache: 744 us for 4 x 2048 x 4096 channels of 16 states where
-// this takes 660 (0.81e12 (token, channel, state) per second, 14 % of the HBM
-// rate).  About 15 multiply-adds and 2.75 exponentials for each of those, 25
-// instructions in all: bound by
-// instruction issue (the FMA pipe is busy a third of the time).  The sums over
+// this takes 660 (0.81e12 (token, channel, state) per second, 1.0 TB/s of HBM
+// traffic).  About 15 multiply-adds and 2.75 exponentials for each of those, 25
+// instructions in all (a pair's count as half): no pipe is full -- issue slots 52 %,
+// FMA 44 %, shared memory 43 %, exponentials 27 % -- and the registers leave 12
+// warps per SM to fill them; with 7 CTAs per SM the kernel spills (857 us).  The
+// first pass (scan_bwd_carry) takes 135 us there, the joins of dB, dC 24 and of the
+// parameters' gradients 14.  The sums over
 // channels for dB and dC are exchanged within a warp in an order that needs no
 // selects (the lanes that exchange hold their four states in orders that differ by
 // the bit they exchange over), joined over the CTA's warps in shared memory, and

@@ -61,6 +61,13 @@ def test_row_lengths(D):
     compare(make(5, D, "f32", seed=D))
 
 
+@pytest.mark.parametrize("D,xdtype", [(2056, "f32"), (3081, "bf16"), (4099, "f32"), (4096, "f32"), (8192, "bf16"),
+                                      (16384, "f32")])
+def test_many_long_rows(D, xdtype):
+    """(more rows than are worked on at a time; long ones are shared by CTAs)"""
+    compare(make(200, D, "bf16", xdtype, seed=D))
+
+
 @pytest.mark.parametrize("rows", [1, 2, 31, 300, (3, 5), (2, 3, 4)])
 @pytest.mark.parametrize("dtype,xdtype", [("bf16", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
 def test_rows_and_types(rows, dtype, xdtype):
