@@ -226,7 +226,7 @@ struct StepP {
 // parameters are read once for all of them; a request's loads are in flight while
 // the one before is worked on.  4096 channels of 16 states: one request 2.4 us in a
 // captured graph, 256 requests 31 us (141 MB, 4.5 TB/s).
-constexpr int kStepThreads = 128, kStepRows = 8;
+constexpr int kStepThreads = 128, kStepRows = 32;
 // 4 states of B or C from global memory (zero past S)
 template <typename T>
 __device__ __forceinline__ void states_of(const T *row, int S, int n0, bool vec, float (&v)[4]) {
@@ -319,10 +319,10 @@ template <typename T, int L>
 cudaError_t step_l(StepP p, cudaStream_t s) {
   constexpr int CH = kStepThreads / L;
   const unsigned tiles = (p.D + CH - 1) / CH;
-  // as many requests per CTA as leave about 8 CTAs per SM (4096 x 16 states: 256
-  // requests in 38 us one per CTA, 31 us eight; one request is latency either way)
-  p.rows = kStepRows;
-  while (p.rows > 1 && (long long)tiles * ((p.N + p.rows - 1) / p.rows) < 152 * 8) p.rows /= 2;
+  // the requests shared out over the 8 CTAs that an SM holds (4096 x 16 states: 256
+  // requests in 38 us one per CTA, 31 us eight, XX us so)
+  const int groups = tiles < 152 * 8 ? 152 * 8 / tiles : 1, rows = (p.N + groups - 1) / groups;
+  p.rows = rows < kStepRows ? rows : kStepRows;
   const dim3 grid((p.N + p.rows - 1) / p.rows, tiles);
   RDN_LAUNCH("scan_step", s, (scan_step_kernel<T, L><<<grid, kStepThreads, 0, s>>>(p)));
   return cudaGetLastError();
