@@ -225,7 +225,8 @@ struct StepP {
 // requests, so that A (as many bytes as one request's states) and the channels'
 // parameters are read once for all of them; a request's loads are in flight while
 // the one before is worked on.  4096 channels of 16 states: one request 2.4 us in a
-// captured graph, 256 requests 31 us (141 MB, 4.5 TB/s).
+// captured graph, 256 requests 29 us (141 MB, 4.9 TB/s; with B and C, too, a request
+// ahead the registers leave 5 CTAs per SM: 36 us).
 constexpr int kStepThreads = 128, kStepRows = 32;
 // 4 states of B or C from global memory (zero past S)
 template <typename T>
@@ -320,7 +321,7 @@ cudaError_t step_l(StepP p, cudaStream_t s) {
   constexpr int CH = kStepThreads / L;
   const unsigned tiles = (p.D + CH - 1) / CH;
   // the requests shared out over the 8 CTAs that an SM holds (4096 x 16 states: 256
-  // requests in 38 us one per CTA, 31 us eight, XX us so)
+  // requests in 38 us one per CTA, 31 us eight in 1.7 waves, 29 us so)
   const int groups = tiles < 152 * 8 ? 152 * 8 / tiles : 1, rows = (p.N + groups - 1) / groups;
   p.rows = rows < kStepRows ? rows : kStepRows;
   const dim3 grid((p.N + p.rows - 1) / p.rows, tiles);
