@@ -10,21 +10,24 @@
 // hold x and z of the same elements, which finish and store them.  The next
 // tile's global loads are in flight during the steps.
 //
-// At 4096 channels of 16 states, bf16, with softplus and gate: 16384 tokens 553 us
-// (first pass 223, main pass 330: 3.3e12 (token, channel, state) per second, of
-// 538 MB), 777 tokens 50 us (21 and 31), 4 x 2048 tokens with the kept states 121
-// and 186 us.  4 multiply-adds and an exponential per state are 116 us of either
+// At 4096 channels of 16 states, bf16, with softplus and gate: 16384 tokens 525 us
+// (first pass 209, main pass 317: 3.4e12 (token, channel, state) per second, of
+// 538 MB), 777 tokens 46 us (20 and 30), 4 x 2048 tokens with the kept states 112
+// and 176 us.  4 multiply-adds and an exponential per state are 116 us of either
 // pipe at 16384 tokens; the main pass issues 8 instructions per state, of which
 // about 3 are work per (token, channel) spread over 16 states (softplus, gate,
 // conversions, stores), and keeps issue slots 59 %, shared memory 51 %, FMA 47 % and
-// exponentials 40 % busy.  More warps do not help: 9 and 10 CTAs per SM take 564 and
-// 572 us where 8 take 552.
+// exponentials 40 % busy (at 552 us in all; the sums over the states after every token
+// instead of after four).  More warps did not help: 9 and 10 CTAs per SM took 564
+// and 572 us where 8 took 552.
 #include <math.h>
 
 #include "scan.cuh"
 
 namespace rdn {
 namespace {
+
+constexpr int kGroup = 4;  // tokens whose sums over the states follow together (16384 tokens: 2 549 us, 4 527, 8 524)
 
 template <typename T, int L, bool VEC>
 struct FwdSmem {
@@ -38,7 +41,7 @@ struct FwdSmem {
 
 // FIRST: the first pass over the units (end state from a zero start, sum of dl).
 template <typename T, int L, bool VEC, bool FIRST>
-__global__ void __launch_bounds__(kScanThreads, 7) scan_fwd_kernel(ScanP p) {
+__global__ void __launch_bounds__(kScanThreads, 8) scan_fwd_kernel(ScanP p) {
   using Sh = ScanShape<T, L, VEC>;
   using K = typename Sh::K;
   constexpr int V = Sh::V;
@@ -123,22 +126,31 @@ __global__ void __launch_bounds__(kScanThreads, 7) scan_fwd_kernel(ScanP p) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) store_pairs(p.chunks, slot, slot < p.slots, p, c0, first + 2 * (j ^ (sl & 1)), nch, n0, h[j]);
     }
-#pragma unroll 4  // (2: 571 us for 16384 tokens, 8: 552 as 4)
-    for (int t = 0; t < ntok; ++t) {
-      f2 bb[4], cc[4], y[2];
-      states4(&sm.B[b][t][n0], 0, bb);
-      if (!FIRST) states4(&sm.C[b][t][n0], 0, cc);
+    // four tokens at a time (those past the end have dl = 0 and change nothing), their
+    // sums after the last: a store between them would hold up the next one's loads
+    for (int t0 = 0; t0 < ntok; t0 += kGroup) {
+      f2 y[kGroup][2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dx[t][at[j]]);
-        if (FIRST) sumd[j] = add2(sumd[j], d.x);
+      for (int u = 0; u < kGroup; ++u) {
+        const int t = t0 + u;
+        f2 bb[4], cc[4];
+        states4(&sm.B[b][t][n0], 0, bb);
+        if (!FIRST) states4(&sm.C[b][t][n0], 0, cc);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          h[j][i] = fma2(decay2(d.x, A2[j][i], shift), h[j][i], mul2(d.y, bb[i]));
-          if (!FIRST) y[j] = i ? fma2(cc[i], h[j][i], y[j]) : mul2(cc[i], h[j][i]);
+        for (int j = 0; j < 2; ++j) {
+          const ulonglong2 d = *reinterpret_cast<const ulonglong2 *>(&sm.dx[t][at[j]]);
+          if (FIRST) sumd[j] = add2(sumd[j], d.x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            h[j][i] = fma2(decay2(d.x, A2[j][i], shift), h[j][i], mul2(d.y, bb[i]));
+            if (!FIRST) y[u][j] = i ? fma2(cc[i], h[j][i], y[u][j]) : mul2(cc[i], h[j][i]);
+          }
         }
       }
-      if (out) sum_states<L>(y, sm.y[t], first, sl);
+      if (out) {
+#pragma unroll
+        for (int u = 0; u < kGroup; ++u) sum_states<L>(y[u], sm.y[t0 + u], first, sl);
+      }
     }
     __syncthreads();
     if (!out) continue;
