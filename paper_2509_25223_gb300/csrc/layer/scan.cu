@@ -12,14 +12,13 @@
 //
 // At 4096 channels of 16 states, bf16, with softplus and gate: 16384 tokens 525 us
 // (first pass 209, main pass 317: 3.4e12 (token, channel, state) per second, of
-// 538 MB), 777 tokens 46 us (20 and 30), 4 x 2048 tokens with the kept states 112
+// 538 MB), 777 tokens 45 us (19 and 29), 4 x 2048 tokens with the kept states 112
 // and 176 us.  4 multiply-adds and an exponential per state are 116 us of either
 // pipe at 16384 tokens; the main pass issues 8 instructions per state, of which
 // about 3 are work per (token, channel) spread over 16 states (softplus, gate,
-// conversions, stores), and keeps issue slots 59 %, shared memory 51 %, FMA 47 % and
-// exponentials 40 % busy (at 552 us in all; the sums over the states after every token
-// instead of after four).  More warps did not help: 9 and 10 CTAs per SM took 564
-// and 572 us where 8 took 552.
+// conversions, stores), and keeps issue slots 62 %, shared memory 54 %, FMA 51 % and
+// exponentials 43 % busy.  More warps do not help: with the sums over the states
+// after every token, 9 and 10 CTAs per SM took 564 and 572 us where 8 took 552.
 #include <math.h>
 
 #include "scan.cuh"
