@@ -61,6 +61,13 @@ def test_row_lengths(D):
     compare(make(5, D, "f32", seed=D))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [300, 515, 520, 700, 1001, 1288, 3080])
+def test_rows_of_some_warps(D, dtype):
+    """(3 to 13 warps of threads a row, on 16 bytes and on single elements)"""
+    compare(make(37, D, dtype, "f32", seed=D))
+
+
 @pytest.mark.parametrize("D,xdtype", [(2056, "f32"), (3081, "bf16"), (4099, "f32"), (4096, "f32"), (8192, "bf16"),
                                       (16384, "f32")])
 def test_many_long_rows(D, xdtype):
