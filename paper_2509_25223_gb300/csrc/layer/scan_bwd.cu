@@ -185,6 +185,7 @@ struct BwdSmem {
   T B[kScanTile][Sh::SP], C[kScanTile][Sh::SP];
 };
 
+// (6 CTAs per SM by registers; of the wide tiles of L = 2 shared memory holds 4)
 template <typename T, int L, bool VEC>
 __global__ void __launch_bounds__(kScanThreads, L == 2 ? 4 : 6) scan_bwd_kernel(ScanP p) {
   using Sh = ScanShape<T, L, VEC>;
