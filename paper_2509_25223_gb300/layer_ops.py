@@ -9,7 +9,9 @@ on a non-OK status; every step runs in the library's CUDA kernels on the
 current stream of the operands' device.
 
 Token rows may be strided: a [B, T, C] operand can be a slice of the last axis
-of a wider, otherwise contiguous tensor (`proj[..., a:b]`), without a copy.
+of a wider, otherwise contiguous tensor (`proj[..., a:b]`), without a copy.  All
+its rows have to be one distance apart: a slice of the tokens of several batch
+rows (`x[:, a:b]`) and expanded tensors are refused (make them contiguous).
 Parameters (weights, biases, A, D, scales) and the scan's states are fp32;
 results and convolution states have the inputs' type (bf16 or fp32).
 """
@@ -45,33 +47,35 @@ def _bad(name, t, shape, dtype, dev):
                      f"(got {tuple(t.shape)} {t.dtype} on {t.device})")
 
 
-def _rows(name, t, shape, dtype, dev):
-    """(address, row stride) of rows that lie along t's last axis, evenly spaced."""
+def _rows(name, t, shape, dtype, dev, lead=2):
+    """(address, row stride) of t's rows: one for each index of the first `lead` axes, of the
+    elements of the others.  Stride 0: contiguous."""
     if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
         _bad(name, t, shape, dtype, dev)
-    return t.data_ptr(), 0 if t.is_contiguous() else _stride(name, t)
+    return t.data_ptr(), 0 if t.is_contiguous() else _stride(name, t, lead)
 
 
-def _stride(name, t):
-    shape = t.shape
-    width, lead = 1, len(shape) - 1  # the trailing axes that are contiguous make up a row
-    while lead >= 0 and (shape[lead] == 1 or t.stride(lead) == width):
-        width *= shape[lead]
-        lead -= 1
-    lead += 1
-    if lead == len(shape):
-        raise ValueError(f"rdn: the last axis of {name} must be contiguous")
-    ld, span = 0, 0
+def _stride(name, t, lead):
+    """The one distance between consecutive rows that the library takes: the elements of a row
+    lie side by side, and every leading axis of more than one element continues the one below
+    it (an expanded axis, of stride 0, does not, nor does a slice of the tokens of several
+    batch rows)."""
+    shape, strides = t.shape, t.stride()
+    width = 1
+    for a in range(len(shape) - 1, lead - 1, -1):
+        if shape[a] != 1 and strides[a] != width:
+            axes = "axis" if len(shape) - lead == 1 else f"{len(shape) - lead} axes"
+            raise ValueError(f"rdn: the last {axes} of {name} must be contiguous")
+        width *= shape[a]
+    ld = span = 0  # distance of the rows; of the next axis's indexes, if the rows go on evenly
     for a in range(lead - 1, -1, -1):
         if shape[a] == 1:
             continue
-        if ld == 0:
-            ld = t.stride(a)
-            span = ld * shape[a]
-        elif t.stride(a) != span:
-            raise ValueError(f"rdn: the rows of {name} must be evenly spaced")
-        else:
-            span *= shape[a]
+        if strides[a] < width if ld == 0 else strides[a] != span:
+            raise ValueError(f"rdn: the rows of {name} must be evenly spaced, without overlap (got strides "
+                             f"{tuple(strides)} of {tuple(shape)}); pass {name}.contiguous()")
+        ld = ld or strides[a]
+        span = strides[a] * shape[a]
     return ld
 
 
@@ -222,13 +226,13 @@ def causal_conv_step(x, weight, state, bias=None, activation="silu", slots=None,
     N, C = shape
     W = weight.shape[-1]
     ty = x.dtype
-    px, x_ld = (x.data_ptr(), 0) if x.is_contiguous() else _rows("x", x, shape, ty, dev)
+    px, x_ld = (x.data_ptr(), 0) if x.is_contiguous() else _rows("x", x, shape, ty, dev, 1)
     if out is None:
         y = torch.empty(shape, dtype=ty, device=dev)
         py, y_ld = y.data_ptr(), 0
     else:
         y = out
-        py, y_ld = _rows("out", y, shape, ty, dev)
+        py, y_ld = _rows("out", y, shape, ty, dev, 1)
     num = state.shape[0]
     args = _abi.CONV_STEP_PACK(
         N, C, W, _code(ty), _silu(activation), num, x_ld, y_ld, px,
@@ -350,17 +354,17 @@ def selective_scan_step(x, dt, A, B, C, h, D=None, z=None, dt_bias=None, dt_soft
         raise ValueError(f"rdn: B must be [N, G, S] (got {tuple(bshape)})")
     g, s = bshape[1], bshape[2]
     ty = x.dtype
-    px, x_ld = (x.data_ptr(), 0) if x.is_contiguous() else _rows("x", x, shape, ty, dev)
-    pdt, dt_ld = _rows("dt", dt, shape, ty, dev)
-    pz, z_ld = (0, 0) if z is None else _rows("z", z, shape, ty, dev)
-    pB, b_ld = _rows("B", B, bshape, ty, dev)
-    pC, c_ld = _rows("C", C, bshape, ty, dev)
+    px, x_ld = (x.data_ptr(), 0) if x.is_contiguous() else _rows("x", x, shape, ty, dev, 1)
+    pdt, dt_ld = _rows("dt", dt, shape, ty, dev, 1)
+    pz, z_ld = (0, 0) if z is None else _rows("z", z, shape, ty, dev, 1)
+    pB, b_ld = _rows("B", B, bshape, ty, dev, 1)
+    pC, c_ld = _rows("C", C, bshape, ty, dev, 1)
     if out is None:
         y = torch.empty(shape, dtype=ty, device=dev)
         py, y_ld = y.data_ptr(), 0
     else:
         y = out
-        py, y_ld = _rows("out", y, shape, ty, dev)
+        py, y_ld = _rows("out", y, shape, ty, dev, 1)
     num = h.shape[0]
     args = _abi.SCAN_STEP_PACK(
         n, d, s, g, _code(ty), 1 if dt_softplus else 0, num, x_ld, dt_ld, z_ld, b_ld, c_ld, y_ld, px,
@@ -382,7 +386,7 @@ class _Norm:
         if dev < 0:
             raise ValueError("rdn: tensors must be on a CUDA device")
         self.shape = shape = first.shape
-        D = shape[-1]
+        D, lead = shape[-1], len(shape) - 1
         self.heads, self.wshape = 1, (D,)
         if f is not None:
             if weight is None:
@@ -400,9 +404,9 @@ class _Norm:
         self.xdtype = x.dtype if x is not None else self.dtype
         self.vec = scale if isinstance(scale, torch.Tensor) else None
         const = 1.0 if scale is None or self.vec is not None else float(scale)
-        pf, f_ld = (0, 0) if f is None else _rows("f", f, shape, self.dtype, dev)
-        pz, z_ld = (0, 0) if z is None else _rows("z", z, shape, self.dtype, dev)
-        px, x_ld = (0, 0) if x is None else _rows("x", x, shape, self.xdtype, dev)
+        pf, f_ld = (0, 0) if f is None else _rows("f", f, shape, self.dtype, dev, lead)
+        pz, z_ld = (0, 0) if z is None else _rows("z", z, shape, self.dtype, dev, lead)
+        px, x_ld = (0, 0) if x is None else _rows("x", x, shape, self.xdtype, dev, lead)
         n = first.numel() // D if D else 0
         self.head = (n, D, self.heads, _DTYPES.get(self.dtype, -1), _DTYPES.get(self.xdtype, -1),
                      _GATES[gate], float(eps), const, f_ld, z_ld, x_ld, pf, pz, px,
