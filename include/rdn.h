@@ -388,7 +388,9 @@ rdn_status_t rdn_bwd_workspace_size(const rdn_bwd_args *args, size_t *bytes);
  *    (pointers, lengths and strides) on whole 16-byte groups take vector
  *    accesses, others single elements.  A and the scan's fp32 states (h0, hT,
  *    h_chunks, dhT, dh0, h) must be 16-byte aligned.
- *  - Outputs may not alias inputs.
+ *  - Outputs may not alias inputs.  Of the states this is checked: those that
+ *    a call writes (stateT, dstate0; hT, h_chunks, dh0) overlap none that it
+ *    reads (state0, dstateT; h0, dhT).
  *  - cu_seqlens / num_seqs as in rdn_fwd_args (B = 1; empty sequences pass
  *    their states through).
  *  - Sums over tokens (parameter gradients) and over channels (dB, dC) are

@@ -42,6 +42,14 @@ rdn_status_t check_ptr(const char *fn, const char *name, const void *p, size_t s
 rdn_status_t check_ptr16(const char *fn, const char *name, const void *p, bool required) {
   return check_ptr(fn, name, p, 16, required);
 }
+// A state that is written against one that other CTAs of the call may still read.
+rdn_status_t check_apart(const char *fn, const char *name, const void *out, size_t bytes, const char *in_name,
+                         const void *in, size_t in_bytes) {
+  const uintptr_t o = (uintptr_t)out, i = (uintptr_t)in;
+  if (out && in && (o < i ? i - o < bytes : o - i < in_bytes))
+    return entry_fail(RDN_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, name, in_name);
+  return RDN_OK;
+}
 // A row stride: 0 stands for contiguous.
 rdn_status_t check_ld(const char *fn, const char *name, long long *ld, long long row) {
   if (*ld == 0) *ld = row;
@@ -102,6 +110,7 @@ rdn_status_t conv_common(const char *fn, const rdn_conv_args *args, bool bwd, cu
   rdn_conv_args copy = *args, *a = &copy;
   TRY(conv_shapes(fn, a));
   const size_t e = dtype_size(a->dtype);
+  const size_t states = (size_t)(a->cu_seqlens ? a->num_seqs : a->B) * (a->W - 1) * a->C * e;
   const bool any = a->T > 0;
   TRY(check_ptr(fn, "x", a->x, e, any));
   TRY(check_ptr(fn, "w", a->w, 4, true));
@@ -110,6 +119,7 @@ rdn_status_t conv_common(const char *fn, const rdn_conv_args *args, bool bwd, cu
   if (!bwd) {
     TRY(check_ptr(fn, "y", a->y, e, any));
     TRY(check_ptr(fn, "stateT", a->stateT, e, false));
+    TRY(check_apart(fn, "stateT", a->stateT, states, "state0", a->state0, states));
     if (a->y && a->y == a->x) return entry_fail(RDN_ERR_INVALID_ARG, "%s: y aliases x", fn);
   } else {
     TRY(check_ptr(fn, "dy", a->dy, e, any));
@@ -118,6 +128,8 @@ rdn_status_t conv_common(const char *fn, const rdn_conv_args *args, bool bwd, cu
     TRY(check_ptr(fn, "dbias", a->dbias, 4, false));
     TRY(check_ptr(fn, "dstateT", a->dstateT, e, false));
     TRY(check_ptr(fn, "dstate0", a->dstate0, e, false));
+    TRY(check_apart(fn, "dstate0", a->dstate0, states, "dstateT", a->dstateT, states));
+    TRY(check_apart(fn, "dstate0", a->dstate0, states, "state0", a->state0, states));
     if (a->dx && (a->dx == a->x || a->dx == a->dy))
       return entry_fail(RDN_ERR_INVALID_ARG, "%s: dx aliases x or dy", fn);
     TRY(check_ws(fn, a->workspace, a->workspace_bytes, rdn::conv_bwd_bytes(*a)));
@@ -155,7 +167,8 @@ rdn_status_t scan_common(const char *fn, const rdn_scan_args *args, bool bwd, cu
   if (!args) return entry_fail(RDN_ERR_INVALID_ARG, "%s: args is NULL", fn);
   rdn_scan_args copy = *args, *a = &copy;
   TRY(scan_shapes(fn, a));
-  const size_t e = dtype_size(a->dtype);
+  const size_t e = dtype_size(a->dtype), row = (size_t)a->D * a->S * 4;
+  const size_t states = (a->cu_seqlens ? a->num_seqs : a->B) * row;
   const bool any = a->T > 0;
   TRY(check_ptr(fn, "x", a->x, e, any));
   TRY(check_ptr(fn, "dt", a->dt, e, any));
@@ -170,6 +183,8 @@ rdn_status_t scan_common(const char *fn, const rdn_scan_args *args, bool bwd, cu
   if (!bwd) {
     TRY(check_ptr(fn, "out", a->out, e, any));
     TRY(check_ptr16(fn, "hT", a->hT, false));
+    TRY(check_apart(fn, "hT", a->hT, states, "h0", a->h0, states));
+    TRY(check_apart(fn, "h_chunks", a->h_chunks, (size_t)rdn::scan_slots(*a) * row, "h0", a->h0, states));
     TRY(check_ws(fn, a->workspace, a->workspace_bytes, rdn::scan_fwd_bytes(*a)));
     TRY(entry_injected(fn));
     return entry_cuda(fn, rdn::launch_scan_fwd(*a, s));
@@ -185,6 +200,7 @@ rdn_status_t scan_common(const char *fn, const rdn_scan_args *args, bool bwd, cu
   TRY(check_ptr(fn, "dD", a->dD, 4, false));
   TRY(check_ptr(fn, "ddt_bias", a->ddt_bias, 4, false));
   TRY(check_ptr16(fn, "dh0", a->dh0, false));
+  TRY(check_apart(fn, "dh0", a->dh0, states, "dhT", a->dhT, states));
   TRY(check_ws(fn, a->workspace, a->workspace_bytes, rdn::scan_bwd_bytes(*a)));
   TRY(entry_injected(fn));
   return entry_cuda(fn, rdn::launch_scan_bwd(*a, s));
