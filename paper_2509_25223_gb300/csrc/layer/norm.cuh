@@ -348,6 +348,9 @@ __global__ void __launch_bounds__(THREADS, 1) bwd_kernel(const NormP p) {
   for (int u = 0; u < R; ++u) {
     const long long row = base + u * slots + threadIdx.x / tpr;
     const int out = row < p.rows ? left : 0;
+    // (rows past the end are worked on as zeros; with the call's eps, which may be 0, their
+    // roots could be infinite and the sums over the rows take 0 times infinity from them)
+    const float eps = out > 0 ? p.eps : 1.f;
     const long long now = o - R * slots * p.D;  // this row's place (the loads are R rows ahead)
     f2 fi[N], zv[N], act[N], r[N], g[N], d[N];  // f i1; z, then its gradient; act; r; its gradient; dh
 #pragma unroll
@@ -366,7 +369,7 @@ __global__ void __launch_bounds__(THREADS, 1) bwd_kernel(const NormP p) {
       for (int k = 0; k < N; ++k) ss = fma2(fi[k], fi[k], ss);
       float sum[1] = {sum2(ss)};
       row_sums<SPLIT>(sum, p, sh, calls);
-      inv = rsqrtf(fmaf(sum[0], invD, p.eps));
+      inv = rsqrtf(fmaf(sum[0], invD, eps));
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         fi[k] = mul2(fi[k], both(inv));
@@ -392,7 +395,7 @@ __global__ void __launch_bounds__(THREADS, 1) bwd_kernel(const NormP p) {
       }
       float sum[2] = {sum2(s2), sum2(sd)};
       row_sums<SPLIT>(sum, p, sh, calls);
-      const float i2 = rsqrtf(fmaf(sum[0], invD, p.eps)), m = -sum[1] * invD * i2 * i2;
+      const float i2 = rsqrtf(fmaf(sum[0], invD, eps)), m = -sum[1] * invD * i2 * i2;
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         an[k] = fma2(mul2(d[k], both(i2)), r[k], an[k]);
