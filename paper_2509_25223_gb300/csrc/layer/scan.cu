@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kScanThreads, 8) scan_fwd_kernel(ScanP p) {
     if (on) load_states(p.A + d * p.S, p.S, n0, a[c]);
     if (on && !FIRST && p.h0) load_states(p.h0 + ((size_t)w.s * p.D + d) * p.S, p.S, n0, v[c]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a[c][i] *= kLog2e;
+    for (int i = 0; i < 4; ++i) a[c][i] = log2_rate(a[c][i]);
   }
   if (!FIRST) chain<Sh::SP>(p, blockIdx.x - w.j, blockIdx.x, 1, c0 + first, nch - first, sl, a, v);
 #pragma unroll
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(StepP p) {
 #pragma unroll
   for (int q = 0; q < 2; ++q)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) A2[q][i] *= kLog2e;
+    for (int i = 0; i < 4; ++i) A2[q][i] = log2_rate(A2[q][i]);
   __syncthreads();
   float hn[2][4] = {}, xn = 0.f, dn = 0.f, zn = 0.f;  // of the next request
   auto load = [&](int r) {

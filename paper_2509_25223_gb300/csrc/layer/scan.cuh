@@ -30,6 +30,15 @@ namespace rdn {
 constexpr int kScanThreads = 64, kScanWarps = 2;  // small CTAs: their number divides over the SMs finely
 constexpr int kScanTile = RDN_SCAN_CHUNK;  // tokens staged at a time, and between kept states
 
+// A's factor in the decay's exponent, A log2 e.  An infinite one (A of -inf: a state without
+// memory) counts as the largest finite number, so that a step of zero, as the tokens past a
+// sequence's end have, makes a decay of one as it does for every other A, not 0 times infinity;
+// NaN stays.
+__device__ __forceinline__ float log2_rate(float A) {
+  const float r = A * kLog2e, most = 3.402823466e38f;
+  return r > most ? most : r < -most ? -most : r;
+}
+
 // exp2 of the decay's exponent.  ex2.approx comes out low by about 2e-8 on
 // average for small arguments; with decays near 1 the factors of a thousand
 // tokens multiply, and the mean error adds up where rounding would average

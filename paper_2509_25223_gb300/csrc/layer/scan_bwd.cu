@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(kScanThreads, 7) scan_bwd_carry_kernel(ScanP p
     sumd[j] = zero2;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      A2[j][i] = pack2(a[0][i] * kLog2e, a[1][i] * kLog2e);
+      A2[j][i] = pack2(log2_rate(a[0][i]), log2_rate(a[1][i]));
       q[j][i] = zero2;
     }
   }
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kScanThreads, L == 2 ? 4 : 6) scan_bwd_kernel(
       if (on) load_states(p.A + d * p.S, p.S, n0, a[c]);
       if (on && w.ok && p.dhT) load_states(p.dhT + ((size_t)w.s * p.D + d) * p.S, p.S, n0, v[c]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a[c][i] *= kLog2e;
+      for (int i = 0; i < 4; ++i) a[c][i] = log2_rate(a[c][i]);
     }
     // q past the unit's end, over the units after it
     if (w.ok) chain<Sh::SP>(p, (int)u - w.j + w.n - 1, (int)u, -1, c0 + first, nch - first, sl, a, v);
