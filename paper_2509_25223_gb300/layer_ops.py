@@ -398,6 +398,9 @@ class _Norm:
                 raise ValueError("rdn: weight must be [D] or [heads, D]")
             if self.wshape[-1] != D:
                 raise ValueError(f"rdn: weight must have {D} columns (got {tuple(self.wshape)})")
+            if self.heads > 1 and lead > 1 and shape[-2] != self.heads:
+                raise ValueError(f"rdn: weight of {self.heads} heads needs f [..., {self.heads}, {D}], or the rows of "
+                                 f"one [rows, {D}] (got {tuple(shape)})")
         if gate not in _GATES:
             raise ValueError('rdn: gate must be "silu" or "sigmoid"')
         self.dtype = h_dtype if f is None and h_dtype is not None else first.dtype
@@ -425,8 +428,8 @@ def block_norm_fwd(f=None, weight=None, z=None, gate="silu", x=None, scale=None,
     weight_next.  f=None: only the norm before a block, r is x itself.
 
     f, z [..., D] (z=None: no gate); x [..., D] in f's type or fp32; weight [D],
-    or [heads, D] for rows [..., heads, D] (without x and weight_next); scale: a
-    [D] fp32 tensor or a number; weight_next [D] fp32.  r has x's type, h f's
+    or [heads, D] for f [..., heads, D], or its rows flattened to [rows, D] with the
+    heads in turn (without x and weight_next); scale: a [D] fp32 tensor or a number; weight_next [D] fp32.  r has x's type, h f's
     (f=None: h_dtype, or x's).  out: (r, h) to write into."""
     a = _Norm(f, weight, z, gate, x, scale, weight_next, eps, h_dtype)
     r, h = out if out is not None else (None, None)
