@@ -120,8 +120,6 @@ __device__ __forceinline__ float sum2(f2 v) {
 
 __device__ __forceinline__ float sigmoidf(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 __device__ __forceinline__ float siluf(float x) { return x * sigmoidf(x); }
-// d silu(x) / dx from x and its sigmoid
-__device__ __forceinline__ float silu_grad(float x, float s) { return s * fmaf(x, 1.f - s, 1.f); }
 
 // silu of a pair; and its derivative
 __device__ __forceinline__ f2 sigmoid2(f2 x) {

@@ -176,7 +176,6 @@ struct ScanShape {
   static constexpr int V = VEC ? kVec<T> : 1;      // channels per global access
   static constexpr int COLS = CT / V;              // accesses per token
   static constexpr int NV = (kScanTile * COLS + kScanThreads - 1) / kScanThreads;  // per thread
-  static constexpr int TOK = kScanThreads / COLS > 0 ? kScanThreads / COLS : 1;    // tokens between a thread's accesses
   using K = Pack<T, V>;
   using Raw = typename K::Raw;
   // access i of this thread: its token and its first channel in the tile
