@@ -121,7 +121,8 @@ __device__ __forceinline__ float sum2(f2 v) {
 __device__ __forceinline__ float sigmoidf(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 __device__ __forceinline__ float siluf(float x) { return x * sigmoidf(x); }
 
-// silu of a pair; and its derivative
+// sigmoid and silu of a pair, and silu's derivative.  (The exponent is rounded: below zero the
+// sigmoid's relative error is up to 7.3e-8 |x| + 7e-7.)
 __device__ __forceinline__ f2 sigmoid2(f2 x) {
   float a, b;
   unpack2(mul2(x, pack2(-kLog2e, -kLog2e)), a, b);
