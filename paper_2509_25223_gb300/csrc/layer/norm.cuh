@@ -59,6 +59,8 @@ constexpr int kF = 4, kX = 8, kH = 16, kAny = -1, kSplit = -2;
 // has so few, and for shared rows.  (With 128 registers those spill: backward of 5979
 // rows of 2055 bf16 305 us instead of 136, of fp32 244 instead of 66; but rows of 4096 with
 // an fp32 residual, shared by two CTAs instead, 157 us, in one of 512 threads 79.)
+// At 512 threads the backward with residual and next norm spills 28 bytes in bf16; rows
+// above 3072 columns with 4-byte operands, which take those threads too, up to 276.
 // Rows of 4104 to 8192 have a CTA of up to 1024 in the forward (46 us for 1500 of 8192,
 // shared by three CTAs 93) and are shared in the backward (147, in one CTA 169).
 constexpr int kThreads = 512, kFewThreads = 384, kMostThreads = 1024, kSplitMost = 6;

@@ -17,8 +17,10 @@
 // pipe at 16384 tokens; the main pass issues 8 instructions per state, of which
 // about 3 are work per (token, channel) spread over 16 states (softplus, gate,
 // conversions, stores), and keeps issue slots 62 %, shared memory 54 %, FMA 51 % and
-// exponentials 43 % busy.  More warps do not help: with the sums over the states
-// after every token, 9 and 10 CTAs per SM took 564 and 572 us where 8 took 552.
+// exponentials 43 % busy.  Registers and shared memory (27 KB a CTA) both hold 8 CTAs per
+// SM; whether more warps would help is open.  Launch bounds of 9 and 10 CTAs, which leave
+// fewer registers but, by the shared memory, no more warps, took 564 and 572 us where 8
+// took 552 (with the sums over the states after every token).
 #include <math.h>
 
 #include "scan.cuh"
@@ -353,8 +355,12 @@ long long scan_slots(const rdn_scan_args &a) {
 
 // Time per token of an SM that has r CTAs of a pass to run, of which `resident`
 // fit at a time: up to about half of those it is latency, the same for one as
-// for several, then issue slots.  In us, measured at 4096 channels of 16 states
-// over cuts of 1 to 28 units (prefill of 16384 tokens, training pass of 4 x 2048).
+// for several, then issue slots.  In us, measured at 4096 bf16 channels of 16 states
+// over cuts of 1 to 28 units (prefill of 16384 tokens, training pass of 4 x 2048), and
+// used for every type and number of states.  `resident` is that instance's too: by its
+// shared memory the forward and its first pass hold 4 CTAs per SM for bf16 with up to 8
+// states, 5 and 3 for fp32 with up to 16 and up to 8; the backward of up to 8 states 4, its
+// first pass 7 (fp32 with up to 8 states 5).  There the cut is a guess.
 struct PassTime {
   int resident;
   double least, fixed, each;

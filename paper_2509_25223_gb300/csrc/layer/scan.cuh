@@ -60,8 +60,8 @@ __device__ __forceinline__ f2 decay2(f2 dl, f2 A2, f2 shift) {
 // with atanh(t) / t as a polynomial in t^2 fitted to 8e-9 on [0, 1/9].  About 14 instructions
 // (the library's log1p takes three times as many, and log2 of 1 + u would lose a small u).  The
 // exponent |v| log2 e is rounded to 32 bits, so below zero the relative error grows with |v|: at
-// most 7.3e-8 |v| + 7e-7, 4 units in the last place on [-1, 1], 16 on [-20, -10], 62 at -80, where
-// the result is 1e-35; above 1 it is one unit.
+// most 7.3e-8 |v| + 7e-7.  (With the other operations exact, 4 units in the last place on [-1, 1],
+// 16 on [-20, -10], 62 at -80, where the result is 1e-35; above 1 one unit.)
 __device__ __forceinline__ float softplusf(float v) {
   const float u = ex2(fabsf(v) * -kLog2e);
   const float t = u * rcp_approx(2.f + u), q = t * t;

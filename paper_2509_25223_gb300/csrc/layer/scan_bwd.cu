@@ -17,7 +17,8 @@
 // traffic).  About 15 multiply-adds and 2.75 exponentials for each of those, 25
 // instructions in all (a pair's count as half): no pipe is full -- issue slots 52 %,
 // FMA 44 %, shared memory 43 %, exponentials 27 % -- and the registers leave 12
-// warps per SM to fill them; with 7 CTAs per SM the kernel spills (857 us).  The
+// warps per SM to fill them.  At these 6 CTAs per SM most instances spill 4 to 16
+// bytes; with the registers of 7 the kernel takes 857 us.  The
 // first pass (scan_bwd_carry) takes 135 us there, the joins of dB, dC 24 and of the
 // parameters' gradients 14.  The sums over
 // channels for dB and dC are exchanged within a warp in an order that needs no
