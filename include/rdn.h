@@ -552,6 +552,121 @@ rdn_status_t rdn_norm_fwd(const rdn_norm_args *args, rdn_stream_t stream);
 rdn_status_t rdn_norm_bwd(const rdn_norm_args *args, rdn_stream_t stream);
 rdn_status_t rdn_norm_bwd_workspace_size(const rdn_norm_args *args, size_t *bytes);
 
+/* Gated linear recurrence: D channels with one state each, whose decay and input
+ * are gated per token and channel (r, i: the gates before their sigmoids):
+ *     la_t = -c softplus(lam) sigmoid(r_t),   a_t = exp(la_t)
+ *     h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(i_t) x_t,   y_t = h_t
+ *   B, T              as above;  1 <= D <= 2^19;  c > 0 and finite.
+ *   dtype             of x, r, i, y, dy and their gradients.
+ *   x, r, i, y        [B,T,D] with row strides.
+ *   lam [D]           fp32.
+ *   h0, hT            [num_seqs or B, D] fp32 or NULL.
+ *   h_chunks          NULL, or [B * ceil(T/64)][D] fp32: the states before tokens
+ *                     0, 64, 128 ... of each row of the batch, whatever sequence
+ *                     they are in (written by the forward, read by the backward,
+ *                     which computes them itself if NULL).
+ * Backward: dy [B,T,D], dhT like hT or NULL -> dx, dr, di [B,T,D] with row
+ * strides, dlam [D] fp32, dh0 like h0 or NULL.  Sigmoids of arguments below -40
+ * are taken at -40. */
+#define RDN_GSCAN_CHUNK 64
+typedef struct {
+  int B, T, D, dtype;
+  float c;
+  long long x_ld, r_ld, i_ld, y_ld;
+  const void *x, *r, *i;
+  const float *lam, *h0;
+  void *y;
+  float *hT, *h_chunks;
+  const int *cu_seqlens;
+  int num_seqs;
+  long long dy_ld, dx_ld, dr_ld, di_ld;
+  const void *dy;
+  const float *dhT;
+  void *dx, *dr, *di;
+  float *dlam, *dh0;
+  void *workspace;
+  size_t workspace_bytes;
+} rdn_gscan_args;
+rdn_status_t rdn_gscan_fwd(const rdn_gscan_args *args, rdn_stream_t stream);
+rdn_status_t rdn_gscan_bwd(const rdn_gscan_args *args, rdn_stream_t stream);
+rdn_status_t rdn_gscan_bwd_workspace_size(const rdn_gscan_args *args, size_t *bytes);
+
+/* One token of it for N requests: x, r, i, y [N,D]; h [num_slots,D] fp32 updated
+ * in place; slots as in rdn_conv_step_args. */
+typedef struct {
+  int N, D, dtype;
+  float c;
+  int num_slots;
+  long long x_ld, r_ld, i_ld, y_ld;
+  const void *x, *r, *i;
+  const float *lam;
+  float *h;
+  const int *slots;
+  void *y;
+} rdn_gscan_step_args;
+rdn_status_t rdn_gscan_step(const rdn_gscan_step_args *args, rdn_stream_t stream);
+
+/* The residual's addition and the norm before a block, with an output in 8 bits
+ * (e4m3: 448 the largest) and a scale per row, the left operand of rdn_linear_fwd:
+ *     r = x + f,   h = r / rms(r) * w,   rms(t) = sqrt(mean(t^2) + eps)
+ *     scale = max(max |h|, 2^-100) / 448,   q = h / scale to the nearest, ties to even
+ * Parts may be left out:  f = NULL: r = x.  w = NULL: h = r (no norm).
+ * r_out = NULL: r is not stored.
+ *   rows, D           rows >= 0, 1 <= D <= 16384.
+ *   x_dtype           of x and r_out;  f_dtype: of f.
+ *   x, f              [rows, D] with row strides;  w [D] fp32.
+ *   q [rows, D] e4m3, scale [rows] fp32, r_out [rows, D], contiguous.
+ * An element of h that is not finite has a NaN code; the other codes and the
+ * scale of its row are unspecified.  Backward: straight through the rounding it is
+ * that of the norm, rdn_norm_bwd with f = NULL, x = r_out and w_next = w. */
+typedef struct {
+  long long rows;
+  int D, x_dtype, f_dtype;
+  float eps;
+  long long x_ld, f_ld;
+  const void *x, *f;
+  const float *w;
+  void *r_out, *q;
+  float *scale;
+} rdn_norm_q8_args;
+rdn_status_t rdn_norm_q8(const rdn_norm_q8_args *args, rdn_stream_t stream);
+
+/* Matrix product with bias, activation and residual:
+ *     p = (x w^T)[m,n] (x_scale[m] w_scale[n]) + bias[n],   y = act(p) + res
+ *   M, N, K           M >= 0 rows; N, K >= 1.  K a multiple of 8 (16 for e4m3), N of 8.
+ *   dtype             of x and w: RDN_BF16 or RDN_E4M3 (forward only; with both scales).
+ *   y_dtype           of y and res: RDN_BF16 or RDN_F32.  bias_dtype: of bias and dbias, the same two.
+ *   act               0 none, 1 SiLU, 2 sigmoid, 3 GELU (x times the normal distribution function).
+ *   x [M,K], res, y [M,N] with row strides;  w [N,K] with row stride w_ld.
+ *   x_scale [M], w_scale [N] fp32 (e4m3);  bias [N] or NULL;  res or NULL.
+ *   pre               NULL, or [M,N] bf16, contiguous: p, for the backward.
+ * Rows of x and w start on 16 bytes (pointers and strides).
+ * Backward (RDN_BF16): dy [M,N] bf16 with row stride, pre (with an activation) ->
+ *     dp = dy act'(pre),   dx = dp w,   dw = dp^T x,   dbias = sum over rows of dp
+ * dx [M,K] bf16 and dw [N,K] of dw_dtype (RDN_BF16 or RDN_F32), contiguous;
+ * each of dx, dw, dbias may be NULL.  (The residual's gradient is dy itself.)  dp is
+ * held in bf16 between the activation's derivative and the products, whose sums
+ * are fp32; dbias is summed from dp in fp32.  dy's rows start on 16 bytes. */
+#define RDN_E4M3 2 /* rdn_linear_args.dtype: 8-bit floating point, 4 bits of exponent */
+typedef struct {
+  long long M;
+  int N, K, dtype, y_dtype, bias_dtype, act;
+  long long x_ld, w_ld, res_ld, y_ld;
+  const void *x, *w;
+  const float *x_scale, *w_scale;
+  const void *bias, *res;
+  void *y, *pre;
+  int dw_dtype;
+  long long dy_ld;
+  const void *dy;
+  void *dx, *dw, *dbias;
+  void *workspace;
+  size_t workspace_bytes;
+} rdn_linear_args;
+rdn_status_t rdn_linear_fwd(const rdn_linear_args *args, rdn_stream_t stream);
+rdn_status_t rdn_linear_bwd(const rdn_linear_args *args, rdn_stream_t stream);
+rdn_status_t rdn_linear_bwd_workspace_size(const rdn_linear_args *args, size_t *bytes);
+
 /* Message describing the last non-OK status returned on this thread
  * ("" if none).  The pointer stays valid until the next call on the
  * thread. */

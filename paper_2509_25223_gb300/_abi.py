@@ -33,9 +33,13 @@ EXPORTS = ["rla_fwd", "rdn_fwd", "rla_bwd", "rdn_bwd", "rdn_decode_step", "rla_f
            "rdn_conv_fwd", "rdn_conv_bwd", "rdn_conv_bwd_workspace_size", "rdn_conv_step",
            "rdn_scan_fwd", "rdn_scan_bwd", "rdn_scan_fwd_workspace_size",
            "rdn_scan_bwd_workspace_size", "rdn_scan_chunk_slots", "rdn_scan_step", "rdn_norm_fwd",
-           "rdn_norm_bwd", "rdn_norm_bwd_workspace_size"]
+           "rdn_norm_bwd", "rdn_norm_bwd_workspace_size", "rdn_gscan_fwd", "rdn_gscan_bwd",
+           "rdn_gscan_bwd_workspace_size", "rdn_gscan_step", "rdn_norm_q8", "rdn_linear_fwd",
+           "rdn_linear_bwd", "rdn_linear_bwd_workspace_size"]
 
 SCAN_CHUNK = 16  # RDN_SCAN_CHUNK
+GSCAN_CHUNK = 64  # RDN_GSCAN_CHUNK
+RDN_E4M3 = 2  # rdn_linear_args.dtype
 
 
 class ProfRecord(ctypes.Structure):
@@ -112,6 +116,16 @@ ScanStepArgs, SCAN_STEP_PACK = _layout(
 NormArgs, NORM_PACK = _layout(
     "NormArgs", "q rows; i D heads dtype x_dtype gate; f eps scale_const; q f_ld z_ld x_ld;"
     " P f z x w scale w_next r_out h dr dh df dz dx dw dscale dw_next workspace; n workspace_bytes")
+GscanArgs, GSCAN_PACK = _layout(
+    "GscanArgs", "i B T D dtype; f c; q x_ld r_ld i_ld y_ld; P x r i lam h0 y hT h_chunks cu_seqlens;"
+    " i num_seqs; q dy_ld dx_ld dr_ld di_ld; P dy dhT dx dr di dlam dh0 workspace; n workspace_bytes")
+GscanStepArgs, GSCAN_STEP_PACK = _layout(
+    "GscanStepArgs", "i N D dtype; f c; i num_slots; q x_ld r_ld i_ld y_ld; P x r i lam h slots y")
+NormQ8Args, NORM_Q8_PACK = _layout(
+    "NormQ8Args", "q rows; i D x_dtype f_dtype; f eps; q x_ld f_ld; P x f w r_out q scale")
+LinearArgs, LINEAR_PACK = _layout(
+    "LinearArgs", "q M; i N K dtype y_dtype bias_dtype act; q x_ld w_ld res_ld y_ld; P x w x_scale"
+    " w_scale bias res y pre; i dw_dtype; q dy_ld; P dy dx dw dbias workspace; n workspace_bytes")
 
 _lib = None
 _decode_step = None
@@ -182,6 +196,14 @@ def load(build_if_missing: bool = True):
                        ("rdn_norm_fwd", [ctypes.POINTER(NormArgs), P]),
                        ("rdn_norm_bwd", [ctypes.POINTER(NormArgs), P]),
                        ("rdn_norm_bwd_workspace_size", [ctypes.POINTER(NormArgs), ctypes.POINTER(ctypes.c_size_t)]),
+                       ("rdn_gscan_fwd", [ctypes.POINTER(GscanArgs), P]),
+                       ("rdn_gscan_bwd", [ctypes.POINTER(GscanArgs), P]),
+                       ("rdn_gscan_bwd_workspace_size", [ctypes.POINTER(GscanArgs), ctypes.POINTER(ctypes.c_size_t)]),
+                       ("rdn_gscan_step", [ctypes.POINTER(GscanStepArgs), P]),
+                       ("rdn_norm_q8", [ctypes.POINTER(NormQ8Args), P]),
+                       ("rdn_linear_fwd", [ctypes.POINTER(LinearArgs), P]),
+                       ("rdn_linear_bwd", [ctypes.POINTER(LinearArgs), P]),
+                       ("rdn_linear_bwd_workspace_size", [ctypes.POINTER(LinearArgs), ctypes.POINTER(ctypes.c_size_t)]),
                        ("rdn_chunk_slots", [ctypes.POINTER(FwdArgs), ctypes.POINTER(ctypes.c_longlong)])]:
         fn = getattr(lib, name)
         fn.argtypes = argt

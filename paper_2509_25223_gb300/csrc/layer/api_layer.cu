@@ -1,5 +1,5 @@
 // api_layer.cu -- the C ABI of the operators around the recurrence (convolution,
-// selective scan, norms; include/rdn.h): argument validation and dispatch to
+// selective scan, norms, gated recurrence, matrix products; include/rdn.h): argument validation and dispatch to
 // the launchers.  No exception or abort crosses this boundary.
 #include <math.h>
 
@@ -18,6 +18,16 @@ cudaError_t launch_scan_bwd(const rdn_scan_args &a, cudaStream_t s);
 cudaError_t launch_scan_step(const rdn_scan_step_args &a, cudaStream_t s);
 size_t norm_bwd_bytes(const rdn_norm_args &a);
 cudaError_t launch_norm(const rdn_norm_args &a, bool bwd, cudaStream_t s);
+long long gscan_slots(const rdn_gscan_args &a);
+long long gscan_ctas(const rdn_gscan_args &a);
+size_t gscan_bwd_bytes(const rdn_gscan_args &a);
+cudaError_t launch_gscan_fwd(const rdn_gscan_args &a, cudaStream_t s);
+cudaError_t launch_gscan_bwd(const rdn_gscan_args &a, cudaStream_t s);
+cudaError_t launch_gscan_step(const rdn_gscan_step_args &a, cudaStream_t s);
+cudaError_t launch_norm_q8(const rdn_norm_q8_args &a, cudaStream_t s);
+size_t linear_bwd_bytes(const rdn_linear_args &a);
+cudaError_t launch_linear_fwd(const rdn_linear_args &a, cudaStream_t s);
+cudaError_t launch_linear_bwd(const rdn_linear_args &a, cudaStream_t s);
 }  // namespace rdn
 
 using rdn::CallRange;
@@ -263,6 +273,140 @@ rdn_status_t norm_common(const char *fn, const rdn_norm_args *args, bool bwd, cu
   return entry_cuda(fn, rdn::launch_norm(*a, bwd, s));
 }
 
+// ---- gated linear recurrence
+
+rdn_status_t gscan_shapes(const char *fn, rdn_gscan_args *a) {
+  TRY(check_seqs(fn, a->B, a->T, a->cu_seqlens, a->num_seqs));
+  if (a->D < 1 || a->D > (1 << 19))
+    return entry_fail(RDN_ERR_INVALID_ARG, "%s: need 1 <= D <= 2^19 (got %d)", fn, a->D);
+  TRY(check_dtype(fn, a->dtype));
+  if (!(a->c > 0.f) || isinf(a->c)) return entry_fail(RDN_ERR_INVALID_ARG, "%s: c must be finite and > 0", fn);
+  if (rdn::gscan_ctas(*a) > 0x7fffffffll)
+    return entry_fail(RDN_ERR_UNSUPPORTED, "%s: B = %d rows of D = %d channels are too many", fn, a->B, a->D);
+  TRY(check_ld(fn, "x_ld", &a->x_ld, a->D));
+  TRY(check_ld(fn, "r_ld", &a->r_ld, a->D));
+  TRY(check_ld(fn, "i_ld", &a->i_ld, a->D));
+  TRY(check_ld(fn, "y_ld", &a->y_ld, a->D));
+  TRY(check_ld(fn, "dy_ld", &a->dy_ld, a->D));
+  TRY(check_ld(fn, "dx_ld", &a->dx_ld, a->D));
+  TRY(check_ld(fn, "dr_ld", &a->dr_ld, a->D));
+  return check_ld(fn, "di_ld", &a->di_ld, a->D);
+}
+
+rdn_status_t gscan_common(const char *fn, const rdn_gscan_args *args, bool bwd, cudaStream_t s) {
+  CallRange range(fn);
+  if (!args) return entry_fail(RDN_ERR_INVALID_ARG, "%s: args is NULL", fn);
+  rdn_gscan_args copy = *args, *a = &copy;
+  TRY(gscan_shapes(fn, a));
+  const size_t e = dtype_size(a->dtype), row = (size_t)a->D * 4;
+  const size_t states = (a->cu_seqlens ? a->num_seqs : a->B) * row, kept = (size_t)rdn::gscan_slots(*a) * row;
+  const bool any = a->T > 0;
+  TRY(check_ptr(fn, "x", a->x, e, any));
+  TRY(check_ptr(fn, "r", a->r, e, any));
+  TRY(check_ptr(fn, "i", a->i, e, any));
+  TRY(check_ptr(fn, "lam", a->lam, 4, true));
+  TRY(check_ptr(fn, "h0", a->h0, 4, false));
+  TRY(check_ptr(fn, "h_chunks", a->h_chunks, 4, false));
+  if (!bwd) {
+    TRY(check_ptr(fn, "y", a->y, e, any));
+    TRY(check_ptr(fn, "hT", a->hT, 4, false));
+    TRY(check_apart(fn, "hT", a->hT, states, "h0", a->h0, states));
+    TRY(check_apart(fn, "h_chunks", a->h_chunks, kept, "h0", a->h0, states));
+    TRY(check_apart(fn, "h_chunks", a->h_chunks, kept, "hT", a->hT, states));
+    if (a->y && (a->y == a->x || a->y == a->r || a->y == a->i))
+      return entry_fail(RDN_ERR_INVALID_ARG, "%s: y aliases an input", fn);
+    TRY(entry_injected(fn));
+    return entry_cuda(fn, rdn::launch_gscan_fwd(*a, s));
+  }
+  TRY(check_ptr(fn, "dy", a->dy, e, any));
+  TRY(check_ptr(fn, "dhT", a->dhT, 4, false));
+  TRY(check_ptr(fn, "dlam", a->dlam, 4, true));
+  TRY(check_ptr(fn, "dh0", a->dh0, 4, false));
+  const void *outs[3] = {a->dx, a->dr, a->di}, *ins[4] = {a->x, a->r, a->i, a->dy};
+  const char *names[3] = {"dx", "dr", "di"};
+  for (int k = 0; k < 3; ++k) {
+    TRY(check_ptr(fn, names[k], outs[k], e, any));
+    for (const void *in : ins)
+      if (any && outs[k] == in) return entry_fail(RDN_ERR_INVALID_ARG, "%s: %s aliases an input", fn, names[k]);
+  }
+  TRY(check_apart(fn, "dh0", a->dh0, states, "dhT", a->dhT, states));
+  TRY(check_apart(fn, "dh0", a->dh0, states, "h0", a->h0, states));
+  TRY(check_apart(fn, "dh0", a->dh0, states, "h_chunks", a->h_chunks, kept));
+  TRY(check_ws(fn, a->workspace, a->workspace_bytes, rdn::gscan_bwd_bytes(*a)));
+  TRY(entry_injected(fn));
+  return entry_cuda(fn, rdn::launch_gscan_bwd(*a, s));
+}
+
+// ---- matrix products
+
+rdn_status_t check_on16(const char *fn, const char *name, const void *p, long long ld, size_t e, bool required) {
+  TRY(check_ptr16(fn, name, p, required));
+  if (p && (ld * e) & 15)
+    return entry_fail(RDN_ERR_MISALIGNED, "%s: rows of %s (%lld elements apart) do not start on 16 bytes", fn, name, ld);
+  return RDN_OK;
+}
+
+rdn_status_t linear_shapes(const char *fn, rdn_linear_args *a, bool bwd) {
+  if (a->M < 0 || a->N < 1 || a->K < 1)
+    return entry_fail(RDN_ERR_INVALID_ARG, "%s: need M >= 0, N, K >= 1 (got M=%lld N=%d K=%d)", fn, a->M, a->N, a->K);
+  if (a->dtype != RDN_BF16 && (bwd || a->dtype != RDN_E4M3))
+    return entry_fail(RDN_ERR_UNSUPPORTED, "%s: dtype %d unsupported (bf16%s)", fn, a->dtype, bwd ? "" : " or e4m3");
+  const int by = a->dtype == RDN_E4M3 ? 16 : 8;
+  if (a->K % by || a->N % 8)
+    return entry_fail(RDN_ERR_UNSUPPORTED, "%s: K must be a multiple of %d and N of 8 (got N=%d K=%d)", fn, by, a->N, a->K);
+  const long long wide = a->N > a->K ? a->N : a->K;
+  if (a->M > (1ll << 30) || wide > (1 << 20) || a->M * wide > (1ll << 40))
+    return entry_fail(RDN_ERR_UNSUPPORTED, "%s: M=%lld N=%d K=%d are too large", fn, a->M, a->N, a->K);
+  if (!dtype_ok(a->y_dtype) || !dtype_ok(a->bias_dtype) || !dtype_ok(a->dw_dtype))
+    return entry_fail(RDN_ERR_UNSUPPORTED, "%s: y_dtype, bias_dtype and dw_dtype are bf16 or fp32", fn);
+  if (a->act < 0 || a->act > 3) return entry_fail(RDN_ERR_INVALID_ARG, "%s: act must be 0 to 3 (got %d)", fn, a->act);
+  TRY(check_ld(fn, "x_ld", &a->x_ld, a->K));
+  TRY(check_ld(fn, "w_ld", &a->w_ld, a->K));
+  TRY(check_ld(fn, "res_ld", &a->res_ld, a->N));
+  TRY(check_ld(fn, "y_ld", &a->y_ld, a->N));
+  // (the tensor maps hold strides below 2^40 bytes)
+  if (a->x_ld >= (1ll << 38) || a->w_ld >= (1ll << 38) || a->dy_ld >= (1ll << 38))
+    return entry_fail(RDN_ERR_UNSUPPORTED, "%s: rows of x, w or dy are too far apart", fn);
+  return check_ld(fn, "dy_ld", &a->dy_ld, a->N);
+}
+
+rdn_status_t linear_common(const char *fn, const rdn_linear_args *args, bool bwd, cudaStream_t s) {
+  CallRange range(fn);
+  if (!args) return entry_fail(RDN_ERR_INVALID_ARG, "%s: args is NULL", fn);
+  rdn_linear_args copy = *args, *a = &copy;
+  TRY(linear_shapes(fn, a, bwd));
+  const bool any = a->M > 0, q8 = a->dtype == RDN_E4M3;
+  const size_t e = q8 ? 1 : 2, ye = dtype_size(a->y_dtype), be = dtype_size(a->bias_dtype);
+  TRY(check_on16(fn, "x", a->x, a->x_ld, e, any));
+  TRY(check_on16(fn, "w", a->w, a->w_ld, e, true));
+  if (!bwd) {
+    TRY(check_ptr(fn, "x_scale", a->x_scale, 4, q8 && any));
+    TRY(check_ptr(fn, "w_scale", a->w_scale, 4, q8));
+    if (!q8 && (a->x_scale || a->w_scale))
+      return entry_fail(RDN_ERR_INVALID_ARG, "%s: scales go with e4m3 operands", fn);
+    TRY(check_ptr(fn, "bias", a->bias, be, false));
+    TRY(check_ptr(fn, "res", a->res, ye, false));
+    TRY(check_ptr(fn, "y", a->y, ye, any));
+    TRY(check_ptr16(fn, "pre", a->pre, false));
+    if (any && (a->y == a->x || a->y == a->w || (a->pre && (a->pre == a->y || a->pre == a->x || a->pre == a->res))))
+      return entry_fail(RDN_ERR_INVALID_ARG, "%s: y or pre aliases another operand", fn);
+    if (any && a->y == a->res && a->y_ld != a->res_ld)
+      return entry_fail(RDN_ERR_INVALID_ARG, "%s: y may be res only with the same rows", fn);
+    TRY(entry_injected(fn));
+    return entry_cuda(fn, rdn::launch_linear_fwd(*a, s));
+  }
+  TRY(check_on16(fn, "dy", a->dy, a->dy_ld, 2, any));
+  TRY(check_ptr16(fn, "pre", a->pre, any && a->act));
+  TRY(check_ptr16(fn, "dx", a->dx, false));
+  TRY(check_ptr(fn, "dw", a->dw, dtype_size(a->dw_dtype), false));
+  TRY(check_ptr(fn, "dbias", a->dbias, be, false));
+  if (any && ((a->dx && (a->dx == a->x || a->dx == a->dy || a->dx == a->pre)) || (a->dw && a->dw == a->w)))
+    return entry_fail(RDN_ERR_INVALID_ARG, "%s: dx or dw aliases an input", fn);
+  TRY(check_ws(fn, a->workspace, a->workspace_bytes, rdn::linear_bwd_bytes(*a)));
+  TRY(entry_injected(fn));
+  return entry_cuda(fn, rdn::launch_linear_bwd(*a, s));
+}
+
 rdn_status_t check_step(const char *fn, int N, int num_slots, const int *slots) {
   if (N < 1) return entry_fail(RDN_ERR_INVALID_ARG, "%s: need N >= 1 (got %d)", fn, N);
   if (num_slots < 1 || (!slots && num_slots < N))
@@ -393,6 +537,92 @@ rdn_status_t rdn_norm_bwd_workspace_size(const rdn_norm_args *args, size_t *byte
   TRY(norm_shapes(fn, &a));
   if (!bytes) return entry_fail(RDN_ERR_INVALID_ARG, "%s: bytes is NULL", fn);
   *bytes = rdn::norm_bwd_bytes(a);
+  return entry_ok();
+}
+
+rdn_status_t rdn_gscan_fwd(const rdn_gscan_args *a, rdn_stream_t stream) {
+  return gscan_common("rdn_gscan_fwd", a, false, (cudaStream_t)stream);
+}
+rdn_status_t rdn_gscan_bwd(const rdn_gscan_args *a, rdn_stream_t stream) {
+  return gscan_common("rdn_gscan_bwd", a, true, (cudaStream_t)stream);
+}
+rdn_status_t rdn_gscan_bwd_workspace_size(const rdn_gscan_args *args, size_t *bytes) {
+  const char *fn = "rdn_gscan_bwd_workspace_size";
+  if (!args) return entry_fail(RDN_ERR_INVALID_ARG, "%s: args is NULL", fn);
+  rdn_gscan_args a = *args;
+  TRY(gscan_shapes(fn, &a));
+  if (!bytes) return entry_fail(RDN_ERR_INVALID_ARG, "%s: bytes is NULL", fn);
+  *bytes = rdn::gscan_bwd_bytes(a);
+  return entry_ok();
+}
+
+rdn_status_t rdn_gscan_step(const rdn_gscan_step_args *args, rdn_stream_t stream) {
+  const char *fn = "rdn_gscan_step";
+  CallRange range(fn);
+  if (!args) return entry_fail(RDN_ERR_INVALID_ARG, "%s: args is NULL", fn);
+  rdn_gscan_step_args copy = *args, *a = &copy;
+  TRY(check_step(fn, a->N, a->num_slots, a->slots));
+  if (a->D < 1 || a->D > (1 << 19))
+    return entry_fail(RDN_ERR_INVALID_ARG, "%s: need 1 <= D <= 2^19 (got %d)", fn, a->D);
+  TRY(check_dtype(fn, a->dtype));
+  if (!(a->c > 0.f) || isinf(a->c)) return entry_fail(RDN_ERR_INVALID_ARG, "%s: c must be finite and > 0", fn);
+  TRY(check_ld(fn, "x_ld", &a->x_ld, a->D));
+  TRY(check_ld(fn, "r_ld", &a->r_ld, a->D));
+  TRY(check_ld(fn, "i_ld", &a->i_ld, a->D));
+  TRY(check_ld(fn, "y_ld", &a->y_ld, a->D));
+  const size_t e = dtype_size(a->dtype);
+  TRY(check_ptr(fn, "x", a->x, e, true));
+  TRY(check_ptr(fn, "r", a->r, e, true));
+  TRY(check_ptr(fn, "i", a->i, e, true));
+  TRY(check_ptr(fn, "lam", a->lam, 4, true));
+  TRY(check_ptr(fn, "h", a->h, 4, true));
+  TRY(check_ptr(fn, "y", a->y, e, true));
+  TRY(entry_injected(fn));
+  return entry_cuda(fn, rdn::launch_gscan_step(*a, (cudaStream_t)stream));
+}
+
+rdn_status_t rdn_norm_q8(const rdn_norm_q8_args *args, rdn_stream_t stream) {
+  const char *fn = "rdn_norm_q8";
+  CallRange range(fn);
+  if (!args) return entry_fail(RDN_ERR_INVALID_ARG, "%s: args is NULL", fn);
+  rdn_norm_q8_args copy = *args, *a = &copy;
+  if (a->rows < 0 || a->rows > (1ll << 30))
+    return entry_fail(RDN_ERR_INVALID_ARG, "%s: rows must be in [0, 2^30] (got %lld)", fn, a->rows);
+  if (a->D < 1) return entry_fail(RDN_ERR_INVALID_ARG, "%s: need D >= 1 (got %d)", fn, a->D);
+  if (a->D > 16384) return entry_fail(RDN_ERR_UNSUPPORTED, "%s: rows of at most 16384 elements (got %d)", fn, a->D);
+  if (!dtype_ok(a->x_dtype) || (a->f && !dtype_ok(a->f_dtype)))
+    return entry_fail(RDN_ERR_UNSUPPORTED, "%s: x_dtype %d or f_dtype %d unsupported", fn, a->x_dtype, a->f_dtype);
+  if (!(a->eps >= 0.f) || isinf(a->eps)) return entry_fail(RDN_ERR_INVALID_ARG, "%s: eps must be finite and >= 0", fn);
+  TRY(check_ld(fn, "x_ld", &a->x_ld, a->D));
+  TRY(check_ld(fn, "f_ld", &a->f_ld, a->D));
+  const bool any = a->rows > 0;
+  const size_t xe = dtype_size(a->x_dtype);
+  TRY(check_ptr(fn, "x", a->x, xe, any));
+  TRY(check_ptr(fn, "f", a->f, a->f ? dtype_size(a->f_dtype) : 1, false));
+  TRY(check_ptr(fn, "w", a->w, 4, false));
+  TRY(check_ptr(fn, "r_out", a->r_out, xe, false));
+  TRY(check_ptr(fn, "q", a->q, 1, any));
+  TRY(check_ptr(fn, "scale", a->scale, 4, any));
+  if (any && a->r_out && (a->r_out == a->f || (a->r_out == a->x && a->x_ld != a->D)))
+    return entry_fail(RDN_ERR_INVALID_ARG, "%s: r_out may be x only where x is contiguous, and not f", fn);
+  if (any && (a->q == a->x || a->q == a->f)) return entry_fail(RDN_ERR_INVALID_ARG, "%s: q aliases an input", fn);
+  TRY(entry_injected(fn));
+  return entry_cuda(fn, rdn::launch_norm_q8(*a, (cudaStream_t)stream));
+}
+
+rdn_status_t rdn_linear_fwd(const rdn_linear_args *a, rdn_stream_t stream) {
+  return linear_common("rdn_linear_fwd", a, false, (cudaStream_t)stream);
+}
+rdn_status_t rdn_linear_bwd(const rdn_linear_args *a, rdn_stream_t stream) {
+  return linear_common("rdn_linear_bwd", a, true, (cudaStream_t)stream);
+}
+rdn_status_t rdn_linear_bwd_workspace_size(const rdn_linear_args *args, size_t *bytes) {
+  const char *fn = "rdn_linear_bwd_workspace_size";
+  if (!args) return entry_fail(RDN_ERR_INVALID_ARG, "%s: args is NULL", fn);
+  rdn_linear_args a = *args;
+  TRY(linear_shapes(fn, &a, true));
+  if (!bytes) return entry_fail(RDN_ERR_INVALID_ARG, "%s: bytes is NULL", fn);
+  *bytes = rdn::linear_bwd_bytes(a);
   return entry_ok();
 }
 

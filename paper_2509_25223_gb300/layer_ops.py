@@ -1,7 +1,8 @@
 """The operators around the recurrence (include/rdn.h, "Operators around the
-recurrence"): the short causal convolution, the selective state space scan and
-the norms before and after a block with its gate and scaled residual; for
-prompts and training, and for single tokens.
+recurrence"): the short causal convolution, the selective state space scan, the
+gated linear recurrence, the norms before and after a block with its gate and
+scaled residual, the norm with an output in 8 bits, and the matrix product with
+bias, activation and residual; for prompts and training, and for single tokens.
 
 As in the rest of the package these functions only check and marshal
 arguments, allocate results and the workspace the library asks for, and raise
@@ -12,8 +13,9 @@ Token rows may be strided: a [B, T, C] operand can be a slice of the last axis
 of a wider, otherwise contiguous tensor (`proj[..., a:b]`), without a copy.  All
 its rows have to be one distance apart: a slice of the tokens of several batch
 rows (`x[:, a:b]`) and expanded tensors are refused (make them contiguous).
-Parameters (weights, biases, A, D, scales) and the scan's states are fp32;
-results and convolution states have the inputs' type (bf16 or fp32).
+Parameters (weights, biases, A, D, scales) and the scans' states are fp32;
+results and convolution states have the inputs' type (bf16 or fp32).  The matrix
+product's operands are bf16, or 8-bit with scales.
 """
 from __future__ import annotations
 
@@ -24,7 +26,8 @@ import torch
 from . import _abi
 
 __all__ = ["causal_conv_fwd", "causal_conv_bwd", "causal_conv_step", "selective_scan_fwd",
-           "selective_scan_bwd", "selective_scan_step", "block_norm_fwd", "block_norm_bwd"]
+           "selective_scan_bwd", "selective_scan_step", "block_norm_fwd", "block_norm_bwd", "gated_scan_fwd",
+           "gated_scan_bwd", "gated_scan_step", "add_norm_q8", "linear_fwd", "linear_bwd"]
 
 _DTYPES = {torch.bfloat16: _abi.RDN_BF16, torch.float32: _abi.RDN_F32}
 _GATES = {"silu": 0, "sigmoid": 1}
@@ -476,4 +479,232 @@ def block_norm_bwd(f=None, weight=None, z=None, gate="silu", x=None, scale=None,
     ws = _workspace(workspace, nbytes, a.dev)
     _call("rdn_norm_bwd", _abi.NORM_PACK(*a.head, *tail, ws.data_ptr(),
                                          ws.numel() * ws.element_size()), a.dev)
+    return res
+
+
+class _Gated:
+    """The operands of a gated recurrence, checked, as the leading values of GSCAN_PACK."""
+
+    def __init__(self, x, r, i, lam, c, h0, cu_seqlens):
+        self.dev, self.shape = _cuda("x", x, 3)
+        dev, self.dtype = self.dev, x.dtype
+        b, t, d = self.shape
+        self.cu, self.ns, self.n = _table(cu_seqlens, b, dev)
+        self.states = (self.n, d)
+        rows = [_rows(n, v, self.shape, x.dtype, dev) for n, v in (("x", x), ("r", r), ("i", i))]
+        self.head = (b, t, d, _code(x.dtype), float(c))
+        self.lds, self.ptrs = [v[1] for v in rows], [v[0] for v in rows]
+        self.params = (_whole("lam", lam, (d,), _F32, dev), _whole("h0", h0, self.states, _F32, dev))
+
+    def chunks(self):
+        """Shape of the kept states."""
+        b, t, d = self.shape
+        return (b, (t + _abi.GSCAN_CHUNK - 1) // _abi.GSCAN_CHUNK, d)
+
+    def pack(self, y=(0, 0), hT=0, chunks=0, grads=(0,) * 11, ws=0, nbytes=0):
+        return _abi.GSCAN_PACK(*self.head, *self.lds, y[1], *self.ptrs, *self.params, y[0], hT, chunks,
+                               self.cu, self.ns, *grads, ws, nbytes)
+
+
+def gated_scan_fwd(x, r, i, lam, c=8.0, h0=None, cu_seqlens=None, return_final_state=True,
+                   return_chunk_states=False, out=None):
+    """Gated linear recurrence over d channels of one state each:
+        a_t = exp(-c softplus(lam) sigmoid(r_t))
+        h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(i_t) x_t,   y_t = h_t
+
+    x, r, i [B,T,d]; lam [d] fp32; h0 [B or num_seqs, d] fp32.  Returns (y, hT);
+    with return_chunk_states also the states before every 64 tokens
+    [B, ceil(T/64), d], which gated_scan_bwd can read instead of computing them
+    again; only y with both off.  cu_seqlens: packed sequences."""
+    a = _Gated(x, r, i, lam, c, h0, cu_seqlens)
+    dev = a.dev
+    y = torch.empty(a.shape, dtype=a.dtype, device=dev) if out is None else out
+    hT = torch.empty(a.states, dtype=_F32, device=dev) if return_final_state else None
+    hc = torch.empty(a.chunks(), dtype=_F32, device=dev) if return_chunk_states else None
+    args = a.pack(_rows("out", y, a.shape, a.dtype, dev), 0 if hT is None else hT.data_ptr(),
+                  0 if hc is None else hc.data_ptr())
+    _call("rdn_gscan_fwd", args, dev)
+    res = (y,) + ((hT,) if return_final_state else ()) + ((hc,) if return_chunk_states else ())
+    return res if len(res) > 1 else y
+
+
+def gated_scan_bwd(x, r, i, lam, dy, c=8.0, h0=None, dhT=None, cu_seqlens=None, h_chunks=None,
+                   workspace=None, out=None):
+    """Backward of gated_scan_fwd.  dy: gradient of y; dhT: of the final states, or
+    None; h_chunks: the forward's return_chunk_states (None: computed again).
+    Returns a dict with dx, dr, di, dlam (fp32) and, with h0, dh0.  out: tensors
+    to write into, by those names."""
+    a = _Gated(x, r, i, lam, c, h0, cu_seqlens)
+    dev, d = a.dev, a.shape[2]
+    res = dict(out) if out else {}
+    for name in ("dx", "dr", "di"):
+        if res.get(name) is None:
+            res[name] = torch.empty(a.shape, dtype=a.dtype, device=dev)
+    if res.get("dlam") is None:
+        res["dlam"] = torch.empty(d, dtype=_F32, device=dev)
+    if h0 is not None and res.get("dh0") is None:
+        res["dh0"] = torch.empty(a.states, dtype=_F32, device=dev)
+    rows = [_rows(n, v, a.shape, a.dtype, dev)
+            for n, v in (("dy", dy), ("dx", res["dx"]), ("dr", res["dr"]), ("di", res["di"]))]
+    grads = ([v[1] for v in rows] + [rows[0][0], _whole("dhT", dhT, a.states, _F32, dev)]
+             + [v[0] for v in rows[1:]] + [_whole("dlam", res["dlam"], (d,), _F32, dev),
+                                           _whole("dh0", res.get("dh0"), a.states, _F32, dev)])
+    hc = _whole("h_chunks", h_chunks, a.chunks(), _F32, dev)
+    ws = _workspace(workspace, _size("rdn_gscan_bwd_workspace_size", a.pack(chunks=hc)), dev)
+    _call("rdn_gscan_bwd", a.pack(chunks=hc, grads=grads, ws=ws.data_ptr(),
+                                  nbytes=ws.numel() * ws.element_size()), dev)
+    return res
+
+
+def gated_scan_step(x, r, i, lam, h, c=8.0, slots=None, out=None):
+    """One token of gated_scan_fwd for N requests: x, r, i [N,d]; h [num_slots,d]
+    fp32 is updated in place.  slots [N] int32: each request's row of h (distinct);
+    a negative one is an idle row (y = 0).  None: row n."""
+    dev, shape = _cuda("x", x, 2)
+    n, d = shape
+    ty = x.dtype
+    rows = [_rows(k, v, shape, ty, dev, 1) for k, v in (("x", x), ("r", r), ("i", i))]
+    if out is None:
+        y = torch.empty(shape, dtype=ty, device=dev)
+        py, y_ld = y.data_ptr(), 0
+    else:
+        y = out
+        py, y_ld = _rows("out", y, shape, ty, dev, 1)
+    num = h.shape[0]
+    args = _abi.GSCAN_STEP_PACK(
+        n, d, _code(ty), float(c), num, *(v[1] for v in rows), y_ld, *(v[0] for v in rows),
+        _whole("lam", lam, (d,), _F32, dev), _whole("h", h, (num, d), _F32, dev),
+        _whole("slots", slots, (n,), torch.int32, dev), py)
+    _call("rdn_gscan_step", args, dev)
+    return y
+
+
+_E4M3 = torch.float8_e4m3fn
+
+
+def add_norm_q8(x, f=None, weight=None, eps=1e-6, out=None):
+    """The residual's addition and the norm before a block, per row of the last
+    axis, with an output in 8 bits and a scale per row:
+        r = x + f                       (f=None: r is x itself)
+        h = r / rms(r) * weight         (weight=None: h = r)
+        scale = max|h| / 448,  q = h / scale rounded to float8_e4m3fn
+    x, f [..., D] (bf16 or fp32, each its own); weight [D] fp32.  Returns
+    (r, q, scale): r in x's type, scale [...] fp32; q and scale are the first
+    operand of linear_fwd.  out: (r, q, scale) to write into; r may be x.
+    Backward (straight through the rounding): block_norm_bwd(x=r,
+    weight_next=weight, dr=dr, dh=dh)["dx"] is the gradient of x and of f."""
+    dev, shape = x.get_device(), x.shape
+    if dev < 0 or not shape:
+        raise ValueError("rdn: tensors must be on a CUDA device, with at least one axis")
+    d, lead = shape[-1], len(shape) - 1
+    r, q, s = out if out is not None else (None, None, None)
+    if f is None:
+        r, pr = x, 0
+    elif r is None:
+        r = torch.empty(shape, dtype=x.dtype, device=dev)
+        pr = r.data_ptr()
+    else:
+        pr = _whole("r", r, shape, x.dtype, dev)
+    q = torch.empty(shape, dtype=_E4M3, device=dev) if q is None else q
+    s = torch.empty(shape[:-1], dtype=_F32, device=dev) if s is None else s
+    px, x_ld = _rows("x", x, shape, x.dtype, dev, lead)
+    pf, f_ld = (0, 0) if f is None else _rows("f", f, shape, f.dtype, dev, lead)
+    rows = x.numel() // d if d else 0
+    args = _abi.NORM_Q8_PACK(rows, d, _code(x.dtype), 0 if f is None else _code(f.dtype), float(eps),
+                             x_ld, f_ld, px, pf, _whole("weight", weight, (d,), _F32, dev), pr,
+                             _whole("q", q, shape, _E4M3, dev), _whole("scale", s, shape[:-1], _F32, dev))
+    _call("rdn_norm_q8", args, dev)
+    return r, q, s
+
+
+_ACTS = {None: 0, "silu": 1, "sigmoid": 2, "gelu": 3}
+
+
+def _act(act):
+    if act not in _ACTS:
+        raise ValueError(f'rdn: act must be None, "silu", "sigmoid" or "gelu" (got {act!r})')
+    return _ACTS[act]
+
+
+def _linear_operands(x, w):
+    """(device, rows' shape, M, N, K, x's and w's (address, row stride))"""
+    dev, shape = x.get_device(), x.shape
+    if dev < 0 or not shape:
+        raise ValueError("rdn: tensors must be on a CUDA device, with at least one axis")
+    if w.dim() != 2 or w.shape[1] != shape[-1]:
+        raise ValueError(f"rdn: w must be [N, {shape[-1]}] (got {tuple(w.shape)})")
+    n, k = w.shape
+    lead = shape[:-1]
+    m = 1
+    for v in lead:
+        m *= v
+    return (dev, lead, m, n, k, _rows("x", x, shape, x.dtype, dev, len(lead)),
+            _rows("w", w, w.shape, x.dtype, dev, 1))
+
+
+def linear_fwd(x, w, bias=None, act=None, residual=None, x_scale=None, w_scale=None, out_dtype=None,
+               return_pre=False, out=None):
+    """Matrix product with bias, activation and residual:
+        p = x w^T (x_scale w_scale) + bias,   y = act(p) + residual
+    act: None, "silu", "sigmoid" or "gelu".
+
+    x [..., K], w [N, K] bf16, or float8_e4m3fn with x_scale [...] and w_scale [N]
+    fp32 (add_norm_q8 makes both); bias [N] bf16 or fp32; residual [..., N] in y's
+    type.  y [..., N]: out_dtype, or the residual's type, or bf16.  K a multiple
+    of 8 (8-bit: 16), N of 8; rows of x and w start on 16 bytes.  Returns y, or
+    (y, p in bf16) with return_pre, which linear_bwd reads.  out: y to write into;
+    it may be the residual."""
+    dev, lead, m, n, k, (px, x_ld), (pw, w_ld) = _linear_operands(x, w)
+    q8 = x.dtype is _E4M3
+    if not q8 and x.dtype is not torch.bfloat16:
+        raise ValueError(f"rdn: unsupported dtype {x.dtype}")
+    if q8 != (x_scale is not None) or q8 != (w_scale is not None):
+        raise ValueError("rdn: x_scale and w_scale go with 8-bit operands")
+    ty = out_dtype or (out.dtype if out is not None else torch.bfloat16 if residual is None else residual.dtype)
+    shape = (*lead, n)
+    pr, r_ld = (0, 0) if residual is None else _rows("residual", residual, shape, ty, dev, len(lead))
+    y = torch.empty(shape, dtype=ty, device=dev) if out is None else out
+    py, y_ld = _rows("out", y, shape, ty, dev, len(lead))
+    pre = torch.empty(shape, dtype=torch.bfloat16, device=dev) if return_pre else None
+    args = _abi.LINEAR_PACK(
+        m, n, k, _abi.RDN_E4M3 if q8 else _abi.RDN_BF16, _code(ty), 0 if bias is None else _code(bias.dtype),
+        _act(act), x_ld, w_ld, r_ld, y_ld, px, pw, _whole("x_scale", x_scale, lead, _F32, dev),
+        _whole("w_scale", w_scale, (n,), _F32, dev),
+        0 if bias is None else _whole("bias", bias, (n,), bias.dtype, dev), pr, py,
+        0 if pre is None else pre.data_ptr(), 0, 0, 0, 0, 0, 0, 0, 0)
+    _call("rdn_linear_fwd", args, dev)
+    return (y, pre) if return_pre else y
+
+
+def linear_bwd(x, w, dy, pre=None, act=None, bias=None, need_dx=True, need_dw=True, dw_dtype=None,
+               workspace=None, out=None):
+    """Backward of linear_fwd in bf16: dp = dy act'(pre), dx = dp w, dw = dp^T x,
+    dbias = the sum of dp's rows; the residual's gradient is dy itself.
+
+    dy [..., N] bf16; pre: linear_fwd's return_pre, needed with an activation;
+    bias: the forward's bias, or None.  Returns a dict with dx (bf16), dw (dw_dtype,
+    or w's type) and, with a bias, dbias in its type.  out: tensors to write into,
+    by those names."""
+    dev, lead, m, n, k, (px, x_ld), (pw, w_ld) = _linear_operands(x, w)
+    bf = torch.bfloat16
+    if x.dtype is not bf:
+        raise ValueError(f"rdn: unsupported dtype {x.dtype}")
+    res = dict(out) if out else {}
+    wt = dw_dtype or (res["dw"].dtype if res.get("dw") is not None else w.dtype)
+    for name, shape, ty, wanted in (("dx", x.shape, bf, need_dx), ("dw", w.shape, wt, need_dw),
+                                    ("dbias", (n,), None if bias is None else bias.dtype, bias is not None)):
+        if wanted and res.get(name) is None:
+            res[name] = torch.empty(shape, dtype=ty, device=dev)
+        elif not wanted:
+            res.pop(name, None)
+    if act is not None and pre is None:
+        raise ValueError("rdn: the backward of an activation needs pre")
+    pdy, dy_ld = _rows("dy", dy, (*lead, n), bf, dev, len(lead))
+    bt = 0 if bias is None else _code(bias.dtype)
+    head = (m, n, k, _abi.RDN_BF16, 0, bt, _act(act), x_ld, w_ld, 0, 0, px, pw, 0, 0, 0, 0, 0,
+            0 if act is None else _whole("pre", pre, (*lead, n), bf, dev), _code(wt), dy_ld, pdy,
+            _whole("dx", res.get("dx"), x.shape, bf, dev), _whole("dw", res.get("dw"), w.shape, wt, dev),
+            0 if bias is None else _whole("dbias", res["dbias"], (n,), bias.dtype, dev))
+    ws = _workspace(workspace, _size("rdn_linear_bwd_workspace_size", _abi.LINEAR_PACK(*head, 0, 0)), dev)
+    _call("rdn_linear_bwd", _abi.LINEAR_PACK(*head, ws.data_ptr(), ws.numel() * ws.element_size()), dev)
     return res
