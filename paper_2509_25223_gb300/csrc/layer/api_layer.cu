@@ -290,7 +290,11 @@ rdn_status_t gscan_shapes(const char *fn, rdn_gscan_args *a) {
   TRY(check_ld(fn, "dy_ld", &a->dy_ld, a->D));
   TRY(check_ld(fn, "dx_ld", &a->dx_ld, a->D));
   TRY(check_ld(fn, "dr_ld", &a->dr_ld, a->D));
-  return check_ld(fn, "di_ld", &a->di_ld, a->D);
+  TRY(check_ld(fn, "di_ld", &a->di_ld, a->D));
+  const long long lds[7] = {a->x_ld, a->r_ld, a->i_ld, a->y_ld, a->dy_ld, a->dx_ld, a->dr_ld};
+  bool far = a->di_ld >= (1 << 24);
+  for (long long ld : lds) far = far || ld >= (1 << 24);
+  return far ? entry_fail(RDN_ERR_UNSUPPORTED, "%s: rows 2^24 elements and more apart", fn) : RDN_OK;
 }
 
 rdn_status_t gscan_common(const char *fn, const rdn_gscan_args *args, bool bwd, cudaStream_t s) {

@@ -3,12 +3,13 @@
 //     h_t = a_t h_{t-1} + m_t s_t x_t,   a = exp(la), la = -c softplus(lam) sigmoid(r),
 //     m = sqrt(1 - a^2), s = sigmoid(i).
 // A span of tokens maps the state before it to the state after it as h -> A h + H, and
-// two spans compose to (A2 A1, A2 H1 + H2).  So a token row is cut three times: a warp
-// takes kTok consecutive tokens of 32 V channels (its lanes), a CTA the kTile tokens of
-// its warps, and a cluster of up to 8 CTAs as many tiles, one round after another.  Each
-// warp works out its span from a zero state with everything in registers; the spans'
-// (A, H) go through shared memory, the tiles' to every CTA of the cluster, and the states
-// follow as h_t = A_t h_in + H_t.  The data are read once and the results written once.
+// two spans compose to (A2 A1, A2 H1 + H2).  So a token row is cut: half a warp takes kTok
+// consecutive tokens of 16 V channels (its lanes), a CTA the kTile tokens of its warps, and,
+// where there are too few rows and channels to fill the GPU, a cluster of up to 8 CTAs as many
+// tiles, one round after another.  Each half warp works out its span from a zero state; the
+// spans' (A, H) go through shared memory, the tiles' to every CTA of the cluster, and the
+// states follow as h_t = A_t h_in + H_t.  The data are read once, a round ahead, and the results
+// written once.
 // The backward is the same over the reversed tokens, with
 //     g_t = dy_t + q_{t+1},  q_t = a_t g_t       (q: the gradient of the state before t)
 // and the states again from those that the forward kept before every tile:
@@ -16,6 +17,7 @@
 //     dr = (1 - sigmoid(r)) w,  dlam = sigmoid(lam) / softplus(lam) sum_t w_t
 // (la / m stays finite where la -> 0: m ~ sqrt(-2 la)).
 #include "rows.cuh"
+#include "status.cuh"
 #include "tc_common.cuh"
 
 namespace rdn {
@@ -47,8 +49,10 @@ struct Pack<__nv_bfloat16, 2> {
 
 namespace gscan {
 
-constexpr int kTok = 8, kWarps = 8, kTile = kTok * kWarps, kThreads = 32 * kWarps;
+constexpr int kTok = 8, kWarps = 8, kTile = 2 * kTok * kWarps, kThreads = 32 * kWarps;
+constexpr int kLanes = 16;   // lanes of a span
 constexpr int kCluster = 8;  // the most CTAs of a cluster
+constexpr int kFwdCtas = 3, kBwdCtas = 2;  // resident on an SM (80 and 128 registers a thread, nothing spilled)
 static_assert(kTile == RDN_GSCAN_CHUNK, "a tile starts at every kept state");
 
 struct GP {
@@ -61,65 +65,162 @@ struct GP {
   float *hT, *chunks, *dh0, *part;
   const int *cu, *slots;
   float *h;
+  int *status;
 };
 
 __device__ __forceinline__ float softplusf(float v) { return v > 20.f ? v : log1pf(expf(v)); }
 
-// The gates of one element.  k = -c softplus(lam).
-struct Gate {
-  float sr, si, nr, ni;  // sigmoid(r), sigmoid(i), 1 - sigmoid(r), 1 - sigmoid(i)
-  float la, a, m;
-};
-// Both sigmoids share one reciprocal (the special function unit is the narrowest part of the
-// forward): 1 / (1 + e^-r) = (1 + e^-i) / ((1 + e^-r)(1 + e^-i)).  The arguments are cut at -40
-// so that the product stays finite (a NaN passes).  u = 1 - a by the series of expm1 where a is
-// near 1, so that 1 - a^2 = u (2 - u) keeps its digits.
-__device__ __forceinline__ Gate gate(float r, float i, float k) {
-  Gate g;
-  r = r < -40.f ? -40.f : r;
-  i = i < -40.f ? -40.f : i;
-  const float er = ex2(-kLog2e * r), ei = ex2(-kLog2e * i);
-  const float pr = 1.f + er, pi = 1.f + ei, R = rcp_approx(pr * pi);
-  g.sr = R * pi;
-  g.si = R * pr;
-  g.nr = er * g.sr;
-  g.ni = ei * g.si;
-  float z = k * g.sr;
-  z = z < -88.f ? -88.f : z;
-  g.la = z;
-  // -expm1(z) = -z (1 + z/2 (1 + z/3 (...))): the term left out is below 0.6^8 / 9! = 5e-8 of the sum
-  float u = 1.f / 40320.f;
-  u = fmaf(u, z, 1.f / 5040.f);
-  u = fmaf(u, z, 1.f / 720.f);
-  u = fmaf(u, z, 1.f / 120.f);
-  u = fmaf(u, z, 1.f / 24.f);
-  u = fmaf(u, z, 1.f / 6.f);
-  u = fmaf(u, z, 0.5f);
-  u = fmaf(u, z, 1.f);
-  u = -z * u;
-  g.a = 1.f - u;
-  if (z < -0.6f) {
-    g.a = ex2(kLog2e * z);
-    u = 1.f - g.a;
-  }
-  g.m = __fsqrt_rn(u * (2.f - u));
-  return g;
+// The arithmetic is on pairs of channels (rows.cuh): one issue slot for two of them.  A lane with
+// one channel (V = 1) has a second one of zeros.
+__device__ __forceinline__ f2 both(float v) { return pack2(v, v); }
+template <typename T, int V>
+__device__ __forceinline__ f2 get2(const typename Pack<T, V>::Raw &raw) {
+  float v[V];
+  Pack<T, V>::get(raw, v);
+  return pack2(v[0], V == 2 ? v[V - 1] : 0.f);
+}
+template <typename T, int V>
+__device__ __forceinline__ void put2(T *p, f2 v) {
+  float lo, hi;
+  unpack2(v, lo, hi);
+  float o[V];
+  o[0] = lo;
+  if (V == 2) o[V - 1] = hi;
+  Pack<T, V>::st(p, Pack<T, V>::put(o));
+}
+template <int V>
+__device__ __forceinline__ f2 ldf(const float *p) { return pack2(p[0], V == 2 ? p[V - 1] : 0.f); }
+template <int V>
+__device__ __forceinline__ void stf(float *p, f2 v) {
+  float lo, hi;
+  unpack2(v, lo, hi);
+  p[0] = lo;
+  if (V == 2) p[V - 1] = hi;
+}
+// The larger of two numbers, or the NaN among them.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.ftz.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// fn of each of a pair.  (Packed instructions take no constants: where one operand is a constant, two
+// plain instructions with it inside cost fewer issue slots than the pair's constants in registers.)
+template <typename Fn>
+__device__ __forceinline__ f2 each(f2 x, Fn fn) {
+  float lo, hi;
+  unpack2(x, lo, hi);
+  return pack2(fn(lo), fn(hi));
+}
+__device__ __forceinline__ f2 sqrt2(f2 x) {
+  return each(x, [](float v) {
+    asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(v));
+    return v;
+  });
+}
+// x^-1/2, a large number for x = 0
+__device__ __forceinline__ f2 rsqrt2(f2 x) {
+  return each(x, [](float v) { return rsqrtf(max_nan(v, 2e-38f)); });
+}
+__device__ __forceinline__ f2 one_minus(f2 x) {
+  return each(x, [](float v) { return 1.f - v; });
+}
+__device__ __forceinline__ f2 sub2(f2 a, f2 b) {
+  float x, y, z, w;
+  unpack2(a, x, y);
+  unpack2(b, z, w);
+  return pack2(x - z, y - w);
 }
 
-// What the two passes over a row share: this thread's place.
-template <typename T, int V>
+// The gates of a pair: s = sigmoid of r and of i, u = 1 - a, t = log2(a).
+//   k = -c softplus(lam) log2(e);  log2 of a decay below 2^-125 is taken as -125.
+// u keeps its digits where a is near 1, so that 1 - a^2 = u (2 - u) does: with t = n + f, n the
+// nearest integer (both exact), 1 - 2^t = (1 - 2^n) - 2^n (2^f - 1), and 2^f - 1 = f P(f) with the
+// polynomial P of degree 5 that has the least largest relative error on |f| <= 1/2, fitted by
+// reweighted least squares: 1.1e-8, u within 1.2e-7.
+struct Gate {
+  f2 sr, si, u;
+};
+__device__ __forceinline__ float sigmoid_of(float x) { return rcp_approx(1.f + ex2(-kLog2e * x)); }
+__device__ __forceinline__ f2 log2_decay(f2 k, f2 sr) {
+  return each(mul2(k, sr), [](float v) { return max_nan(v, -125.f); });
+}
+__device__ __forceinline__ float decayed(float t) {  // 1 - 2^t, -125 <= t <= 0
+  constexpr float kRound = 12582912.f;               // 1.5 * 2^23
+  const float nr = t + kRound, f = t - (nr - kRound);
+  float q = fmaf(1.5403510769829154e-4f, f, 1.3390735257416964e-3f);
+  q = fmaf(q, f, 9.618237614631653e-3f);
+  q = fmaf(q, f, 5.550357326865196e-2f);
+  q = fmaf(q, f, 0.24022649228572845f);
+  q = fmaf(q, f, 0.6931471824645996f);
+  const float s = __uint_as_float((__float_as_uint(nr) << 23) + 0x3f800000u);  // 2^n
+  return fmaf(-s, q * f, 1.f - s);
+}
+__device__ __forceinline__ Gate gate(f2 r, f2 i, f2 k) {
+  Gate g;
+  g.sr = each(r, sigmoid_of);
+  g.si = each(i, sigmoid_of);
+  g.u = each(log2_decay(k, g.sr), decayed);
+  return g;
+}
+// 1 - a^2
+__device__ __forceinline__ f2 rest(f2 u) {
+  return mul2(u, each(u, [](float v) { return 2.f - v; }));
+}
+
+constexpr float kLn2 = 0.69314718f;
+template <int V>
+__device__ __forceinline__ f2 rate(const GP &p, int ch) {  // -c softplus(lam) log2(e)
+  return mul2(pack2(softplusf(p.lam[ch]), V == 2 ? softplusf(p.lam[ch + V - 1]) : 0.f), both(-p.c * kLog2e));
+}
+
+// The map h -> A h + H of a span of tokens, for a pair of channels.  A = -1 stands for a span in
+// which a packed sequence starts: what comes before it does not enter, not even as 0 times an
+// infinity or NaN.
+struct alignas(16) Span {
+  f2 A, H;
+};
+__device__ __forceinline__ bool cuts(f2 A) {
+  float lo, hi;
+  unpack2(A, lo, hi);
+  return lo < 0.f;
+}
+template <bool kPacked>
+__device__ __forceinline__ f2 over(const Span &s, f2 h) {
+  const f2 r = fma2(s.A, h, s.H);
+  return kPacked && cuts(s.A) ? s.H : r;
+}
+// s1, then s2
+template <bool kPacked>
+__device__ __forceinline__ Span then(const Span &s1, const Span &s2) {
+  const f2 A = mul2(s1.A, s2.A);
+  return {kPacked && (cuts(s1.A) || cuts(s2.A)) ? both(-1.f) : A, over<kPacked>(s2, s1.H)};
+}
+// s, then the token h -> a h + b
+template <bool kPacked>
+__device__ __forceinline__ void step(Span &s, f2 a, f2 b) {
+  const f2 A = mul2(s.A, a);
+  s.A = kPacked && cuts(s.A) ? s.A : A;
+  s.H = fma2(a, s.H, b);
+}
+
+// This thread's place.
+template <int V>
 struct Place {
-  int lane, warp, rank, b, ch;
-  bool live;  // whether the lane's channels exist
+  int lane, half, warp, rank, b, strip, ch;
+  bool live;  // whether the lane's channels exist (if not, it reads the strip's first ones)
   __device__ explicit Place(const GP &p) {
-    lane = threadIdx.x & 31;
+    lane = threadIdx.x & (kLanes - 1);
+    half = (threadIdx.x >> 4) & 1;
     warp = threadIdx.x >> 5;
     rank = blockIdx.x % p.nc;
     const int unit = blockIdx.x / p.nc;
     b = unit / p.strips;
-    ch = ((unit % p.strips) * 32 + lane) * V;
-    live = ch < p.D;
+    strip = (unit % p.strips) * kLanes * V;
+    live = strip + lane * V < p.D;
+    ch = live ? strip + lane * V : strip;
   }
+  // token of the tile that this thread's span starts at
+  __device__ int token() const { return (2 * warp + half) * kTok; }
 };
 
 // Sequence that starts / ends at each token of the tile (-1: none).
@@ -136,349 +237,372 @@ __device__ __forceinline__ void mark_tile(const GP &p, int t0, int2 *mark) {
   }
 }
 
-__device__ __forceinline__ void st_cluster(uint32_t addr, float2 v) {
-  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory");
+// Addresses of a row operand: row (of the B T token rows), 32-bit (a row is below 2^24 elements).
+// One instruction an address (a wide multiply-add) where 64-bit sums of offsets would be three.
+__device__ __forceinline__ const char *row_at(const char *p, uint32_t row, uint32_t ld) {
+  const char *q;
+  asm("mad.wide.u32 %0, %1, %2, %3;" : "=l"(q) : "r"(row), "r"(ld), "l"(p));
+  __builtin_assume(__isGlobal(q));
+  return q;
+}
+template <typename T>
+struct Rows {
+  const char *p;  // the lane's channels of token row `row`
+  uint32_t ld;    // bytes
+  __device__ Rows(const void *base, long long ld_, uint32_t row, int ch)
+      : ld((uint32_t)ld_ * (uint32_t)sizeof(T)) {
+    p = row_at(static_cast<const char *>(base) + ch * (int)sizeof(T), row, ld);
+  }
+  __device__ T *operator[](uint32_t j) const { return reinterpret_cast<T *>(const_cast<char *>(row_at(p, j, ld))); }
+};
+// (left: tokens of the row of the batch from the first one on)
+template <typename T, int V>
+__device__ __forceinline__ void load_rows(typename Pack<T, V>::Raw (&v)[kTok], const void *base, long long ld, uint32_t row,
+                                          int ch, bool full, int left) {
+  const Rows<T> rows(base, ld, row, ch);
+  if (full) {
+#pragma unroll
+    for (int j = 0; j < kTok; ++j) v[j] = Pack<T, V>::ld(rows[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kTok; ++j) v[j] = j < left ? Pack<T, V>::ld(rows[j]) : Pack<T, V>::zero();
+  }
 }
 
-// (A, H) of two spans in turn.  A = -1 stands for a span in which a packed sequence starts:
-// what comes before it does not enter, not even as 0 times an infinity or NaN.
-template <bool kPacked>
-__device__ __forceinline__ float over(float2 s, float h) {
-  const float r = fmaf(s.x, h, s.y);
-  return kPacked && s.x < 0.f ? s.y : r;
+__device__ __forceinline__ Span from_other_half(const Span &s) {
+  return {__shfl_xor_sync(0xffffffffu, s.A, kLanes), __shfl_xor_sync(0xffffffffu, s.H, kLanes)};
 }
-template <bool kPacked>
-__device__ __forceinline__ float2 then(float2 s1, float2 s2) {
-  const float A = kPacked && (s1.x < 0.f || s2.x < 0.f) ? -1.f : s1.x * s2.x;
-  return make_float2(A, over<kPacked>(s2, s1.y));
+
+// Leaves the warp's span, of its halves' (kBack: the upper one first).
+template <bool kBack, bool kPacked>
+__device__ __forceinline__ void leave(Span (*spans)[kLanes], int warp, int lane, int half, const Span &own,
+                                      const Span &other) {
+  if (half == (kBack ? 1 : 0)) spans[warp][lane] = then<kPacked>(own, other);
 }
 
 // Sends the composition of the CTA's warps' spans (in the order 0.. or, kBack, 7..) to the
-// slot of this CTA in every CTA of the cluster, and waits until all have.
-template <int V, bool kBack, bool kPacked>
-__device__ __forceinline__ void exchange(const float2 (*spans)[32 * V], float2 (*tiles)[32 * V], int rank, int nc) {
-  if (nc > 1) {
-    const int c = threadIdx.x % (32 * V);
-    float2 all = spans[kBack ? kWarps - 1 : 0][c];
+// slot of this CTA in every CTA of the cluster, and waits until all have come.  The stores
+// themselves tell the receiver's barrier: a barrier of the cluster would hold this thread
+// until its global stores of the round before are done.  (A slot is written again two rounds
+// later, by a CTA that has had this CTA's spans of the round between, sent when all its warps
+// had read the slot.)
+template <bool kBack, bool kPacked>
+__device__ __forceinline__ void exchange(const GP &p, const Span (*spans)[kLanes], Span (*tiles)[kLanes], uint64_t *bar,
+                                         uint32_t phase, int rank) {
+  if (p.nc == 1) return;
+  const int lane = threadIdx.x & (kLanes - 1), to = threadIdx.x >> 4;
+  static_assert(2 * kWarps >= kCluster, "half a warp for each CTA of the cluster");
+  if (threadIdx.x == 0) tc::mbar_expect_tx(bar, (uint32_t)(p.nc * kLanes * sizeof(Span)));
+  if (to < p.nc) {
+    Span all = spans[kBack ? kWarps - 1 : 0][lane];
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) all = then<kPacked>(all, spans[kBack ? kWarps - 1 - w : w][c]);
-    for (int q = threadIdx.x / (32 * V); q < nc; q += kThreads / (32 * V))
-      st_cluster(tc::map_rank(&tiles[rank][c], q), all);
-    tc::cluster_sync();
+    for (int w = 1; w < kWarps; ++w) all = then<kPacked>(all, spans[kBack ? kWarps - 1 - w : w][lane]);
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(
+                     tc::map_rank(&tiles[rank][lane], to)),
+                 "l"(all.A), "l"(all.H), "r"(tc::map_rank(bar, to))
+                 : "memory");
   }
+  __syncwarp();
+  if (!tc::mbar_wait_cluster(bar, phase, 2000000000ll) && p.status) atomicExch(p.status, (int)RDN_ERR_TIMEOUT);
+}
+// Before the first exchange: the barriers are there, and every CTA of the cluster runs.
+__device__ __forceinline__ void exchange_init(const GP &p, uint64_t *bars) {
+  if (p.nc == 1) return;
+  if (threadIdx.x == 0) {
+    tc::mbar_init(&bars[0], 1);
+    tc::mbar_init(&bars[1], 1);
+    tc::fence_mbar_init();
+  }
+  __syncthreads();
+  tc::cluster_sync();
 }
 
-// The state that comes into this warp's span, and the one that leaves the cluster's round.
-template <int V, bool kBack, bool kPacked>
-__device__ __forceinline__ void fold(const float2 (*spans)[32 * V], const float2 (*tiles)[32 * V], int c, int rank,
-                                     int nc, int warp, float &carry, float &in) {
-  float h = carry;
-  in = h;
+// The state that comes into this warp's span; carry: into and out of the cluster's round.
+template <bool kBack, bool kPacked>
+__device__ __forceinline__ f2 fold(const Span (*spans)[kLanes], const Span (*tiles)[kLanes], int lane, int rank, int nc,
+                                   int warp, f2 &carry) {
+  f2 run = carry;
   if (nc > 1) {
+    f2 h = carry;
+#pragma unroll 1
     for (int q = 0; q < nc; ++q) {
       const int k = kBack ? nc - 1 - q : q;
-      if (k == rank) in = h;
-      h = over<kPacked>(tiles[k][c], h);
+      if (k == rank) run = h;
+      h = over<kPacked>(tiles[k][lane], h);
     }
+    carry = h;
   }
-  float run = in;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    const int k = kBack ? kWarps - 1 - w : w;
-    if (k == warp) in = run;
-    run = over<kPacked>(spans[k][c], run);
+  const int before = kBack ? kWarps - 1 - warp : warp;  // warps whose spans come first
+  int w = 0;
+#pragma unroll 1
+  for (; w < before; ++w) run = over<kPacked>(spans[kBack ? kWarps - 1 - w : w][lane], run);
+  const f2 in = run;
+  if (nc == 1) {
+#pragma unroll 1
+    for (; w < kWarps; ++w) run = over<kPacked>(spans[kBack ? kWarps - 1 - w : w][lane], run);
+    carry = run;
   }
-  carry = nc > 1 ? h : run;
+  return in;
 }
 
-template <typename T, int V, bool kPacked>
-__global__ void __launch_bounds__(kThreads) fwd_kernel(const GP p) {
-  using P = Pack<T, V>;
-  __shared__ float2 spans[2][kWarps][32 * V], tiles[2][kCluster][32 * V];
-  __shared__ int2 mark[2][kTile];
-  const Place<T, V> at(p);
-  const T *x = static_cast<const T *>(p.x), *r = static_cast<const T *>(p.r), *gi = static_cast<const T *>(p.i);
-  T *y = static_cast<T *>(p.y);
-  const long long row0 = (long long)at.b * p.T;
-  const int ntiles = (p.T + kTile - 1) / kTile;
-
-  float k[V], carry[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    k[v] = at.live ? -p.c * softplusf(p.lam[at.ch + v]) : 0.f;
-    carry[v] = !kPacked && at.live && p.h0 ? p.h0[(size_t)at.b * p.D + at.ch + v] : 0.f;
-  }
-  if (p.hT && at.live) {  // sequences without tokens
-    if (!kPacked) {
-      if (p.T == 0 && at.rank == 0 && at.warp == 0)
-#pragma unroll
-        for (int v = 0; v < V; ++v) p.hT[(size_t)at.b * p.D + at.ch + v] = carry[v];
-    } else {
-      for (int s = at.rank * kWarps + at.warp; s < p.num_seqs; s += p.nc * kWarps)
-        if (cu_at(p.cu, p.num_seqs, p.T, s + 1) <= cu_at(p.cu, p.num_seqs, p.T, s))
-#pragma unroll
-          for (int v = 0; v < V; ++v) {
-            const size_t o = (size_t)s * p.D + at.ch + v;
-            p.hT[o] = p.h0 ? p.h0[o] : 0.f;
-          }
-    }
-  }
-
-  if (p.nc > 1) tc::cluster_sync();  // every CTA runs before another writes its shared memory
-  int par = 0;
-  for (int base = 0; base < p.T; base += p.nc * kTile, par ^= 1) {
-    const int tile0 = base + at.rank * kTile, t0 = tile0 + at.warp * kTok;
-    typename P::Raw xr[kTok], rr[kTok], ir[kTok];
-#pragma unroll
-    for (int j = 0; j < kTok; ++j) {
-      const bool ok = at.live && t0 + j < p.T;
-      const long long row = row0 + t0 + j;
-      xr[j] = ok ? P::ld(x + row * p.x_ld + at.ch) : P::zero();
-      rr[j] = ok ? P::ld(r + row * p.r_ld + at.ch) : P::zero();
-      ir[j] = ok ? P::ld(gi + row * p.i_ld + at.ch) : P::zero();
-    }
-    if (kPacked) {
-      mark_tile(p, tile0, mark[par]);
-      __syncthreads();
-    }
-    float A[kTok][V], H[kTok][V], Ac[V], Hc[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) { Ac[v] = 1.f; Hc[v] = 0.f; }
-#pragma unroll
-    for (int j = 0; j < kTok; ++j) {
-      float xv[V], rv[V], iv[V];
-      P::get(xr[j], xv);
-      P::get(rr[j], rv);
-      P::get(ir[j], iv);
-      const int start = kPacked ? mark[par][at.warp * kTok + j].x : -1;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (t0 + j < p.T) {
-          const Gate g = gate(rv[v], iv[v], k[v]);
-          float a = g.a, b = g.m * g.si * xv[v];
-          if (kPacked && start >= 0) {
-            if (p.h0 && at.live) b = fmaf(a, p.h0[(size_t)start * p.D + at.ch + v], b);
-            Ac[v] = -1.f;
-            Hc[v] = b;
-          } else {
-            if (!kPacked || Ac[v] >= 0.f) Ac[v] *= a;
-            Hc[v] = fmaf(a, Hc[v], b);
-          }
-        }
-        A[j][v] = Ac[v];
-        H[j][v] = Hc[v];
+// States of sequences without tokens: out = in, or 0.
+template <int V, bool kPacked>
+__device__ __forceinline__ void pass_through(const GP &p, const Place<V> &at, const float *in, float *out) {
+  if (!out || !at.live || at.half) return;
+  if (!kPacked) {
+    const size_t o = (size_t)at.b * p.D + at.ch;
+    if (p.T == 0 && at.rank == 0 && at.warp == 0) stf<V>(out + o, in ? ldf<V>(in + o) : both(0.f));
+  } else {
+    for (int s = at.rank * kWarps + at.warp; s < p.num_seqs; s += p.nc * kWarps)
+      if (cu_at(p.cu, p.num_seqs, p.T, s + 1) <= cu_at(p.cu, p.num_seqs, p.T, s)) {
+        const size_t o = (size_t)s * p.D + at.ch;
+        stf<V>(out + o, in ? ldf<V>(in + o) : both(0.f));
       }
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) spans[par][at.warp][at.lane * V + v] = make_float2(Ac[v], Hc[v]);
-    __syncthreads();
-    exchange<V, false, kPacked>(spans[par], tiles[par], at.rank, p.nc);
-    float in[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-      fold<V, false, kPacked>(spans[par], tiles[par], at.lane * V + v, at.rank, p.nc, at.warp, carry[v], in[v]);
-    if (at.live) {
-      if (p.chunks && at.warp == 0 && tile0 < p.T)
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-          p.chunks[((size_t)at.b * ntiles + tile0 / kTile) * p.D + at.ch + v] = in[v];
-#pragma unroll
-      for (int j = 0; j < kTok; ++j) {
-        if (t0 + j >= p.T) break;
-        float h[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = over<kPacked>(make_float2(A[j][v], H[j][v]), in[v]);
-        if (y) P::st(y + (row0 + t0 + j) * p.y_ld + at.ch, P::put(h));
-        const int end = kPacked ? mark[par][at.warp * kTok + j].y : t0 + j == p.T - 1 ? at.b : -1;
-        if (p.hT && end >= 0)
-#pragma unroll
-          for (int v = 0; v < V; ++v) p.hT[(size_t)end * p.D + at.ch + v] = h[v];
-      }
-    }
-    __syncwarp();
   }
 }
 
 template <typename T, int V, bool kPacked>
-__global__ void __launch_bounds__(kThreads, 2) bwd_kernel(const GP p) {
-  using P = Pack<T, V>;
-  __shared__ float2 fspans[2][kWarps][32 * V], spans[2][kWarps][32 * V], tiles[2][kCluster][32 * V];
-  __shared__ int2 mark[2][kTile];
-  const Place<T, V> at(p);
-  const T *x = static_cast<const T *>(p.x), *r = static_cast<const T *>(p.r), *gi = static_cast<const T *>(p.i);
-  const T *dy = static_cast<const T *>(p.dy);
-  T *dx = static_cast<T *>(p.dx), *dr = static_cast<T *>(p.dr), *di = static_cast<T *>(p.di);
-  const long long row0 = (long long)at.b * p.T;
-  const int ntiles = (p.T + kTile - 1) / kTile;
+__global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
+  using Raw = typename Pack<T, V>::Raw;
+  __shared__ Span kept[kTok][kThreads];  // the span up to each token of a thread
+  __shared__ Span spans[2][kWarps][kLanes], tiles[2][kCluster][kLanes];
+  __shared__ int2 mark[2][kPacked ? kTile : 1];
+  __shared__ uint64_t bars[2];
+  const Place<V> at(p);
+  const int me = threadIdx.x;
+  const uint32_t row0 = (uint32_t)at.b * (uint32_t)p.T + (uint32_t)at.token();  // (B T is at most 2^30)
+  const int ntiles = (p.T + kTile - 1) / kTile, round = p.nc * kTile;
+  const f2 k = rate<V>(p, at.ch);
+  f2 carry = !kPacked && p.h0 ? ldf<V>(p.h0 + (size_t)at.b * p.D + at.ch) : both(0.f);
+  pass_through<V, kPacked>(p, at, p.h0, p.hT);
 
-  float k[V], carry[V], sum[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    k[v] = at.live ? -p.c * softplusf(p.lam[at.ch + v]) : 0.f;
-    carry[v] = !kPacked && at.live && p.dhT ? p.dhT[(size_t)at.b * p.D + at.ch + v] : 0.f;
-    sum[v] = 0.f;
-  }
-  if (p.dh0 && at.live) {  // sequences without tokens
-    if (!kPacked) {
-      if (p.T == 0 && at.rank == 0 && at.warp == 0)
-#pragma unroll
-        for (int v = 0; v < V; ++v) p.dh0[(size_t)at.b * p.D + at.ch + v] = carry[v];
-    } else {
-      for (int s = at.rank * kWarps + at.warp; s < p.num_seqs; s += p.nc * kWarps)
-        if (cu_at(p.cu, p.num_seqs, p.T, s + 1) <= cu_at(p.cu, p.num_seqs, p.T, s))
-#pragma unroll
-          for (int v = 0; v < V; ++v) {
-            const size_t o = (size_t)s * p.D + at.ch + v;
-            p.dh0[o] = p.dhT ? p.dhT[o] : 0.f;
-          }
-    }
-  }
-
-  if (p.nc > 1) tc::cluster_sync();  // every CTA runs before another writes its shared memory
-  int par = 0;
-  const int round = p.nc * kTile;
-  for (int base = (p.T - 1) / round * round; base >= 0 && p.T > 0; base -= round, par ^= 1) {
-    const int tile0 = base + at.rank * kTile, t0 = tile0 + at.warp * kTok;
-    typename P::Raw xr[kTok], rr[kTok], ir[kTok], gr[kTok];
-#pragma unroll
-    for (int j = 0; j < kTok; ++j) {
-      const bool ok = at.live && t0 + j < p.T;
-      const long long row = row0 + t0 + j;
-      xr[j] = ok ? P::ld(x + row * p.x_ld + at.ch) : P::zero();
-      rr[j] = ok ? P::ld(r + row * p.r_ld + at.ch) : P::zero();
-      ir[j] = ok ? P::ld(gi + row * p.i_ld + at.ch) : P::zero();
-      gr[j] = ok ? P::ld(dy + row * p.dy_ld + at.ch) : P::zero();
-    }
-    float h[V];  // the state before the tile
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-      h[v] = at.live && tile0 < p.T ? p.chunks[((size_t)at.b * ntiles + tile0 / kTile) * p.D + at.ch + v] : 0.f;
+  exchange_init(p, bars);
+  int par = 0, tile0 = at.rank * kTile;
+  uint32_t phase = 0;
+  Raw xr[kTok], rr[kTok], ir[kTok];
+  auto fetch = [&](int t) {
+    const bool full = t + kTile <= p.T;
+    const int left = p.T - t - at.token();
+    load_rows<T, V>(rr, p.r, p.r_ld, row0 + t, at.ch, full, left);
+    load_rows<T, V>(ir, p.i, p.i_ld, row0 + t, at.ch, full, left);
+    load_rows<T, V>(xr, p.x, p.x_ld, row0 + t, at.ch, full, left);
+  };
+  fetch(tile0);
+  for (int base = 0; base < p.T; base += round, tile0 += round, phase ^= par, par ^= 1) {
+    const int left = p.T - tile0 - at.token();
     if (kPacked) {
       mark_tile(p, tile0, mark[par]);
       __syncthreads();
     }
-    // this warp's span from a zero state, both ways
-    float a[kTok][V], Af[V], Hf[V], Ab[V], Hb[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) { Af[v] = 1.f; Hf[v] = 0.f; Ab[v] = 1.f; Hb[v] = 0.f; }
-#pragma unroll
-    for (int j = 0; j < kTok; ++j) {
-      float xv[V], rv[V], iv[V];
-      P::get(xr[j], xv);
-      P::get(rr[j], rv);
-      P::get(ir[j], iv);
-      const int start = kPacked ? mark[par][at.warp * kTok + j].x : -1;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        a[j][v] = 1.f;
-        if (t0 + j < p.T) {
-          const Gate g = gate(rv[v], iv[v], k[v]);
-          a[j][v] = g.a;
-          float b = g.m * g.si * xv[v];
-          if (kPacked && start >= 0) {
-            if (p.h0 && at.live) b = fmaf(g.a, p.h0[(size_t)start * p.D + at.ch + v], b);
-            Af[v] = -1.f;
-            Hf[v] = b;
-          } else {
-            if (!kPacked || Af[v] >= 0.f) Af[v] *= g.a;
-            Hf[v] = fmaf(g.a, Hf[v], b);
-          }
-        }
+    Span all = {both(1.f), both(0.f)};
+    auto token = [&](int j) {
+      const Gate g = gate(get2<T, V>(rr[j]), get2<T, V>(ir[j]), k);
+      const f2 a = one_minus(g.u);
+      f2 b = mul2(mul2(sqrt2(rest(g.u)), g.si), get2<T, V>(xr[j]));
+      const int start = kPacked ? mark[par][at.token() + j].x : -1;
+      if (kPacked && start >= 0) {
+        if (p.h0) b = fma2(a, ldf<V>(p.h0 + (size_t)start * p.D + at.ch), b);
+        all = {both(-1.f), b};
+      } else {
+        step<kPacked>(all, a, b);
       }
-    }
+      kept[j][me] = all;
+    };
+    if (tile0 + kTile <= p.T) {
 #pragma unroll
-    for (int j = kTok - 1; j >= 0; --j) {
-      float gv[V];
-      P::get(gr[j], gv);
-      const int end = kPacked ? mark[par][at.warp * kTok + j].y : -1;
+      for (int j = 0; j < kTok; ++j) token(j);
+    } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (kPacked && end >= 0) {
-          Ab[v] = -1.f;
-          Hb[v] = p.dhT && at.live ? p.dhT[(size_t)end * p.D + at.ch + v] : 0.f;
-        }
-        if (!kPacked || Ab[v] >= 0.f) Ab[v] *= a[j][v];
-        Hb[v] = a[j][v] * (gv[v] + Hb[v]);
-      }
+      for (int j = 0; j < kTok; ++j)
+        if (j < left) token(j);
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      fspans[par][at.warp][at.lane * V + v] = make_float2(Af[v], Hf[v]);
-      spans[par][at.warp][at.lane * V + v] = make_float2(Ab[v], Hb[v]);
-    }
+    // the next round's rows are on their way while the spans are joined
+    if (base + round < p.T) fetch(tile0 + round);
+    const Span other = from_other_half(all);
+    leave<false, kPacked>(spans[par], at.warp, at.lane, at.half, all, other);
     __syncthreads();
-    exchange<V, true, kPacked>(spans[par], tiles[par], at.rank, p.nc);
-    float q[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = at.lane * V + v;
-      fold<V, true, kPacked>(spans[par], tiles[par], c, at.rank, p.nc, at.warp, carry[v], q[v]);
-      for (int w = 0; w < at.warp; ++w) h[v] = over<kPacked>(fspans[par][w][c], h[v]);
-    }
+    exchange<false, kPacked>(p, spans[par], tiles[par], &bars[par], phase, at.rank);
+    f2 in = fold<false, kPacked>(spans[par], tiles[par], at.lane, at.rank, p.nc, at.warp, carry);
+    if (p.chunks && at.live && at.warp == 0 && at.half == 0 && tile0 < p.T)
+      stf<V>(p.chunks + ((size_t)at.b * ntiles + tile0 / kTile) * p.D + at.ch, in);
+    if (at.half) in = over<kPacked>(other, in);
     if (at.live) {
-      float before[kTok][V];  // the state before each token
+      if (p.y) {
+        const Rows<T> y(p.y, p.y_ld, row0 + tile0, at.ch);
+        if (tile0 + kTile <= p.T) {
 #pragma unroll
-      for (int j = 0; j < kTok; ++j) {
-        float xv[V], rv[V], iv[V];
-        P::get(xr[j], xv);
-        P::get(rr[j], rv);
-        P::get(ir[j], iv);
-        const int start = kPacked ? mark[par][at.warp * kTok + j].x : -1;
+          for (int j = 0; j < kTok; ++j) put2<T, V>(y[j], over<kPacked>(kept[j][me], in));
+        } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          if (kPacked && start >= 0) h[v] = p.h0 ? p.h0[(size_t)start * p.D + at.ch + v] : 0.f;
-          before[j][v] = h[v];
-          const Gate g = gate(rv[v], iv[v], k[v]);
-          h[v] = fmaf(g.a, h[v], g.m * g.si * xv[v]);
+          for (int j = 0; j < kTok; ++j)
+            if (j < left) put2<T, V>(y[j], over<kPacked>(kept[j][me], in));
         }
       }
-#pragma unroll
-      for (int j = kTok - 1; j >= 0; --j) {
-        if (t0 + j >= p.T) continue;
-        float xv[V], rv[V], iv[V], gv[V], ox[V], orr[V], oi[V];
-        P::get(xr[j], xv);
-        P::get(rr[j], rv);
-        P::get(ir[j], iv);
-        P::get(gr[j], gv);
-        const int2 f = kPacked ? mark[par][at.warp * kTok + j] : make_int2(t0 + j == 0 ? at.b : -1, -1);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          if (kPacked && f.y >= 0) q[v] = p.dhT ? p.dhT[(size_t)f.y * p.D + at.ch + v] : 0.f;
-          const float g = gv[v] + q[v];
-          const Gate e = gate(rv[v], iv[v], k[v]);
-          const float gs = g * e.si, gm = gs * e.m;
-          ox[v] = gm;
-          oi[v] = gm * xv[v] * e.ni;
-          const float lam = e.m > 0.f ? __fdividef(e.la, e.m) : 0.f;
-          const float w = e.a * (g * before[j][v] * e.la - e.a * (gs * xv[v]) * lam);
-          orr[v] = e.nr * w;
-          sum[v] += w;
-          q[v] = e.a * g;
-          if (p.dh0 && f.x >= 0) p.dh0[(size_t)f.x * p.D + at.ch + v] = q[v];
+      if (p.hT) {
+        if (kPacked) {
+          for (int j = 0; j < kTok; ++j) {
+            const int end = mark[par][at.token() + j].y;
+            if (end >= 0) stf<V>(p.hT + (size_t)end * p.D + at.ch, over<kPacked>(kept[j][me], in));
+          }
+        } else if (left >= 1 && left <= kTok) {  // the row's last token
+          stf<V>(p.hT + (size_t)at.b * p.D + at.ch, over<kPacked>(all, in));
         }
-        const long long row = row0 + t0 + j;
-        P::st(dx + row * p.dx_ld + at.ch, P::put(ox));
-        P::st(dr + row * p.dr_ld + at.ch, P::put(orr));
-        P::st(di + row * p.di_ld + at.ch, P::put(oi));
       }
     }
     __syncwarp();
   }
-  // sum of w over this CTA's tokens, the warps in order
-  __syncthreads();
-#pragma unroll
-  for (int v = 0; v < V; ++v) fspans[0][at.warp][at.lane * V + v] = make_float2(sum[v], 0.f);
-  __syncthreads();
-  if (at.warp == 0 && at.live)
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      float s = 0.f;
-      for (int w = 0; w < kWarps; ++w) s += fspans[0][w][at.lane * V + v].x;
-      p.part[((size_t)at.b * p.nc + at.rank) * p.D + at.ch + v] = s;
-    }
+  if (p.nc > 1) tc::cluster_sync();  // (what this CTA sent has arrived)
 }
 
-// dlam = sigmoid(lam) / softplus(lam) times the sum of the CTAs' sums, in order: 16 interleaved
+// What the first pass over a tile leaves for the second, in shared memory: thread-private, a
+// pair of each at [token][thread].  (before: the state before each token.)
+struct Kept {
+  f2 sr[kTok][kThreads], si[kTok][kThreads], u[kTok][kThreads], before[kTok][kThreads];
+};
+
+template <typename T, int V, bool kPacked>
+__global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
+  using Raw = typename Pack<T, V>::Raw;
+  extern __shared__ __align__(16) unsigned char dynamic[];
+  Kept &kept = *reinterpret_cast<Kept *>(dynamic);
+  __shared__ Span fspans[2][kWarps][kLanes], spans[2][kWarps][kLanes], tiles[2][kCluster][kLanes];
+  __shared__ int2 mark[2][kPacked ? kTile : 1];
+  __shared__ uint64_t bars[2];
+  const Place<V> at(p);
+  const int me = threadIdx.x;
+  const uint32_t row0 = (uint32_t)at.b * (uint32_t)p.T + (uint32_t)at.token();  // (B T is at most 2^30)
+  const int ntiles = (p.T + kTile - 1) / kTile, round = p.nc * kTile;
+  const f2 k = rate<V>(p, at.ch), one = both(1.f);
+  f2 carry = !kPacked && p.dhT ? ldf<V>(p.dhT + (size_t)at.b * p.D + at.ch) : both(0.f);
+  f2 sum = both(0.f);
+  pass_through<V, kPacked>(p, at, p.dhT, p.dh0);
+
+  exchange_init(p, bars);
+  int par = 0;
+  uint32_t phase = 0;
+  const int last = p.T > 0 ? (p.T - 1) / round * round : -1;
+  int tile0 = last + at.rank * kTile;
+  Raw rr[kTok], ir[kTok];
+  auto fetch = [&](int t) {
+    const bool full = t + kTile <= p.T;
+    const int left = p.T - t - at.token();
+    load_rows<T, V>(rr, p.r, p.r_ld, row0 + t, at.ch, full, left);
+    load_rows<T, V>(ir, p.i, p.i_ld, row0 + t, at.ch, full, left);
+  };
+  if (last >= 0) fetch(tile0);
+  for (int base = last; base >= 0; base -= round, tile0 -= round, phase ^= par, par ^= 1) {
+    const int left = p.T - tile0 - at.token();
+    const bool full = tile0 + kTile <= p.T;
+    Raw xr[kTok], gr[kTok];
+    load_rows<T, V>(xr, p.x, p.x_ld, row0 + tile0, at.ch, full, left);
+    load_rows<T, V>(gr, p.dy, p.dy_ld, row0 + tile0, at.ch, full, left);
+    f2 h = tile0 < p.T ? ldf<V>(p.chunks + ((size_t)at.b * ntiles + tile0 / kTile) * p.D + at.ch) : both(0.f);
+    if (kPacked) {
+      mark_tile(p, tile0, mark[par]);
+      __syncthreads();
+    }
+    // this thread's span from a zero state, both ways
+    Span fwd = {one, both(0.f)}, back = fwd;
+    auto ahead = [&](int j) {
+      const Gate g = gate(get2<T, V>(rr[j]), get2<T, V>(ir[j]), k);
+      kept.sr[j][me] = g.sr;
+      kept.si[j][me] = g.si;
+      kept.u[j][me] = g.u;
+      const f2 a = one_minus(g.u);
+      f2 b = mul2(mul2(sqrt2(rest(g.u)), g.si), get2<T, V>(xr[j]));
+      const int start = kPacked ? mark[par][at.token() + j].x : -1;
+      if (kPacked && start >= 0) {
+        if (p.h0) b = fma2(a, ldf<V>(p.h0 + (size_t)start * p.D + at.ch), b);
+        fwd = {both(-1.f), b};
+      } else {
+        step<kPacked>(fwd, a, b);
+      }
+    };
+    auto behind = [&](int j) {
+      const f2 a = one_minus(kept.u[j][me]);
+      const int end = kPacked ? mark[par][at.token() + j].y : -1;
+      if (kPacked && end >= 0) back = {both(-1.f), p.dhT ? ldf<V>(p.dhT + (size_t)end * p.D + at.ch) : both(0.f)};
+      step<kPacked>(back, a, mul2(a, get2<T, V>(gr[j])));
+    };
+    if (full) {
+#pragma unroll
+      for (int j = 0; j < kTok; ++j) ahead(j);
+#pragma unroll
+      for (int j = kTok - 1; j >= 0; --j) behind(j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kTok; ++j)
+        if (j < left) ahead(j);
+#pragma unroll
+      for (int j = kTok - 1; j >= 0; --j)
+        if (j < left) behind(j);
+    }
+    // the next round's gates are on their way while the spans are joined
+    if (base >= round) fetch(tile0 - round);
+    const Span fother = from_other_half(fwd), other = from_other_half(back);
+    leave<false, kPacked>(fspans[par], at.warp, at.lane, at.half, fwd, fother);
+    leave<true, kPacked>(spans[par], at.warp, at.lane, at.half, back, other);
+    __syncthreads();
+    exchange<true, kPacked>(p, spans[par], tiles[par], &bars[par], phase, at.rank);
+    f2 q = fold<true, kPacked>(spans[par], tiles[par], at.lane, at.rank, p.nc, at.warp, carry);
+    for (int w = 0; w < at.warp; ++w) h = over<kPacked>(fspans[par][w][at.lane], h);
+    if (at.half) h = over<kPacked>(fother, h);
+    else q = over<kPacked>(other, q);
+    auto again = [&](int j) {
+      const int start = kPacked ? mark[par][at.token() + j].x : -1;
+      if (kPacked && start >= 0) h = p.h0 ? ldf<V>(p.h0 + (size_t)start * p.D + at.ch) : both(0.f);
+      kept.before[j][me] = h;
+      const f2 u = kept.u[j][me];
+      h = fma2(one_minus(u), h, mul2(mul2(sqrt2(rest(u)), kept.si[j][me]), get2<T, V>(xr[j])));
+    };
+    const Rows<T> dx(p.dx, p.dx_ld, row0 + tile0, at.ch), dr(p.dr, p.dr_ld, row0 + tile0, at.ch),
+        di(p.di, p.di_ld, row0 + tile0, at.ch);
+    auto grads = [&](int j) {
+      const int2 f = kPacked ? mark[par][at.token() + j] : make_int2(-1, -1);
+      if (kPacked && f.y >= 0) q = p.dhT ? ldf<V>(p.dhT + (size_t)f.y * p.D + at.ch) : both(0.f);
+      const f2 xv = get2<T, V>(xr[j]), u = kept.u[j][me], sr = kept.sr[j][me], si = kept.si[j][me];
+      const f2 a = one_minus(u), t = log2_decay(k, sr), v = rest(u), rs = rsqrt2(v);
+      const f2 g = add2(get2<T, V>(gr[j]), q), gs = mul2(g, si), gm = mul2(gs, mul2(v, rs));
+      // w / ln 2 = a (g h_{t-1} t - a (g s x) t / m); t / m = t (1 - a^2)^-1/2, 0 where a is 1
+      const f2 w = mul2(a, sub2(mul2(mul2(g, kept.before[j][me]), t), mul2(mul2(a, mul2(t, rs)), mul2(gs, xv))));
+      sum = add2(sum, w);
+      q = mul2(a, g);
+      put2<T, V>(dx[j], gm);
+      put2<T, V>(dr[j], mul2(w, each(sr, [](float s) { return fmaf(s, -kLn2, kLn2); })));
+      put2<T, V>(di[j], mul2(mul2(gm, xv), one_minus(si)));
+      if (kPacked && p.dh0 && f.x >= 0) stf<V>(p.dh0 + (size_t)f.x * p.D + at.ch, q);
+    };
+    if (at.live) {
+      if (full) {
+#pragma unroll
+        for (int j = 0; j < kTok; ++j) again(j);
+#pragma unroll
+        for (int j = kTok - 1; j >= 0; --j) grads(j);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kTok; ++j)
+          if (j < left) again(j);
+#pragma unroll
+        for (int j = kTok - 1; j >= 0; --j)
+          if (j < left) grads(j);
+      }
+      if (!kPacked && p.dh0 && tile0 + at.token() == 0) stf<V>(p.dh0 + (size_t)at.b * p.D + at.ch, q);
+    }
+    __syncwarp();
+  }
+  // sum of w over this CTA's tokens, the spans in order
+  __syncthreads();
+  if (p.nc > 1) tc::cluster_sync();  // (what this CTA sent has arrived)
+  kept.u[0][me] = sum;
+  __syncthreads();
+  if (at.warp == 0 && at.half == 0 && at.live) {
+    f2 s = kept.u[0][at.lane];
+    for (int w = 1; w < 2 * kWarps; ++w) s = add2(s, kept.u[0][w * kLanes + at.lane]);
+    stf<V>(p.part + ((size_t)at.b * p.nc + at.rank) * p.D + at.ch, s);
+  }
+}
+
+// dlam = sigmoid(lam) / softplus(lam) times the sum of the CTAs' sums (of w / ln 2), in order: 16 interleaved
 // sums, joined in order.
 __global__ void __launch_bounds__(512) dlam_kernel(const GP p, long long parts, float *dlam) {
   __shared__ float sh[16][32];
@@ -494,49 +618,48 @@ __global__ void __launch_bounds__(512) dlam_kernel(const GP p, long long parts, 
   const float lam = p.lam[ch], sp = softplusf(lam);
   // (both are e^lam to the last digit where lam is far below zero)
   const float ratio = lam < -20.f ? 1.f : __fdividef(1.f, (1.f + expf(-lam)) * sp);
-  dlam[ch] = a * ratio;
+  dlam[ch] = a * ratio * kLn2;
 }
 
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads) step_kernel(const GP p) {
-  using P = Pack<T, V>;
-  const int ch = (blockIdx.x * kThreads + threadIdx.x) * V, n = blockIdx.y;
+  const int ch = (blockIdx.x * kThreads + threadIdx.x) * V;
   if (ch >= p.D) return;
-  for (int row = n; row < p.B; row += gridDim.y) {
+  const f2 k = rate<V>(p, ch);
+  for (int row = blockIdx.y; row < p.B; row += gridDim.y) {
     const int slot = p.slots ? p.slots[row] : row;
-    float y[V];
-    if (slot < 0 || slot >= p.num_slots) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) y[v] = 0.f;
-    } else {
-      float xv[V], rv[V], iv[V];
-      P::get(P::ld(static_cast<const T *>(p.x) + row * p.x_ld + ch), xv);
-      P::get(P::ld(static_cast<const T *>(p.r) + row * p.r_ld + ch), rv);
-      P::get(P::ld(static_cast<const T *>(p.i) + row * p.i_ld + ch), iv);
+    f2 y = both(0.f);
+    if (slot >= 0 && slot < p.num_slots) {
       float *h = p.h + (size_t)slot * p.D + ch;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const Gate g = gate(rv[v], iv[v], -p.c * softplusf(p.lam[ch + v]));
-        y[v] = fmaf(g.a, h[v], g.m * g.si * xv[v]);
-        h[v] = y[v];
-      }
+      const f2 x = get2<T, V>(Pack<T, V>::ld(static_cast<const T *>(p.x) + row * p.x_ld + ch));
+      const Gate g = gate(get2<T, V>(Pack<T, V>::ld(static_cast<const T *>(p.r) + row * p.r_ld + ch)),
+                          get2<T, V>(Pack<T, V>::ld(static_cast<const T *>(p.i) + row * p.i_ld + ch)), k);
+      y = fma2(one_minus(g.u), ldf<V>(h), mul2(mul2(sqrt2(rest(g.u)), g.si), x));
+      stf<V>(h, y);
     }
-    P::st(static_cast<T *>(p.y) + row * p.y_ld + ch, P::put(y));
+    put2<T, V>(static_cast<T *>(p.y) + row * p.y_ld + ch, y);
   }
 }
 
-// CTAs of a cluster: the tiles of a row, at most 8.
-int cluster_of(int T) {
-  int nc = 1;
-  while (nc < kCluster && (long long)nc * kTile < T) nc *= 2;
-  return nc;
+// CTAs of a cluster for `units` rows of strips: what fills the places of the GPU (95 % of them: clusters
+// do not take every SM) in one go.  Where the units fill them by themselves, two that share a
+// unit even out what the last ones leave idle, until there are twice as many units as places
+// (512 units of 4096 tokens: forward 145 us with two, 168 with one; 1024 units of 700: 66 and 60).
+int cluster_of(int T, long long units, bool bwd) {
+  const int tiles = (T + kTile - 1) / kTile, places = 152 * (bwd ? kBwdCtas : kFwdCtas) * 95 / 100;
+  const long long nc = units >= 2 * places ? 1 : units > places ? 2 : places / units;
+  const int most = tiles < 1 ? 1 : tiles < kCluster ? tiles : kCluster;
+  return nc < most ? (int)nc : most;
+}
+long long units_of(const rdn_gscan_args &a, int V) {
+  return (long long)a.B * ((a.D + kLanes * V - 1) / (kLanes * V));
 }
 
-GP params(const rdn_gscan_args &a, int V) {
+GP params(const rdn_gscan_args &a, int V, bool bwd) {
   GP p{};
   p.B = a.B; p.T = a.T; p.D = a.D; p.c = a.c;
-  p.nc = cluster_of(a.T);
-  p.strips = (a.D + 32 * V - 1) / (32 * V);
+  p.strips = (a.D + kLanes * V - 1) / (kLanes * V);
+  p.nc = cluster_of(a.T, units_of(a, V), bwd);
   p.num_seqs = a.num_seqs; p.cu = a.cu_seqlens;
   p.x_ld = a.x_ld; p.r_ld = a.r_ld; p.i_ld = a.i_ld; p.y_ld = a.y_ld;
   p.dy_ld = a.dy_ld; p.dx_ld = a.dx_ld; p.dr_ld = a.dr_ld; p.di_ld = a.di_ld;
@@ -544,6 +667,7 @@ GP params(const rdn_gscan_args &a, int V) {
   p.lam = a.lam; p.h0 = a.h0; p.dhT = a.dhT;
   p.y = a.y; p.dx = a.dx; p.dr = a.dr; p.di = a.di;
   p.hT = a.hT; p.chunks = a.h_chunks; p.dh0 = a.dh0;
+  p.status = status_word();
   return p;
 }
 
@@ -571,7 +695,12 @@ cudaError_t run(const GP &p, bool bwd, const char *name, cudaStream_t s) {
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  cudaError_t e;
+  cudaError_t e = cudaSuccess;
+  if (bwd) {
+    cfg.dynamicSmemBytes = sizeof(Kept);
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Kept));
+    if (e != cudaSuccess) return e;
+  }
   RDN_LAUNCH(name, s, (e = cudaLaunchKernelEx(&cfg, kern, p)));
   return e;
 }
@@ -581,8 +710,10 @@ cudaError_t run(const GP &p, bool bwd, int dtype, int V, const char *name, cudaS
   return V == 2 ? run<float, 2>(p, bwd, name, s) : run<float, 1>(p, bwd, name, s);
 }
 
+// (for one or two channels a lane: the query sees no pointers)
 size_t part_bytes(const rdn_gscan_args &a) {
-  return round256(sizeof(float) * (size_t)a.B * cluster_of(a.T) * a.D);
+  const int one = cluster_of(a.T, units_of(a, 1), true), two = cluster_of(a.T, units_of(a, 2), true);
+  return round256(sizeof(float) * (size_t)a.B * (one > two ? one : two) * a.D);
 }
 
 }  // namespace gscan
@@ -592,7 +723,7 @@ long long gscan_slots(const rdn_gscan_args &a) {
 }
 // CTAs of a call at one channel a lane, the most it may take.
 long long gscan_ctas(const rdn_gscan_args &a) {
-  return (long long)a.B * ((a.D + 31) / 32) * gscan::cluster_of(a.T);
+  return gscan::units_of(a, 1) * gscan::kCluster;
 }
 size_t gscan_bwd_bytes(const rdn_gscan_args &a) {
   const size_t states = a.h_chunks ? 0 : round256(sizeof(float) * (size_t)gscan_slots(a) * a.D);
@@ -602,7 +733,7 @@ size_t gscan_bwd_bytes(const rdn_gscan_args &a) {
 cudaError_t launch_gscan_fwd(const rdn_gscan_args &a, cudaStream_t s) {
   const size_t e = a.dtype == RDN_BF16 ? 2 : 4;
   const int V = gscan::pairs_ok(a.D, e, {a.x, a.r, a.i, a.y}, {a.x_ld, a.r_ld, a.i_ld, a.y_ld}) ? 2 : 1;
-  return gscan::run(gscan::params(a, V), false, a.dtype, V, "gscan_fwd", s);
+  return gscan::run(gscan::params(a, V, false), false, a.dtype, V, "gscan_fwd", s);
 }
 
 cudaError_t launch_gscan_bwd(const rdn_gscan_args &a, cudaStream_t s) {
@@ -620,7 +751,7 @@ cudaError_t launch_gscan_bwd(const rdn_gscan_args &a, cudaStream_t s) {
   }
   const int V = gscan::pairs_ok(a.D, el, {a.x, a.r, a.i, a.dy, a.dx, a.dr, a.di},
                                 {a.x_ld, a.r_ld, a.i_ld, a.dy_ld, a.dx_ld, a.dr_ld, a.di_ld}) ? 2 : 1;
-  gscan::GP p = gscan::params(c, V);
+  gscan::GP p = gscan::params(c, V, true);
   p.part = static_cast<float *>(a.workspace);
   cudaError_t e = gscan::run(p, true, a.dtype, V, "gscan_bwd", s);
   if (e != cudaSuccess) return e;

@@ -37,105 +37,191 @@ __device__ __forceinline__ void tile_at(const GemmP &p, int t, int &tm, int &tn)
   tm = g * 8 + r - tn * rows;
 }
 
-// 16 columns n.. of row m, from the sums v.
-__device__ __forceinline__ void put16(const Epilogue &e, long long m, long long n, long long N, float sx, float (&v)[16],
-                                      bool wide) {
-  const bool two = n + 16 <= N;  // (N is a multiple of 8)
-  if (e.ws) {
+// ---- the epilogue: 32 columns of a lane's row at a time.  A lane reads and writes whole 32-byte
+// sectors of its row where rows allow it (kSectors), 16 bytes or single elements else.
+enum Access { kSingle = 0, kVectors = 1, kSectors = 2 };
+struct alignas(32) U8 { uint32_t w[8]; };
+__device__ __forceinline__ U8 ld32(const void *p) {
+  U8 v;
+  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]), "=r"(v.w[6]), "=r"(v.w[7])
+               : "l"(p));
+  return v;
+}
+__device__ __forceinline__ void st32(void *p, const U8 &v) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v.w[0]), "r"(v.w[1]), "r"(v.w[2]),
+               "r"(v.w[3]), "r"(v.w[4]), "r"(v.w[5]), "r"(v.w[6]), "r"(v.w[7])
+               : "memory");
+}
+
+// 32 elements of a row, `cols` of them (a multiple of 8) there, as loaded.
+template <typename T>
+struct Row32 {
+  static constexpr int kPer = 32 / sizeof(T), kN = 32 / kPer;  // elements of a U8, U8s of a row
+  U8 v[kN];
+  __device__ void load(const T *p, int cols, int access) {
+    if (access == kSectors && cols >= 32) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] *= sx * (n + j < N ? __ldg(e.ws + n + j) : 0.f);
-  }
-  if (e.bias) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (h && !two) break;
-      float b[8];
-      if (e.bias_f32) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) b[j] = __ldg(static_cast<const float *>(e.bias) + n + 8 * h + j);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) b[j] = to_f32(__ldg(static_cast<const __nv_bfloat16 *>(e.bias) + n + 8 * h + j));
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[8 * h + j] += b[j];
+      for (int k = 0; k < kN; ++k) v[k] = ld32(p + k * kPer);
+      return;
     }
-  }
-  using P8 = Pack<__nv_bfloat16, 8>;
-  using P4 = Pack<float, 4>;
-  auto half = [&](int h, float (&o)[8]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = v[8 * h + j];
-  };
-  if (e.pre) {
+    for (int k = 0; k < kN; ++k)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (!h || two) {
-        float o[8];
-        half(h, o);
-        P8::st(e.pre + m * e.pre_ld + n + 8 * h, P8::put(o));
-      }
-  }
-  if (e.act) {
+      for (int h = 0; h < 2; ++h) {  // 16 bytes each
+        const int at = (2 * k + h) * (kPer / 2);
+        uint4 u = make_uint4(0u, 0u, 0u, 0u);
+        if (at < cols) {
+          if (access != kSingle) {
+            u = *reinterpret_cast<const uint4 *>(p + at);
+          } else {
+            float e[kPer / 2];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = act_of(e.act, v[j]);
-  }
-  if (e.res) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (h && !two) break;
-      if (!e.out_f32) {
-        const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(e.res) + m * e.res_ld + n + 8 * h;
-        float b[8];
-        if (wide) {
-          P8::get(P8::ld(q), b);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) b[j] = to_f32(q[j]);
+            for (int j = 0; j < kPer / 2; ++j) e[j] = to_f32<T>(p[at + j]);
+            const auto w = Pack<T, kPer / 2>::put(e);
+            u = *reinterpret_cast<const uint4 *>(&w);
+          }
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[8 * h + j] += b[j];
-      } else {
-        const float *q = static_cast<const float *>(e.res) + m * e.res_ld + n + 8 * h;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[8 * h + j] += q[j];
+        v[k].w[4 * h] = u.x; v[k].w[4 * h + 1] = u.y; v[k].w[4 * h + 2] = u.z; v[k].w[4 * h + 3] = u.w;
       }
-    }
   }
+  __device__ void store(T *p, int cols, int access) const {
+    if (access == kSectors && cols >= 32) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (h && !two) break;
-    float o[8];
-    half(h, o);
-    if (!e.out_f32) {
-      __nv_bfloat16 *q = static_cast<__nv_bfloat16 *>(e.y) + m * e.y_ld + n + 8 * h;
-      if (wide) {
-        P8::st(q, P8::put(o));
-      } else {
+      for (int k = 0; k < kN; ++k) st32(p + k * kPer, v[k]);
+      return;
+    }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = from_f32<__nv_bfloat16>(o[j]);
+    for (int k = 0; k < kN; ++k)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = (2 * k + h) * (kPer / 2);
+        if (at >= cols) continue;
+        const uint4 u = make_uint4(v[k].w[4 * h], v[k].w[4 * h + 1], v[k].w[4 * h + 2], v[k].w[4 * h + 3]);
+        if (access != kSingle) {
+          *reinterpret_cast<uint4 *>(p + at) = u;
+        } else {
+          float e[kPer / 2];
+          typename Pack<T, kPer / 2>::Raw w;
+          *reinterpret_cast<uint4 *>(&w) = u;
+          Pack<T, kPer / 2>::get(w, e);
+#pragma unroll
+          for (int j = 0; j < kPer / 2; ++j) p[at + j] = from_f32<T>(e[j]);
+        }
       }
-    } else {
-      float *q = static_cast<float *>(e.y) + m * e.y_ld + n + 8 * h;
-      if (wide) {
-        float a[4] = {o[0], o[1], o[2], o[3]}, b[4] = {o[4], o[5], o[6], o[7]};
-        P4::st(q, P4::put(a));
-        P4::st(q + 4, P4::put(b));
-      } else {
+  }
+  __device__ void add_to(float (&o)[32]) const {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = o[j];
+    for (int k = 0; k < kN; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (sizeof(T) == 4) {
+          o[8 * k + j] += __uint_as_float(v[k].w[j]);
+        } else {
+          o[16 * k + 2 * j] += __uint_as_float(v[k].w[j] << 16);
+          o[16 * k + 2 * j + 1] += __uint_as_float(v[k].w[j] & 0xffff0000u);
+        }
+      }
+  }
+  __device__ void round_from(const float (&o)[32]) {
+#pragma unroll
+    for (int k = 0; k < kN; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (sizeof(T) == 4) {
+          v[k].w[j] = __float_as_uint(o[8 * k + j]);
+        } else {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(o[16 * k + 2 * j], o[16 * k + 2 * j + 1]);
+          v[k].w[j] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+      }
+  }
+};
+
+template <int kAct>
+__device__ __forceinline__ void act32(float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] = act_of(kAct, v[j]);
+}
+
+// A warp's 32 rows x kCols columns from column n0 on; cols: [0] scales and [1] biases of its columns.
+// A bf16 residual is loaded a chunk ahead (r: the first chunk's); fp32 ones would not leave registers.
+template <typename T, int kCols, typename Taken>
+__device__ __forceinline__ void finish(const GemmP &p, uint32_t ta, long long m, long long n0, float sx,
+                                       const float (*cols)[kCols], Row32<__nv_bfloat16> r, int res_access, int y_access,
+                                       int pre_access, Taken taken) {
+  constexpr bool kAhead = sizeof(T) == 2;
+  const Epilogue &e = p.e;
+  const bool live = m < p.M;
+  const T *res = e.res ? static_cast<const T *>(e.res) + m * e.res_ld + n0 : nullptr;
+  T *y = static_cast<T *>(e.y) + m * e.y_ld + n0;
+  __nv_bfloat16 *pre = e.pre ? e.pre + m * e.pre_ld + n0 : nullptr;
+#pragma unroll 1
+  for (int c = 0; c < kCols; c += 32) {
+    const int left = (int)min((long long)32, p.N - n0 - c);  // columns of the chunk that exist
+    float v[32];
+    {
+      float a[16], b[16];
+      tc::tmem_ld16x2(ta + c, a, ta + c + 16, b);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) { v[j] = a[j]; v[16 + j] = b[j]; }
+    }
+    if (c + 32 == kCols) taken();
+    Row32<__nv_bfloat16> next;
+    if constexpr (kAhead)
+      if (res && live && c + 32 < kCols && p.N - n0 > c + 32)
+        next.load(res + c + 32, (int)min((long long)32, p.N - n0 - c - 32), res_access);
+    if (e.ws) {
+#pragma unroll
+      for (int j = 0; j < 32; j += 4) {
+        const float4 s = *reinterpret_cast<const float4 *>(&cols[0][c + j]);
+        v[j] *= sx * s.x; v[j + 1] *= sx * s.y; v[j + 2] *= sx * s.z; v[j + 3] *= sx * s.w;
       }
     }
+    if (e.bias) {
+#pragma unroll
+      for (int j = 0; j < 32; j += 4) {
+        const float4 s = *reinterpret_cast<const float4 *>(&cols[1][c + j]);
+        v[j] += s.x; v[j + 1] += s.y; v[j + 2] += s.z; v[j + 3] += s.w;
+      }
+    }
+    if (live && left > 0) {
+      if (pre) {
+        Row32<__nv_bfloat16> o;
+        o.round_from(v);
+        o.store(pre + c, left, pre_access);
+      }
+      if (e.act == 1) act32<1>(v);
+      else if (e.act == 2) act32<2>(v);
+      else if (e.act == 3) act32<3>(v);
+      if (res) {
+        if constexpr (kAhead) {
+          r.add_to(v);
+        } else {
+          Row32<T> now;
+          now.load(res + c, left, res_access);
+          now.add_to(v);
+        }
+      }
+      Row32<T> o;
+      o.round_from(v);
+      o.store(y + c, left, y_access);
+    }
+    if constexpr (kAhead) r = next;
+    __syncwarp();
   }
 }
 
 template <int kBN, bool kFp8, bool kAmn, bool kBmn>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    tiles_kernel(const __grid_constant__ GemmP p, const __grid_constant__ Maps maps, int wide) {
+    tiles_kernel(const __grid_constant__ GemmP p, const __grid_constant__ Maps maps, int res_access, int y_access,
+                 int pre_access) {
   using S = Smem<kBN>;
   constexpr int kStages = S::kStages;
+  constexpr int kCols = kBN / 2;  // columns of an epilogue warp
   extern __shared__ unsigned char raw[];
   __shared__ Bars b;
+  __shared__ alignas(16) float cols[kEpiWarps][2][kCols];
   unsigned char *tiles = raw + ((1024 - (tc::smem_u32(raw) & 1023)) & 1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_rank();
@@ -223,12 +309,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else {
     const int quarter = warp & 3, part = (warp - 2) >> 2;
-    constexpr int kCols = kBN / 2;  // columns of a warp
+    float(*mine)[kCols] = cols[warp - 2];
     int it = 0;
     for (int t = pair; t < ntiles; t += pairs, ++it) {
       int tm, tn;
       tile_at(p, t, tm, tn);
       const int acc = it & 1;
+      const long long m = (long long)tm * 256 + rank * 128 + quarter * 32 + lane;
+      const long long n0 = (long long)tn * kBN + part * kCols;
+      // what the sums meet is fetched before they are waited for
+      const float sx = p.e.xs && m < p.M ? p.e.xs[m] : 1.f;
+      for (int c = lane; c < kCols; c += 32) {
+        const bool in = n0 + c < p.N;
+        if (p.e.ws) mine[0][c] = in ? p.e.ws[n0 + c] : 0.f;
+        if (p.e.bias)
+          mine[1][c] = !in ? 0.f : p.e.bias_f32 ? static_cast<const float *>(p.e.bias)[n0 + c]
+                                                : to_f32(static_cast<const __nv_bfloat16 *>(p.e.bias)[n0 + c]);
+      }
+      Row32<__nv_bfloat16> rb;
+      const int have = (int)max(0ll, min((long long)32, p.N - n0));
+      if (p.e.res && !p.e.out_f32 && m < p.M && have)
+        rb.load(static_cast<const __nv_bfloat16 *>(p.e.res) + m * p.e.res_ld + n0, have, res_access);
+      __syncwarp();
       bool ok = !*dead;
       if (ok && !tc::mbar_wait(&b.done[acc], (uint32_t)(it / 2) & 1)) {
         fail();
@@ -236,25 +338,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
       if (!__all_sync(0xffffffffu, ok)) break;
       tc::fence_after_sync();
-      const long long m = (long long)tm * 256 + rank * 128 + quarter * 32 + lane;
-      const float sx = p.e.xs && m < p.M ? p.e.xs[m] : 1.f;
-      const long long n0 = (long long)tn * kBN + part * kCols;
       const uint32_t ta = tmem + ((uint32_t)(quarter * 32) << 16) + acc * kBN + part * kCols;
-#pragma unroll 1
-      for (int c = 0; c < kCols; c += 32) {
-        float v0[16], v1[16];
-        tc::tmem_ld16x2(ta + c, v0, ta + c + 16, v1);
-        if (c + 32 == kCols) {  // the sums are in registers: the next tile but one may be summed up here
-          tc::fence_before_sync();
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive_remote_relaxed(tc::map_rank(&b.taken[acc], 0));
-        }
-        if (m < p.M) {
-          if (n0 + c < p.N) put16(p.e, m, n0 + c, p.N, sx, v0, wide);
-          if (n0 + c + 16 < p.N) put16(p.e, m, n0 + c + 16, p.N, sx, v1, wide);
-        }
+      auto taken = [&] {  // the sums are in registers: the next tile but one may be summed up in their place
+        tc::fence_before_sync();
         __syncwarp();
-      }
+        if (lane == 0) tc::mbar_arrive_remote_relaxed(tc::map_rank(&b.taken[acc], 0));
+      };
+      if (p.e.out_f32) finish<float, kCols>(p, ta, m, n0, sx, mine, rb, res_access, y_access, pre_access, taken);
+      else finish<__nv_bfloat16, kCols>(p, ta, m, n0, sx, mine, rb, res_access, y_access, pre_access, taken);
     }
     __syncwarp();
   }
@@ -264,21 +355,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp == 0) tmem_free<true>(tmem, 2 * kBN);
 }
 
+// Rows (pointer and distance in bytes) on 32 bytes, 16 bytes or neither.
+int access_of(const void *p, long long bytes) {
+  const uintptr_t v = (uintptr_t)p | (uintptr_t)bytes;
+  return v % 32 == 0 ? kSectors : v % 16 == 0 ? kVectors : kSingle;
+}
+
 template <int kBN, bool kFp8, bool kAmn, bool kBmn>
-cudaError_t go(const Maps &maps, const GemmP &p, bool wide, cudaStream_t s) {
+cudaError_t go(const Maps &maps, const GemmP &p, cudaStream_t s) {
   auto kern = tiles_kernel<kBN, kFp8, kAmn, kBmn>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<kBN>::kBytes);
   if (e != cudaSuccess) return e;
   const long long n = (long long)p.tiles_m * p.tiles_n;
   const int ctas = 2 * (int)(n < 76 ? n : 76);
-  RDN_LAUNCH("linear_tiles", s, (kern<<<ctas, kThreads, Smem<kBN>::kBytes, s>>>(p, maps, wide)));
+  const size_t e_size = p.e.out_f32 ? 4 : 2;
+  RDN_LAUNCH("linear_tiles", s, (kern<<<ctas, kThreads, Smem<kBN>::kBytes, s>>>(p, maps, access_of(p.e.res, p.e.res_ld * e_size), access_of(p.e.y, p.e.y_ld * e_size), access_of(p.e.pre, p.e.pre_ld * 2))));
   return cudaGetLastError();
 }
 template <int kBN>
-cudaError_t pick(const Maps &maps, const GemmP &p, bool fp8, bool amn, bool bmn, bool wide, cudaStream_t s) {
-  if (fp8) return go<kBN, true, false, false>(maps, p, wide, s);
-  if (amn) return go<kBN, false, true, true>(maps, p, wide, s);
-  return bmn ? go<kBN, false, false, true>(maps, p, wide, s) : go<kBN, false, false, false>(maps, p, wide, s);
+cudaError_t pick(const Maps &maps, const GemmP &p, bool fp8, bool amn, bool bmn, cudaStream_t s) {
+  if (fp8) return go<kBN, true, false, false>(maps, p, s);
+  if (amn) return go<kBN, false, true, true>(maps, p, s);
+  return bmn ? go<kBN, false, false, true>(maps, p, s) : go<kBN, false, false, false>(maps, p, s);
 }
 
 }  // namespace
@@ -290,9 +388,7 @@ cudaError_t run_tiles(const Operand &a, const Operand &b, GemmP p, bool fp8, cud
   p.tiles_n = (int)((p.N + bn - 1) / bn);
   Maps maps;
   if (!make_map(&maps.a, a, fp8 ? 1 : 2, 128) || !make_map(&maps.b, b, fp8 ? 1 : 2, bn / 2)) return cudaErrorInvalidValue;
-  const size_t e = p.e.out_f32 ? 4 : 2;
-  const bool wide = (((uintptr_t)p.e.y | (uintptr_t)p.e.res | (p.e.y_ld * e) | (p.e.res ? p.e.res_ld * e : 0)) & 15) == 0;
-  return bn == 256 ? pick<256>(maps, p, fp8, a.mn, b.mn, wide, s) : pick<128>(maps, p, fp8, a.mn, b.mn, wide, s);
+  return bn == 256 ? pick<256>(maps, p, fp8, a.mn, b.mn, s) : pick<128>(maps, p, fp8, a.mn, b.mn, s);
 }
 
 }  // namespace lin

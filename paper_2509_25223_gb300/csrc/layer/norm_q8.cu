@@ -130,13 +130,13 @@ __global__ void __launch_bounds__(NV == 8 ? 256 : NV == 4 ? 512 : 1024) norm_q8_
 #pragma unroll
         for (int e = 0; e < 8; ++e) s = fmaf(r[n][e], r[n][e], s);
       s = over_row<false>(s, sh[0], p.warps);
-      const float inv = rsqrtf(s / (float)p.D + p.eps);
+      const float inv = __frsqrt_rn(__fdiv_rn(s, (float)p.D) + p.eps);
 #pragma unroll
       for (int n = 0; n < NV; ++n) {
         float w[8];
         load8<float, kVec>(p.w, (n * 32 * p.warps + t) * 8, p.D, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r[n][e] *= inv * w[e];
+        for (int e = 0; e < 8; ++e) r[n][e] = r[n][e] * inv * w[e];
       }
     }
     float m = 0.f;
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(NV == 8 ? 256 : NV == 4 ? 512 : 1024) norm_q8_
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(r[n][e]));
     m = fmaxf(over_row<true>(m, sh[1], p.warps), kFloor);
-    const float up = kTop / m;
+    const float up = __fdiv_rn(kTop, m);
     if (live) {
 #pragma unroll
       for (int n = 0; n < NV; ++n) {

@@ -34,15 +34,15 @@ def make(B, T, D, dtype, lens=None, state=True, pad=0, seed=0):
 
 
 def loop(v, c, lens):
-    """(y, last states, states before every 64th token of a row)"""
+    """(y, last states, states before every 128th token of a row)"""
     la = -c * torch.nn.functional.softplus(v["lam"], threshold=700.0) * torch.sigmoid(v["r"])
     a, b = torch.exp(la), torch.sqrt(-torch.expm1(2 * la)) * torch.sigmoid(v["i"]) * v["x"]
     y, last, kept, D = [], [], [], v["x"].shape[2]
     for s, (row, lo, hi) in enumerate(ref.spans(v["x"], lens)):
         h = torch.zeros(D, dtype=torch.float64) if v["h0"] is None else v["h0"][s]
         for t in range(lo, hi):
-            if t % 64 == 0 and t > lo:
-                kept.append((row, t // 64, h.detach()))
+            if t % 128 == 0 and t > lo:
+                kept.append((row, t // 128, h.detach()))
             h = a[row, t] * h + b[row, t]
             y.append(h)
         last.append(h)
@@ -71,7 +71,7 @@ def compare(x, c=8.0, lens=None, dhT=True, keep=True):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 63, 64, 65, 129, 400])
+@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 63, 64, 65, 127, 128, 129, 400])
 def test_lengths(T, dtype):
     compare(make(2, T, 40, dtype, seed=T))
 

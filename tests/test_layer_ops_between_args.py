@@ -37,7 +37,7 @@ def test_struct_layouts_match_the_header(tmp_path):
 
 
 def _gscan(**kw):
-    base = dict(B=2, T=100, D=128, dtype=_abi.RDN_BF16, c=8.0, x=FAKE, r=FAKE, i=FAKE, lam=FAKE, y=FAKE + 4096, dy=FAKE,
+    base = dict(B=2, T=200, D=128, dtype=_abi.RDN_BF16, c=8.0, x=FAKE, r=FAKE, i=FAKE, lam=FAKE, y=FAKE + 4096, dy=FAKE,
                 dx=FAKE + 4096, dr=FAKE + 8192, di=FAKE + 12288, dlam=FAKE, workspace=FAKE, workspace_bytes=1 << 40)
     return _fill(_abi.GscanArgs, **{**base, **kw})
 
