@@ -14,18 +14,60 @@ namespace {
 
 constexpr int kThreads = 256, kStageA = 128 * 128;
 
+// (two CTAs on an SM: clusters of several do not take every SM, and what one waits for the other hides)
 template <int kBN>
 struct Smem {
   static constexpr int kStage = kStageA + kBN * 128;
-  static constexpr int kStages = kBN == 128 ? 6 : 8;
+  static constexpr int kStages = kBN <= 32 ? 5 : kBN == 64 ? 4 : 3;
   static constexpr int kBytes = 1024 + kStages * kStage;
   static_assert(kBN * 128 * 4 <= kStages * kStage, "the sums take the stages' place");
+  static_assert(2 * (kBytes + 2048) <= 227 * 1024, "two CTAs an SM");
 };
 
-// (A: columns of the result, p.N; B: its rows, p.M)
+// 4 elements from p on: in one access where `vec`.
+__device__ __forceinline__ void load4(float (&v)[4], const void *p, bool f32, bool vec) {
+  if (f32) {
+    const float *q = static_cast<const float *>(p);
+    if (vec) Pack<float, 4>::get(Pack<float, 4>::ld(q), v);
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = q[j];
+  } else {
+    const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p);
+    if (vec) Pack<__nv_bfloat16, 4>::get(Pack<__nv_bfloat16, 4>::ld(q), v);
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = to_f32(q[j]);
+  }
+}
+__device__ __forceinline__ void store4(void *p, const float (&v)[4], bool f32, bool vec) {
+  if (f32) {
+    float *q = static_cast<float *>(p);
+    if (vec) Pack<float, 4>::st(q, Pack<float, 4>::put(v));
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j) q[j] = v[j];
+  } else {
+    __nv_bfloat16 *q = static_cast<__nv_bfloat16 *>(p);
+    if (vec) Pack<__nv_bfloat16, 4>::st(q, Pack<__nv_bfloat16, 4>::put(v));
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j) q[j] = from_f32<__nv_bfloat16>(v[j]);
+  }
+}
+__device__ __forceinline__ const void *at4(const void *p, long long i, bool f32) {
+  return static_cast<const char *>(p) + i * (f32 ? 4 : 2);
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+// (A: columns of the result, p.N; B: its rows, p.M;  vec: rows of y, res allow accesses of 4 elements)
 template <int kBN, bool kFp8, bool kAmn, bool kBmn>
-__global__ void __launch_bounds__(kThreads, 1)
-    split_kernel(const __grid_constant__ GemmP p, const __grid_constant__ Maps maps) {
+__global__ void __launch_bounds__(kThreads, 2)
+    split_kernel(const __grid_constant__ GemmP p, const __grid_constant__ Maps maps, int vec) {
   using S = Smem<kBN>;
   constexpr int kStages = S::kStages, kTmem = kBN < 32 ? 32 : kBN;
   extern __shared__ unsigned char raw[];
@@ -37,6 +79,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int q = blockIdx.x % p.splits, unit = blockIdx.x / p.splits;
   const int tn = unit % p.tiles_n, tm = unit / p.tiles_n;
   const int kb0 = (int)((long long)q * p.kblocks / p.splits), kb1 = (int)((long long)(q + 1) * p.kblocks / p.splits);
+  auto copy = [&](int n) {  // this CTA's k block n
+    const int s = n % kStages;
+    unsigned char *at = tiles + s * S::kStage;
+    tc::mbar_expect_tx(&full[s], S::kStage);
+    load_tile<false, kAmn, kFp8, 128>(at, &maps.a, tn * 128, kb0 + n, tc::smem_u32(&full[s]));
+    load_tile<false, kBmn, kFp8, kBN>(at + kStageA, &maps.b, tm * kBN, kb0 + n, tc::smem_u32(&full[s]));
+  };
+  const int count = kb1 - kb0;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -46,9 +96,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc::mbar_init(&done, 1);
     dead_ = 0;
     tc::fence_mbar_init();
+    for (int n = 0; n < min(count, kStages); ++n) copy(n);  // ahead of everything else
   }
-  __syncthreads();
-  if (warp == 0) tc::tmem_alloc(&slot, kTmem);
+  __syncwarp();
+  if (warp == 1) tc::tmem_alloc(&slot, kTmem);
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
@@ -61,15 +112,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == 0) {
     if (lane == 0) {
-      int n = 0;
-      for (int kb = kb0; kb < kb1; ++kb, ++n) {
-        const int s = n % kStages;
-        if (!tc::mbar_wait(&empty[s], (uint32_t)(n / kStages + 1) & 1)) fail();
+      int n = min(count, kStages);
+      for (; n < count; ++n) {
+        if (!tc::mbar_wait(&empty[n % kStages], (uint32_t)(n / kStages + 1) & 1)) fail();
         if (*dead) break;
-        unsigned char *at = tiles + s * S::kStage;
-        tc::mbar_expect_tx(&full[s], S::kStage);
-        load_tile<false, kAmn, kFp8, 128>(at, &maps.a, tn * 128, kb, tc::smem_u32(&full[s]));
-        load_tile<false, kBmn, kFp8, kBN>(at + kStageA, &maps.b, tm * kBN, kb, tc::smem_u32(&full[s]));
+        copy(n);
       }
       for (int c = n > kStages ? n - kStages : 0; c < n; ++c)  // every copy has landed
         if (!tc::mbar_wait(&full[c % kStages], (uint32_t)(c / kStages) & 1)) fail();
@@ -78,8 +125,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == 1) {
     if (lane == 0) {
       constexpr uint32_t idesc = idesc_of<kFp8>(128, kBN, kAmn, kBmn);
-      int n = 0;
-      for (int kb = kb0; kb < kb1; ++kb, ++n) {
+      for (int n = 0; n < count; ++n) {
         const int s = n % kStages;
         if (!tc::mbar_wait(&full[s], (uint32_t)(n / kStages) & 1)) fail();
         if (*dead) break;
@@ -96,13 +142,30 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   }
+
+  // what the sums meet: this lane's 4 columns, and the warp's first row of the residual
+  const Epilogue &e = p.e;
+  const long long n0 = (long long)tn * 128 + lane * 4;
+  const bool in = n0 < p.N;  // (N is a multiple of 8)
+  const int rows = (int)min((long long)kBN, p.M - (long long)tm * kBN);
+  const int r0 = q * rows / p.splits + warp, r1 = (q + 1) * rows / p.splits;
+  float sw[4] = {1.f, 1.f, 1.f, 1.f}, bias[4] = {0.f, 0.f, 0.f, 0.f}, res[4] = {0.f, 0.f, 0.f, 0.f};
+  auto row_res = [&](int r) {
+    if (e.res && r < r1) load4(res, at4(e.res, ((long long)tm * kBN + r) * e.res_ld + n0, e.out_f32), e.out_f32, vec);
+  };
+  if (in) {
+    if (e.ws) load4(sw, e.ws + n0, true, false);
+    if (e.bias) load4(bias, at4(e.bias, n0, e.bias_f32), e.bias_f32, false);
+    row_res(r0);
+  }
   __syncthreads();  // the products are done (or given up)
   tc::fence_after_sync();
-  float *part = reinterpret_cast<float *>(tiles);  // [kBN rows of the result][128 columns]
+  float *part = reinterpret_cast<float *>(tiles);  // [rows of the result][128 columns]
   if (warp >= 4) {
     const int quarter = warp & 3;
 #pragma unroll
     for (int c = 0; c < kBN; c += 16) {
+      if (c >= rows) break;
       float v[16];
       tc::tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + c, v);
 #pragma unroll
@@ -113,47 +176,44 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (p.splits > 1) tc::cluster_sync();
   else __syncthreads();
 
-  const Epilogue &e = p.e;
-  const int i = threadIdx.x & 127;
-  const long long n = (long long)tn * 128 + i;
-  const int r0 = q * kBN / p.splits, r1 = (q + 1) * kBN / p.splits;
-  if (n < p.N && !*dead) {
-    const float sw = e.ws ? e.ws[n] : 1.f;
-    const float bias = !e.bias ? 0.f : e.bias_f32 ? static_cast<const float *>(e.bias)[n]
-                                                  : to_f32(static_cast<const __nv_bfloat16 *>(e.bias)[n]);
-    for (int r = r0 + (threadIdx.x >> 7); r < r1; r += 2) {
+  if (in && !*dead) {
+    for (int r = r0; r < r1; r += kThreads / 32) {
       const long long m = (long long)tm * kBN + r;
-      if (m >= p.M) break;
-      float v = 0.f;
-      if (p.splits > 1) {
-        float w[8];
+      float4 w[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < p.splits)
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w[k]) : "r"(tc::map_rank(part + r * 128 + i, k)) : "memory");
+      for (int k = 0; k < 8; ++k)
+        if (k < p.splits) w[k] = ld_cluster4(tc::map_rank(part + r * 128 + lane * 4, k));
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < p.splits) v += w[k];
-      } else {
-        v = part[r * 128 + i];
+      for (int k = 0; k < 8; ++k)  // in order
+        if (k < p.splits) {
+          v[0] += w[k].x; v[1] += w[k].y; v[2] += w[k].z; v[3] += w[k].w;
+        }
+      const float sx = e.ws ? e.xs[m] : 1.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = fmaf(v[j], sx * sw[j], bias[j]);
+      if (e.pre) store4(e.pre + m * e.pre_ld + n0, v, false, true);
+      if (e.act == 1) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = act_of(1, v[j]);
+      } else if (e.act == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = act_of(2, v[j]);
+      } else if (e.act == 3) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = act_of(3, v[j]);
       }
-      if (e.ws) v *= e.xs[m] * sw;
-      if (e.bias) v += bias;
-      if (e.pre) e.pre[m * e.pre_ld + n] = from_f32<__nv_bfloat16>(v);
-      v = act_of(e.act, v);
-      if (e.out_f32) {
-        if (e.res) v += static_cast<const float *>(e.res)[m * e.res_ld + n];
-        static_cast<float *>(e.y)[m * e.y_ld + n] = v;
-      } else {
-        if (e.res) v += to_f32(static_cast<const __nv_bfloat16 *>(e.res)[m * e.res_ld + n]);
-        static_cast<__nv_bfloat16 *>(e.y)[m * e.y_ld + n] = from_f32<__nv_bfloat16>(v);
-      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] += res[j];
+      row_res(r + kThreads / 32);
+      store4(const_cast<void *>(at4(e.y, m * e.y_ld + n0, e.out_f32)), v, e.out_f32, vec);
     }
   }
   __syncwarp();
-  if (p.splits > 1) tc::cluster_sync();  // the others have read this CTA's sums
-  else __syncthreads();
-  if (warp == 0) tc::tmem_dealloc(tmem, kTmem);
+  // the others have read this CTA's sums (nothing that it wrote is waited for)
+  if (p.splits > 1)
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+  if (warp == 1) tc::tmem_dealloc(tmem, kTmem);
 }
 
 template <int kBN, bool kFp8, bool kAmn, bool kBmn>
@@ -172,7 +232,11 @@ cudaError_t go(const Maps &maps, const GemmP &p, cudaStream_t s) {
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  RDN_LAUNCH("linear_split", s, (e = cudaLaunchKernelEx(&cfg, kern, p, maps)));
+  // rows on 4 elements
+  const size_t by = p.e.out_f32 ? 16 : 8, el = p.e.out_f32 ? 4 : 2;
+  auto on = [&](const void *q, long long ld) { return !q || (((uintptr_t)q | (ld * el)) & (by - 1)) == 0; };
+  const int vec = on(p.e.y, p.e.y_ld) && on(p.e.res, p.e.res_ld);
+  RDN_LAUNCH("linear_split", s, (e = cudaLaunchKernelEx(&cfg, kern, p, maps, vec)));
   return e;
 }
 template <int kBN>
@@ -194,7 +258,7 @@ cudaError_t run_split(const Operand &a, const Operand &b, GemmP p, bool fp8, cud
   p.tiles_n = (int)((p.N + 127) / 128);
   const long long tiles = (long long)p.tiles_m * p.tiles_n;
   p.splits = 1;
-  while (p.splits < 8 && tiles * (p.splits + 1) <= 152 && p.splits < p.kblocks) ++p.splits;
+  while (p.splits < 8 && tiles * (p.splits + 1) <= 240 && p.splits < p.kblocks) ++p.splits;
   Maps maps;
   if (!make_map(&maps.a, b, fp8 ? 1 : 2, 128) || !make_map(&maps.b, a, fp8 ? 1 : 2, bn)) return cudaErrorInvalidValue;
   switch (bn) {
