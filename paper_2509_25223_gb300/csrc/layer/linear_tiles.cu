@@ -22,6 +22,19 @@ struct Smem {
   static constexpr int kBytes = 1024 + kStages * kStage;  // (tiles on 1024 bytes)
 };
 
+// A place in the ring of stages, and the parity of its use.
+template <int kStages>
+struct Ring {
+  int s = 0;
+  uint32_t phase = 0;
+  __device__ void next() {
+    if (++s == kStages) {
+      s = 0;
+      phase ^= 1;
+    }
+  }
+};
+
 struct Bars {
   uint64_t full[8], empty[8], done[2], taken[2], drained;
   uint32_t tmem;
@@ -248,6 +261,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   tc::fence_after_sync();
   const uint32_t tmem = b.tmem;
   volatile int *dead = &b.dead;
+  const uint32_t full0 = tc::map_rank(&b.full[0], 0);
   // A wait that gives up ends every role of the CTA at its next wait.
   auto fail = [&] {
     *dead = 1;
@@ -256,20 +270,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 
   if (warp == 0) {
     if (lane == 0) {
+      Ring<kStages> at;
       long long n = 0;  // k blocks copied
       for (int t = pair; t < ntiles && !*dead; t += pairs) {
         int tm, tn;
         tile_at(p, t, tm, tn);
-        for (int kb = 0; kb < p.kblocks; ++kb, ++n) {
-          const int s = (int)(n % kStages);
-          if (!tc::mbar_wait(&b.empty[s], (uint32_t)(n / kStages + 1) & 1)) fail();
+        const int ra = tm * 256 + (int)rank * 128, rb = tn * kBN + (int)rank * (kBN / 2);
+        for (int kb = 0; kb < p.kblocks; ++kb, at.next(), ++n) {
+          if (!tc::mbar_wait(&b.empty[at.s], at.phase ^ 1)) fail();
           if (*dead) break;
-          unsigned char *at = tiles + s * S::kStage;
+          unsigned char *to = tiles + at.s * S::kStage;
           // both CTAs' copies complete on the first one's barrier
-          const uint32_t bar = tc::map_rank(&b.full[s], 0);
-          if (rank == 0) tc::mbar_expect_tx(&b.full[s], 2 * S::kStage);
-          load_tile<true, kAmn, kFp8, 128>(at, &maps.a, tm * 256 + (int)rank * 128, kb, bar);
-          load_tile<true, kBmn, kFp8, kBN / 2>(at + kStageA, &maps.b, tn * kBN + (int)rank * (kBN / 2), kb, bar);
+          if (rank == 0) tc::mbar_expect_tx(&b.full[at.s], 2 * S::kStage);
+          const uint32_t bar = full0 + at.s * 8;
+          load_tile<true, kAmn, kFp8, 128>(to, &maps.a, ra, kb, bar);
+          load_tile<true, kBmn, kFp8, kBN / 2>(to + kStageA, &maps.b, rb, kb, bar);
         }
       }
       if (rank == 0)  // every copy has landed
@@ -280,24 +295,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
       constexpr uint32_t idesc = idesc_of<kFp8>(256, kBN, kAmn, kBmn);
-      long long n = 0;
+      const uint64_t da0 = tile_desc<kAmn>(tc::smem_u32(tiles)), db0 = tile_desc<kBmn>(tc::smem_u32(tiles) + kStageA);
+      Ring<kStages> at;
       int it = 0;
       for (int t = pair; t < ntiles && !*dead; t += pairs, ++it) {
         const int acc = it & 1;
         if (!tc::mbar_wait_cluster(&b.taken[acc], (uint32_t)(it / 2 + 1) & 1, 2000000000ll)) fail();
         if (*dead) break;
         tc::fence_after_sync();
-        for (int kb = 0; kb < p.kblocks; ++kb, ++n) {
-          const int s = (int)(n % kStages);
-          if (!tc::mbar_wait(&b.full[s], (uint32_t)(n / kStages) & 1)) fail();
-          if (*dead) break;
+        for (int kb = 0; kb < p.kblocks; ++kb, at.next()) {
+          if (!tc::mbar_wait(&b.full[at.s], at.phase)) {
+            fail();
+            break;
+          }
           tc::fence_after_sync();
-          const uint32_t at = tc::smem_u32(tiles + s * S::kStage);
-          const uint64_t da = tile_desc<kAmn>(at), db = tile_desc<kBmn>(at + kStageA);
+          const uint64_t to = tc::desc_off((uint32_t)(at.s * S::kStage));
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            mma_step<true, kFp8>(tmem + acc * kBN, da + tile_step<kAmn>(j), db + tile_step<kBmn>(j), idesc, kb + j > 0);
-          commit<true>(&b.empty[s]);
+            mma_step<true, kFp8>(tmem + acc * kBN, da0 + to + tile_step<kAmn>(j), db0 + to + tile_step<kBmn>(j), idesc, kb + j > 0);
+          commit<true>(&b.empty[at.s]);
         }
         if (!*dead) commit<true>(&b.done[acc]);
       }
