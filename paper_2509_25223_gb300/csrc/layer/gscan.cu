@@ -13,9 +13,11 @@
 // The backward is the same over the reversed tokens, with
 //     g_t = dy_t + q_{t+1},  q_t = a_t g_t       (q: the gradient of the state before t)
 // and the states again from those that the forward kept before every tile:
-//     dx = g m s,  di = g m x s (1 - s),  w_t = g (a h_{t-1} la - a^2 s x la / m),
+// with b = m s x, the token's own part of h:
+//     dx = g m s,  di = g b (1 - s),  w_t = a g la (h_{t-1} - a b / (1 - a^2)),
 //     dr = (1 - sigmoid(r)) w,  dlam = sigmoid(lam) / softplus(lam) sum_t w_t
-// (la / m stays finite where la -> 0: m ~ sqrt(-2 la)).
+// (la b / (1 - a^2) stays finite where la -> 0: it is la s x / m, and m ~ sqrt(-2 la)).
+#include "maps.cuh"
 #include "rows.cuh"
 #include "status.cuh"
 #include "tc_common.cuh"
@@ -117,9 +119,9 @@ __device__ __forceinline__ f2 sqrt2(f2 x) {
     return v;
   });
 }
-// x^-1/2, a large number for x = 0
-__device__ __forceinline__ f2 rsqrt2(f2 x) {
-  return each(x, [](float v) { return rsqrtf(max_nan(v, 2e-38f)); });
+// 1 / x, a large number for x = 0
+__device__ __forceinline__ f2 rcp2(f2 x) {
+  return each(x, [](float v) { return rcp_approx(max_nan(v, 2e-38f)); });
 }
 __device__ __forceinline__ f2 one_minus(f2 x) {
   return each(x, [](float v) { return 1.f - v; });
@@ -224,9 +226,10 @@ struct Place {
 };
 
 // Sequence that starts / ends at each token of the tile (-1: none).
+template <int kTokens = kTile>
 __device__ __forceinline__ void mark_tile(const GP &p, int t0, int2 *mark) {
   const int k = threadIdx.x;
-  if (k < kTile) {
+  if (k < kTokens) {
     int2 f = make_int2(-1, -1);
     if (t0 + k < p.T) {
       const SeqSpan q = find_seq(p.cu, p.num_seqs, p.T, 0, t0 + k);
@@ -280,19 +283,39 @@ __device__ __forceinline__ void leave(Span (*spans)[kLanes], int warp, int lane,
   if (half == (kBack ? 1 : 0)) spans[warp][lane] = then<kPacked>(own, other);
 }
 
+// tc::mbar_wait_cluster that looks without acquiring until the phase is over: an acquire at cluster scope drops
+// the SM's L1 each time it looks.
+__device__ __forceinline__ bool wait_cluster(uint64_t *bar, uint32_t parity) {
+  const long long t0 = clock64();
+  while (true) {
+    uint32_t over;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2, 2000;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(over)
+        : "r"(tc::smem_u32(bar)), "r"(parity)
+        : "memory");
+    if (over) return tc::mbar_try_wait_cluster(bar, parity);
+    if (clock64() - t0 > 2000000000ll) return false;
+  }
+}
+
 // Sends the composition of the CTA's warps' spans (in the order 0.. or, kBack, 7..) to the
 // slot of this CTA in every CTA of the cluster, and waits until all have come.  The stores
 // themselves tell the receiver's barrier: a barrier of the cluster would hold this thread
 // until its global stores of the round before are done.  (A slot is written again two rounds
 // later, by a CTA that has had this CTA's spans of the round between, sent when all its warps
 // had read the slot.)
-template <bool kBack, bool kPacked>
-__device__ __forceinline__ void exchange(const GP &p, const Span (*spans)[kLanes], Span (*tiles)[kLanes], uint64_t *bar,
+template <bool kBack, bool kPacked, int kN>
+__device__ __forceinline__ void exchange(const GP &p, const Span (*spans)[kN], Span (*tiles)[kN], uint64_t *bar,
                                          uint32_t phase, int rank) {
   if (p.nc == 1) return;
-  const int lane = threadIdx.x & (kLanes - 1), to = threadIdx.x >> 4;
-  static_assert(2 * kWarps >= kCluster, "half a warp for each CTA of the cluster");
-  if (threadIdx.x == 0) tc::mbar_expect_tx(bar, (uint32_t)(p.nc * kLanes * sizeof(Span)));
+  const int lane = threadIdx.x % kN, to = threadIdx.x / kN;
+  static_assert(kThreads / kN >= kCluster, "lanes for each CTA of the cluster");
+  if (threadIdx.x == 0) tc::mbar_expect_tx(bar, (uint32_t)(p.nc * kN * sizeof(Span)));
   if (to < p.nc) {
     Span all = spans[kBack ? kWarps - 1 : 0][lane];
 #pragma unroll
@@ -303,7 +326,7 @@ __device__ __forceinline__ void exchange(const GP &p, const Span (*spans)[kLanes
                  : "memory");
   }
   __syncwarp();
-  if (!tc::mbar_wait_cluster(bar, phase, 2000000000ll) && p.status) atomicExch(p.status, (int)RDN_ERR_TIMEOUT);
+  if (!wait_cluster(bar, phase) && p.status) atomicExch(p.status, (int)RDN_ERR_TIMEOUT);
 }
 // Before the first exchange: the barriers are there, and every CTA of the cluster runs.
 __device__ __forceinline__ void exchange_init(const GP &p, uint64_t *bars) {
@@ -318,9 +341,9 @@ __device__ __forceinline__ void exchange_init(const GP &p, uint64_t *bars) {
 }
 
 // The state that comes into this warp's span; carry: into and out of the cluster's round.
-template <bool kBack, bool kPacked>
-__device__ __forceinline__ f2 fold(const Span (*spans)[kLanes], const Span (*tiles)[kLanes], int lane, int rank, int nc,
-                                   int warp, f2 &carry) {
+template <bool kBack, bool kPacked, int kN>
+__device__ __forceinline__ f2 fold(const Span (*spans)[kN], const Span (*tiles)[kN], int lane, int rank, int nc, int warp,
+                                   f2 &carry) {
   f2 run = carry;
   if (nc > 1) {
     f2 h = carry;
@@ -346,8 +369,8 @@ __device__ __forceinline__ f2 fold(const Span (*spans)[kLanes], const Span (*til
 }
 
 // States of sequences without tokens: out = in, or 0.
-template <int V, bool kPacked>
-__device__ __forceinline__ void pass_through(const GP &p, const Place<V> &at, const float *in, float *out) {
+template <int V, bool kPacked, typename At>
+__device__ __forceinline__ void pass_through(const GP &p, const At &at, const float *in, float *out) {
   if (!out || !at.live || at.half) return;
   if (!kPacked) {
     const size_t o = (size_t)at.b * p.D + at.ch;
@@ -454,10 +477,138 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
   if (p.nc > 1) tc::cluster_sync();  // (what this CTA sent has arrived)
 }
 
+// ---- forward for bf16 rows on 16 bytes: tiles by TMA.  As fwd_kernel, but a warp takes kTok tokens of 64
+// channels, so that a tile is 64 tokens of 128 bytes, and the tiles come to shared memory a round ahead
+// (and go from there) as whole boxes: no addresses are worked out per row, which are a quarter of
+// fwd_kernel's instructions, and the spans of a thread's tokens stay in its registers.
+constexpr int kWide = 64, kTileTma = kTok * kWarps;  // channels and tokens of a box
+struct alignas(64) TileMap { unsigned char b[128]; };
+struct FwdMaps { TileMap x, r, i, y; };
+struct FwdTiles {
+  __nv_bfloat16 in[2][3][kTileTma][kWide], y[kTileTma][kWide];
+};
+
+struct WidePlace {
+  int lane, warp, rank, b, strip, ch;
+  bool live;
+  static constexpr int half = 0;
+  __device__ explicit WidePlace(const GP &p) {
+    lane = threadIdx.x & 31;
+    warp = threadIdx.x >> 5;
+    rank = blockIdx.x % p.nc;
+    const int unit = blockIdx.x / p.nc;
+    b = unit / p.strips;
+    strip = (unit % p.strips) * kWide;
+    live = strip + lane * 2 < p.D;
+    ch = live ? strip + lane * 2 : strip;
+  }
+};
+
+template <bool kPacked>
+__global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p, const __grid_constant__ FwdMaps maps) {
+  using bf = __nv_bfloat16;
+  extern __shared__ __align__(128) unsigned char dynamic[];
+  FwdTiles &sm = *reinterpret_cast<FwdTiles *>(dynamic + ((128 - (tc::smem_u32(dynamic) & 127)) & 127));
+  __shared__ Span spans[2][kWarps][32], tiles[2][kCluster][32];
+  __shared__ int2 mark[2][kPacked ? kTileTma : 1];
+  __shared__ uint64_t bars[2], full[2];
+  const WidePlace at(p);
+  const int round = p.nc * kTileTma, nchunks = (p.T + kTile - 1) / kTile;
+  auto fetch = [&](int t, int s) {  // by one thread
+    tc::mbar_expect_tx(&full[s], (uint32_t)sizeof(sm.in[s]));
+    tc::tma_load_3d(sm.in[s][0], &maps.r, at.strip, t, at.b, &full[s]);
+    tc::tma_load_3d(sm.in[s][1], &maps.i, at.strip, t, at.b, &full[s]);
+    tc::tma_load_3d(sm.in[s][2], &maps.x, at.strip, t, at.b, &full[s]);
+  };
+  int tile0 = at.rank * kTileTma;
+  if (threadIdx.x == 0) {
+    tc::mbar_init(&full[0], 1);
+    tc::mbar_init(&full[1], 1);
+    tc::mbar_init(&bars[0], 1);
+    tc::mbar_init(&bars[1], 1);
+    tc::fence_mbar_init();
+    for (int s = 0; s < 2; ++s)
+      if (s * round < p.T) fetch(tile0 + s * round, s);
+  }
+  const f2 k = rate<2>(p, at.ch);
+  f2 carry = !kPacked && p.h0 ? ldf<2>(p.h0 + (size_t)at.b * p.D + at.ch) : both(0.f);
+  pass_through<2, kPacked>(p, at, p.h0, p.hT);
+  __syncthreads();
+  if (p.nc > 1) tc::cluster_sync();  // the barriers are there, and every CTA of the cluster runs
+
+  int par = 0;  // also the stage
+  uint32_t phase = 0;
+  for (int base = 0; base < p.T; base += round, tile0 += round, phase ^= par, par ^= 1) {
+    const int first = at.warp * kTok, left = p.T - tile0 - first;
+    if (kPacked) {
+      mark_tile<kTileTma>(p, tile0, mark[par]);
+      __syncthreads();
+    }
+    if (!tc::mbar_wait(&full[par], phase) && p.status) atomicExch(p.status, (int)RDN_ERR_TIMEOUT);
+    // (tokens past the row's end are zeros, which nothing that is kept follows)
+    Span all = {both(1.f), both(0.f)}, kept[kTok];
+#pragma unroll
+    for (int j = 0; j < kTok; ++j) {
+      const Gate g = gate(get2<bf, 2>(Pack<bf, 2>::ld(&sm.in[par][0][first + j][at.lane * 2])),
+                          get2<bf, 2>(Pack<bf, 2>::ld(&sm.in[par][1][first + j][at.lane * 2])), k);
+      const f2 a = one_minus(g.u);
+      f2 b = mul2(mul2(sqrt2(rest(g.u)), g.si), get2<bf, 2>(Pack<bf, 2>::ld(&sm.in[par][2][first + j][at.lane * 2])));
+      const int start = kPacked ? mark[par][first + j].x : -1;
+      if (kPacked && start >= 0) {
+        if (p.h0) b = fma2(a, ldf<2>(p.h0 + (size_t)start * p.D + at.ch), b);
+        all = {both(-1.f), b};
+      } else {
+        step<kPacked>(all, a, b);
+      }
+      kept[j] = all;
+    }
+    spans[par][at.warp][at.lane] = all;
+    __syncthreads();
+    if (threadIdx.x == 0 && base + 2 * round < p.T) fetch(tile0 + 2 * round, par);  // the stage has been read
+    __syncwarp();
+    exchange<false, kPacked>(p, spans[par], tiles[par], &bars[par], phase, at.rank);
+    const f2 in = fold<false, kPacked>(spans[par], tiles[par], at.lane, at.rank, p.nc, at.warp, carry);
+    if (p.chunks && at.live && at.warp == 0 && tile0 < p.T && tile0 % kTile == 0)
+      stf<2>(p.chunks + ((size_t)at.b * nchunks + tile0 / kTile) * p.D + at.ch, in);
+    if (p.y) {
+      if (at.lane == 0) tc::bulk_wait_read();  // the round before has left the warp's rows
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < kTok; ++j) put2<bf, 2>(&sm.y[first + j][at.lane * 2], over<kPacked>(kept[j], in));
+      tc::fence_async_smem();
+      __syncwarp();
+      if (at.lane == 0 && left > 0) {  // (what is past the tensor's ends is left out)
+        tc::tma_store_3d(&maps.y, at.strip, tile0 + first, at.b, sm.y[first]);
+        tc::bulk_commit();
+      }
+    }
+    if (p.hT && at.live) {
+      if (kPacked) {
+        for (int j = 0; j < kTok; ++j) {
+          const int end = mark[par][first + j].y;
+          if (end >= 0) {
+#pragma unroll
+            for (int q = 0; q < kTok; ++q)
+              if (q == j) stf<2>(p.hT + (size_t)end * p.D + at.ch, over<kPacked>(kept[q], in));
+          }
+        }
+      } else if (left >= 1 && left <= kTok) {  // the row's last token
+#pragma unroll
+        for (int q = 0; q < kTok; ++q)
+          if (q == left - 1) stf<2>(p.hT + (size_t)at.b * p.D + at.ch, over<kPacked>(kept[q], in));
+      }
+    }
+    __syncwarp();
+  }
+  if (at.lane == 0) tc::bulk_wait_all();
+  __syncwarp();
+  if (p.nc > 1) tc::cluster_sync();  // (what this CTA sent has arrived)
+}
+
 // What the first pass over a tile leaves for the second, in shared memory: thread-private, a
-// pair of each at [token][thread].  (before: the state before each token.)
+// pair of each at [token][thread].  (ms: m s; before: the state before each token.)
 struct Kept {
-  f2 sr[kTok][kThreads], si[kTok][kThreads], u[kTok][kThreads], before[kTok][kThreads];
+  f2 sr[kTok][kThreads], si[kTok][kThreads], u[kTok][kThreads], ms[kTok][kThreads], before[kTok][kThreads];
 };
 
 template <typename T, int V, bool kPacked>
@@ -508,8 +659,9 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
       kept.sr[j][me] = g.sr;
       kept.si[j][me] = g.si;
       kept.u[j][me] = g.u;
-      const f2 a = one_minus(g.u);
-      f2 b = mul2(mul2(sqrt2(rest(g.u)), g.si), get2<T, V>(xr[j]));
+      const f2 a = one_minus(g.u), ms = mul2(sqrt2(rest(g.u)), g.si);
+      kept.ms[j][me] = ms;
+      f2 b = mul2(ms, get2<T, V>(xr[j]));
       const int start = kPacked ? mark[par][at.token() + j].x : -1;
       if (kPacked && start >= 0) {
         if (p.h0) b = fma2(a, ldf<V>(p.h0 + (size_t)start * p.D + at.ch), b);
@@ -552,24 +704,23 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
       const int start = kPacked ? mark[par][at.token() + j].x : -1;
       if (kPacked && start >= 0) h = p.h0 ? ldf<V>(p.h0 + (size_t)start * p.D + at.ch) : both(0.f);
       kept.before[j][me] = h;
-      const f2 u = kept.u[j][me];
-      h = fma2(one_minus(u), h, mul2(mul2(sqrt2(rest(u)), kept.si[j][me]), get2<T, V>(xr[j])));
+      h = fma2(one_minus(kept.u[j][me]), h, mul2(kept.ms[j][me], get2<T, V>(xr[j])));
     };
     const Rows<T> dx(p.dx, p.dx_ld, row0 + tile0, at.ch), dr(p.dr, p.dr_ld, row0 + tile0, at.ch),
         di(p.di, p.di_ld, row0 + tile0, at.ch);
     auto grads = [&](int j) {
       const int2 f = kPacked ? mark[par][at.token() + j] : make_int2(-1, -1);
       if (kPacked && f.y >= 0) q = p.dhT ? ldf<V>(p.dhT + (size_t)f.y * p.D + at.ch) : both(0.f);
-      const f2 xv = get2<T, V>(xr[j]), u = kept.u[j][me], sr = kept.sr[j][me], si = kept.si[j][me];
-      const f2 a = one_minus(u), t = log2_decay(k, sr), v = rest(u), rs = rsqrt2(v);
-      const f2 g = add2(get2<T, V>(gr[j]), q), gs = mul2(g, si), gm = mul2(gs, mul2(v, rs));
-      // w / ln 2 = a (g h_{t-1} t - a (g s x) t / m); t / m = t (1 - a^2)^-1/2, 0 where a is 1
-      const f2 w = mul2(a, sub2(mul2(mul2(g, kept.before[j][me]), t), mul2(mul2(a, mul2(t, rs)), mul2(gs, xv))));
+      const f2 u = kept.u[j][me], sr = kept.sr[j][me], ms = kept.ms[j][me];
+      const f2 a = one_minus(u), t = log2_decay(k, sr), b = mul2(ms, get2<T, V>(xr[j]));
+      const f2 g = add2(get2<T, V>(gr[j]), q), ag = mul2(a, g);
+      // w / ln 2 = a g t (h_{t-1} - a b / (1 - a^2)): 0 where a is 1, for t and b are
+      const f2 w = mul2(mul2(ag, t), sub2(kept.before[j][me], mul2(mul2(a, b), rcp2(rest(u)))));
       sum = add2(sum, w);
-      q = mul2(a, g);
-      put2<T, V>(dx[j], gm);
+      q = ag;
+      put2<T, V>(dx[j], mul2(g, ms));
       put2<T, V>(dr[j], mul2(w, each(sr, [](float s) { return fmaf(s, -kLn2, kLn2); })));
-      put2<T, V>(di[j], mul2(mul2(gm, xv), one_minus(si)));
+      put2<T, V>(di[j], mul2(mul2(g, b), one_minus(kept.si[j][me])));
       if (kPacked && p.dh0 && f.x >= 0) stf<V>(p.dh0 + (size_t)f.x * p.D + at.ch, q);
     };
     if (at.live) {
@@ -710,6 +861,51 @@ cudaError_t run(const GP &p, bool bwd, int dtype, int V, const char *name, cudaS
   return V == 2 ? run<float, 2>(p, bwd, name, s) : run<float, 1>(p, bwd, name, s);
 }
 
+// Tensor maps over [B][T][D] bf16 rows of distance ld, boxes of 64 channels and `tokens` tokens.
+bool make_tiles(TileMap *m, const void *p, const rdn_gscan_args &a, long long ld, int tokens) {
+  return rdn::make_rows_map(m, p, a.D, a.T, a.B, ld, kWide, tokens);
+}
+// bf16, an even D, rows (pointers and distances) on 16 bytes, and distances that a map can hold.
+bool tma_ok(const rdn_gscan_args &a) {
+  if (a.dtype != RDN_BF16 || (a.D & 1) || a.T < 1) return false;
+  for (long long ld : {a.x_ld, a.r_ld, a.i_ld, a.y_ld})
+    if (ld * 2 * a.T >= (1ll << 40)) return false;
+  const uintptr_t bits = (uintptr_t)a.x | (uintptr_t)a.r | (uintptr_t)a.i | (uintptr_t)a.y | (uintptr_t)(a.x_ld * 2) |
+                         (uintptr_t)(a.r_ld * 2) | (uintptr_t)(a.i_ld * 2) | (uintptr_t)(a.y_ld * 2);
+  return (bits & 15) == 0;
+}
+cudaError_t run_tma(const rdn_gscan_args &a, cudaStream_t s) {
+  FwdMaps maps{};
+  if (!make_tiles(&maps.x, a.x, a, a.x_ld, kTileTma) || !make_tiles(&maps.r, a.r, a, a.r_ld, kTileTma) ||
+      !make_tiles(&maps.i, a.i, a, a.i_ld, kTileTma) || (a.y && !make_tiles(&maps.y, a.y, a, a.y_ld, kTok)))
+    return cudaErrorInvalidValue;
+  GP p = params(a, 2, false);
+  p.strips = (a.D + kWide - 1) / kWide;
+  // CTAs of a cluster: what fills 95 % of the places in one go, and no more: a round costs a CTA more in a
+  // cluster (256 units of 4096 tokens 136 us with one, 145 with two; 128 units 77 with three, 97 with
+  // one); of 8 few clusters find a place (64 units of 16384 tokens: 148 us with six, 183 with eight).
+  const long long units = (long long)a.B * p.strips, places = 152 * kFwdCtas * 95 / 100, tiles = (a.T + kTileTma - 1) / kTileTma;
+  const long long nc = units > places ? 1 : places / units, most = tiles < 6 ? tiles : 6;
+  p.nc = (int)(nc < most ? nc : most);
+  auto kern = a.cu_seqlens ? fwd_tma_kernel<true> : fwd_tma_kernel<false>;
+  constexpr int kBytes = sizeof(FwdTiles) + 128;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)((long long)p.B * p.strips * p.nc));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kBytes;
+  cfg.stream = s;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = p.nc;
+  at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  RDN_LAUNCH("gscan_fwd", s, (e = cudaLaunchKernelEx(&cfg, kern, p, maps)));
+  return e;
+}
+
 // (for one or two channels a lane: the query sees no pointers)
 size_t part_bytes(const rdn_gscan_args &a) {
   const int one = cluster_of(a.T, units_of(a, 1), true), two = cluster_of(a.T, units_of(a, 2), true);
@@ -732,6 +928,7 @@ size_t gscan_bwd_bytes(const rdn_gscan_args &a) {
 
 cudaError_t launch_gscan_fwd(const rdn_gscan_args &a, cudaStream_t s) {
   const size_t e = a.dtype == RDN_BF16 ? 2 : 4;
+  if (gscan::tma_ok(a)) return gscan::run_tma(a, s);
   const int V = gscan::pairs_ok(a.D, e, {a.x, a.r, a.i, a.y}, {a.x_ld, a.r_ld, a.i_ld, a.y_ld}) ? 2 : 1;
   return gscan::run(gscan::params(a, V, false), false, a.dtype, V, "gscan_fwd", s);
 }

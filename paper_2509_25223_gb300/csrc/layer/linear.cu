@@ -2,6 +2,7 @@
 // rdn_linear_*): the tensor maps, the choice of the kernel, and what the backward does
 // besides its two products: dp = dy act'(pre) and the bias's gradient.
 #include "linear.cuh"
+#include "maps.cuh"
 
 #include <cuda.h>
 #include <cudaTypedefs.h>
@@ -36,6 +37,22 @@ bool make_map(Map *m, const Operand &o, int elem, int box) {
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+}  // namespace lin
+
+bool make_rows_map(void *map128, const void *p, int cols, int rows, int depth, long long ld, int box_cols, int box_rows) {
+  const auto enc = lin::encoder();
+  if (!enc) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)depth};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * rows};
+  const cuuint32_t boxes[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
+  const cuuint32_t one[3] = {1, 1, 1};
+  return enc(reinterpret_cast<CUtensorMap *>(map128), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims,
+             strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+namespace lin {
 
 cudaError_t run_product(const Operand &a, const Operand &b, GemmP p, bool fp8, cudaStream_t s) {
   p.status = status_word();
