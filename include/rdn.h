@@ -561,15 +561,15 @@ rdn_status_t rdn_norm_bwd_workspace_size(const rdn_norm_args *args, size_t *byte
  *   x, r, i, y        [B,T,D] with row strides.
  *   lam [D]           fp32.
  *   h0, hT            [num_seqs or B, D] fp32 or NULL.
- *   h_chunks          NULL, or [B * ceil(T/128)][D] fp32: the states before tokens
- *                     0, 128, 256 ... of each row of the batch, whatever sequence
+ *   h_chunks          NULL, or [B * ceil(T/64)][D] fp32: the states before tokens
+ *                     0, 64, 128 ... of each row of the batch, whatever sequence
  *                     they are in (written by the forward, read by the backward,
  *                     which computes them itself if NULL).
  * Backward: dy [B,T,D], dhT like hT or NULL -> dx, dr, di [B,T,D] with row
  * strides, dlam [D] fp32, dh0 like h0 or NULL.  lam is finite or -infinity;
  * decays below 2^-125 are taken as that.  Row strides of its tensors are below
  * 2^24 elements. */
-#define RDN_GSCAN_CHUNK 128
+#define RDN_GSCAN_CHUNK 64
 typedef struct {
   int B, T, D, dtype;
   float c;

@@ -38,7 +38,7 @@ EXPORTS = ["rla_fwd", "rdn_fwd", "rla_bwd", "rdn_bwd", "rdn_decode_step", "rla_f
            "rdn_linear_bwd", "rdn_linear_bwd_workspace_size"]
 
 SCAN_CHUNK = 16  # RDN_SCAN_CHUNK
-GSCAN_CHUNK = 128  # RDN_GSCAN_CHUNK
+GSCAN_CHUNK = 64  # RDN_GSCAN_CHUNK
 RDN_E4M3 = 2  # rdn_linear_args.dtype
 
 

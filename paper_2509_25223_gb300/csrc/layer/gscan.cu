@@ -55,7 +55,8 @@ constexpr int kTok = 8, kWarps = 8, kTile = 2 * kTok * kWarps, kThreads = 32 * k
 constexpr int kLanes = 16;   // lanes of a span
 constexpr int kCluster = 8;  // the most CTAs of a cluster
 constexpr int kFwdCtas = 3, kBwdCtas = 2;  // resident on an SM (80 and 128 registers a thread, nothing spilled)
-static_assert(kTile == RDN_GSCAN_CHUNK, "a tile starts at every kept state");
+constexpr int kKeep = RDN_GSCAN_CHUNK;  // tokens from one kept state to the next
+static_assert(kKeep == kTok * kWarps && kTile == 2 * kKeep, "a tile, and its half, start at a kept state");
 
 struct GP {
   int B, T, D, nc, strips, num_seqs, num_slots;
@@ -394,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
   const Place<V> at(p);
   const int me = threadIdx.x;
   const uint32_t row0 = (uint32_t)at.b * (uint32_t)p.T + (uint32_t)at.token();  // (B T is at most 2^30)
-  const int ntiles = (p.T + kTile - 1) / kTile, round = p.nc * kTile;
+  const int nkept = (p.T + kKeep - 1) / kKeep, round = p.nc * kTile;
   const f2 k = rate<V>(p, at.ch);
   f2 carry = !kPacked && p.h0 ? ldf<V>(p.h0 + (size_t)at.b * p.D + at.ch) : both(0.f);
   pass_through<V, kPacked>(p, at, p.h0, p.hT);
@@ -446,8 +447,8 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
     __syncthreads();
     exchange<false, kPacked>(p, spans[par], tiles[par], &bars[par], phase, at.rank);
     f2 in = fold<false, kPacked>(spans[par], tiles[par], at.lane, at.rank, p.nc, at.warp, carry);
-    if (p.chunks && at.live && at.warp == 0 && at.half == 0 && tile0 < p.T)
-      stf<V>(p.chunks + ((size_t)at.b * ntiles + tile0 / kTile) * p.D + at.ch, in);
+    if (p.chunks && at.live && at.token() % kKeep == 0 && left > 0)
+      stf<V>(p.chunks + ((size_t)at.b * nkept + (tile0 + at.token()) / kKeep) * p.D + at.ch, in);
     if (at.half) in = over<kPacked>(other, in);
     if (at.live) {
       if (p.y) {
@@ -481,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
 // channels, so that a tile is 64 tokens of 128 bytes, and the tiles come to shared memory a round ahead
 // (and go from there) as whole boxes: no addresses are worked out per row, which are a quarter of
 // fwd_kernel's instructions, and the spans of a thread's tokens stay in its registers.
-constexpr int kWide = 64, kTileTma = kTok * kWarps;  // channels and tokens of a box
+constexpr int kWide = 64, kTileTma = kKeep;  // channels and tokens of a box
 struct alignas(64) TileMap { unsigned char b[128]; };
 struct FwdMaps { TileMap x, r, i, y; };
 struct FwdTiles {
@@ -513,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
   __shared__ int2 mark[2][kPacked ? kTileTma : 1];
   __shared__ uint64_t bars[2], full[2];
   const WidePlace at(p);
-  const int round = p.nc * kTileTma, nchunks = (p.T + kTile - 1) / kTile;
+  const int round = p.nc * kTileTma, nkept = (p.T + kKeep - 1) / kKeep;
   auto fetch = [&](int t, int s) {  // by one thread
     tc::mbar_expect_tx(&full[s], (uint32_t)sizeof(sm.in[s]));
     tc::tma_load_3d(sm.in[s][0], &maps.r, at.strip, t, at.b, &full[s]);
@@ -568,8 +569,8 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
     __syncwarp();
     exchange<false, kPacked>(p, spans[par], tiles[par], &bars[par], phase, at.rank);
     const f2 in = fold<false, kPacked>(spans[par], tiles[par], at.lane, at.rank, p.nc, at.warp, carry);
-    if (p.chunks && at.live && at.warp == 0 && tile0 < p.T && tile0 % kTile == 0)
-      stf<2>(p.chunks + ((size_t)at.b * nchunks + tile0 / kTile) * p.D + at.ch, in);
+    if (p.chunks && at.live && at.warp == 0 && tile0 < p.T)
+      stf<2>(p.chunks + ((size_t)at.b * nkept + tile0 / kKeep) * p.D + at.ch, in);
     if (p.y) {
       if (at.lane == 0) tc::bulk_wait_read();  // the round before has left the warp's rows
       __syncwarp();
@@ -622,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
   const Place<V> at(p);
   const int me = threadIdx.x;
   const uint32_t row0 = (uint32_t)at.b * (uint32_t)p.T + (uint32_t)at.token();  // (B T is at most 2^30)
-  const int ntiles = (p.T + kTile - 1) / kTile, round = p.nc * kTile;
+  const int nkept = (p.T + kKeep - 1) / kKeep, round = p.nc * kTile;
   const f2 k = rate<V>(p, at.ch), one = both(1.f);
   f2 carry = !kPacked && p.dhT ? ldf<V>(p.dhT + (size_t)at.b * p.D + at.ch) : both(0.f);
   f2 sum = both(0.f);
@@ -647,7 +648,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
     Raw xr[kTok], gr[kTok];
     load_rows<T, V>(xr, p.x, p.x_ld, row0 + tile0, at.ch, full, left);
     load_rows<T, V>(gr, p.dy, p.dy_ld, row0 + tile0, at.ch, full, left);
-    f2 h = tile0 < p.T ? ldf<V>(p.chunks + ((size_t)at.b * ntiles + tile0 / kTile) * p.D + at.ch) : both(0.f);
+    f2 h = tile0 < p.T ? ldf<V>(p.chunks + ((size_t)at.b * nkept + tile0 / kKeep) * p.D + at.ch) : both(0.f);
     if (kPacked) {
       mark_tile(p, tile0, mark[par]);
       __syncthreads();
@@ -750,6 +751,150 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
     f2 s = kept.u[0][at.lane];
     for (int w = 1; w < 2 * kWarps; ++w) s = add2(s, kept.u[0][w * kLanes + at.lane]);
     stf<V>(p.part + ((size_t)at.b * p.nc + at.rank) * p.D + at.ch, s);
+  }
+}
+
+// ---- backward for bf16 rows on 16 bytes: tiles by TMA, as fwd_tma_kernel.  The results take the inputs'
+// places in the stage, from where they are copied out while the next round runs on the other.
+struct BwdMaps { TileMap x, r, i, dy, dx, dr, di; };
+struct BwdTiles {
+  __nv_bfloat16 in[2][4][kTileTma][kWide];  // r, i, x, dy; then dr, di, dx
+  f2 si[kTok][kThreads];
+};
+
+template <bool kPacked>
+__global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p, const __grid_constant__ BwdMaps maps) {
+  using bf = __nv_bfloat16;
+  extern __shared__ __align__(128) unsigned char dynamic[];
+  BwdTiles &sm = *reinterpret_cast<BwdTiles *>(dynamic + ((128 - (tc::smem_u32(dynamic) & 127)) & 127));
+  __shared__ Span fspans[2][kWarps][32], spans[2][kWarps][32], tiles[2][kCluster][32];
+  __shared__ int2 mark[2][kPacked ? kTileTma : 1];
+  __shared__ uint64_t bars[2], full[2];
+  const WidePlace at(p);
+  const int me = threadIdx.x, first = at.warp * kTok;
+  const int round = p.nc * kTileTma, nkept = (p.T + kKeep - 1) / kKeep;
+  auto fetch = [&](int t, int s) {  // by one thread
+    tc::mbar_expect_tx(&full[s], (uint32_t)sizeof(sm.in[s]));
+    tc::tma_load_3d(sm.in[s][0], &maps.r, at.strip, t, at.b, &full[s]);
+    tc::tma_load_3d(sm.in[s][1], &maps.i, at.strip, t, at.b, &full[s]);
+    tc::tma_load_3d(sm.in[s][2], &maps.x, at.strip, t, at.b, &full[s]);
+    tc::tma_load_3d(sm.in[s][3], &maps.dy, at.strip, t, at.b, &full[s]);
+  };
+  const int last = (p.T - 1) / round * round;
+  int tile0 = last + at.rank * kTileTma;
+  if (threadIdx.x == 0) {
+    tc::mbar_init(&full[0], 1);
+    tc::mbar_init(&full[1], 1);
+    tc::mbar_init(&bars[0], 1);
+    tc::mbar_init(&bars[1], 1);
+    tc::fence_mbar_init();
+    fetch(tile0, 0);
+  }
+  const f2 k = rate<2>(p, at.ch), one = both(1.f);
+  f2 carry = !kPacked && p.dhT ? ldf<2>(p.dhT + (size_t)at.b * p.D + at.ch) : both(0.f);
+  f2 sum = both(0.f);
+  pass_through<2, kPacked>(p, at, p.dhT, p.dh0);
+  __syncthreads();
+  if (p.nc > 1) tc::cluster_sync();  // the barriers are there, and every CTA of the cluster runs
+
+  int par = 0;  // also the stage
+  uint32_t phase = 0;
+  for (int base = last; base >= 0; base -= round, tile0 -= round, phase ^= par, par ^= 1) {
+    const int left = p.T - tile0 - first;
+    f2 h = tile0 < p.T ? ldf<2>(p.chunks + ((size_t)at.b * nkept + tile0 / kKeep) * p.D + at.ch) : both(0.f);
+    if (kPacked) {
+      mark_tile<kTileTma>(p, tile0, mark[par]);
+      __syncthreads();
+    }
+    if (!tc::mbar_wait(&full[par], phase) && p.status) atomicExch(p.status, (int)RDN_ERR_TIMEOUT);
+    auto cell = [&](int which, int j) { return &sm.in[par][which][first + j][at.lane * 2]; };
+    auto word = [&](int which, int j) -> uint32_t & { return *reinterpret_cast<uint32_t *>(cell(which, j)); };
+    // this thread's span from a zero state, both ways
+    Span fwd = {one, both(0.f)}, back = fwd;
+    f2 u[kTok], ms[kTok];
+#pragma unroll
+    for (int j = 0; j < kTok; ++j) {
+      const Gate g = gate(get2<bf, 2>(Pack<bf, 2>::ld(cell(0, j))), get2<bf, 2>(Pack<bf, 2>::ld(cell(1, j))), k);
+      float lo, hi;  // sigmoid(r) stays in the two cells that it came from
+      unpack2(g.sr, lo, hi);
+      word(0, j) = __float_as_uint(lo);
+      word(1, j) = __float_as_uint(hi);
+      sm.si[j][me] = g.si;
+      // (a token past the row's end changes nothing: a = 1, no input)
+      u[j] = j < left ? g.u : both(0.f);
+      ms[j] = mul2(sqrt2(rest(u[j])), g.si);
+      const f2 a = one_minus(u[j]);
+      f2 b = mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j))));
+      const int start = kPacked ? mark[par][first + j].x : -1;
+      if (kPacked && start >= 0) {
+        if (p.h0) b = fma2(a, ldf<2>(p.h0 + (size_t)start * p.D + at.ch), b);
+        fwd = {both(-1.f), b};
+      } else {
+        step<kPacked>(fwd, a, b);
+      }
+    }
+#pragma unroll
+    for (int j = kTok - 1; j >= 0; --j) {
+      const f2 a = one_minus(u[j]);
+      const int end = kPacked ? mark[par][first + j].y : -1;
+      if (kPacked && end >= 0) back = {both(-1.f), p.dhT ? ldf<2>(p.dhT + (size_t)end * p.D + at.ch) : both(0.f)};
+      step<kPacked>(back, a, mul2(a, get2<bf, 2>(Pack<bf, 2>::ld(cell(3, j)))));
+    }
+    fspans[par][at.warp][at.lane] = fwd;
+    spans[par][at.warp][at.lane] = back;
+    if (at.lane == 0) tc::bulk_wait_read();  // the round before has left the other stage
+    __syncthreads();
+    if (threadIdx.x == 0 && base >= round) fetch(tile0 - round, par ^ 1);
+    __syncwarp();
+    exchange<true, kPacked>(p, spans[par], tiles[par], &bars[par], phase, at.rank);
+    f2 q = fold<true, kPacked>(spans[par], tiles[par], at.lane, at.rank, p.nc, at.warp, carry);
+#pragma unroll 1
+    for (int w = 0; w < at.warp; ++w) h = over<kPacked>(fspans[par][w][at.lane], h);
+    f2 before[kTok];  // the state before each token
+#pragma unroll
+    for (int j = 0; j < kTok; ++j) {
+      const int start = kPacked ? mark[par][first + j].x : -1;
+      if (kPacked && start >= 0) h = p.h0 ? ldf<2>(p.h0 + (size_t)start * p.D + at.ch) : both(0.f);
+      before[j] = h;
+      h = fma2(one_minus(u[j]), h, mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j)))));
+    }
+#pragma unroll
+    for (int j = kTok - 1; j >= 0; --j) {
+      const int2 f = kPacked ? mark[par][first + j] : make_int2(-1, -1);
+      if (kPacked && f.y >= 0) q = p.dhT ? ldf<2>(p.dhT + (size_t)f.y * p.D + at.ch) : both(0.f);
+      const f2 sr = pack2(__uint_as_float(word(0, j)), __uint_as_float(word(1, j)));
+      const f2 a = one_minus(u[j]), t = log2_decay(k, sr), b = mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j))));
+      const f2 g = add2(get2<bf, 2>(Pack<bf, 2>::ld(cell(3, j))), q), ag = mul2(a, g);
+      // w / ln 2 = a g t (h_{t-1} - a b / (1 - a^2)): 0 where a is 1, for t and b are
+      const f2 w = mul2(mul2(ag, t), sub2(before[j], mul2(mul2(a, b), rcp2(rest(u[j])))));
+      if (j < left) sum = add2(sum, w);
+      q = ag;
+      put2<bf, 2>(cell(2, j), mul2(g, ms[j]));
+      put2<bf, 2>(cell(0, j), mul2(w, each(sr, [](float s) { return fmaf(s, -kLn2, kLn2); })));
+      put2<bf, 2>(cell(1, j), mul2(mul2(g, b), one_minus(sm.si[j][me])));
+      if (kPacked && p.dh0 && at.live && f.x >= 0) stf<2>(p.dh0 + (size_t)f.x * p.D + at.ch, q);
+    }
+    tc::fence_async_smem();
+    __syncwarp();
+    if (at.lane == 0 && left > 0) {  // (what is past the tensors' ends is left out)
+      tc::tma_store_3d(&maps.dr, at.strip, tile0 + first, at.b, sm.in[par][0][first]);
+      tc::tma_store_3d(&maps.di, at.strip, tile0 + first, at.b, sm.in[par][1][first]);
+      tc::tma_store_3d(&maps.dx, at.strip, tile0 + first, at.b, sm.in[par][2][first]);
+      tc::bulk_commit();
+    }
+    if (!kPacked && p.dh0 && at.live && tile0 + first == 0) stf<2>(p.dh0 + (size_t)at.b * p.D + at.ch, q);
+    __syncwarp();
+  }
+  if (at.lane == 0) tc::bulk_wait_all();
+  // sum of w over this CTA's tokens, the warps in order
+  __syncthreads();
+  if (p.nc > 1) tc::cluster_sync();  // (what this CTA sent has arrived)
+  sm.si[0][me] = sum;
+  __syncthreads();
+  if (at.warp == 0 && at.live) {
+    f2 s = sm.si[0][at.lane];
+    for (int w = 1; w < kWarps; ++w) s = add2(s, sm.si[0][w * 32 + at.lane]);
+    stf<2>(p.part + ((size_t)at.b * p.nc + at.rank) * p.D + at.ch, s);
   }
 }
 
@@ -866,35 +1011,42 @@ bool make_tiles(TileMap *m, const void *p, const rdn_gscan_args &a, long long ld
   return rdn::make_rows_map(m, p, a.D, a.T, a.B, ld, kWide, tokens);
 }
 // bf16, an even D, rows (pointers and distances) on 16 bytes, and distances that a map can hold.
-bool tma_ok(const rdn_gscan_args &a) {
+bool tma_ok(const rdn_gscan_args &a, std::initializer_list<const void *> ptrs, std::initializer_list<long long> lds) {
   if (a.dtype != RDN_BF16 || (a.D & 1) || a.T < 1) return false;
-  for (long long ld : {a.x_ld, a.r_ld, a.i_ld, a.y_ld})
-    if (ld * 2 * a.T >= (1ll << 40)) return false;
-  const uintptr_t bits = (uintptr_t)a.x | (uintptr_t)a.r | (uintptr_t)a.i | (uintptr_t)a.y | (uintptr_t)(a.x_ld * 2) |
-                         (uintptr_t)(a.r_ld * 2) | (uintptr_t)(a.i_ld * 2) | (uintptr_t)(a.y_ld * 2);
-  return (bits & 15) == 0;
+  for (const void *q : ptrs)
+    if ((uintptr_t)q & 15) return false;
+  for (long long ld : lds)
+    if ((ld * 2) & 15 || ld * 2 * a.T >= (1ll << 40)) return false;
+  return true;
 }
-cudaError_t run_tma(const rdn_gscan_args &a, cudaStream_t s) {
-  FwdMaps maps{};
-  if (!make_tiles(&maps.x, a.x, a, a.x_ld, kTileTma) || !make_tiles(&maps.r, a.r, a, a.r_ld, kTileTma) ||
-      !make_tiles(&maps.i, a.i, a, a.i_ld, kTileTma) || (a.y && !make_tiles(&maps.y, a.y, a, a.y_ld, kTok)))
-    return cudaErrorInvalidValue;
-  GP p = params(a, 2, false);
-  p.strips = (a.D + kWide - 1) / kWide;
-  // CTAs of a cluster: what fills 95 % of the places in one go, and no more: a round costs a CTA more in a
-  // cluster (256 units of 4096 tokens 136 us with one, 145 with two; 128 units 77 with three, 97 with
-  // one); of 8 few clusters find a place (64 units of 16384 tokens: 148 us with six, 183 with eight).
-  const long long units = (long long)a.B * p.strips, places = 152 * kFwdCtas * 95 / 100, tiles = (a.T + kTileTma - 1) / kTileTma;
-  const long long nc = units > places ? 1 : places / units, most = tiles < 6 ? tiles : 6;
-  p.nc = (int)(nc < most ? nc : most);
-  auto kern = a.cu_seqlens ? fwd_tma_kernel<true> : fwd_tma_kernel<false>;
-  constexpr int kBytes = sizeof(FwdTiles) + 128;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+bool fwd_tma_ok(const rdn_gscan_args &a) {
+  return tma_ok(a, {a.x, a.r, a.i, a.y}, {a.x_ld, a.r_ld, a.i_ld, a.y_ld});
+}
+bool bwd_tma_ok(const rdn_gscan_args &a) {
+  return tma_ok(a, {a.x, a.r, a.i, a.dy, a.dx, a.dr, a.di},
+                {a.x_ld, a.r_ld, a.i_ld, a.dy_ld, a.dx_ld, a.dr_ld, a.di_ld});
+}
+// Strips, and CTAs of a cluster: what fills 95 % of the places in one go, and no more: a round costs a CTA more
+// in a cluster (forward, 256 units of 4096 tokens 136 us with one, 145 with two; 128 units 77 with three, 97
+// with one); of 8 few clusters find a place (64 units of 16384 tokens 148 us with six, 183 with eight).
+int tma_strips(const rdn_gscan_args &a) { return (a.D + kWide - 1) / kWide; }
+int tma_cluster(const rdn_gscan_args &a, bool bwd) {
+  const long long units = (long long)a.B * tma_strips(a), places = 152 * (bwd ? kBwdCtas : kFwdCtas) * 95 / 100;
+  const long long tiles = (a.T + kTileTma - 1) / kTileTma, nc = units > places ? 1 : places / units;
+  const long long most = tiles < 1 ? 1 : tiles < 6 ? tiles : 6;
+  return (int)(nc < most ? nc : most);
+}
+template <typename Kern, typename M>
+cudaError_t go_tma(Kern kern, GP p, const M &maps, const rdn_gscan_args &a, bool bwd, size_t bytes, const char *name,
+                   cudaStream_t s) {
+  p.strips = tma_strips(a);
+  p.nc = tma_cluster(a, bwd);
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes + 128);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)((long long)p.B * p.strips * p.nc));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kBytes;
+  cfg.dynamicSmemBytes = bytes + 128;
   cfg.stream = s;
   cudaLaunchAttribute at;
   at.id = cudaLaunchAttributeClusterDimension;
@@ -902,20 +1054,41 @@ cudaError_t run_tma(const rdn_gscan_args &a, cudaStream_t s) {
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  RDN_LAUNCH("gscan_fwd", s, (e = cudaLaunchKernelEx(&cfg, kern, p, maps)));
+  RDN_LAUNCH(name, s, (e = cudaLaunchKernelEx(&cfg, kern, p, maps)));
   return e;
 }
+cudaError_t run_fwd_tma(const rdn_gscan_args &a, cudaStream_t s) {
+  FwdMaps m{};
+  if (!make_tiles(&m.x, a.x, a, a.x_ld, kTileTma) || !make_tiles(&m.r, a.r, a, a.r_ld, kTileTma) ||
+      !make_tiles(&m.i, a.i, a, a.i_ld, kTileTma) || (a.y && !make_tiles(&m.y, a.y, a, a.y_ld, kTok)))
+    return cudaErrorInvalidValue;
+  return go_tma(a.cu_seqlens ? fwd_tma_kernel<true> : fwd_tma_kernel<false>, params(a, 2, false), m, a, false,
+                sizeof(FwdTiles), "gscan_fwd", s);
+}
+cudaError_t run_bwd_tma(const rdn_gscan_args &a, const GP &p, cudaStream_t s) {
+  BwdMaps m{};
+  if (!make_tiles(&m.x, a.x, a, a.x_ld, kTileTma) || !make_tiles(&m.r, a.r, a, a.r_ld, kTileTma) ||
+      !make_tiles(&m.i, a.i, a, a.i_ld, kTileTma) || !make_tiles(&m.dy, a.dy, a, a.dy_ld, kTileTma) ||
+      !make_tiles(&m.dx, a.dx, a, a.dx_ld, kTok) || !make_tiles(&m.dr, a.dr, a, a.dr_ld, kTok) ||
+      !make_tiles(&m.di, a.di, a, a.di_ld, kTok))
+    return cudaErrorInvalidValue;
+  return go_tma(a.cu_seqlens ? bwd_tma_kernel<true> : bwd_tma_kernel<false>, p, m, a, true, sizeof(BwdTiles), "gscan_bwd", s);
+}
 
-// (for one or two channels a lane: the query sees no pointers)
+// (the largest of the kernels' clusters: the query sees no pointers)
 size_t part_bytes(const rdn_gscan_args &a) {
-  const int one = cluster_of(a.T, units_of(a, 1), true), two = cluster_of(a.T, units_of(a, 2), true);
-  return round256(sizeof(float) * (size_t)a.B * (one > two ? one : two) * a.D);
+  int most = tma_cluster(a, true);
+  for (int V = 1; V <= 2; ++V) {
+    const int nc = cluster_of(a.T, units_of(a, V), true);
+    if (nc > most) most = nc;
+  }
+  return round256(sizeof(float) * (size_t)a.B * most * a.D);
 }
 
 }  // namespace gscan
 
 long long gscan_slots(const rdn_gscan_args &a) {
-  return (long long)a.B * ((a.T + gscan::kTile - 1) / gscan::kTile);
+  return (long long)a.B * ((a.T + gscan::kKeep - 1) / gscan::kKeep);
 }
 // CTAs of a call at one channel a lane, the most it may take.
 long long gscan_ctas(const rdn_gscan_args &a) {
@@ -928,7 +1101,7 @@ size_t gscan_bwd_bytes(const rdn_gscan_args &a) {
 
 cudaError_t launch_gscan_fwd(const rdn_gscan_args &a, cudaStream_t s) {
   const size_t e = a.dtype == RDN_BF16 ? 2 : 4;
-  if (gscan::tma_ok(a)) return gscan::run_tma(a, s);
+  if (gscan::fwd_tma_ok(a)) return gscan::run_fwd_tma(a, s);
   const int V = gscan::pairs_ok(a.D, e, {a.x, a.r, a.i, a.y}, {a.x_ld, a.r_ld, a.i_ld, a.y_ld}) ? 2 : 1;
   return gscan::run(gscan::params(a, V, false), false, a.dtype, V, "gscan_fwd", s);
 }
@@ -950,10 +1123,11 @@ cudaError_t launch_gscan_bwd(const rdn_gscan_args &a, cudaStream_t s) {
                                 {a.x_ld, a.r_ld, a.i_ld, a.dy_ld, a.dx_ld, a.dr_ld, a.di_ld}) ? 2 : 1;
   gscan::GP p = gscan::params(c, V, true);
   p.part = static_cast<float *>(a.workspace);
-  cudaError_t e = gscan::run(p, true, a.dtype, V, "gscan_bwd", s);
+  const bool tma = gscan::bwd_tma_ok(c);
+  cudaError_t e = tma ? gscan::run_bwd_tma(c, p, s) : gscan::run(p, true, a.dtype, V, "gscan_bwd", s);
   if (e != cudaSuccess) return e;
-  RDN_LAUNCH("gscan_dlam", s,
-             (gscan::dlam_kernel<<<(a.D + 31) / 32, dim3(32, 16), 0, s>>>(p, (long long)p.B * p.nc, a.dlam)));
+  const long long parts = (long long)p.B * (tma ? gscan::tma_cluster(c, true) : p.nc);
+  RDN_LAUNCH("gscan_dlam", s, (gscan::dlam_kernel<<<(a.D + 31) / 32, dim3(32, 16), 0, s>>>(p, parts, a.dlam)));
   return cudaGetLastError();
 }
 

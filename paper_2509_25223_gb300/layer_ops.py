@@ -513,8 +513,8 @@ def gated_scan_fwd(x, r, i, lam, c=8.0, h0=None, cu_seqlens=None, return_final_s
         h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(i_t) x_t,   y_t = h_t
 
     x, r, i [B,T,d]; lam [d] fp32; h0 [B or num_seqs, d] fp32.  Returns (y, hT);
-    with return_chunk_states also the states before every 128 tokens
-    [B, ceil(T/128), d], which gated_scan_bwd can read instead of computing them
+    with return_chunk_states also the states before every 64 tokens
+    [B, ceil(T/64), d], which gated_scan_bwd can read instead of computing them
     again; only y with both off.  cu_seqlens: packed sequences."""
     a = _Gated(x, r, i, lam, c, h0, cu_seqlens)
     dev = a.dev

@@ -34,15 +34,15 @@ def make(B, T, D, dtype, lens=None, state=True, pad=0, seed=0):
 
 
 def loop(v, c, lens):
-    """(y, last states, states before every 128th token of a row)"""
+    """(y, last states, states before every 64th token of a row)"""
     la = -c * torch.nn.functional.softplus(v["lam"], threshold=700.0) * torch.sigmoid(v["r"])
     a, b = torch.exp(la), torch.sqrt(-torch.expm1(2 * la)) * torch.sigmoid(v["i"]) * v["x"]
     y, last, kept, D = [], [], [], v["x"].shape[2]
     for s, (row, lo, hi) in enumerate(ref.spans(v["x"], lens)):
         h = torch.zeros(D, dtype=torch.float64) if v["h0"] is None else v["h0"][s]
         for t in range(lo, hi):
-            if t % 128 == 0 and t > lo:
-                kept.append((row, t // 128, h.detach()))
+            if t % 64 == 0 and t > lo:
+                kept.append((row, t // 64, h.detach()))
             h = a[row, t] * h + b[row, t]
             y.append(h)
         last.append(h)
@@ -50,23 +50,23 @@ def loop(v, c, lens):
     return y, torch.stack(last), kept
 
 
-def compare(x, c=8.0, lens=None, dhT=True, keep=True):
+def compare(x, c=8.0, lens=None, dhT=True, keep=True, times=1):
     y, hT, hc = rdn.gated_scan_fwd(x["x"], x["r"], x["i"], x["lam"], c, x["h0"], x["cu"], return_chunk_states=True)
     v = {k: ref.double(x[k], True) for k in ("x", "r", "i", "lam", "h0")}
     yr, hr, kept = loop(v, c, lens)
-    ref.check("y", y, yr, T32)
-    ref.check("hT", hT, hr, T32)
+    ref.check("y", y, yr, times * T32)
+    ref.check("hT", hT, hr, times * T32)
     for row, k, h in kept:
-        ref.check("h_chunks", hc[row, k], h, T32)
+        ref.check("h_chunks", hc[row, k], h, times * T32)
     d = rdn.gated_scan_bwd(x["x"], x["r"], x["i"], x["lam"], x["dy"], c, x["h0"], x["dhT"] if dhT else None, x["cu"],
                            h_chunks=hc if keep else None)
     g = ref.grads([(yr, ref.double(x["dy"]))] + ([(hr, ref.double(x["dhT"]))] if dhT else []), v)
     for k, n in (("dx", "x"), ("dr", "r"), ("di", "i")):
-        ref.check(k, d[k], g[n], TGRAD)
-    ref.check("dlam", d["dlam"], g["lam"], TSUM)
+        ref.check(k, d[k], g[n], times * TGRAD)
+    ref.check("dlam", d["dlam"], g["lam"], times * TSUM)
     assert ("dh0" in d) == (x["h0"] is not None)
     if x["h0"] is not None:
-        ref.check("dh0", d["dh0"], g["h0"], TGRAD)
+        ref.check("dh0", d["dh0"], g["h0"], times * TGRAD)
     return y, hT, hc, d
 
 
@@ -76,7 +76,7 @@ def test_lengths(T, dtype):
     compare(make(2, T, 40, dtype, seed=T))
 
 
-@pytest.mark.parametrize("D", [1, 2, 3, 31, 33, 64, 65, 130, 512])
+@pytest.mark.parametrize("D", [1, 2, 3, 8, 31, 33, 40, 64, 65, 72, 130, 512])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_channels(D, dtype):
     compare(make(2, 70, D, dtype, seed=D))
@@ -88,9 +88,10 @@ def test_options(state, dhT, keep):
     compare(make(3, 150, 64, "bf16", state=state), dhT=dhT, keep=keep)
 
 
-def test_many_rounds():
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rounds(dtype):
     """Rows longer than the tokens that a cluster has at one time, kept states or not: the same bits."""
-    x = make(1, 1300, 66, "f32", seed=4)
+    x = make(1, 1300, 72, dtype, seed=4)
     a = rdn.gated_scan_fwd(x["x"], x["r"], x["i"], x["lam"], h0=x["h0"], return_chunk_states=True)
     v = {k: ref.double(x[k]) for k in ("x", "r", "i", "lam", "h0")}
     yr, hr, _ = loop(v, 8.0, None)
@@ -108,12 +109,13 @@ def test_strided_rows(pad, dtype):
     compare(make(2, 40, 96, dtype, pad=pad))
 
 
-def test_odd_addresses():
-    x = make(1, 70, 64, "bf16")
-    wide = {k: torch.cat([x[k][..., :1], x[k]], -1)[..., 1:] for k in ("x", "r", "i", "dy")}
-    a, b = compare(x)[3], compare({**x, **wide})[3]
-    for k in a:
-        assert torch.equal(a[k], b[k]), k
+@pytest.mark.parametrize("lens", [None, [30, 0, 100, 70]])
+@pytest.mark.parametrize("off", [1, 2])
+def test_odd_addresses(off, lens):
+    """Rows that do not start on 16 bytes."""
+    x = make(1, 200, 64, "bf16", lens=lens)
+    wide = {k: torch.cat([x[k][..., :off], x[k]], -1)[..., off:] for k in ("x", "r", "i", "dy")}
+    compare({**x, **wide}, lens=lens)
 
 
 @pytest.mark.parametrize("lens", [[5], [0, 1, 2, 3, 0, 40, 64, 0], [1] * 20, [0, 0], [130, 0, 7], [64, 64, 1], [200, 199]])
@@ -123,27 +125,11 @@ def test_packed(lens, D):
     compare(make(1, sum(lens), D, "bf16", lens=lens, state=False), lens=lens, keep=False)
 
 
-def test_packed_many_rounds():
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_packed_many_rounds(dtype):
+    """(sequences of up to 700 tokens: 2^-25 of the state a token, twice the bounds above)"""
     lens = [600, 0, 3, 700, 64, 1]
-    x = make(1, sum(lens), 64, "f32", lens=lens, seed=9)
-    y, hT, hc = rdn.gated_scan_fwd(x["x"], x["r"], x["i"], x["lam"], h0=x["h0"], cu_seqlens=x["cu"],
-                                   return_chunk_states=True)
-    d = rdn.gated_scan_bwd(x["x"], x["r"], x["i"], x["lam"], x["dy"], h0=x["h0"], dhT=x["dhT"], cu_seqlens=x["cu"],
-                           h_chunks=hc)
-    at = 0
-    for s, n in enumerate(lens):
-        if not n:
-            assert torch.equal(hT[s], x["h0"][s]) and torch.equal(d["dh0"][s], x["dhT"][s])
-            continue
-        p = {k: x[k][:, at:at + n].contiguous() for k in ("x", "r", "i", "dy")}
-        y1, h1 = rdn.gated_scan_fwd(p["x"], p["r"], p["i"], x["lam"], h0=x["h0"][s:s + 1])
-        d1 = rdn.gated_scan_bwd(p["x"], p["r"], p["i"], x["lam"], p["dy"], h0=x["h0"][s:s + 1], dhT=x["dhT"][s:s + 1])
-        ref.check("y", y[:, at:at + n], y1.double().cpu(), 2 * T32)
-        ref.check("hT", hT[s], h1[0].double().cpu(), 2 * T32)
-        for k in ("dx", "dr", "di"):
-            ref.check(k, d[k][:, at:at + n], d1[k].double().cpu(), 2 * TGRAD)
-        ref.check("dh0", d["dh0"][s], d1["dh0"][0].double().cpu(), 2 * TGRAD)
-        at += n
+    compare(make(1, sum(lens), 64, dtype, lens=lens, seed=9), lens=lens, times=2)
 
 
 def test_no_tokens():
@@ -246,19 +232,28 @@ def test_gradient_by_differences():
         assert abs(slope - want) <= 1e-2 * abs(want), (n, slope, want)
 
 
-def test_outputs_given_and_their_surroundings():
-    """Results written into slices of wider tensors leave what is beside them."""
+@pytest.mark.parametrize("off", [8, 4])
+def test_outputs_given_and_their_surroundings(off):
+    """Results written into slices of wider tensors leave what is beside them.  (Rows that do not start on 16
+    bytes take other kernels, which add up in another order: each within its bound of the exact
+    values, so within twice that of one another.)"""
     x = make(2, 70, 40, "bf16")
     y, _, hc = rdn.gated_scan_fwd(x["x"], x["r"], x["i"], x["lam"], h0=x["h0"], return_chunk_states=True)
     d = rdn.gated_scan_bwd(x["x"], x["r"], x["i"], x["lam"], x["dy"], h0=x["h0"], h_chunks=hc)
-    wide = {k: torch.full((2, 70, 48), 7.0, device="cuda", dtype=torch.bfloat16) for k in ("y", "dx", "dr", "di")}
-    rdn.gated_scan_fwd(x["x"], x["r"], x["i"], x["lam"], h0=x["h0"], out=wide["y"][..., 4:44])
+    wide = {k: torch.full((2, 70, 56), 7.0, device="cuda", dtype=torch.bfloat16) for k in ("y", "dx", "dr", "di")}
+    rdn.gated_scan_fwd(x["x"], x["r"], x["i"], x["lam"], h0=x["h0"], out=wide["y"][..., off:off + 40])
     rdn.gated_scan_bwd(x["x"], x["r"], x["i"], x["lam"], x["dy"], h0=x["h0"], h_chunks=hc,
-                       out={k: wide[k][..., 4:44] for k in ("dx", "dr", "di")})
+                       out={k: wide[k][..., off:off + 40] for k in ("dx", "dr", "di")})
     for k, t in dict(d, y=y).items():
         if k in wide:
-            assert torch.equal(wide[k][..., 4:44], t), k
-            assert (wide[k][..., :4] == 7).all() and (wide[k][..., 44:] == 7).all()
+            got = wide[k][..., off:off + 40]
+            if off == 8:
+                assert torch.equal(got, t), k
+            else:
+                g, r = got.double(), t.double()
+                most = torch.maximum(g.abs(), r.abs())
+                assert ((g - r).abs() <= 2 * (TGRAD * (most + r.pow(2).mean().sqrt()) + 2.0 ** -8 * most)).all(), k
+            assert (wide[k][..., :off] == 7).all() and (wide[k][..., off + 40:] == 7).all()
 
 
 def test_same_bits_other_stream_and_graph():
