@@ -73,6 +73,11 @@ struct DpP {
   __nv_bfloat16 *dp;
   float *part;  // [gridDim.y][N], or NULL
 };
+template <int kAct>
+__device__ __forceinline__ void scale_by_grad(float (&g)[8], const float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) g[j] *= act_grad(kAct, v[j]);
+}
 __global__ void __launch_bounds__(256) dp_kernel(const DpP p) {
   using P8 = Pack<__nv_bfloat16, 8>;
   __shared__ float sh[8][32 * 8 + 8];
@@ -82,20 +87,33 @@ __global__ void __launch_bounds__(256) dp_kernel(const DpP p) {
   float sum[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum[j] = 0.f;
-  if (live)
-    for (long long m = (long long)blockIdx.y * 8 + warp; m < p.M; m += (long long)gridDim.y * 8) {
+  if (live) {
+    // two rows at a time: their loads are in flight together
+    const long long stride = (long long)gridDim.y * 8;
+    auto put = [&](long long m, const typename P8::Raw &gy, const typename P8::Raw &gp) {
       float g[8];
-      P8::get(P8::ld(p.dy + m * p.dy_ld + n), g);
+      P8::get(gy, g);
       if (p.act) {
         float v[8];
-        P8::get(P8::ld(p.pre + m * p.N + n), v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] *= act_grad(p.act, v[j]);
+        P8::get(gp, v);
+        if (p.act == 1) scale_by_grad<1>(g, v);
+        else if (p.act == 2) scale_by_grad<2>(g, v);
+        else scale_by_grad<3>(g, v);
         if (p.dp) P8::st(p.dp + m * p.N + n, P8::put(g));
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[j] += g[j];
+    };
+    for (long long m = (long long)blockIdx.y * 8 + warp; m < p.M; m += 2 * stride) {
+      const bool two = m + stride < p.M;
+      const typename P8::Raw g0 = P8::ld(p.dy + m * p.dy_ld + n);
+      const typename P8::Raw g1 = two ? P8::ld(p.dy + (m + stride) * p.dy_ld + n) : P8::zero();
+      const typename P8::Raw v0 = p.act ? P8::ld(p.pre + m * p.N + n) : P8::zero();
+      const typename P8::Raw v1 = p.act && two ? P8::ld(p.pre + (m + stride) * p.N + n) : P8::zero();
+      put(m, g0, v0);
+      if (two) put(m + stride, g1, v1);
     }
+  }
   if (!p.part) return;
 #pragma unroll
   for (int j = 0; j < 8; ++j) sh[warp][j * 33 + lane] = sum[j];

@@ -191,7 +191,7 @@ cudaError_t launch_norm_q8(const rdn_norm_q8_args &a, cudaStream_t s) {
   p.warps = (groups + nv - 1) / nv;
   const int per = p.warps >= 4 ? 1 : 4 / p.warps;
   const int threads = 32 * p.warps * per;
-  const long long need = (a.rows + per - 1) / per, most = (long long)kSMs * 16;
+  const long long need = (a.rows + per - 1) / per, most = (long long)kSMs * 4;
   const int ctas = (int)(need < most ? need : most);
   const bool xb = a.x_dtype == RDN_BF16, fb = a.f ? a.f_dtype == RDN_BF16 : xb;
   typedef __nv_bfloat16 bf;
