@@ -64,6 +64,11 @@ def _stride(name, t, lead):
     it (an expanded axis, of stride 0, does not, nor does a slice of the tokens of several
     batch rows)."""
     shape, strides = t.shape, t.stride()
+    if lead == 2 and len(shape) == 3:  # (the common case: a slice of a projection's rows)
+        n0, n1, width = shape
+        s0, ld, one = strides
+        if one == 1 and ld >= width and n1 > 1 and (n0 == 1 or s0 == ld * n1):
+            return ld
     width = 1
     for a in range(len(shape) - 1, lead - 1, -1):
         if shape[a] != 1 and strides[a] != width:
@@ -486,14 +491,16 @@ class _Gated:
     """The operands of a gated recurrence, checked, as the leading values of GSCAN_PACK."""
 
     def __init__(self, x, r, i, lam, c, h0, cu_seqlens):
-        self.dev, self.shape = _cuda("x", x, 3)
-        dev, self.dtype = self.dev, x.dtype
-        b, t, d = self.shape
+        self.dev, self.shape = dev, shape = _cuda("x", x, 3)
+        self.dtype = ty = x.dtype
+        b, t, d = shape
         self.cu, self.ns, self.n = _table(cu_seqlens, b, dev)
         self.states = (self.n, d)
-        rows = [_rows(n, v, self.shape, x.dtype, dev) for n, v in (("x", x), ("r", r), ("i", i))]
-        self.head = (b, t, d, _code(x.dtype), float(c))
-        self.lds, self.ptrs = [v[1] for v in rows], [v[0] for v in rows]
+        px, x_ld = _rows("x", x, shape, ty, dev)
+        pr, r_ld = _rows("r", r, shape, ty, dev)
+        pi, i_ld = _rows("i", i, shape, ty, dev)
+        self.head = (b, t, d, _code(ty), float(c))
+        self.lds, self.ptrs = (x_ld, r_ld, i_ld), (px, pr, pi)
         self.params = (_whole("lam", lam, (d,), _F32, dev), _whole("h0", h0, self.states, _F32, dev))
 
     def chunks(self):
@@ -517,15 +524,25 @@ def gated_scan_fwd(x, r, i, lam, c=8.0, h0=None, cu_seqlens=None, return_final_s
     [B, ceil(T/64), d], which gated_scan_bwd can read instead of computing them
     again; only y with both off.  cu_seqlens: packed sequences."""
     a = _Gated(x, r, i, lam, c, h0, cu_seqlens)
-    dev = a.dev
-    y = torch.empty(a.shape, dtype=a.dtype, device=dev) if out is None else out
-    hT = torch.empty(a.states, dtype=_F32, device=dev) if return_final_state else None
-    hc = torch.empty(a.chunks(), dtype=_F32, device=dev) if return_chunk_states else None
-    args = a.pack(_rows("out", y, a.shape, a.dtype, dev), 0 if hT is None else hT.data_ptr(),
-                  0 if hc is None else hc.data_ptr())
-    _call("rdn_gscan_fwd", args, dev)
-    res = (y,) + ((hT,) if return_final_state else ()) + ((hc,) if return_chunk_states else ())
-    return res if len(res) > 1 else y
+    dev, shape = a.dev, a.shape
+    hT = hc = None
+    phT = phc = 0
+    if out is None:
+        y = torch.empty(shape, dtype=a.dtype, device=dev)
+        py = (y.data_ptr(), 0)
+    else:
+        y = out
+        py = _rows("out", y, shape, a.dtype, dev)
+    if return_final_state:
+        hT = torch.empty(a.states, dtype=_F32, device=dev)
+        phT = hT.data_ptr()
+    if return_chunk_states:
+        hc = torch.empty(a.chunks(), dtype=_F32, device=dev)
+        phc = hc.data_ptr()
+    _call("rdn_gscan_fwd", a.pack(py, phT, phc), dev)
+    if return_final_state:
+        return (y, hT, hc) if return_chunk_states else (y, hT)
+    return (y, hc) if return_chunk_states else y
 
 
 def gated_scan_bwd(x, r, i, lam, dy, c=8.0, h0=None, dhT=None, cu_seqlens=None, h_chunks=None,
@@ -563,7 +580,9 @@ def gated_scan_step(x, r, i, lam, h, c=8.0, slots=None, out=None):
     dev, shape = _cuda("x", x, 2)
     n, d = shape
     ty = x.dtype
-    rows = [_rows(k, v, shape, ty, dev, 1) for k, v in (("x", x), ("r", r), ("i", i))]
+    px, x_ld = _rows("x", x, shape, ty, dev, 1)
+    pr, r_ld = _rows("r", r, shape, ty, dev, 1)
+    pi, i_ld = _rows("i", i, shape, ty, dev, 1)
     if out is None:
         y = torch.empty(shape, dtype=ty, device=dev)
         py, y_ld = y.data_ptr(), 0
@@ -572,9 +591,8 @@ def gated_scan_step(x, r, i, lam, h, c=8.0, slots=None, out=None):
         py, y_ld = _rows("out", y, shape, ty, dev, 1)
     num = h.shape[0]
     args = _abi.GSCAN_STEP_PACK(
-        n, d, _code(ty), float(c), num, *(v[1] for v in rows), y_ld, *(v[0] for v in rows),
-        _whole("lam", lam, (d,), _F32, dev), _whole("h", h, (num, d), _F32, dev),
-        _whole("slots", slots, (n,), torch.int32, dev), py)
+        n, d, _code(ty), float(c), num, x_ld, r_ld, i_ld, y_ld, px, pr, pi, _whole("lam", lam, (d,), _F32, dev),
+        _whole("h", h, (num, d), _F32, dev), _whole("slots", slots, (n,), torch.int32, dev), py)
     _call("rdn_gscan_step", args, dev)
     return y
 
@@ -593,26 +611,36 @@ def add_norm_q8(x, f=None, weight=None, eps=1e-6, out=None):
     operand of linear_fwd.  out: (r, q, scale) to write into; r may be x.
     Backward (straight through the rounding): block_norm_bwd(x=r,
     weight_next=weight, dr=dr, dh=dh)["dx"] is the gradient of x and of f."""
-    dev, shape = x.get_device(), x.shape
+    dev, shape, ty = x.get_device(), x.shape, x.dtype
     if dev < 0 or not shape:
         raise ValueError("rdn: tensors must be on a CUDA device, with at least one axis")
-    d, lead = shape[-1], len(shape) - 1
-    r, q, s = out if out is not None else (None, None, None)
-    if f is None:
-        r, pr = x, 0
-    elif r is None:
-        r = torch.empty(shape, dtype=x.dtype, device=dev)
-        pr = r.data_ptr()
+    d, lead, over = shape[-1], len(shape) - 1, shape[:-1]
+    px, x_ld = _rows("x", x, shape, ty, dev, lead)
+    pf = f_ld = pr = fc = 0
+    if f is not None:
+        pf, f_ld = _rows("f", f, shape, f.dtype, dev, lead)
+        fc = _code(f.dtype)
+    if out is None:
+        if f is None:
+            r = x
+        else:
+            r = torch.empty(shape, dtype=ty, device=dev)
+            pr = r.data_ptr()
+        q = torch.empty(shape, dtype=_E4M3, device=dev)
+        s = torch.empty(over, dtype=_F32, device=dev)
+        pq, ps = q.data_ptr(), s.data_ptr()
     else:
-        pr = _whole("r", r, shape, x.dtype, dev)
-    q = torch.empty(shape, dtype=_E4M3, device=dev) if q is None else q
-    s = torch.empty(shape[:-1], dtype=_F32, device=dev) if s is None else s
-    px, x_ld = _rows("x", x, shape, x.dtype, dev, lead)
-    pf, f_ld = (0, 0) if f is None else _rows("f", f, shape, f.dtype, dev, lead)
-    rows = x.numel() // d if d else 0
-    args = _abi.NORM_Q8_PACK(rows, d, _code(x.dtype), 0 if f is None else _code(f.dtype), float(eps),
-                             x_ld, f_ld, px, pf, _whole("weight", weight, (d,), _F32, dev), pr,
-                             _whole("q", q, shape, _E4M3, dev), _whole("scale", s, shape[:-1], _F32, dev))
+        r, q, s = out
+        if f is None:
+            r = x
+        else:
+            r = torch.empty(shape, dtype=ty, device=dev) if r is None else r
+            pr = _whole("r", r, shape, ty, dev)
+        q = torch.empty(shape, dtype=_E4M3, device=dev) if q is None else q
+        s = torch.empty(over, dtype=_F32, device=dev) if s is None else s
+        pq, ps = _whole("q", q, shape, _E4M3, dev), _whole("scale", s, over, _F32, dev)
+    args = _abi.NORM_Q8_PACK(over.numel(), d, _code(ty), fc, float(eps), x_ld, f_ld, px, pf,
+                             _whole("weight", weight, (d,), _F32, dev), pr, pq, ps)
     _call("rdn_norm_q8", args, dev)
     return r, q, s
 
@@ -628,18 +656,14 @@ def _act(act):
 
 def _linear_operands(x, w):
     """(device, rows' shape, M, N, K, x's and w's (address, row stride))"""
-    dev, shape = x.get_device(), x.shape
+    dev, shape, ty = x.get_device(), x.shape, x.dtype
     if dev < 0 or not shape:
         raise ValueError("rdn: tensors must be on a CUDA device, with at least one axis")
-    if w.dim() != 2 or w.shape[1] != shape[-1]:
-        raise ValueError(f"rdn: w must be [N, {shape[-1]}] (got {tuple(w.shape)})")
-    n, k = w.shape
-    lead = shape[:-1]
-    m = 1
-    for v in lead:
-        m *= v
-    return (dev, lead, m, n, k, _rows("x", x, shape, x.dtype, dev, len(lead)),
-            _rows("w", w, w.shape, x.dtype, dev, 1))
+    ws, lead = w.shape, shape[:-1]
+    if len(ws) != 2 or ws[1] != shape[-1]:
+        raise ValueError(f"rdn: w must be [N, {shape[-1]}] (got {tuple(ws)})")
+    n, k = ws
+    return (dev, lead, lead.numel(), n, k, _rows("x", x, shape, ty, dev, len(lead)), _rows("w", w, ws, ty, dev, 1))
 
 
 def linear_fwd(x, w, bias=None, act=None, residual=None, x_scale=None, w_scale=None, out_dtype=None,
@@ -658,20 +682,33 @@ def linear_fwd(x, w, bias=None, act=None, residual=None, x_scale=None, w_scale=N
     q8 = x.dtype is _E4M3
     if not q8 and x.dtype is not torch.bfloat16:
         raise ValueError(f"rdn: unsupported dtype {x.dtype}")
-    if q8 != (x_scale is not None) or q8 != (w_scale is not None):
+    pxs = pws = pb = bt = pr = r_ld = pp = 0
+    if q8:
+        if x_scale is None or w_scale is None:
+            raise ValueError("rdn: 8-bit operands need x_scale and w_scale")
+        pxs, pws = _whole("x_scale", x_scale, lead, _F32, dev), _whole("w_scale", w_scale, (n,), _F32, dev)
+    elif x_scale is not None or w_scale is not None:
         raise ValueError("rdn: x_scale and w_scale go with 8-bit operands")
-    ty = out_dtype or (out.dtype if out is not None else torch.bfloat16 if residual is None else residual.dtype)
     shape = (*lead, n)
-    pr, r_ld = (0, 0) if residual is None else _rows("residual", residual, shape, ty, dev, len(lead))
-    y = torch.empty(shape, dtype=ty, device=dev) if out is None else out
-    py, y_ld = _rows("out", y, shape, ty, dev, len(lead))
-    pre = torch.empty(shape, dtype=torch.bfloat16, device=dev) if return_pre else None
-    args = _abi.LINEAR_PACK(
-        m, n, k, _abi.RDN_E4M3 if q8 else _abi.RDN_BF16, _code(ty), 0 if bias is None else _code(bias.dtype),
-        _act(act), x_ld, w_ld, r_ld, y_ld, px, pw, _whole("x_scale", x_scale, lead, _F32, dev),
-        _whole("w_scale", w_scale, (n,), _F32, dev),
-        0 if bias is None else _whole("bias", bias, (n,), bias.dtype, dev), pr, py,
-        0 if pre is None else pre.data_ptr(), 0, 0, 0, 0, 0, 0, 0, 0)
+    if out_dtype is not None:
+        ty = out_dtype
+    else:
+        ty = out.dtype if out is not None else torch.bfloat16 if residual is None else residual.dtype
+    if residual is not None:
+        pr, r_ld = _rows("residual", residual, shape, ty, dev, len(lead))
+    if bias is not None:
+        bt, pb = _code(bias.dtype), _whole("bias", bias, (n,), bias.dtype, dev)
+    if out is None:
+        y = torch.empty(shape, dtype=ty, device=dev)
+        py, y_ld = y.data_ptr(), 0
+    else:
+        y = out
+        py, y_ld = _rows("out", y, shape, ty, dev, len(lead))
+    if return_pre:
+        pre = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        pp = pre.data_ptr()
+    args = _abi.LINEAR_PACK(m, n, k, _abi.RDN_E4M3 if q8 else _abi.RDN_BF16, _code(ty), bt, _act(act), x_ld, w_ld,
+                            r_ld, y_ld, px, pw, pxs, pws, pb, pr, py, pp, 0, 0, 0, 0, 0, 0, 0, 0)
     _call("rdn_linear_fwd", args, dev)
     return (y, pre) if return_pre else y
 

@@ -78,6 +78,9 @@ CASES = [
     ("rdn_gscan_fwd", _gscan(c=float("nan")), INVALID, "c must be"),
     ("rdn_gscan_fwd", _gscan(c=float("inf")), INVALID, "c must be"),
     ("rdn_gscan_fwd", _gscan(r_ld=127), INVALID, "r_ld"),
+    ("rdn_gscan_fwd", _gscan(i_ld=1 << 24), UNSUPPORTED, "2^24"),
+    ("rdn_gscan_bwd", _gscan(di_ld=1 << 24), UNSUPPORTED, "2^24"),
+    ("rdn_gscan_fwd", _gscan(i_ld=(1 << 24) - 1), LAUNCH, "injected"),
     ("rdn_gscan_fwd", _gscan(x=0), INVALID, "x is NULL"),
     ("rdn_gscan_fwd", _gscan(T=0, x=0, r=0, i=0, y=0), LAUNCH, "injected"),
     ("rdn_gscan_fwd", _gscan(i=FAKE + 1), MISALIGNED, "i is not"),
@@ -88,7 +91,7 @@ CASES = [
     ("rdn_gscan_fwd", _gscan(B=1, cu_seqlens=FAKE, num_seqs=0), INVALID, "num_seqs"),
     ("rdn_gscan_fwd", _gscan(h0=AT, hT=AT + 2 * 128 * 4 - 4), INVALID, "overlaps"),
     ("rdn_gscan_fwd", _gscan(h0=AT, hT=AT + 2 * 128 * 4), LAUNCH, "injected"),
-    ("rdn_gscan_fwd", _gscan(h0=AT, h_chunks=AT - 2 * 2 * 128 * 4 + 4), INVALID, "overlaps"),
+    ("rdn_gscan_fwd", _gscan(h0=AT, h_chunks=AT - 2 * 4 * 128 * 4 + 4), INVALID, "overlaps"),
     ("rdn_gscan_fwd", _gscan(hT=AT, h_chunks=AT), INVALID, "overlaps"),
     ("rdn_gscan_bwd", _gscan(), LAUNCH, "injected"),
     ("rdn_gscan_bwd", _gscan(dy=0), INVALID, "dy"),
@@ -171,8 +174,8 @@ def test_entry_points(fn, args, status, says):
 
 def test_workspace_sizes():
     lib, n = _abi.load(), ctypes.c_size_t(0)
-    # the sums of 2 x 2 CTAs a strip, and the kept states where they are not given
-    for kept, want in ((0, 2 * 2 * 128 * 4 * 2), (FAKE, 2 * 2 * 128 * 4)):
+    # the sums of a row's CTAs (4 tiles of 64 tokens: 4), and the kept states where they are not given
+    for kept, want in ((0, 2 * 4 * 128 * 4 * 2), (FAKE, 2 * 4 * 128 * 4)):
         assert lib.rdn_gscan_bwd_workspace_size(ctypes.byref(_gscan(h_chunks=kept)), ctypes.byref(n)) == 0
         assert n.value == want
     assert lib.rdn_gscan_bwd_workspace_size(ctypes.byref(_gscan()), None) == INVALID
