@@ -126,6 +126,8 @@ NormQ8Args, NORM_Q8_PACK = _layout(
 LinearArgs, LINEAR_PACK = _layout(
     "LinearArgs", "q M; i N K dtype y_dtype bias_dtype act; q x_ld w_ld res_ld y_ld; P x w x_scale"
     " w_scale bias res y pre; i dw_dtype; q dy_ld; P dy dx dw dbias workspace; n workspace_bytes")
+# the workspace and its size at the end of GscanArgs and LinearArgs, put in once the size is known
+WORKSPACE_PACK = struct.Struct("@PN").pack
 
 _lib = None
 _decode_step = None

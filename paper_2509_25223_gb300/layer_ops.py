@@ -155,6 +155,13 @@ def _workspace(workspace, nbytes, dev):
     return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=dev)
 
 
+def _with_workspace(query, args, workspace, dev):
+    """args, whose last two fields are the workspace and its bytes, with a workspace of the size that `query`
+    asks for."""
+    ws = _workspace(workspace, _size(query, args), dev)
+    return ws, args[:-16] + _abi.WORKSPACE_PACK(ws.data_ptr(), ws.numel() * ws.element_size())
+
+
 def _silu(activation):
     if activation not in ("silu", None):
         raise ValueError('rdn: activation must be "silu" or None')
@@ -552,24 +559,33 @@ def gated_scan_bwd(x, r, i, lam, dy, c=8.0, h0=None, dhT=None, cu_seqlens=None, 
     Returns a dict with dx, dr, di, dlam (fp32) and, with h0, dh0.  out: tensors
     to write into, by those names."""
     a = _Gated(x, r, i, lam, c, h0, cu_seqlens)
-    dev, d = a.dev, a.shape[2]
-    res = dict(out) if out else {}
-    for name in ("dx", "dr", "di"):
-        if res.get(name) is None:
-            res[name] = torch.empty(a.shape, dtype=a.dtype, device=dev)
-    if res.get("dlam") is None:
-        res["dlam"] = torch.empty(d, dtype=_F32, device=dev)
-    if h0 is not None and res.get("dh0") is None:
-        res["dh0"] = torch.empty(a.states, dtype=_F32, device=dev)
-    rows = [_rows(n, v, a.shape, a.dtype, dev)
-            for n, v in (("dy", dy), ("dx", res["dx"]), ("dr", res["dr"]), ("di", res["di"]))]
-    grads = ([v[1] for v in rows] + [rows[0][0], _whole("dhT", dhT, a.states, _F32, dev)]
-             + [v[0] for v in rows[1:]] + [_whole("dlam", res["dlam"], (d,), _F32, dev),
-                                           _whole("dh0", res.get("dh0"), a.states, _F32, dev)])
-    hc = _whole("h_chunks", h_chunks, a.chunks(), _F32, dev)
-    ws = _workspace(workspace, _size("rdn_gscan_bwd_workspace_size", a.pack(chunks=hc)), dev)
-    _call("rdn_gscan_bwd", a.pack(chunks=hc, grads=grads, ws=ws.data_ptr(),
-                                  nbytes=ws.numel() * ws.element_size()), dev)
+    dev, shape, ty = a.dev, a.shape, a.dtype
+    d = shape[2]
+    pdy, dy_ld = _rows("dy", dy, shape, ty, dev)
+    if out is None:
+        dx, dr = torch.empty(shape, dtype=ty, device=dev), torch.empty(shape, dtype=ty, device=dev)
+        di, dlam = torch.empty(shape, dtype=ty, device=dev), torch.empty(d, dtype=_F32, device=dev)
+        res = dict(dx=dx, dr=dr, di=di, dlam=dlam)
+        if h0 is not None:
+            res["dh0"] = torch.empty(a.states, dtype=_F32, device=dev)
+    else:
+        res = dict(out)
+        for name in ("dx", "dr", "di"):
+            if res.get(name) is None:
+                res[name] = torch.empty(shape, dtype=ty, device=dev)
+        if res.get("dlam") is None:
+            res["dlam"] = torch.empty(d, dtype=_F32, device=dev)
+        if h0 is not None and res.get("dh0") is None:
+            res["dh0"] = torch.empty(a.states, dtype=_F32, device=dev)
+        dx, dr, di, dlam = res["dx"], res["dr"], res["di"], res["dlam"]
+    pdx, dx_ld = _rows("dx", dx, shape, ty, dev)
+    pdr, dr_ld = _rows("dr", dr, shape, ty, dev)
+    pdi, di_ld = _rows("di", di, shape, ty, dev)
+    grads = (dy_ld, dx_ld, dr_ld, di_ld, pdy, _whole("dhT", dhT, a.states, _F32, dev), pdx, pdr, pdi,
+             _whole("dlam", dlam, (d,), _F32, dev), _whole("dh0", res.get("dh0"), a.states, _F32, dev))
+    args = a.pack(chunks=_whole("h_chunks", h_chunks, a.chunks(), _F32, dev), grads=grads)
+    ws, args = _with_workspace("rdn_gscan_bwd_workspace_size", args, workspace, dev)
+    _call("rdn_gscan_bwd", args, dev)
     return res
 
 
@@ -726,22 +742,35 @@ def linear_bwd(x, w, dy, pre=None, act=None, bias=None, need_dx=True, need_dw=Tr
     bf = torch.bfloat16
     if x.dtype is not bf:
         raise ValueError(f"rdn: unsupported dtype {x.dtype}")
-    res = dict(out) if out else {}
-    wt = dw_dtype or (res["dw"].dtype if res.get("dw") is not None else w.dtype)
-    for name, shape, ty, wanted in (("dx", x.shape, bf, need_dx), ("dw", w.shape, wt, need_dw),
-                                    ("dbias", (n,), None if bias is None else bias.dtype, bias is not None)):
-        if wanted and res.get(name) is None:
-            res[name] = torch.empty(shape, dtype=ty, device=dev)
-        elif not wanted:
-            res.pop(name, None)
     if act is not None and pre is None:
         raise ValueError("rdn: the backward of an activation needs pre")
     pdy, dy_ld = _rows("dy", dy, (*lead, n), bf, dev, len(lead))
-    bt = 0 if bias is None else _code(bias.dtype)
-    head = (m, n, k, _abi.RDN_BF16, 0, bt, _act(act), x_ld, w_ld, 0, 0, px, pw, 0, 0, 0, 0, 0,
-            0 if act is None else _whole("pre", pre, (*lead, n), bf, dev), _code(wt), dy_ld, pdy,
-            _whole("dx", res.get("dx"), x.shape, bf, dev), _whole("dw", res.get("dw"), w.shape, wt, dev),
-            0 if bias is None else _whole("dbias", res["dbias"], (n,), bias.dtype, dev))
-    ws = _workspace(workspace, _size("rdn_linear_bwd_workspace_size", _abi.LINEAR_PACK(*head, 0, 0)), dev)
-    _call("rdn_linear_bwd", _abi.LINEAR_PACK(*head, ws.data_ptr(), ws.numel() * ws.element_size()), dev)
+    res = dict(out) if out else {}
+    pdx = pdw = pdb = bt = pp = 0
+    wt = dw_dtype or (res["dw"].dtype if res.get("dw") is not None else w.dtype)
+    if need_dx:
+        if res.get("dx") is None:
+            res["dx"] = torch.empty(x.shape, dtype=bf, device=dev)
+        pdx = _whole("dx", res["dx"], x.shape, bf, dev)
+    else:
+        res.pop("dx", None)
+    if need_dw:
+        if res.get("dw") is None:
+            res["dw"] = torch.empty(w.shape, dtype=wt, device=dev)
+        pdw = _whole("dw", res["dw"], w.shape, wt, dev)
+    else:
+        res.pop("dw", None)
+    if bias is not None:
+        bt = _code(bias.dtype)
+        if res.get("dbias") is None:
+            res["dbias"] = torch.empty(n, dtype=bias.dtype, device=dev)
+        pdb = _whole("dbias", res["dbias"], (n,), bias.dtype, dev)
+    else:
+        res.pop("dbias", None)
+    if act is not None:
+        pp = _whole("pre", pre, (*lead, n), bf, dev)
+    args = _abi.LINEAR_PACK(m, n, k, _abi.RDN_BF16, 0, bt, _act(act), x_ld, w_ld, 0, 0, px, pw, 0, 0, 0, 0, 0, pp,
+                            _code(wt), dy_ld, pdy, pdx, pdw, pdb, 0, 0)
+    ws, args = _with_workspace("rdn_linear_bwd_workspace_size", args, workspace, dev)
+    _call("rdn_linear_bwd", args, dev)
     return res
