@@ -385,6 +385,19 @@ __device__ __forceinline__ void pass_through(const GP &p, const At &at, const fl
   }
 }
 
+// Whether a tile of packed tokens holds no first or last token of a sequence: the sequence (begin, end) of its
+// first token, kept from round to round, answers it without a look at the table.
+struct Inside {
+  int begin = 0, end = 0;
+  __device__ bool plain(int tile0, int tokens) const { return begin < tile0 && tile0 + tokens < end; }
+  __device__ void move(const GP &p, int tile0) {  // to the tile at tile0
+    if (tile0 < 0 || tile0 >= p.T || (begin <= tile0 && tile0 < end)) return;
+    const SeqSpan q = find_seq(p.cu, p.num_seqs, p.T, 0, tile0);
+    begin = (int)q.begin;
+    end = (int)q.end;
+  }
+};
+
 template <typename T, int V, bool kPacked>
 __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
   using Raw = typename Pack<T, V>::Raw;
@@ -403,6 +416,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
   exchange_init(p, bars);
   int par = 0, tile0 = at.rank * kTile;
   uint32_t phase = 0;
+  Inside inside;
   Raw xr[kTok], rr[kTok], ir[kTok];
   auto fetch = [&](int t) {
     const bool full = t + kTile <= p.T;
@@ -414,7 +428,9 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
   fetch(tile0);
   for (int base = 0; base < p.T; base += round, tile0 += round, phase ^= par, par ^= 1) {
     const int left = p.T - tile0 - at.token();
-    if (kPacked) {
+    if (kPacked) inside.move(p, tile0);
+    const bool marked = kPacked && !inside.plain(tile0, kTile);
+    if (marked) {
       mark_tile(p, tile0, mark[par]);
       __syncthreads();
     }
@@ -423,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
       const Gate g = gate(get2<T, V>(rr[j]), get2<T, V>(ir[j]), k);
       const f2 a = one_minus(g.u);
       f2 b = mul2(mul2(sqrt2(rest(g.u)), g.si), get2<T, V>(xr[j]));
-      const int start = kPacked ? mark[par][at.token() + j].x : -1;
+      const int start = marked ? mark[par][at.token() + j].x : -1;
       if (kPacked && start >= 0) {
         if (p.h0) b = fma2(a, ldf<V>(p.h0 + (size_t)start * p.D + at.ch), b);
         all = {both(-1.f), b};
@@ -463,12 +479,12 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
         }
       }
       if (p.hT) {
-        if (kPacked) {
+        if (marked) {
           for (int j = 0; j < kTok; ++j) {
             const int end = mark[par][at.token() + j].y;
             if (end >= 0) stf<V>(p.hT + (size_t)end * p.D + at.ch, over<kPacked>(kept[j][me], in));
           }
-        } else if (left >= 1 && left <= kTok) {  // the row's last token
+        } else if (!kPacked && left >= 1 && left <= kTok) {  // the row's last token
           stf<V>(p.hT + (size_t)at.b * p.D + at.ch, over<kPacked>(all, in));
         }
       }
@@ -483,6 +499,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
 // (and go from there) as whole boxes: no addresses are worked out per row, which are a quarter of
 // fwd_kernel's instructions, and the spans of a thread's tokens stay in its registers.
 constexpr int kWide = 64, kTileTma = kKeep;  // channels and tokens of a box
+constexpr int kTmaUnits = 36;
 struct alignas(64) TileMap { unsigned char b[128]; };
 struct FwdMaps { TileMap x, r, i, y; };
 struct FwdTiles {
@@ -539,9 +556,12 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
 
   int par = 0;  // also the stage
   uint32_t phase = 0;
+  Inside inside;
   for (int base = 0; base < p.T; base += round, tile0 += round, phase ^= par, par ^= 1) {
     const int first = at.warp * kTok, left = p.T - tile0 - first;
-    if (kPacked) {
+    if (kPacked) inside.move(p, tile0);
+    const bool marked = kPacked && !inside.plain(tile0, kTileTma);
+    if (marked) {
       mark_tile<kTileTma>(p, tile0, mark[par]);
       __syncthreads();
     }
@@ -554,7 +574,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
                           get2<bf, 2>(Pack<bf, 2>::ld(&sm.in[par][1][first + j][at.lane * 2])), k);
       const f2 a = one_minus(g.u);
       f2 b = mul2(mul2(sqrt2(rest(g.u)), g.si), get2<bf, 2>(Pack<bf, 2>::ld(&sm.in[par][2][first + j][at.lane * 2])));
-      const int start = kPacked ? mark[par][first + j].x : -1;
+      const int start = marked ? mark[par][first + j].x : -1;
       if (kPacked && start >= 0) {
         if (p.h0) b = fma2(a, ldf<2>(p.h0 + (size_t)start * p.D + at.ch), b);
         all = {both(-1.f), b};
@@ -584,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
       }
     }
     if (p.hT && at.live) {
-      if (kPacked) {
+      if (marked) {
         for (int j = 0; j < kTok; ++j) {
           const int end = mark[par][first + j].y;
           if (end >= 0) {
@@ -593,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
               if (q == j) stf<2>(p.hT + (size_t)end * p.D + at.ch, over<kPacked>(kept[q], in));
           }
         }
-      } else if (left >= 1 && left <= kTok) {  // the row's last token
+      } else if (!kPacked && left >= 1 && left <= kTok) {  // the row's last token
 #pragma unroll
         for (int q = 0; q < kTok; ++q)
           if (q == left - 1) stf<2>(p.hT + (size_t)at.b * p.D + at.ch, over<kPacked>(kept[q], in));
@@ -615,7 +635,7 @@ struct Kept {
 template <typename T, int V, bool kPacked>
 __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
   using Raw = typename Pack<T, V>::Raw;
-  extern __shared__ __align__(16) unsigned char dynamic[];
+  extern __shared__ __align__(128) unsigned char dynamic[];
   Kept &kept = *reinterpret_cast<Kept *>(dynamic);
   __shared__ Span fspans[2][kWarps][kLanes], spans[2][kWarps][kLanes], tiles[2][kCluster][kLanes];
   __shared__ int2 mark[2][kPacked ? kTile : 1];
@@ -632,6 +652,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
   exchange_init(p, bars);
   int par = 0;
   uint32_t phase = 0;
+  Inside inside;
   const int last = p.T > 0 ? (p.T - 1) / round * round : -1;
   int tile0 = last + at.rank * kTile;
   Raw rr[kTok], ir[kTok];
@@ -649,7 +670,9 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
     load_rows<T, V>(xr, p.x, p.x_ld, row0 + tile0, at.ch, full, left);
     load_rows<T, V>(gr, p.dy, p.dy_ld, row0 + tile0, at.ch, full, left);
     f2 h = tile0 < p.T ? ldf<V>(p.chunks + ((size_t)at.b * nkept + tile0 / kKeep) * p.D + at.ch) : both(0.f);
-    if (kPacked) {
+    if (kPacked) inside.move(p, tile0);
+    const bool marked = kPacked && !inside.plain(tile0, kTile);
+    if (marked) {
       mark_tile(p, tile0, mark[par]);
       __syncthreads();
     }
@@ -663,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
       const f2 a = one_minus(g.u), ms = mul2(sqrt2(rest(g.u)), g.si);
       kept.ms[j][me] = ms;
       f2 b = mul2(ms, get2<T, V>(xr[j]));
-      const int start = kPacked ? mark[par][at.token() + j].x : -1;
+      const int start = marked ? mark[par][at.token() + j].x : -1;
       if (kPacked && start >= 0) {
         if (p.h0) b = fma2(a, ldf<V>(p.h0 + (size_t)start * p.D + at.ch), b);
         fwd = {both(-1.f), b};
@@ -673,7 +696,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
     };
     auto behind = [&](int j) {
       const f2 a = one_minus(kept.u[j][me]);
-      const int end = kPacked ? mark[par][at.token() + j].y : -1;
+      const int end = marked ? mark[par][at.token() + j].y : -1;
       if (kPacked && end >= 0) back = {both(-1.f), p.dhT ? ldf<V>(p.dhT + (size_t)end * p.D + at.ch) : both(0.f)};
       step<kPacked>(back, a, mul2(a, get2<T, V>(gr[j])));
     };
@@ -702,7 +725,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
     if (at.half) h = over<kPacked>(fother, h);
     else q = over<kPacked>(other, q);
     auto again = [&](int j) {
-      const int start = kPacked ? mark[par][at.token() + j].x : -1;
+      const int start = marked ? mark[par][at.token() + j].x : -1;
       if (kPacked && start >= 0) h = p.h0 ? ldf<V>(p.h0 + (size_t)start * p.D + at.ch) : both(0.f);
       kept.before[j][me] = h;
       h = fma2(one_minus(kept.u[j][me]), h, mul2(kept.ms[j][me], get2<T, V>(xr[j])));
@@ -710,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
     const Rows<T> dx(p.dx, p.dx_ld, row0 + tile0, at.ch), dr(p.dr, p.dr_ld, row0 + tile0, at.ch),
         di(p.di, p.di_ld, row0 + tile0, at.ch);
     auto grads = [&](int j) {
-      const int2 f = kPacked ? mark[par][at.token() + j] : make_int2(-1, -1);
+      const int2 f = marked ? mark[par][at.token() + j] : make_int2(-1, -1);
       if (kPacked && f.y >= 0) q = p.dhT ? ldf<V>(p.dhT + (size_t)f.y * p.D + at.ch) : both(0.f);
       const f2 u = kept.u[j][me], sr = kept.sr[j][me], ms = kept.ms[j][me];
       const f2 a = one_minus(u), t = log2_decay(k, sr), b = mul2(ms, get2<T, V>(xr[j]));
@@ -799,10 +822,13 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
 
   int par = 0;  // also the stage
   uint32_t phase = 0;
+  Inside inside;
   for (int base = last; base >= 0; base -= round, tile0 -= round, phase ^= par, par ^= 1) {
     const int left = p.T - tile0 - first;
     f2 h = tile0 < p.T ? ldf<2>(p.chunks + ((size_t)at.b * nkept + tile0 / kKeep) * p.D + at.ch) : both(0.f);
-    if (kPacked) {
+    if (kPacked) inside.move(p, tile0);
+    const bool marked = kPacked && !inside.plain(tile0, kTileTma);
+    if (marked) {
       mark_tile<kTileTma>(p, tile0, mark[par]);
       __syncthreads();
     }
@@ -825,7 +851,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
       ms[j] = mul2(sqrt2(rest(u[j])), g.si);
       const f2 a = one_minus(u[j]);
       f2 b = mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j))));
-      const int start = kPacked ? mark[par][first + j].x : -1;
+      const int start = marked ? mark[par][first + j].x : -1;
       if (kPacked && start >= 0) {
         if (p.h0) b = fma2(a, ldf<2>(p.h0 + (size_t)start * p.D + at.ch), b);
         fwd = {both(-1.f), b};
@@ -836,7 +862,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
 #pragma unroll
     for (int j = kTok - 1; j >= 0; --j) {
       const f2 a = one_minus(u[j]);
-      const int end = kPacked ? mark[par][first + j].y : -1;
+      const int end = marked ? mark[par][first + j].y : -1;
       if (kPacked && end >= 0) back = {both(-1.f), p.dhT ? ldf<2>(p.dhT + (size_t)end * p.D + at.ch) : both(0.f)};
       step<kPacked>(back, a, mul2(a, get2<bf, 2>(Pack<bf, 2>::ld(cell(3, j)))));
     }
@@ -853,14 +879,14 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
     f2 before[kTok];  // the state before each token
 #pragma unroll
     for (int j = 0; j < kTok; ++j) {
-      const int start = kPacked ? mark[par][first + j].x : -1;
+      const int start = marked ? mark[par][first + j].x : -1;
       if (kPacked && start >= 0) h = p.h0 ? ldf<2>(p.h0 + (size_t)start * p.D + at.ch) : both(0.f);
       before[j] = h;
       h = fma2(one_minus(u[j]), h, mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j)))));
     }
 #pragma unroll
     for (int j = kTok - 1; j >= 0; --j) {
-      const int2 f = kPacked ? mark[par][first + j] : make_int2(-1, -1);
+      const int2 f = marked ? mark[par][first + j] : make_int2(-1, -1);
       if (kPacked && f.y >= 0) q = p.dhT ? ldf<2>(p.dhT + (size_t)f.y * p.D + at.ch) : both(0.f);
       const f2 sr = pack2(__uint_as_float(word(0, j)), __uint_as_float(word(1, j)));
       const f2 a = one_minus(u[j]), t = log2_decay(k, sr), b = mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j))));
@@ -1010,9 +1036,12 @@ cudaError_t run(const GP &p, bool bwd, int dtype, int V, const char *name, cudaS
 bool make_tiles(TileMap *m, const void *p, const rdn_gscan_args &a, long long ld, int tokens) {
   return rdn::make_rows_map(m, p, a.D, a.T, a.B, ld, kWide, tokens);
 }
-// bf16, an even D, rows (pointers and distances) on 16 bytes, and distances that a map can hold.
+// bf16, an even D, rows (pointers and distances) on 16 bytes, distances that a map can hold, and enough strips:
+// the other kernels' are half as wide, and with few of them fill more of the GPU (32 strips of 32768 tokens
+// 211 us by TMA, 174 without; 40 strips of 4096 tokens 35 and 38).
 bool tma_ok(const rdn_gscan_args &a, std::initializer_list<const void *> ptrs, std::initializer_list<long long> lds) {
   if (a.dtype != RDN_BF16 || (a.D & 1) || a.T < 1) return false;
+  if ((long long)a.B * ((a.D + kWide - 1) / kWide) < kTmaUnits) return false;
   for (const void *q : ptrs)
     if ((uintptr_t)q & 15) return false;
   for (long long ld : lds)

@@ -69,6 +69,23 @@ def test_rows_that_stay_on_a_cta():
             compare(x, x, w)
 
 
+@pytest.mark.parametrize("n,D", [(80001, 64), (80003, 40), (40001, 128), (20001, 256), (20003, 504), (20002, 1000)])
+def test_several_rows_a_lane(n, D):
+    compare(rows(n, D, seed=D), rows(n, D, dtype="f32", seed=D + 1), 1 + 0.1 * rows(D, dtype="f32"))
+
+
+@pytest.mark.parametrize("D", [9, 57, 58, 121, 249, 250, 1001, 2055, 4097])
+@pytest.mark.parametrize("n", [1, 2, 9, 2000])
+def test_rows_between_16_bytes(n, D):
+    """Rows one after the other of a length that is no multiple of 8: each starts elsewhere in its 16 bytes, and
+    the last ends with the tensor."""
+    x, f, w = rows(n, D, dtype="f32", seed=D), rows(n, D, seed=D + 1), 1 + 0.1 * rows(D, dtype="f32")
+    compare(x, f, w)
+    compare(f, None, w)
+    wide = rows(n, D + 8, seed=D)
+    compare(wide[:, :D], f, w)
+
+
 @pytest.mark.parametrize("pad", [8, 3])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strided_rows_and_axes(pad, dtype):
