@@ -566,8 +566,8 @@ rdn_status_t rdn_norm_bwd_workspace_size(const rdn_norm_args *args, size_t *byte
  *                     they are in (written by the forward, read by the backward,
  *                     which computes them itself if NULL).
  * Backward: dy [B,T,D], dhT like hT or NULL -> dx, dr, di [B,T,D] with row
- * strides, dlam [D] fp32, dh0 like h0 or NULL.  lam is finite or -infinity;
- * decays below 2^-125 are taken as that.  Row strides of its tensors are below
+ * strides, dlam [D] fp32, dh0 like h0 or NULL.  Decays below 2^-125 are
+ * taken as that (lam may be infinite).  Row strides of its tensors are below
  * 2^24 elements. */
 #define RDN_GSCAN_CHUNK 64
 typedef struct {
@@ -646,8 +646,11 @@ rdn_status_t rdn_norm_q8(const rdn_norm_q8_args *args, rdn_stream_t stream);
  *     dp = dy act'(pre),   dx = dp w,   dw = dp^T x,   dbias = sum over rows of dp
  * dx [M,K] bf16 and dw [N,K] of dw_dtype (RDN_BF16 or RDN_F32), contiguous;
  * each of dx, dw, dbias may be NULL.  (The residual's gradient is dy itself.)  dp is
- * held in bf16 between the activation's derivative and the products, whose sums
- * are fp32; dbias is summed from dp in fp32.  dy's rows start on 16 bytes. */
+ * held in bf16 between the activation's derivative and the products; dbias is
+ * summed from dp before that, in fp32.  dy's rows start on 16 bytes.
+ * The products' sums are the tensor core's: fp32, cut (not rounded) after every 16
+ * products (e4m3: 32), so that a sum of n products comes out low by about n 2^-30
+ * of itself (dw of 65536 rows: 7e-5). */
 #define RDN_E4M3 2 /* rdn_linear_args.dtype: 8-bit floating point, 4 bits of exponent */
 typedef struct {
   long long M;

@@ -173,7 +173,8 @@ __device__ __forceinline__ f2 rest(f2 u) {
 constexpr float kLn2 = 0.69314718f;
 template <int V>
 __device__ __forceinline__ f2 rate(const GP &p, int ch) {  // -c softplus(lam) log2(e)
-  return mul2(pack2(softplusf(p.lam[ch]), V == 2 ? softplusf(p.lam[ch + V - 1]) : 0.f), both(-p.c * kLog2e));
+  const f2 k = mul2(pack2(softplusf(p.lam[ch]), V == 2 ? softplusf(p.lam[ch + V - 1]) : 0.f), both(-p.c * kLog2e));
+  return each(k, [](float v) { return max_nan(v, -1e30f); });  // (finite: a closed gate's 0 times it is 0)
 }
 
 // The map h -> A h + H of a span of tokens, for a pair of channels.  A = -1 stands for a span in

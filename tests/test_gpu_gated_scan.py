@@ -172,7 +172,7 @@ def test_gates_at_their_ends():
     x = make(1, 100, 64, "f32")
     x["r"][0, :, :16], x["r"][0, :, 16:32] = -200.0, 200.0
     x["i"][0, :, 32:40], x["i"][0, :, 40:48] = -200.0, 200.0
-    x["lam"][48:52], x["lam"][52:56], x["lam"][16:20] = -120.0, -float("inf"), 60.0
+    x["lam"][48:52], x["lam"][52:56], x["lam"][16:20], x["lam"][56:60] = -120.0, -float("inf"), 60.0, float("inf")
     y, hT = rdn.gated_scan_fwd(x["x"], x["r"], x["i"], x["lam"], h0=x["h0"])
     d = rdn.gated_scan_bwd(x["x"], x["r"], x["i"], x["lam"], x["dy"], h0=x["h0"])
     for t in (y, hT, *d.values()):
