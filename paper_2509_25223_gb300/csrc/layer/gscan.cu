@@ -106,8 +106,7 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.ftz.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-// fn of each of a pair.  (Packed instructions take no constants: where one operand is a constant, two
-// plain instructions with it inside cost fewer issue slots than the pair's constants in registers.)
+// fn of each of a pair.
 template <typename Fn>
 __device__ __forceinline__ f2 each(f2 x, Fn fn) {
   float lo, hi;
@@ -123,9 +122,6 @@ __device__ __forceinline__ f2 sqrt2(f2 x) {
 // 1 / x, a large number for x = 0
 __device__ __forceinline__ f2 rcp2(f2 x) {
   return each(x, [](float v) { return rcp_approx(max_nan(v, 2e-38f)); });
-}
-__device__ __forceinline__ f2 one_minus(f2 x) {
-  return each(x, [](float v) { return 1.f - v; });
 }
 __device__ __forceinline__ f2 sub2(f2 a, f2 b) {
   float x, y, z, w;
@@ -143,31 +139,59 @@ __device__ __forceinline__ f2 sub2(f2 a, f2 b) {
 struct Gate {
   f2 sr, si, u;
 };
+// The steps are packed ones (kPairs) in the kernels by TMA: packed instructions take no constants, so that each
+// constant is a pair of registers, and those kernels have them (16384 tokens of 4096 channels 148 -> 138 us).
+// The others do not: with two plain instructions that hold the constant they stay under their register limits.
 __device__ __forceinline__ float sigmoid_of(float x) { return rcp_approx(1.f + ex2(-kLog2e * x)); }
 __device__ __forceinline__ f2 log2_decay(f2 k, f2 sr) {
   return each(mul2(k, sr), [](float v) { return max_nan(v, -125.f); });
 }
+constexpr float kRound = 12582912.f;  // 1.5 * 2^23
+constexpr float kP0 = 0.6931471824645996f, kP1 = 0.24022649228572845f, kP2 = 5.550357326865196e-2f,
+                kP3 = 9.618237614631653e-3f, kP4 = 1.3390735257416964e-3f, kP5 = 1.5403510769829154e-4f;
 __device__ __forceinline__ float decayed(float t) {  // 1 - 2^t, -125 <= t <= 0
-  constexpr float kRound = 12582912.f;               // 1.5 * 2^23
   const float nr = t + kRound, f = t - (nr - kRound);
-  float q = fmaf(1.5403510769829154e-4f, f, 1.3390735257416964e-3f);
-  q = fmaf(q, f, 9.618237614631653e-3f);
-  q = fmaf(q, f, 5.550357326865196e-2f);
-  q = fmaf(q, f, 0.24022649228572845f);
-  q = fmaf(q, f, 0.6931471824645996f);
+  float q = fmaf(kP5, f, kP4);
+  q = fmaf(q, f, kP3);
+  q = fmaf(q, f, kP2);
+  q = fmaf(q, f, kP1);
+  q = fmaf(q, f, kP0);
   const float s = __uint_as_float((__float_as_uint(nr) << 23) + 0x3f800000u);  // 2^n
   return fmaf(-s, q * f, 1.f - s);
 }
-__device__ __forceinline__ Gate gate(f2 r, f2 i, f2 k) {
-  Gate g;
-  g.sr = each(r, sigmoid_of);
-  g.si = each(i, sigmoid_of);
-  g.u = each(log2_decay(k, g.sr), decayed);
-  return g;
+template <bool kPairs>
+__device__ __forceinline__ f2 one_minus(f2 x) {
+  if (kPairs) return fma2(x, both(-1.f), both(1.f));
+  return each(x, [](float v) { return 1.f - v; });
 }
 // 1 - a^2
+template <bool kPairs>
 __device__ __forceinline__ f2 rest(f2 u) {
+  if (kPairs) return mul2(u, fma2(u, both(-1.f), both(2.f)));
   return mul2(u, each(u, [](float v) { return 2.f - v; }));
+}
+template <bool kPairs>
+__device__ __forceinline__ Gate gate(f2 r, f2 i, f2 k) {
+  Gate g;
+  if (!kPairs) {
+    g.sr = each(r, sigmoid_of);
+    g.si = each(i, sigmoid_of);
+    g.u = each(log2_decay(k, g.sr), decayed);
+    return g;
+  }
+  const f2 one = both(1.f);
+  g.sr = each(add2(each(mul2(r, both(-kLog2e)), ex2), one), rcp_approx);
+  g.si = each(add2(each(mul2(i, both(-kLog2e)), ex2), one), rcp_approx);
+  const f2 t = log2_decay(k, g.sr), nr = add2(t, both(kRound));
+  const f2 f = fma2(add2(nr, both(-kRound)), both(-1.f), t);
+  f2 q = fma2(both(kP5), f, both(kP4));
+  q = fma2(q, f, both(kP3));
+  q = fma2(q, f, both(kP2));
+  q = fma2(q, f, both(kP1));
+  q = fma2(q, f, both(kP0));
+  const f2 s = each(nr, [](float v) { return __uint_as_float((__float_as_uint(v) << 23) + 0xbf800000u); });  // -2^n
+  g.u = fma2(s, mul2(q, f), add2(one, s));
+  return g;
 }
 
 constexpr float kLn2 = 0.69314718f;
@@ -437,9 +461,9 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
     }
     Span all = {both(1.f), both(0.f)};
     auto token = [&](int j) {
-      const Gate g = gate(get2<T, V>(rr[j]), get2<T, V>(ir[j]), k);
-      const f2 a = one_minus(g.u);
-      f2 b = mul2(mul2(sqrt2(rest(g.u)), g.si), get2<T, V>(xr[j]));
+      const Gate g = gate<false>(get2<T, V>(rr[j]), get2<T, V>(ir[j]), k);
+      const f2 a = one_minus<false>(g.u);
+      f2 b = mul2(mul2(sqrt2(rest<false>(g.u)), g.si), get2<T, V>(xr[j]));
       const int start = marked ? mark[par][at.token() + j].x : -1;
       if (kPacked && start >= 0) {
         if (p.h0) b = fma2(a, ldf<V>(p.h0 + (size_t)start * p.D + at.ch), b);
@@ -571,10 +595,11 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
     Span all = {both(1.f), both(0.f)}, kept[kTok];
 #pragma unroll
     for (int j = 0; j < kTok; ++j) {
-      const Gate g = gate(get2<bf, 2>(Pack<bf, 2>::ld(&sm.in[par][0][first + j][at.lane * 2])),
+      const Gate g = gate<true>(get2<bf, 2>(Pack<bf, 2>::ld(&sm.in[par][0][first + j][at.lane * 2])),
                           get2<bf, 2>(Pack<bf, 2>::ld(&sm.in[par][1][first + j][at.lane * 2])), k);
-      const f2 a = one_minus(g.u);
-      f2 b = mul2(mul2(sqrt2(rest(g.u)), g.si), get2<bf, 2>(Pack<bf, 2>::ld(&sm.in[par][2][first + j][at.lane * 2])));
+      const f2 a = one_minus<true>(g.u);
+      f2 b = mul2(mul2(sqrt2(rest<true>(g.u)), g.si),
+                  get2<bf, 2>(Pack<bf, 2>::ld(&sm.in[par][2][first + j][at.lane * 2])));
       const int start = marked ? mark[par][first + j].x : -1;
       if (kPacked && start >= 0) {
         if (p.h0) b = fma2(a, ldf<2>(p.h0 + (size_t)start * p.D + at.ch), b);
@@ -680,11 +705,11 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
     // this thread's span from a zero state, both ways
     Span fwd = {one, both(0.f)}, back = fwd;
     auto ahead = [&](int j) {
-      const Gate g = gate(get2<T, V>(rr[j]), get2<T, V>(ir[j]), k);
+      const Gate g = gate<false>(get2<T, V>(rr[j]), get2<T, V>(ir[j]), k);
       kept.sr[j][me] = g.sr;
       kept.si[j][me] = g.si;
       kept.u[j][me] = g.u;
-      const f2 a = one_minus(g.u), ms = mul2(sqrt2(rest(g.u)), g.si);
+      const f2 a = one_minus<false>(g.u), ms = mul2(sqrt2(rest<false>(g.u)), g.si);
       kept.ms[j][me] = ms;
       f2 b = mul2(ms, get2<T, V>(xr[j]));
       const int start = marked ? mark[par][at.token() + j].x : -1;
@@ -696,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
       }
     };
     auto behind = [&](int j) {
-      const f2 a = one_minus(kept.u[j][me]);
+      const f2 a = one_minus<false>(kept.u[j][me]);
       const int end = marked ? mark[par][at.token() + j].y : -1;
       if (kPacked && end >= 0) back = {both(-1.f), p.dhT ? ldf<V>(p.dhT + (size_t)end * p.D + at.ch) : both(0.f)};
       step<kPacked>(back, a, mul2(a, get2<T, V>(gr[j])));
@@ -729,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
       const int start = marked ? mark[par][at.token() + j].x : -1;
       if (kPacked && start >= 0) h = p.h0 ? ldf<V>(p.h0 + (size_t)start * p.D + at.ch) : both(0.f);
       kept.before[j][me] = h;
-      h = fma2(one_minus(kept.u[j][me]), h, mul2(kept.ms[j][me], get2<T, V>(xr[j])));
+      h = fma2(one_minus<false>(kept.u[j][me]), h, mul2(kept.ms[j][me], get2<T, V>(xr[j])));
     };
     const Rows<T> dx(p.dx, p.dx_ld, row0 + tile0, at.ch), dr(p.dr, p.dr_ld, row0 + tile0, at.ch),
         di(p.di, p.di_ld, row0 + tile0, at.ch);
@@ -737,15 +762,15 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
       const int2 f = marked ? mark[par][at.token() + j] : make_int2(-1, -1);
       if (kPacked && f.y >= 0) q = p.dhT ? ldf<V>(p.dhT + (size_t)f.y * p.D + at.ch) : both(0.f);
       const f2 u = kept.u[j][me], sr = kept.sr[j][me], ms = kept.ms[j][me];
-      const f2 a = one_minus(u), t = log2_decay(k, sr), b = mul2(ms, get2<T, V>(xr[j]));
+      const f2 a = one_minus<false>(u), t = log2_decay(k, sr), b = mul2(ms, get2<T, V>(xr[j]));
       const f2 g = add2(get2<T, V>(gr[j]), q), ag = mul2(a, g);
       // w / ln 2 = a g t (h_{t-1} - a b / (1 - a^2)): 0 where a is 1, for t and b are
-      const f2 w = mul2(mul2(ag, t), sub2(kept.before[j][me], mul2(mul2(a, b), rcp2(rest(u)))));
+      const f2 w = mul2(mul2(ag, t), sub2(kept.before[j][me], mul2(mul2(a, b), rcp2(rest<false>(u)))));
       sum = add2(sum, w);
       q = ag;
       put2<T, V>(dx[j], mul2(g, ms));
       put2<T, V>(dr[j], mul2(w, each(sr, [](float s) { return fmaf(s, -kLn2, kLn2); })));
-      put2<T, V>(di[j], mul2(mul2(g, b), one_minus(kept.si[j][me])));
+      put2<T, V>(di[j], mul2(mul2(g, b), one_minus<false>(kept.si[j][me])));
       if (kPacked && p.dh0 && f.x >= 0) stf<V>(p.dh0 + (size_t)f.x * p.D + at.ch, q);
     };
     if (at.live) {
@@ -841,7 +866,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
     f2 u[kTok], ms[kTok];
 #pragma unroll
     for (int j = 0; j < kTok; ++j) {
-      const Gate g = gate(get2<bf, 2>(Pack<bf, 2>::ld(cell(0, j))), get2<bf, 2>(Pack<bf, 2>::ld(cell(1, j))), k);
+      const Gate g = gate<true>(get2<bf, 2>(Pack<bf, 2>::ld(cell(0, j))), get2<bf, 2>(Pack<bf, 2>::ld(cell(1, j))), k);
       float lo, hi;  // sigmoid(r) stays in the two cells that it came from
       unpack2(g.sr, lo, hi);
       word(0, j) = __float_as_uint(lo);
@@ -849,8 +874,8 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
       sm.si[j][me] = g.si;
       // (a token past the row's end changes nothing: a = 1, no input)
       u[j] = j < left ? g.u : both(0.f);
-      ms[j] = mul2(sqrt2(rest(u[j])), g.si);
-      const f2 a = one_minus(u[j]);
+      ms[j] = mul2(sqrt2(rest<true>(u[j])), g.si);
+      const f2 a = one_minus<true>(u[j]);
       f2 b = mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j))));
       const int start = marked ? mark[par][first + j].x : -1;
       if (kPacked && start >= 0) {
@@ -862,7 +887,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
     }
 #pragma unroll
     for (int j = kTok - 1; j >= 0; --j) {
-      const f2 a = one_minus(u[j]);
+      const f2 a = one_minus<true>(u[j]);
       const int end = marked ? mark[par][first + j].y : -1;
       if (kPacked && end >= 0) back = {both(-1.f), p.dhT ? ldf<2>(p.dhT + (size_t)end * p.D + at.ch) : both(0.f)};
       step<kPacked>(back, a, mul2(a, get2<bf, 2>(Pack<bf, 2>::ld(cell(3, j)))));
@@ -883,22 +908,22 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
       const int start = marked ? mark[par][first + j].x : -1;
       if (kPacked && start >= 0) h = p.h0 ? ldf<2>(p.h0 + (size_t)start * p.D + at.ch) : both(0.f);
       before[j] = h;
-      h = fma2(one_minus(u[j]), h, mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j)))));
+      h = fma2(one_minus<true>(u[j]), h, mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j)))));
     }
 #pragma unroll
     for (int j = kTok - 1; j >= 0; --j) {
       const int2 f = marked ? mark[par][first + j] : make_int2(-1, -1);
       if (kPacked && f.y >= 0) q = p.dhT ? ldf<2>(p.dhT + (size_t)f.y * p.D + at.ch) : both(0.f);
       const f2 sr = pack2(__uint_as_float(word(0, j)), __uint_as_float(word(1, j)));
-      const f2 a = one_minus(u[j]), t = log2_decay(k, sr), b = mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j))));
+      const f2 a = one_minus<true>(u[j]), t = log2_decay(k, sr), b = mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j))));
       const f2 g = add2(get2<bf, 2>(Pack<bf, 2>::ld(cell(3, j))), q), ag = mul2(a, g);
       // w / ln 2 = a g t (h_{t-1} - a b / (1 - a^2)): 0 where a is 1, for t and b are
-      const f2 w = mul2(mul2(ag, t), sub2(before[j], mul2(mul2(a, b), rcp2(rest(u[j])))));
+      const f2 w = mul2(mul2(ag, t), sub2(before[j], mul2(mul2(a, b), rcp2(rest<true>(u[j])))));
       if (j < left) sum = add2(sum, w);
       q = ag;
       put2<bf, 2>(cell(2, j), mul2(g, ms[j]));
       put2<bf, 2>(cell(0, j), mul2(w, each(sr, [](float s) { return fmaf(s, -kLn2, kLn2); })));
-      put2<bf, 2>(cell(1, j), mul2(mul2(g, b), one_minus(sm.si[j][me])));
+      put2<bf, 2>(cell(1, j), mul2(mul2(g, b), one_minus<true>(sm.si[j][me])));
       if (kPacked && p.dh0 && at.live && f.x >= 0) stf<2>(p.dh0 + (size_t)f.x * p.D + at.ch, q);
     }
     tc::fence_async_smem();
@@ -955,9 +980,9 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const GP p) {
     if (slot >= 0 && slot < p.num_slots) {
       float *h = p.h + (size_t)slot * p.D + ch;
       const f2 x = get2<T, V>(Pack<T, V>::ld(static_cast<const T *>(p.x) + row * p.x_ld + ch));
-      const Gate g = gate(get2<T, V>(Pack<T, V>::ld(static_cast<const T *>(p.r) + row * p.r_ld + ch)),
+      const Gate g = gate<false>(get2<T, V>(Pack<T, V>::ld(static_cast<const T *>(p.r) + row * p.r_ld + ch)),
                           get2<T, V>(Pack<T, V>::ld(static_cast<const T *>(p.i) + row * p.i_ld + ch)), k);
-      y = fma2(one_minus(g.u), ldf<V>(h), mul2(mul2(sqrt2(rest(g.u)), g.si), x));
+      y = fma2(one_minus<false>(g.u), ldf<V>(h), mul2(mul2(sqrt2(rest<false>(g.u)), g.si), x));
       stf<V>(h, y);
     }
     put2<T, V>(static_cast<T *>(p.y) + row * p.y_ld + ch, y);
@@ -1039,7 +1064,7 @@ bool make_tiles(TileMap *m, const void *p, const rdn_gscan_args &a, long long ld
 }
 // bf16, an even D, rows (pointers and distances) on 16 bytes, distances that a map can hold, and enough strips:
 // the other kernels' are half as wide, and with few of them fill more of the GPU (32 strips of 32768 tokens
-// 211 us by TMA, 174 without; 40 strips of 4096 tokens 35 and 38).
+// 199 us by TMA, 173 without; 16 strips of 777 tokens 15.2 and 13.1; 40 strips of 4096 tokens 34 and 38).
 bool tma_ok(const rdn_gscan_args &a, std::initializer_list<const void *> ptrs, std::initializer_list<long long> lds) {
   if (a.dtype != RDN_BF16 || (a.D & 1) || a.T < 1) return false;
   if ((long long)a.B * ((a.D + kWide - 1) / kWide) < kTmaUnits) return false;
@@ -1057,8 +1082,9 @@ bool bwd_tma_ok(const rdn_gscan_args &a) {
                 {a.x_ld, a.r_ld, a.i_ld, a.dy_ld, a.dx_ld, a.dr_ld, a.di_ld});
 }
 // Strips, and CTAs of a cluster: what fills 95 % of the places in one go, and no more: a round costs a CTA more
-// in a cluster (forward, 256 units of 4096 tokens 136 us with one, 145 with two; 128 units 77 with three, 97
-// with one); of 8 few clusters find a place (64 units of 16384 tokens 148 us with six, 183 with eight).
+// in a cluster (forward, 256 units of 4096 tokens 129 us with one, 135 with two; 128 units 71 with three, 95
+// with one; 64 units of 16384 tokens 138 us with six, 159 with five, 185 with three); of 8 few clusters find a
+// place (the same 64 units, before the gates were worked out in pairs: 148 us with six, 183 with eight).
 int tma_strips(const rdn_gscan_args &a) { return (a.D + kWide - 1) / kWide; }
 int tma_cluster(const rdn_gscan_args &a, bool bwd) {
   const long long units = (long long)a.B * tma_strips(a), places = 152 * (bwd ? kBwdCtas : kFwdCtas) * 95 / 100;
