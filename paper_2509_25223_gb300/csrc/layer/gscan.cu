@@ -17,6 +17,7 @@
 //     dx = g m s,  di = g b (1 - s),  w_t = a g la (h_{t-1} - a b / (1 - a^2)),
 //     dr = (1 - sigmoid(r)) w,  dlam = sigmoid(lam) / softplus(lam) sum_t w_t
 // (la b / (1 - a^2) stays finite where la -> 0: it is la s x / m, and m ~ sqrt(-2 la)).
+#include "launch.cuh"
 #include "maps.cuh"
 #include "rows.cuh"
 #include "status.cuh"
@@ -1029,13 +1030,15 @@ bool pairs_ok(int D, size_t e, std::initializer_list<const void *> ptrs, std::in
   return true;
 }
 
-template <typename T, int V>
-cudaError_t run(const GP &p, bool bwd, const char *name, cudaStream_t s) {
-  auto kern = bwd ? (p.cu ? bwd_kernel<T, V, true> : bwd_kernel<T, V, false>)
-                  : (p.cu ? fwd_kernel<T, V, true> : fwd_kernel<T, V, false>);
+// A launch of p.nc CTAs a cluster, with `bytes` of dynamic shared memory.
+template <auto kKernel, typename... Args>
+cudaError_t go(const GP &p, int bytes, const char *name, cudaStream_t s, const Args &...args) {
+  cudaError_t e = bytes ? let_smem<kKernel>(bytes) : cudaSuccess;
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)((long long)p.B * p.strips * p.nc));
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = bytes;
   cfg.stream = s;
   cudaLaunchAttribute at;
   at.id = cudaLaunchAttributeClusterDimension;
@@ -1043,14 +1046,15 @@ cudaError_t run(const GP &p, bool bwd, const char *name, cudaStream_t s) {
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  cudaError_t e = cudaSuccess;
-  if (bwd) {
-    cfg.dynamicSmemBytes = sizeof(Kept);
-    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Kept));
-    if (e != cudaSuccess) return e;
-  }
-  RDN_LAUNCH(name, s, (e = cudaLaunchKernelEx(&cfg, kern, p)));
+  RDN_LAUNCH(name, s, (e = cudaLaunchKernelEx(&cfg, kKernel, p, args...)));
   return e;
+}
+template <typename T, int V>
+cudaError_t run(const GP &p, bool bwd, const char *name, cudaStream_t s) {
+  if (bwd)
+    return p.cu ? go<bwd_kernel<T, V, true>>(p, sizeof(Kept), name, s)
+                : go<bwd_kernel<T, V, false>>(p, sizeof(Kept), name, s);
+  return p.cu ? go<fwd_kernel<T, V, true>>(p, 0, name, s) : go<fwd_kernel<T, V, false>>(p, 0, name, s);
 }
 cudaError_t run(const GP &p, bool bwd, int dtype, int V, const char *name, cudaStream_t s) {
   if (dtype == RDN_BF16)
@@ -1092,43 +1096,32 @@ int tma_cluster(const rdn_gscan_args &a, bool bwd) {
   const long long most = tiles < 1 ? 1 : tiles < 6 ? tiles : 6;
   return (int)(nc < most ? nc : most);
 }
-template <typename Kern, typename M>
-cudaError_t go_tma(Kern kern, GP p, const M &maps, const rdn_gscan_args &a, bool bwd, size_t bytes, const char *name,
-                   cudaStream_t s) {
+GP tma_params(GP p, const rdn_gscan_args &a, bool bwd) {
   p.strips = tma_strips(a);
   p.nc = tma_cluster(a, bwd);
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes + 128);
-  if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)((long long)p.B * p.strips * p.nc));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = bytes + 128;
-  cfg.stream = s;
-  cudaLaunchAttribute at;
-  at.id = cudaLaunchAttributeClusterDimension;
-  at.val.clusterDim.x = p.nc;
-  at.val.clusterDim.y = at.val.clusterDim.z = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
-  RDN_LAUNCH(name, s, (e = cudaLaunchKernelEx(&cfg, kern, p, maps)));
-  return e;
+  return p;
 }
 cudaError_t run_fwd_tma(const rdn_gscan_args &a, cudaStream_t s) {
   FwdMaps m{};
   if (!make_tiles(&m.x, a.x, a, a.x_ld, kTileTma) || !make_tiles(&m.r, a.r, a, a.r_ld, kTileTma) ||
       !make_tiles(&m.i, a.i, a, a.i_ld, kTileTma) || (a.y && !make_tiles(&m.y, a.y, a, a.y_ld, kTok)))
     return cudaErrorInvalidValue;
-  return go_tma(a.cu_seqlens ? fwd_tma_kernel<true> : fwd_tma_kernel<false>, params(a, 2, false), m, a, false,
-                sizeof(FwdTiles), "gscan_fwd", s);
+  const GP p = tma_params(params(a, 2, false), a, false);
+  constexpr int kBytes = sizeof(FwdTiles) + 128;  // (tiles on 128 bytes)
+  return p.cu ? go<fwd_tma_kernel<true>>(p, kBytes, "gscan_fwd", s, m)
+              : go<fwd_tma_kernel<false>>(p, kBytes, "gscan_fwd", s, m);
 }
-cudaError_t run_bwd_tma(const rdn_gscan_args &a, const GP &p, cudaStream_t s) {
+cudaError_t run_bwd_tma(const rdn_gscan_args &a, GP p, cudaStream_t s) {
   BwdMaps m{};
   if (!make_tiles(&m.x, a.x, a, a.x_ld, kTileTma) || !make_tiles(&m.r, a.r, a, a.r_ld, kTileTma) ||
       !make_tiles(&m.i, a.i, a, a.i_ld, kTileTma) || !make_tiles(&m.dy, a.dy, a, a.dy_ld, kTileTma) ||
       !make_tiles(&m.dx, a.dx, a, a.dx_ld, kTok) || !make_tiles(&m.dr, a.dr, a, a.dr_ld, kTok) ||
       !make_tiles(&m.di, a.di, a, a.di_ld, kTok))
     return cudaErrorInvalidValue;
-  return go_tma(a.cu_seqlens ? bwd_tma_kernel<true> : bwd_tma_kernel<false>, p, m, a, true, sizeof(BwdTiles), "gscan_bwd", s);
+  p = tma_params(p, a, true);
+  constexpr int kBytes = sizeof(BwdTiles) + 128;
+  return p.cu ? go<bwd_tma_kernel<true>>(p, kBytes, "gscan_bwd", s, m)
+              : go<bwd_tma_kernel<false>>(p, kBytes, "gscan_bwd", s, m);
 }
 
 // (the largest of the kernels' clusters: the query sees no pointers)

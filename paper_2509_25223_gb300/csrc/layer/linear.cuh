@@ -2,6 +2,7 @@
 // tensor maps, the tensor-core instructions in both element types and for one CTA
 // or a pair, and the epilogue.
 #pragma once
+#include "launch.cuh"
 #include "rows.cuh"
 #include "status.cuh"
 #include "tc_common.cuh"

@@ -218,8 +218,8 @@ __global__ void __launch_bounds__(kThreads, 2)
 
 template <int kBN, bool kFp8, bool kAmn, bool kBmn>
 cudaError_t go(const Maps &maps, const GemmP &p, cudaStream_t s) {
-  auto kern = split_kernel<kBN, kFp8, kAmn, kBmn>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<kBN>::kBytes);
+  constexpr auto kern = split_kernel<kBN, kFp8, kAmn, kBmn>;
+  cudaError_t e = let_smem<kern>(Smem<kBN>::kBytes);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)((long long)p.tiles_m * p.tiles_n * p.splits));

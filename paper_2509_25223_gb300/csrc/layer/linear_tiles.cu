@@ -57,13 +57,14 @@ struct alignas(32) U8 { uint32_t w[8]; };
 __device__ __forceinline__ U8 ld32(const void *p) {
   U8 v;
   asm volatile("ld.global.L1::no_allocate.L2::evict_first.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]), "=r"(v.w[6]), "=r"(v.w[7])
+               : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]), "=r"(v.w[6]),
+                 "=r"(v.w[7])
                : "l"(p));
   return v;
 }
 __device__ __forceinline__ void st32(void *p, const U8 &v) {
-  asm volatile("st.global.L1::no_allocate.L2::evict_first.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v.w[0]), "r"(v.w[1]), "r"(v.w[2]),
-               "r"(v.w[3]), "r"(v.w[4]), "r"(v.w[5]), "r"(v.w[6]), "r"(v.w[7])
+  asm volatile("st.global.L1::no_allocate.L2::evict_first.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p),
+               "r"(v.w[0]), "r"(v.w[1]), "r"(v.w[2]), "r"(v.w[3]), "r"(v.w[4]), "r"(v.w[5]), "r"(v.w[6]), "r"(v.w[7])
                : "memory");
 }
 
@@ -312,7 +313,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           const uint64_t to = tc::desc_off((uint32_t)(at.s * S::kStage));
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            mma_step<true, kFp8>(tmem + acc * kBN, da0 + to + tile_step<kAmn>(j), db0 + to + tile_step<kBmn>(j), idesc, kb + j > 0);
+            mma_step<true, kFp8>(tmem + acc * kBN, da0 + to + tile_step<kAmn>(j), db0 + to + tile_step<kBmn>(j), idesc,
+                                 kb + j > 0);
           commit<true>(&b.empty[at.s]);
         }
         if (!*dead) commit<true>(&b.done[acc]);
@@ -379,13 +381,15 @@ int access_of(const void *p, long long bytes) {
 
 template <int kBN, bool kFp8, bool kAmn, bool kBmn>
 cudaError_t go(const Maps &maps, const GemmP &p, cudaStream_t s) {
-  auto kern = tiles_kernel<kBN, kFp8, kAmn, kBmn>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<kBN>::kBytes);
+  constexpr auto kern = tiles_kernel<kBN, kFp8, kAmn, kBmn>;
+  cudaError_t e = let_smem<kern>(Smem<kBN>::kBytes);
   if (e != cudaSuccess) return e;
   const long long n = (long long)p.tiles_m * p.tiles_n;
   const int ctas = 2 * (int)(n < 76 ? n : 76);
   const size_t e_size = p.e.out_f32 ? 4 : 2;
-  RDN_LAUNCH("linear_tiles", s, (kern<<<ctas, kThreads, Smem<kBN>::kBytes, s>>>(p, maps, access_of(p.e.res, p.e.res_ld * e_size), access_of(p.e.y, p.e.y_ld * e_size), access_of(p.e.pre, p.e.pre_ld * 2))));
+  const int res = access_of(p.e.res, p.e.res_ld * e_size), y = access_of(p.e.y, p.e.y_ld * e_size);
+  const int pre = access_of(p.e.pre, p.e.pre_ld * 2);
+  RDN_LAUNCH("linear_tiles", s, (kern<<<ctas, kThreads, Smem<kBN>::kBytes, s>>>(p, maps, res, y, pre)));
   return cudaGetLastError();
 }
 template <int kBN>

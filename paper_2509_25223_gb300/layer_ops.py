@@ -562,12 +562,15 @@ def gated_scan_bwd(x, r, i, lam, dy, c=8.0, h0=None, dhT=None, cu_seqlens=None, 
     dev, shape, ty = a.dev, a.shape, a.dtype
     d = shape[2]
     pdy, dy_ld = _rows("dy", dy, shape, ty, dev)
+    dx_ld = dr_ld = di_ld = pdh = 0
     if out is None:
         dx, dr = torch.empty(shape, dtype=ty, device=dev), torch.empty(shape, dtype=ty, device=dev)
         di, dlam = torch.empty(shape, dtype=ty, device=dev), torch.empty(d, dtype=_F32, device=dev)
+        pdx, pdr, pdi, pdl = dx.data_ptr(), dr.data_ptr(), di.data_ptr(), dlam.data_ptr()
         res = dict(dx=dx, dr=dr, di=di, dlam=dlam)
         if h0 is not None:
-            res["dh0"] = torch.empty(a.states, dtype=_F32, device=dev)
+            res["dh0"] = dh = torch.empty(a.states, dtype=_F32, device=dev)
+            pdh = dh.data_ptr()
     else:
         res = dict(out)
         for name in ("dx", "dr", "di"):
@@ -577,12 +580,12 @@ def gated_scan_bwd(x, r, i, lam, dy, c=8.0, h0=None, dhT=None, cu_seqlens=None, 
             res["dlam"] = torch.empty(d, dtype=_F32, device=dev)
         if h0 is not None and res.get("dh0") is None:
             res["dh0"] = torch.empty(a.states, dtype=_F32, device=dev)
-        dx, dr, di, dlam = res["dx"], res["dr"], res["di"], res["dlam"]
-    pdx, dx_ld = _rows("dx", dx, shape, ty, dev)
-    pdr, dr_ld = _rows("dr", dr, shape, ty, dev)
-    pdi, di_ld = _rows("di", di, shape, ty, dev)
-    grads = (dy_ld, dx_ld, dr_ld, di_ld, pdy, _whole("dhT", dhT, a.states, _F32, dev), pdx, pdr, pdi,
-             _whole("dlam", dlam, (d,), _F32, dev), _whole("dh0", res.get("dh0"), a.states, _F32, dev))
+        pdx, dx_ld = _rows("dx", res["dx"], shape, ty, dev)
+        pdr, dr_ld = _rows("dr", res["dr"], shape, ty, dev)
+        pdi, di_ld = _rows("di", res["di"], shape, ty, dev)
+        pdl = _whole("dlam", res["dlam"], (d,), _F32, dev)
+        pdh = _whole("dh0", res.get("dh0"), a.states, _F32, dev)
+    grads = (dy_ld, dx_ld, dr_ld, di_ld, pdy, _whole("dhT", dhT, a.states, _F32, dev), pdx, pdr, pdi, pdl, pdh)
     args = a.pack(chunks=_whole("h_chunks", h_chunks, a.chunks(), _F32, dev), grads=grads)
     ws, args = _with_workspace("rdn_gscan_bwd_workspace_size", args, workspace, dev)
     _call("rdn_gscan_bwd", args, dev)
