@@ -1,6 +1,6 @@
 // api_layer.cu -- the C ABI of the operators around the recurrence (convolution,
-// selective scan, norms, gated recurrence, matrix products; include/rdn.h): argument validation and dispatch to
-// the launchers.  No exception or abort crosses this boundary.
+// selective scan, norms, gated recurrence, matrix products; include/rdn.h): argument
+// validation and dispatch to the launchers.  No exception or abort crosses this boundary.
 #include <math.h>
 
 #include "common.cuh"

@@ -287,8 +287,8 @@ struct Rows {
 };
 // (left: tokens of the row of the batch from the first one on)
 template <typename T, int V>
-__device__ __forceinline__ void load_rows(typename Pack<T, V>::Raw (&v)[kTok], const void *base, long long ld, uint32_t row,
-                                          int ch, bool full, int left) {
+__device__ __forceinline__ void load_rows(typename Pack<T, V>::Raw (&v)[kTok], const void *base, long long ld,
+                                          uint32_t row, int ch, bool full, int left) {
   const Rows<T> rows(base, ld, row, ch);
   if (full) {
 #pragma unroll
@@ -369,8 +369,8 @@ __device__ __forceinline__ void exchange_init(const GP &p, uint64_t *bars) {
 
 // The state that comes into this warp's span; carry: into and out of the cluster's round.
 template <bool kBack, bool kPacked, int kN>
-__device__ __forceinline__ f2 fold(const Span (*spans)[kN], const Span (*tiles)[kN], int lane, int rank, int nc, int warp,
-                                   f2 &carry) {
+__device__ __forceinline__ f2 fold(const Span (*spans)[kN], const Span (*tiles)[kN], int lane, int rank, int nc,
+                                   int warp, f2 &carry) {
   f2 run = carry;
   if (nc > 1) {
     f2 h = carry;
@@ -916,7 +916,8 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
       const int2 f = marked ? mark[par][first + j] : make_int2(-1, -1);
       if (kPacked && f.y >= 0) q = p.dhT ? ldf<2>(p.dhT + (size_t)f.y * p.D + at.ch) : both(0.f);
       const f2 sr = pack2(__uint_as_float(word(0, j)), __uint_as_float(word(1, j)));
-      const f2 a = one_minus<true>(u[j]), t = log2_decay(k, sr), b = mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j))));
+      const f2 a = one_minus<true>(u[j]), t = log2_decay(k, sr);
+      const f2 b = mul2(ms[j], get2<bf, 2>(Pack<bf, 2>::ld(cell(2, j))));
       const f2 g = add2(get2<bf, 2>(Pack<bf, 2>::ld(cell(3, j))), q), ag = mul2(a, g);
       // w / ln 2 = a g t (h_{t-1} - a b / (1 - a^2)): 0 where a is 1, for t and b are
       const f2 w = mul2(mul2(ag, t), sub2(before[j], mul2(mul2(a, b), rcp2(rest<true>(u[j])))));

@@ -32,15 +32,16 @@ bool make_map(Map *m, const Operand &o, int elem, int box) {
   const cuuint64_t strides[1] = {(cuuint64_t)o.ld * elem};
   const cuuint32_t boxes[2] = {(cuuint32_t)(128 / elem), (cuuint32_t)(o.mn ? 64 : box)};
   const cuuint32_t one[2] = {1, 1};
-  return enc(reinterpret_cast<CUtensorMap *>(m), elem == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
-             2, const_cast<void *>(o.p), dims, strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return enc(reinterpret_cast<CUtensorMap *>(m),
+             elem == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(o.p),
+             dims, strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace lin
 
-bool make_rows_map(void *map128, const void *p, int cols, int rows, int depth, long long ld, int box_cols, int box_rows) {
+bool make_rows_map(void *map128, const void *p, int cols, int rows, int depth, long long ld, int box_cols,
+                   int box_rows) {
   const auto enc = lin::encoder();
   if (!enc) return false;
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)depth};
@@ -48,8 +49,8 @@ bool make_rows_map(void *map128, const void *p, int cols, int rows, int depth, l
   const cuuint32_t boxes[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
   const cuuint32_t one[3] = {1, 1, 1};
   return enc(reinterpret_cast<CUtensorMap *>(map128), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims,
-             strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+             strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 namespace lin {
@@ -58,8 +59,7 @@ cudaError_t run_product(const Operand &a, const Operand &b, GemmP p, bool fp8, c
   p.status = status_word();
   const int per = fp8 ? 128 : 64;  // elements of 128 bytes
   p.kblocks = (int)((a.k + per - 1) / per);
-  const long long tiles = ((p.M + 255) / 256) * ((p.N + 127) / 128);
-  return tiles >= 60 ? run_tiles(a, b, p, fp8, s) : run_split(a, b, p, fp8, s);
+  return split_fits(a, b, p.kblocks) ? run_split(a, b, p, fp8, s) : run_tiles(a, b, p, fp8, s);
 }
 
 namespace {

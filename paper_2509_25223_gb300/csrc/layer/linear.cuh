@@ -150,6 +150,8 @@ __device__ __forceinline__ void load_tile(unsigned char *dst, const Map *map, in
 
 cudaError_t run_tiles(const Operand &a, const Operand &b, GemmP p, bool fp8, cudaStream_t s);
 cudaError_t run_split(const Operand &a, const Operand &b, GemmP p, bool fp8, cudaStream_t s);
+// Whether run_split is the faster one.
+bool split_fits(const Operand &a, const Operand &b, int kblocks);
 // out = A B^T by the kernel that suits the sizes.
 cudaError_t run_product(const Operand &a, const Operand &b, GemmP p, bool fp8, cudaStream_t s);
 

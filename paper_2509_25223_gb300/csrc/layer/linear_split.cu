@@ -60,7 +60,9 @@ __device__ __forceinline__ const void *at4(const void *p, long long i, bool f32)
 }
 __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
   float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(addr)
+               : "memory");
   return v;
 }
 
@@ -248,19 +250,45 @@ cudaError_t pick(const Maps &maps, const GemmP &p, bool fp8, bool amn, bool bmn,
   return amn ? go<kBN, false, true, false>(maps, p, s) : go<kBN, false, false, false>(maps, p, s);
 }
 
+// Parts of the sum over k: as many as give an SM one CTA (a cluster needs SMs side by side, so fewer than 152 in
+// all; 128 rows by 4096, K = 2048: four parts 8.6 us, five 10.2, seven 11.4; 256 by 1280: six 7.8, seven 10.0), or
+// two, where the parts stay long and would be few (512 by 2048, K = 2048: two 12.1 us, four 10.9, five 16.2) or the
+// tiles are narrow, so that one CTA's stages are too few bytes on their way (1 by 4096, K = 4096: four 9.2, six 8.2).
+int splits_of(long long tiles, int kblocks, int bn) {
+  const int most = (bn == 16 && kblocks >= 32) || tiles <= 8 ? 8 : 6;
+  int one = 1, two = 1;
+  for (int s = 2; s <= most && s <= kblocks; ++s) {
+    if (tiles * s <= (s == 4 ? 144 : 136)) one = s;
+    if (tiles * s <= (s <= 3 ? 288 : s == 6 ? 240 : 256)) two = s;
+  }
+  return kblocks >= 8 * one && (one < 4 || bn <= 32) ? two : one;
+}
+
+// Rows of a tile: all of them, at most 128 (an MN-major operand's boxes are 64 wide).
+int rows_of(const Operand &a) {
+  return a.rows <= 16 && !a.mn ? 16 : a.rows <= 32 && !a.mn ? 32 : a.rows <= 64 ? 64 : 128;
+}
+
 }  // namespace
+
+// Up to 64 rows run_tiles multiplies mostly zeros (1 by 16384, K = 4096: 25.5 us here, 39 there; 64 by 16384 28.0 and
+// 28.9).  Beyond, the join costs more than what it lets the SMs share unless the tiles are few or k is long (split
+// and tiles: 1280 by 1024, 80 tiles, K = 512 9.1 and 7.0 us, 1024 10.2 and 9.5, 2048 12.4 and 14.0; 512 by 4096,
+// 128 tiles, K = 2048 15.0 and 14.3, 4096 21.6 and 23.4; 1024 by 1024, 64 tiles, K = 512 7.8 and 7.1, 1024 9.3 and 9.4).
+bool split_fits(const Operand &a, const Operand &b, int kblocks) {
+  const long long tiles = (a.rows + 127) / 128 * ((b.rows + 127) / 128);
+  return a.rows <= 64 || tiles <= (kblocks < 16 ? 48 : kblocks < 32 ? 64 : kblocks < 64 ? 96 : 128);
+}
 
 // (a holds the result's rows, b its columns, as for run_tiles)
 cudaError_t run_split(const Operand &a, const Operand &b, GemmP p, bool fp8, cudaStream_t s) {
-  // rows a tile: all of them, at most 128 (an MN-major operand's boxes are 64 wide)
-  const int bn = p.M <= 16 && !a.mn ? 16 : p.M <= 32 && !a.mn ? 32 : p.M <= 64 ? 64 : 128;
+  const int bn = rows_of(a);
   p.tiles_m = (int)((p.M + bn - 1) / bn);
   p.tiles_n = (int)((p.N + 127) / 128);
-  const long long tiles = (long long)p.tiles_m * p.tiles_n;
-  p.splits = 1;
-  while (p.splits < 8 && tiles * (p.splits + 1) <= 240 && p.splits < p.kblocks) ++p.splits;
+  p.splits = splits_of((long long)p.tiles_m * p.tiles_n, p.kblocks, bn);
   Maps maps;
-  if (!make_map(&maps.a, b, fp8 ? 1 : 2, 128) || !make_map(&maps.b, a, fp8 ? 1 : 2, bn)) return cudaErrorInvalidValue;
+  if (!make_map(&maps.a, b, fp8 ? 1 : 2, 128) || !make_map(&maps.b, a, fp8 ? 1 : 2, bn))
+    return cudaErrorInvalidValue;
   switch (bn) {
     case 16: return pick<16>(maps, p, fp8, b.mn, a.mn, s);
     case 32: return pick<32>(maps, p, fp8, b.mn, a.mn, s);

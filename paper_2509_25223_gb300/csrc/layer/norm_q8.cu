@@ -151,7 +151,8 @@ __device__ __forceinline__ float over_row(float a, float *sh, int lanes) {
   return a;
 }
 
-// R rows of a lane, NV groups of 8 elements each.  (A row of 16384 elements has 64 groups a lane of one warp, a shifted one 65.)
+// R rows of a lane, NV groups of 8 elements each.  (A row of 16384 elements has 64 groups a lane of one warp, a
+// shifted one 65.)
 template <typename XT, typename FT, int NV, int R, int kLie>
 __global__ void __launch_bounds__(R > 1 ? 128 : NV == 8 ? 256 : NV == 4 ? 544 : 1024, R > 1 ? 4 : NV == 8 ? 2 : 1)
     norm_q8_kernel(const Q8P p) {
@@ -162,7 +163,9 @@ __global__ void __launch_bounds__(R > 1 ? 128 : NV == 8 ? 256 : NV == 4 ? 544 : 
   const FT *f = static_cast<const FT *>(p.f);
   for (long long first = (long long)blockIdx.x * per * R; first < p.rows; first += (long long)gridDim.x * per * R) {
     auto row_of = [&](int k) { return first + k * per + mine; };
-    auto i_of = [&](int k, int n) { return place<kLie>(n, t, lanes, kLie == kShifted ? (int)(row_of(k) * p.D & 7) : 0); };
+    auto i_of = [&](int k, int n) {
+      return place<kLie>(n, t, lanes, kLie == kShifted ? (int)(row_of(k) * p.D & 7) : 0);
+    };
     // the rows' loads go out before the first is waited for (fp32 rows leave no registers for f's beside them)
     constexpr bool kAhead = sizeof(XT) == 2;
     Raw8<XT> rx[R][NV];
@@ -311,7 +314,8 @@ cudaError_t launch_norm_q8(const rdn_norm_q8_args &a, cudaStream_t s) {
   // single elements), where the rows fill the GPU's 152 x 16 warps all the same, and then several rows a lane
   const int span = a.D + (lie == kShifted ? 7 : 0), groups = (span + 255) / 256;  // (groups of 8 that a row touches)
   Shape h{1, 1};
-  while (h.nv < (vec ? 8 : 4) && (groups > 32 * h.nv || (a.rows * groups > kSMs * 16 * h.nv && groups > h.nv))) h.nv *= 2;
+  while (h.nv < (vec ? 8 : 4) && (groups > 32 * h.nv || (a.rows * groups > kSMs * 16 * h.nv && groups > h.nv)))
+    h.nv *= 2;
   p.lanes = 32 * ((groups + h.nv - 1) / h.nv);
   if (groups == 1) p.lanes = span <= 64 ? 8 : span <= 128 ? 16 : 32;
   if (vec && p.lanes <= 32 && h.nv < 8 && a.rows * p.lanes / 32 * h.nv >= kSMs * 16 * 8) h.r = 8 / h.nv;

@@ -72,6 +72,15 @@ def test_many_tiles(M, N, K, kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("M,N,K", [(1, 16392, 1040), (40, 12296, 208), (64, 40008, 64), (3, 2048, 2064),
+                                   (128, 4096, 1024), (250, 1288, 2048), (512, 2048, 2048), (500, 4096, 4096),
+                                   (2048, 136, 4096)])
+def test_parts_of_the_sum(M, N, K, kind):
+    """Few rows of wide results, and one to eight parts of the sum over k, on one and two CTAs an SM."""
+    compare(make(M, N, K, kind, seed=K), "silu")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("M,N", [(5, 136), (2050, 2056)])
 @pytest.mark.parametrize("act", [None, "silu", "sigmoid", "gelu"])
 def test_options(M, N, act, kind):
