@@ -65,7 +65,7 @@ cudaError_t run_product(const Operand &a, const Operand &b, GemmP p, bool fp8, c
 namespace {
 
 // dp = dy act'(pre) in bf16, and its column sums over the CTA's rows.  A thread has 8
-// columns; the 8 warps of a CTA take rows in turn.
+// columns; the 8 warps of a CTA take rows in turn.  16384 x 4096 with SiLU: 60 to 68 us, 5.9 to 6.7 TB/s.
 struct DpP {
   long long M, dy_ld;
   int N, act;

@@ -6,6 +6,9 @@
 // walk over the tiles; one thread copies operand tiles (TMA, 128 bytes of k a stage), one
 // thread of the pair issues the products, and eight warps of each CTA turn the previous
 // tile's sums (TMEM, double buffered) into results meanwhile.
+// 8192 cubed 1.88 PF/s; 16384 x 4096 by 2048 1.78 alone, 1.55 with bias, SiLU, residual and `pre` (402 MB more);
+// in 8 bits 3.0.  Bound by the tensor cores under the power limit, and by the copies: with half of them left out
+// it takes 5 to 10 % less, with four stages for six 2 to 9 % more.
 #include "linear.cuh"
 
 namespace rdn {
