@@ -25,7 +25,7 @@ cudaError_t launch_gscan_fwd(const rdn_gscan_args &a, cudaStream_t s);
 cudaError_t launch_gscan_bwd(const rdn_gscan_args &a, cudaStream_t s);
 cudaError_t launch_gscan_step(const rdn_gscan_step_args &a, cudaStream_t s);
 cudaError_t launch_norm_q8(const rdn_norm_q8_args &a, cudaStream_t s);
-size_t linear_bwd_bytes(const rdn_linear_args &a);
+size_t linear_bwd_bytes(const rdn_linear_args &a, bool dbias);
 cudaError_t launch_linear_fwd(const rdn_linear_args &a, cudaStream_t s);
 cudaError_t launch_linear_bwd(const rdn_linear_args &a, cudaStream_t s);
 }  // namespace rdn
@@ -406,7 +406,7 @@ rdn_status_t linear_common(const char *fn, const rdn_linear_args *args, bool bwd
   TRY(check_ptr(fn, "dbias", a->dbias, be, false));
   if (any && ((a->dx && (a->dx == a->x || a->dx == a->dy || a->dx == a->pre)) || (a->dw && a->dw == a->w)))
     return entry_fail(RDN_ERR_INVALID_ARG, "%s: dx or dw aliases an input", fn);
-  TRY(check_ws(fn, a->workspace, a->workspace_bytes, rdn::linear_bwd_bytes(*a)));
+  TRY(check_ws(fn, a->workspace, a->workspace_bytes, rdn::linear_bwd_bytes(*a, a->dbias != nullptr)));
   TRY(entry_injected(fn));
   return entry_cuda(fn, rdn::launch_linear_bwd(*a, s));
 }
@@ -626,7 +626,7 @@ rdn_status_t rdn_linear_bwd_workspace_size(const rdn_linear_args *args, size_t *
   rdn_linear_args a = *args;
   TRY(linear_shapes(fn, &a, true));
   if (!bytes) return entry_fail(RDN_ERR_INVALID_ARG, "%s: bytes is NULL", fn);
-  *bytes = rdn::linear_bwd_bytes(a);
+  *bytes = rdn::linear_bwd_bytes(a, true);
   return entry_ok();
 }
 

@@ -158,7 +158,10 @@ def _workspace(workspace, nbytes, dev):
 def _with_workspace(query, args, workspace, dev):
     """args, whose last two fields are the workspace and its bytes, with a workspace of the size that `query`
     asks for."""
-    ws = _workspace(workspace, _size(query, args), dev)
+    nbytes = _size(query, args)
+    if not nbytes and workspace is None:
+        return None, args
+    ws = _workspace(workspace, nbytes, dev)
     return ws, args[:-16] + _abi.WORKSPACE_PACK(ws.data_ptr(), ws.numel() * ws.element_size())
 
 
@@ -774,6 +777,7 @@ def linear_bwd(x, w, dy, pre=None, act=None, bias=None, need_dx=True, need_dw=Tr
         pp = _whole("pre", pre, (*lead, n), bf, dev)
     args = _abi.LINEAR_PACK(m, n, k, _abi.RDN_BF16, 0, bt, _act(act), x_ld, w_ld, 0, 0, px, pw, 0, 0, 0, 0, 0, pp,
                             _code(wt), dy_ld, pdy, pdx, pdw, pdb, 0, 0)
-    ws, args = _with_workspace("rdn_linear_bwd_workspace_size", args, workspace, dev)
+    if act is not None or bias is not None:
+        ws, args = _with_workspace("rdn_linear_bwd_workspace_size", args, workspace, dev)
     _call("rdn_linear_bwd", args, dev)
     return res

@@ -173,7 +173,8 @@ def backward(M, N, K, act, bias=BF, dw_dtype=None, seed=0):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 16, 64), (5, 136, 208), (64, 1000, 64), (200, 128, 1000), (300, 16, 2048),
-                                   (2500, 264, 128), (128, 4096, 2048), (4100, 2056, 136), (3000, 2048, 2048)])
+                                   (2500, 264, 128), (128, 4096, 2048), (4100, 2056, 136), (3000, 2048, 2048),
+                                   (63, 136, 64), (512, 264, 64), (513, 264, 64)])
 def test_backward_sizes(M, N, K):
     backward(M, N, K, "silu", seed=M)
 

@@ -163,7 +163,8 @@ CASES = [
     ("rdn_linear_bwd", _linear(dx=FAKE + 16384), INVALID, "aliases"),
     ("rdn_linear_bwd", _linear(dw=FAKE + 4096), INVALID, "aliases"),
     ("rdn_linear_bwd", _linear(dw_dtype=5), UNSUPPORTED, "dw_dtype"),
-    ("rdn_linear_bwd", _linear(workspace=0), WORKSPACE, "workspace"),
+    ("rdn_linear_bwd", _linear(workspace=0, act=1, pre=FAKE), WORKSPACE, "workspace"),
+    ("rdn_linear_bwd", _linear(workspace=0, M=1000, dbias=FAKE), WORKSPACE, "workspace"),
 ]
 
 
@@ -174,9 +175,9 @@ def test_entry_points(fn, args, status, says):
 
 def test_workspace_sizes():
     lib, n = _abi.load(), ctypes.c_size_t(0)
-    # the sums of a row's CTAs (4 tiles of 64 tokens: 4), and the kept states where they are not given
-    for kept, want in ((0, 2 * 4 * 128 * 4 * 2), (FAKE, 2 * 4 * 128 * 4)):
-        assert lib.rdn_gscan_bwd_workspace_size(ctypes.byref(_gscan(h_chunks=kept)), ctypes.byref(n)) == 0
+    # the sums of the batch's rows, if several, and the kept states (4 a row) where they are not given
+    for B, kept, want in ((2, 0, 2 * 128 * 4 * (1 + 4)), (2, FAKE, 2 * 128 * 4), (1, 0, 128 * 4 * 4), (1, FAKE, 0)):
+        assert lib.rdn_gscan_bwd_workspace_size(ctypes.byref(_gscan(B=B, h_chunks=kept)), ctypes.byref(n)) == 0
         assert n.value == want
     assert lib.rdn_gscan_bwd_workspace_size(ctypes.byref(_gscan()), None) == INVALID
     assert lib.rdn_linear_bwd_workspace_size(ctypes.byref(_linear(M=100)), ctypes.byref(n)) == 0
