@@ -95,6 +95,9 @@ __device__ __forceinline__ void load_weight(const float *w, int i, int D, float 
     Raw8<float> raw;
     load8<float, kVectors>(w, i, D, true, raw);
     raw.get(v);
+  } else if (kLie == kShifted && i >= 0 && i + 8 <= D) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __ldg(w + i + e);
   } else if (i < D && i > -8) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = __ldg(w + min(max(i + e, 0), D - 1));
@@ -154,7 +157,7 @@ __device__ __forceinline__ float over_row(float a, float *sh, int lanes) {
 // R rows of a lane, NV groups of 8 elements each.  (A row of 16384 elements has 64 groups a lane of one warp, a
 // shifted one 65.)
 template <typename XT, typename FT, int NV, int R, int kLie>
-__global__ void __launch_bounds__(R > 1 ? 128 : NV == 8 ? 256 : NV == 4 ? 544 : 1024, R > 1 ? 4 : NV == 8 ? 2 : 1)
+__global__ void __launch_bounds__(R > 1 ? 128 : NV == 8 ? 256 : NV >= 3 ? 544 : 1024, R > 1 ? 4 : NV == 8 ? 2 : 1)
     norm_q8_kernel(const Q8P p) {
   __shared__ float sh[2][32];
   const int lanes = p.lanes, per = blockDim.x / lanes;  // rows of a CTA at one time, R times
@@ -280,6 +283,8 @@ cudaError_t run(const Q8P &p, Shape h, int ctas, int threads, cudaStream_t s) {
   auto kern = norm_q8_kernel<XT, FT, 1, 1, kLie>;
   if (h.nv == 2) kern = norm_q8_kernel<XT, FT, 2, 1, kLie>;
   if (h.nv == 4) kern = norm_q8_kernel<XT, FT, 4, 1, kLie>;
+  if constexpr (kLie == kShifted)
+    if (h.nv == 3) kern = norm_q8_kernel<XT, FT, 3, 1, kLie>;
   if constexpr (kLie == kVectors) {
     if (h.nv == 8) kern = norm_q8_kernel<XT, FT, 8, 1, kVectors>;
     if (h.r == 2) kern = norm_q8_kernel<XT, FT, 4, 2, kVectors>;
@@ -316,6 +321,9 @@ cudaError_t launch_norm_q8(const rdn_norm_q8_args &a, cudaStream_t s) {
   Shape h{1, 1};
   while (h.nv < (vec ? 8 : 4) && (groups > 32 * h.nv || (a.rows * groups > kSMs * 16 * h.nv && groups > h.nv)))
     h.nv *= 2;
+  // (of a shifted row of 2055 elements four groups a lane would leave three of twelve without any: 231 us, with
+  // three 203; wider rows, 17 groups and more, have few idle ones: 4097 elements 214 and 213, 8191 224 and 258)
+  if (lie == kShifted && h.nv == 4 && groups <= 16 && (groups + 2) / 3 * 3 < (groups + 3) / 4 * 4) h.nv = 3;
   p.lanes = 32 * ((groups + h.nv - 1) / h.nv);
   if (groups == 1) p.lanes = span <= 64 ? 8 : span <= 128 ? 16 : 32;
   if (vec && p.lanes <= 32 && h.nv < 8 && a.rows * p.lanes / 32 * h.nv >= kSMs * 16 * 8) h.r = 8 / h.nv;
