@@ -90,6 +90,7 @@ __global__ void __launch_bounds__(256) dp_kernel(const DpP p) {
   using P8 = Pack<__nv_bfloat16, 8>;
   __shared__ float sh[8][32 * 8 + 8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (kJoin) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   const long long n = (long long)blockIdx.x * 256 + lane * 8;
   const bool live = n < p.N;
   float sum[8];
@@ -134,6 +135,7 @@ __global__ void __launch_bounds__(256) dp_kernel(const DpP p) {
   if constexpr (kJoin) {
     __shared__ float joined[8][256];
     const uint32_t to = tc::map_rank(&joined[blockIdx.y][c], 0);
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // every CTA of the cluster runs
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(a) : "memory");
     tc::cluster_sync();
     if (blockIdx.y || at >= p.N) return;

@@ -86,6 +86,14 @@ def test_rows_between_16_bytes(n, D):
     compare(wide[:, :D], f, w)
 
 
+@pytest.mark.parametrize("dtypes", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("D", [1023, 2055])
+def test_many_odd_rows(D, dtypes):
+    """Three groups of elements a lane."""
+    compare(rows(3001, D, dtype=dtypes[0], seed=D), rows(3001, D, dtype=dtypes[1], seed=D + 1),
+            1 + 0.1 * rows(D, dtype="f32"))
+
+
 @pytest.mark.parametrize("pad", [8, 3])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strided_rows_and_axes(pad, dtype):
