@@ -10,6 +10,7 @@
 // 32768 rows of 2048 in bf16: 77 us, 6.1 TB/s.
 #include <cuda_fp8.h>
 
+#include "q8_rows.cuh"
 #include "rows.cuh"
 
 namespace rdn {
@@ -19,7 +20,8 @@ constexpr float kTop = 448.f, kFloor = 0x1p-100f;
 
 struct Q8P {
   long long rows, x_ld, f_ld;
-  int D, lanes;  // of a row: 8, 16, or a multiple of 32
+  long long inner;  // rows before the last near_end_rows(D)
+  int D, lanes;     // of a row: 8, 16, or a multiple of 32
   float eps;
   const void *x, *f;
   const float *w;
@@ -27,20 +29,6 @@ struct Q8P {
   float *scale;
 };
 
-// How a row lies: its rows on 16 bytes (kVectors); every row the same number of elements behind a group of 8 on
-// 16 bytes in all operands, as rows of an odd length one after the other are (kShifted: the groups inside the
-// row in vectors, the two at its ends, which its neighbours share, element by element); or neither.
-enum Lie { kSingle, kShifted, kVectors };
-
-// Lane t's group n of a row of D that is `off` elements behind: the row's elements i.. i + 7.
-template <int kLie>
-__device__ __forceinline__ int place(int n, int t, int lanes, int off) {
-  return (n * lanes + t) * 8 - (kLie == kShifted ? off : 0);
-}
-template <int kLie>
-__device__ __forceinline__ bool whole(int i, int D) {
-  return kLie == kVectors ? i < D : kLie == kShifted && i >= 0 && i + 8 <= D;
-}
 // 8 elements as loaded
 template <typename T>
 struct Raw8;
@@ -65,27 +53,24 @@ struct Raw8<float> {
     b = make_float4(v[4], v[5], v[6], v[7]);
   }
 };
-// (last: no row follows, so a group over the row's end is read element by element)
 template <typename T, int kLie>
-__device__ __forceinline__ void load8(const T *row, int i, int D, bool last, Raw8<T> &raw) {
+__device__ __forceinline__ void load8(const T *row, int i, int D, bool near_end, Raw8<T> &raw) {
   raw.zero();
-  if (kLie == kVectors) {
-    if (i < D) raw.load(row + i);
-  } else if (i < D && i > -8) {
-    float v[8];
-    if (kLie == kShifted && (i + 8 <= D || !last)) {
-      raw.load(row + i);
-      if (i < 0 || i + 8 > D) {
-        raw.get(v);
+  const Read how = read_of<kLie>(i, D, near_end);
+  if (how == kGroup) {
+    raw.load(row + i);
+    if (kLie == kShifted && (i < 0 || i + 8 > D)) {
+      float v[8];
+      raw.get(v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = i + e >= 0 && i + e < D ? v[e] : 0.f;
-        raw.put(v);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = i + e >= 0 && i + e < D ? to_f32<T>(row[i + e]) : 0.f;
+      for (int e = 0; e < 8; ++e) v[e] = i + e >= 0 && i + e < D ? v[e] : 0.f;
       raw.put(v);
     }
+  } else if (how == kElements) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = i + e >= 0 && i + e < D ? to_f32<T>(row[i + e]) : 0.f;
+    raw.put(v);
   }
 }
 // (the weight is on 16 bytes where all the rows are; elsewhere what is outside the row is not used)
@@ -175,7 +160,7 @@ __global__ void __launch_bounds__(R > 1 ? 128 : NV == 8 ? 256 : NV >= 3 ? 544 : 
     Raw8<FT> rf[kAhead ? R : 1][kAhead ? NV : 1];
     auto load_f = [&](int k, int n, Raw8<FT> &raw) {
       const bool live = row_of(k) < p.rows;
-      load8<FT, kLie>(f + (live ? row_of(k) * p.f_ld : 0), i_of(k, n), live ? p.D : -8, row_of(k) >= p.rows - 1, raw);
+      load8<FT, kLie>(f + (live ? row_of(k) * p.f_ld : 0), i_of(k, n), live ? p.D : -8, row_of(k) >= p.inner, raw);
     };
 #pragma unroll
     for (int k = 0; k < R; ++k) {
@@ -183,7 +168,7 @@ __global__ void __launch_bounds__(R > 1 ? 128 : NV == 8 ? 256 : NV >= 3 ? 544 : 
       const XT *row = x + (live ? row_of(k) * p.x_ld : 0);
 #pragma unroll
       for (int n = 0; n < NV; ++n)
-        load8<XT, kLie>(row, i_of(k, n), live ? p.D : -8, row_of(k) >= p.rows - 1, rx[k][n]);
+        load8<XT, kLie>(row, i_of(k, n), live ? p.D : -8, row_of(k) >= p.inner, rx[k][n]);
     }
     if (kAhead && f) {
 #pragma unroll
@@ -307,7 +292,7 @@ cudaError_t launch_norm_q8(const rdn_norm_q8_args &a, cudaStream_t s) {
   if (a.rows == 0) return cudaSuccess;
   constexpr int kSMs = 152;
   Q8P p{};
-  p.rows = a.rows; p.x_ld = a.x_ld; p.f_ld = a.f_ld; p.D = a.D; p.eps = a.eps;
+  p.rows = a.rows; p.inner = a.rows - near_end_rows(a.D); p.x_ld = a.x_ld; p.f_ld = a.f_ld; p.D = a.D; p.eps = a.eps;
   p.x = a.x; p.f = a.f; p.w = a.w; p.r = a.r_out; p.q = a.q; p.scale = a.scale;
   const size_t xe = a.x_dtype == RDN_BF16 ? 2 : 4, fe = a.f_dtype == RDN_BF16 ? 2 : 4;
   auto on = [](const void *q, size_t bytes) { return !q || (((uintptr_t)q | bytes) & 15) == 0; };
