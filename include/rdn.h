@@ -390,7 +390,7 @@ rdn_status_t rdn_bwd_workspace_size(const rdn_bwd_args *args, size_t *bytes);
  *    h_chunks, dhT, dh0, h) must be 16-byte aligned.
  *  - Outputs may not alias inputs.  Of the states this is checked: those that
  *    a call writes (stateT, dstate0; hT, h_chunks, dh0) overlap none that it
- *    reads (state0, dstateT; h0, dhT).
+ *    reads (state0, dstateT; h0, dhT).  Of rdn_linear_* all of it is.
  *  - cu_seqlens / num_seqs as in rdn_fwd_args (B = 1; empty sequences pass
  *    their states through).
  *  - Sums over tokens (parameter gradients) and over channels (dB, dC) are
@@ -641,7 +641,8 @@ rdn_status_t rdn_norm_q8(const rdn_norm_q8_args *args, rdn_stream_t stream);
  *   x [M,K], res, y [M,N] with row strides;  w [N,K] with row stride w_ld.
  *   x_scale [M], w_scale [N] fp32 (e4m3);  bias [N] or NULL;  res or NULL.
  *   pre               NULL, or [M,N] bf16, contiguous: p, for the backward.
- * Rows of x and w start on 16 bytes (pointers and strides).
+ * Rows of x and w start on 16 bytes (pointers and strides).  Results that share memory with
+ * an operand or with one another are refused; y may be res, with the same rows.
  * Backward (RDN_BF16): dy [M,N] bf16 with row stride, pre (with an activation) ->
  *     dp = dy act'(pre),   dx = dp w,   dw = dp^T x,   dbias = sum over rows of dp
  * dx [M,K] bf16 and dw [N,K] of dw_dtype (RDN_BF16 or RDN_F32), contiguous;

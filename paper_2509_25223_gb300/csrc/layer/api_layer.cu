@@ -60,6 +60,41 @@ rdn_status_t check_apart(const char *fn, const char *name, const void *out, size
     return entry_fail(RDN_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, name, in_name);
   return RDN_OK;
 }
+// Rows of an operand, in bytes: `rows` of them, `width` each, `ld` from one to the next.
+struct Bytes {
+  const char *name;
+  const void *p;
+  long long rows, ld, width;
+  bool dense() const { return rows == 1 || ld == width; }
+  long long size() const {  // (no tensor is as long as 2^60: products of the largest rows and distances pass 63 bits)
+    return rows > 1 && ld > (1ll << 60) / rows ? 1ll << 60 : (rows - 1) * ld + width;
+  }
+};
+// Whether two operands share a byte.  Slices of the columns of one wider tensor do not, though each lies between
+// the other's rows.  (Rows of two distances, both with gaps: by the ranges from their first to their last byte.)
+bool share(const Bytes &a, const Bytes &b) {
+  if (!a.p || !b.p || a.rows < 1 || b.rows < 1 || a.width < 1 || b.width < 1) return false;
+  const long long d = (long long)((uintptr_t)b.p - (uintptr_t)a.p);  // from a's first byte to b's
+  if (d >= a.size() || -d >= b.size()) return false;
+  if (a.dense() && b.dense()) return true;
+  if (b.dense()) return share(b, a);
+  if (a.dense()) {  // the last row of b that starts before a's end
+    long long k = (a.size() - 1 - d) / b.ld;
+    if (k > b.rows - 1) k = b.rows - 1;
+    return d + k * b.ld + b.width > 0;
+  }
+  if (a.ld != b.ld) return true;
+  // b's row j starts `at` behind a's row j + k
+  const long long k = d >= 0 ? d / a.ld : -((-d + a.ld - 1) / a.ld), at = d - k * a.ld;
+  return (at < a.width && k < a.rows && k > -b.rows) || (at + b.width > a.ld && k + 1 < a.rows && k + 1 > -b.rows);
+}
+// A result against what other CTAs of the call may still read, or write.
+template <size_t N>
+rdn_status_t check_alone(const char *fn, const Bytes &out, const Bytes (&others)[N]) {
+  for (const Bytes &o : others)
+    if (share(out, o)) return entry_fail(RDN_ERR_INVALID_ARG, "%s: %s aliases %s", fn, out.name, o.name);
+  return RDN_OK;
+}
 // A row stride: 0 stands for contiguous.
 rdn_status_t check_ld(const char *fn, const char *name, long long *ld, long long row) {
   if (*ld == 0) *ld = row;
@@ -392,10 +427,16 @@ rdn_status_t linear_common(const char *fn, const rdn_linear_args *args, bool bwd
     TRY(check_ptr(fn, "res", a->res, ye, false));
     TRY(check_ptr(fn, "y", a->y, ye, any));
     TRY(check_ptr16(fn, "pre", a->pre, false));
-    if (any && (a->y == a->x || a->y == a->w || (a->pre && (a->pre == a->y || a->pre == a->x || a->pre == a->res))))
-      return entry_fail(RDN_ERR_INVALID_ARG, "%s: y or pre aliases another operand", fn);
-    if (any && a->y == a->res && a->y_ld != a->res_ld)
+    const Bytes x{"x", a->x, a->M, a->x_ld * (long long)e, a->K * (long long)e};
+    const Bytes w{"w", a->w, a->N, a->w_ld * (long long)e, a->K * (long long)e};
+    const Bytes xs{"x_scale", a->x_scale, 1, 0, a->M * 4}, ws{"w_scale", a->w_scale, 1, 0, a->N * 4ll};
+    const Bytes bias{"bias", a->bias, 1, 0, a->N * (long long)be};
+    const Bytes res{"res", a->res, a->M, a->res_ld * (long long)ye, a->N * (long long)ye};
+    const Bytes y{"y", a->y, a->M, a->y_ld * (long long)ye, a->N * (long long)ye};
+    TRY(check_alone(fn, y, {x, w, xs, ws, bias}));
+    if (any && !(a->y == a->res && a->y_ld == a->res_ld) && share(y, res))
       return entry_fail(RDN_ERR_INVALID_ARG, "%s: y may be res only with the same rows", fn);
+    TRY(check_alone(fn, {"pre", a->pre, a->M, a->N * 2ll, a->N * 2ll}, {x, w, xs, ws, bias, res, y}));
     TRY(entry_injected(fn));
     return entry_cuda(fn, rdn::launch_linear_fwd(*a, s));
   }
@@ -404,9 +445,15 @@ rdn_status_t linear_common(const char *fn, const rdn_linear_args *args, bool bwd
   TRY(check_ptr16(fn, "dx", a->dx, false));
   TRY(check_ptr(fn, "dw", a->dw, dtype_size(a->dw_dtype), false));
   TRY(check_ptr(fn, "dbias", a->dbias, be, false));
-  if (any && ((a->dx && (a->dx == a->x || a->dx == a->dy || a->dx == a->pre)) || (a->dw && a->dw == a->w)))
-    return entry_fail(RDN_ERR_INVALID_ARG, "%s: dx or dw aliases an input", fn);
   TRY(check_ws(fn, a->workspace, a->workspace_bytes, rdn::linear_bwd_bytes(*a, a->dbias != nullptr)));
+  const Bytes x{"x", a->x, a->M, a->x_ld * 2, a->K * 2ll}, w{"w", a->w, a->N, a->w_ld * 2, a->K * 2ll};
+  const Bytes dy{"dy", a->dy, a->M, a->dy_ld * 2, a->N * 2ll};
+  const Bytes pre{"pre", a->act ? a->pre : nullptr, a->M, a->N * 2ll, a->N * 2ll};
+  const long long wide = a->K * (long long)dtype_size(a->dw_dtype);
+  const Bytes dx{"dx", a->dx, a->M, a->K * 2ll, a->K * 2ll}, dw{"dw", a->dw, a->N, wide, wide};
+  TRY(check_alone(fn, dx, {x, w, dy, pre}));
+  TRY(check_alone(fn, dw, {x, w, dy, pre, dx}));
+  TRY(check_alone(fn, {"dbias", a->dbias, 1, 0, a->N * (long long)be}, {x, w, dy, pre, dx, dw}));
   TRY(entry_injected(fn));
   return entry_cuda(fn, rdn::launch_linear_bwd(*a, s));
 }
