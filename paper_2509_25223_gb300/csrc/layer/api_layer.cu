@@ -367,6 +367,9 @@ rdn_status_t gscan_common(const char *fn, const rdn_gscan_args *args, bool bwd, 
     TRY(check_ptr(fn, names[k], outs[k], e, any));
     for (const void *in : ins)
       if (any && outs[k] == in) return entry_fail(RDN_ERR_INVALID_ARG, "%s: %s aliases an input", fn, names[k]);
+    for (int q = 0; q < k; ++q)
+      if (any && outs[k] == outs[q])
+        return entry_fail(RDN_ERR_INVALID_ARG, "%s: %s aliases %s", fn, names[k], names[q]);
   }
   TRY(check_apart(fn, "dh0", a->dh0, states, "dhT", a->dhT, states));
   TRY(check_apart(fn, "dh0", a->dh0, states, "h0", a->h0, states));

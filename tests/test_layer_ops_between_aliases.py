@@ -5,8 +5,8 @@ import random
 import pytest
 
 from paper_2509_25223_gb300 import _abi
-from tests.test_layer_ops_args import INVALID, _refused
-from tests.test_layer_ops_between_args import AT, LAUNCH, _linear
+from tests.test_layer_ops_args import FAKE, INVALID, _refused
+from tests.test_layer_ops_between_args import AT, LAUNCH, _gscan, _linear
 
 FAR = 1 << 40  # (clear of AT)
 
@@ -93,3 +93,12 @@ def test_far_apart_rows_of_many():
              INVALID, "y aliases x")
     _refused("rdn_linear_fwd", _linear(M=1 << 30, N=8, K=8, x=AT, x_ld=1 << 30, w=AT + 128, y=AT + 256, y_ld=1 << 30),
              LAUNCH, "injected")
+
+
+@pytest.mark.parametrize("a,b", [("dr", "dx"), ("di", "dx"), ("di", "dr")])
+def test_gradients_of_the_recurrence_over_one_another(a, b):
+    for cu in (dict(), dict(B=1, cu_seqlens=FAKE, num_seqs=3)):
+        _refused("rdn_gscan_bwd", _gscan(**{a: AT, b: AT}, **cu), INVALID, f"{a} aliases {b}")
+    _refused("rdn_gscan_bwd", _gscan(**{a: AT, b: AT}, T=0), LAUNCH, "injected")
+    # slices of one tensor's columns
+    _refused("rdn_gscan_bwd", _gscan(**{a: AT, b: AT + 256, a + "_ld": 384, b + "_ld": 384}), LAUNCH, "injected")
