@@ -657,9 +657,13 @@ rdn_status_t rdn_norm_q8(const rdn_norm_q8_args *args, rdn_stream_t stream) {
   TRY(check_ptr(fn, "r_out", a->r_out, xe, false));
   TRY(check_ptr(fn, "q", a->q, 1, any));
   TRY(check_ptr(fn, "scale", a->scale, 4, any));
-  if (any && a->r_out && (a->r_out == a->f || (a->r_out == a->x && a->x_ld != a->D)))
+  const long long fe = a->f ? (long long)dtype_size(a->f_dtype) : 1, wide = a->D * (long long)xe;
+  const Bytes x{"x", a->x, a->rows, a->x_ld * (long long)xe, wide}, f{"f", a->f, a->rows, a->f_ld * fe, a->D * fe};
+  const Bytes w{"w", a->w, 1, 0, a->D * 4ll}, r{"r_out", a->r_out, a->rows, wide, wide};
+  if (share(r, f) || (share(r, x) && !(a->r_out == a->x && a->x_ld == a->D)))
     return entry_fail(RDN_ERR_INVALID_ARG, "%s: r_out may be x only where x is contiguous, and not f", fn);
-  if (any && (a->q == a->x || a->q == a->f)) return entry_fail(RDN_ERR_INVALID_ARG, "%s: q aliases an input", fn);
+  TRY(check_alone(fn, r, {w}));
+  TRY(check_alone(fn, {"q", a->q, a->rows, a->D, a->D}, {x, f, w, r}));
   TRY(entry_injected(fn));
   return entry_cuda(fn, rdn::launch_norm_q8(*a, (cudaStream_t)stream));
 }

@@ -6,7 +6,7 @@ import pytest
 
 from paper_2509_25223_gb300 import _abi
 from tests.test_layer_ops_args import FAKE, INVALID, _refused
-from tests.test_layer_ops_between_args import AT, LAUNCH, _gscan, _linear
+from tests.test_layer_ops_between_args import AT, LAUNCH, _gscan, _linear, _q8
 
 FAR = 1 << 40  # (clear of AT)
 
@@ -102,3 +102,18 @@ def test_gradients_of_the_recurrence_over_one_another(a, b):
     _refused("rdn_gscan_bwd", _gscan(**{a: AT, b: AT}, T=0), LAUNCH, "injected")
     # slices of one tensor's columns
     _refused("rdn_gscan_bwd", _gscan(**{a: AT, b: AT + 256, a + "_ld": 384, b + "_ld": 384}), LAUNCH, "injected")
+
+
+@pytest.mark.parametrize("name,size", [("x", 768), ("f", 768), ("w", 256)])
+def test_results_of_the_norm_over_operands(name, size):
+    base = dict(x=AT, f=AT + 0x10000, w=AT + 0x20000, r_out=FAR, q=FAR + 0x10000)
+    at = base[name]
+    for out, own in (("r_out", 768), ("q", 384)):
+        for place, refused in ((at + 16, 1), (at + size - 16, 1), (at - own + 16, 1), (at + size, 0), (at - own, 0)):
+            _refused("rdn_norm_q8", _q8(**{**base, out: place}), INVALID if refused else LAUNCH,
+                     "injected" if not refused else f"{out} aliases {name}" if out == "q" or name == "w" else "r_out may be")
+    for place in (FAR, FAR + 16, FAR + 752, FAR - 368):
+        _refused("rdn_norm_q8", _q8(**{**base, "q": place}), INVALID, "q aliases r_out")
+    _refused("rdn_norm_q8", _q8(**{**base, "r_out": base["x"]}), LAUNCH, "injected")
+    # r_out in the columns beside x's
+    _refused("rdn_norm_q8", _q8(**{**base, "rows": 1, "r_out": AT + 128}), LAUNCH, "injected")
