@@ -617,7 +617,7 @@ rdn_status_t rdn_gscan_step(const rdn_gscan_step_args *args, rdn_stream_t stream
  *   x_dtype           of x and r_out;  f_dtype: of f.
  *   x, f              [rows, D] with row strides;  w [D] fp32.
  *   q [rows, D] e4m3, scale [rows] fp32, r_out [rows, D], contiguous.  r_out may be x;
- *                     r_out and q that share memory with an operand, or with one another, are refused else.
+ *                     r_out and q that share memory with x or f, or with one another, are refused else.
  * An element of h that is not finite has a NaN code; the other codes and the
  * scale of its row are unspecified.  Backward: straight through the rounding it is
  * that of the norm, rdn_norm_bwd with f = NULL, x = r_out and w_next = w. */

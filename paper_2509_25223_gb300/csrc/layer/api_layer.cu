@@ -662,7 +662,6 @@ rdn_status_t rdn_norm_q8(const rdn_norm_q8_args *args, rdn_stream_t stream) {
   const Bytes w{"w", a->w, 1, 0, a->D * 4ll}, r{"r_out", a->r_out, a->rows, wide, wide};
   if (share(r, f) || (share(r, x) && !(a->r_out == a->x && a->x_ld == a->D)))
     return entry_fail(RDN_ERR_INVALID_ARG, "%s: r_out may be x only where x is contiguous, and not f", fn);
-  TRY(check_alone(fn, r, {w}));
   TRY(check_alone(fn, {"q", a->q, a->rows, a->D, a->D}, {x, f, w, r}));
   TRY(entry_injected(fn));
   return entry_cuda(fn, rdn::launch_norm_q8(*a, (cudaStream_t)stream));

@@ -109,9 +109,11 @@ def test_results_of_the_norm_over_operands(name, size):
     base = dict(x=AT, f=AT + 0x10000, w=AT + 0x20000, r_out=FAR, q=FAR + 0x10000)
     at = base[name]
     for out, own in (("r_out", 768), ("q", 384)):
+        if (out, name) == ("r_out", "w"):
+            continue
         for place, refused in ((at + 16, 1), (at + size - 16, 1), (at - own + 16, 1), (at + size, 0), (at - own, 0)):
             _refused("rdn_norm_q8", _q8(**{**base, out: place}), INVALID if refused else LAUNCH,
-                     "injected" if not refused else f"{out} aliases {name}" if out == "q" or name == "w" else "r_out may be")
+                     "injected" if not refused else f"q aliases {name}" if out == "q" else "r_out may be")
     for place in (FAR, FAR + 16, FAR + 752, FAR - 368):
         _refused("rdn_norm_q8", _q8(**{**base, "q": place}), INVALID, "q aliases r_out")
     _refused("rdn_norm_q8", _q8(**{**base, "r_out": base["x"]}), LAUNCH, "injected")
