@@ -1148,8 +1148,8 @@ cudaError_t run_fwd_tma(const rdn_gscan_args &a, cudaStream_t s) {
     return cudaErrorInvalidValue;
   const GP p = tma_params(params(a, 2, false), a, false);
   constexpr int kBytes = sizeof(FwdTiles) + 128;  // (tiles on 128 bytes)
-  return p.cu ? go<fwd_tma_kernel<true>>(p, kBytes, "gscan_fwd", s, m)
-              : go<fwd_tma_kernel<false>>(p, kBytes, "gscan_fwd", s, m);
+  return p.cu ? go<fwd_tma_kernel<true>>(p, kBytes, "gscan_fwd_tma", s, m)
+              : go<fwd_tma_kernel<false>>(p, kBytes, "gscan_fwd_tma", s, m);
 }
 cudaError_t run_bwd_tma(const rdn_gscan_args &a, GP p, cudaStream_t s) {
   BwdMaps m{};
@@ -1160,8 +1160,8 @@ cudaError_t run_bwd_tma(const rdn_gscan_args &a, GP p, cudaStream_t s) {
     return cudaErrorInvalidValue;
   p = tma_params(p, a, true);
   constexpr int kBytes = sizeof(BwdTiles) + 128;
-  return p.cu ? go<bwd_tma_kernel<true>>(p, kBytes, "gscan_bwd", s, m)
-              : go<bwd_tma_kernel<false>>(p, kBytes, "gscan_bwd", s, m);
+  return p.cu ? go<bwd_tma_kernel<true>>(p, kBytes, "gscan_bwd_tma", s, m)
+              : go<bwd_tma_kernel<false>>(p, kBytes, "gscan_bwd_tma", s, m);
 }
 
 size_t part_bytes(const rdn_gscan_args &a) { return a.B > 1 ? round256(sizeof(float) * (size_t)a.B * a.D) : 0; }
