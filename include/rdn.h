@@ -347,11 +347,12 @@ rdn_status_t rla_fwd_workspace_size(const rdn_fwd_args *args, size_t *bytes);
 /* Device-side failures.  A kernel whose bounded wait for its own copies or
  * tensor-core work gives up (RDN_ERR_TIMEOUT), or that finds its shared
  * memory misaligned (RDN_ERR_CUDA), records the code in a per-device status
- * word, skips the rest of its work and exits, leaving the context usable;
- * the outputs of that call are then invalid.  rdn_device_status waits for
- * `stream`, returns in *status the code recorded since the previous query
- * (RDN_OK if none) and clears it.  The word is shared by all streams of the
- * device.
+ * word, skips the rest of its work (of the gated linear recurrence, where rows
+ * are addressed one by one, the rest of its waits) and exits, leaving the
+ * context usable; the outputs of that call are then invalid.
+ * rdn_device_status waits for `stream`, returns in *status the code recorded
+ * since the previous query (RDN_OK if none) and clears it.  The word is shared
+ * by all streams of the device.
  * Device state held by the library: the status word and the built-in
  * scratch of rdn_fwd_noalloc are device variables whose addresses the
  * library looks up once per device and keeps for the life of the process.
@@ -363,7 +364,8 @@ rdn_status_t rla_fwd_workspace_size(const rdn_fwd_args *args, size_t *bytes);
  * before enqueueing anything; with "device_wait" the tensor-core forward
  * scan (bf16, Dk = 128), and with "device_wait_bwd" the tensor-core
  * backward chain, makes its first bounded wait give up, records
- * RDN_ERR_TIMEOUT here and drains its work in flight. */
+ * RDN_ERR_TIMEOUT here and drains its work in flight.  The gated linear
+ * recurrence's forward and backward take the two likewise. */
 rdn_status_t rdn_device_status(rdn_stream_t stream, int *status);
 
 /* Number of Dk x Dv blocks in each of S_chunks and R_chunks:

@@ -17,6 +17,8 @@
 //     dx = g m s,  di = g b (1 - s),  w_t = a g la (h_{t-1} - a b / (1 - a^2)),
 //     dr = (1 - sigmoid(r)) w,  dlam = sigmoid(lam) / softplus(lam) sum_t w_t
 // (la b / (1 - a^2) stays finite where la -> 0: it is la s x / m, and m ~ sqrt(-2 la)).
+#include <limits.h>
+
 #include "launch.cuh"
 #include "maps.cuh"
 #include "rows.cuh"
@@ -61,6 +63,7 @@ static_assert(kKeep == kTok * kWarps && kTile == 2 * kKeep, "a tile, and its hal
 
 struct GP {
   int B, T, D, nc, strips, num_seqs, num_slots;
+  int inject;  // a test: the copies of each cluster's first CTA seem short, or it sends nothing to the others
   float c;
   long long x_ld, r_ld, i_ld, y_ld, dy_ld, dx_ld, dr_ld, di_ld;
   const void *x, *r, *i, *dy;
@@ -310,10 +313,24 @@ __device__ __forceinline__ void leave(Span (*spans)[kLanes], int warp, int lane,
   if (half == (kBack ? 1 : 0)) spans[warp][lane] = then<kPacked>(own, other);
 }
 
+// A wait that gives up (after about a second; a test's sooner) tells the status word.  The kernels by TMA then leave
+// their rounds: the bound that a round's end is compared with lies in shared memory, read behind the round's barrier
+// (an instruction a round; a flag and a branch take 1 to 3 %).  The others run their remaining rounds on what is
+// there, without exchanges.  Nothing in flight is left behind: a CTA waits for the copies that it began, and the CTAs
+// of a cluster for one another and for what they were sent.  No barrier is armed again for which a wait was given up.
+struct Lost {
+  int end[2];  // by TMA: the bound of even and odd rounds.  One that is given up is set before the round's barrier.
+  int gone;    // rows addressed one by one: no further exchange
+  int owed;    // by thread 0: 4 + 2 parity + barrier of the last exchange that it gave up
+};
+__device__ __forceinline__ uint32_t wait_limit(const GP &p) { return p.inject ? 10000000u : 2000000000u; }
+__device__ __forceinline__ void tell(const GP &p) {
+  if (p.status) atomicExch(p.status, (int)RDN_ERR_TIMEOUT);
+}
 // tc::mbar_wait_cluster that looks without acquiring until the phase is over: an acquire at cluster scope drops
 // the SM's L1 each time it looks.
-__device__ __forceinline__ bool wait_cluster(uint64_t *bar, uint32_t parity) {
-  const long long t0 = clock64();
+__device__ __forceinline__ bool wait_cluster(uint64_t *bar, uint32_t parity, uint32_t limit) {
+  const uint32_t t0 = (uint32_t)clock();
   while (true) {
     uint32_t over;
     asm volatile(
@@ -326,7 +343,7 @@ __device__ __forceinline__ bool wait_cluster(uint64_t *bar, uint32_t parity) {
         : "r"(tc::smem_u32(bar)), "r"(parity)
         : "memory");
     if (over) return tc::mbar_try_wait_cluster(bar, parity);
-    if (clock64() - t0 > 2000000000ll) return false;
+    if ((uint32_t)clock() - t0 > limit) return false;
   }
 }
 
@@ -335,15 +352,15 @@ __device__ __forceinline__ bool wait_cluster(uint64_t *bar, uint32_t parity) {
 // themselves tell the receiver's barrier: a barrier of the cluster would hold this thread
 // until its global stores of the round before are done.  (A slot is written again two rounds
 // later, by a CTA that has had this CTA's spans of the round between, sent when all its warps
-// had read the slot.)
+// had read the slot.)  on: it takes part.  Returns whether it did, and its wait did not give up.
 template <bool kBack, bool kPacked, int kN>
-__device__ __forceinline__ void exchange(const GP &p, const Span (*spans)[kN], Span (*tiles)[kN], uint64_t *bar,
-                                         uint32_t phase, int rank) {
-  if (p.nc == 1) return;
+__device__ __forceinline__ bool exchange(const GP &p, const Span (*spans)[kN], Span (*tiles)[kN], uint64_t *bars,
+                                         Lost &lost, bool on, int par, uint32_t phase, int rank) {
+  uint64_t *bar = &bars[par];
   const int lane = threadIdx.x % kN, to = threadIdx.x / kN;
   static_assert(kThreads / kN >= kCluster, "lanes for each CTA of the cluster");
-  if (threadIdx.x == 0) tc::mbar_expect_tx(bar, (uint32_t)(p.nc * kN * sizeof(Span)));
-  if (to < p.nc) {
+  if (threadIdx.x == 0 && on) tc::mbar_expect_tx(bar, (uint32_t)(p.nc * kN * sizeof(Span)));
+  if (to < p.nc && on) {
     Span all = spans[kBack ? kWarps - 1 : 0][lane];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) all = then<kPacked>(all, spans[kBack ? kWarps - 1 - w : w][lane]);
@@ -353,12 +370,24 @@ __device__ __forceinline__ void exchange(const GP &p, const Span (*spans)[kN], S
                  : "memory");
   }
   __syncwarp();
-  if (!wait_cluster(bar, phase) && p.status) atomicExch(p.status, (int)RDN_ERR_TIMEOUT);
+  if (on && !wait_cluster(bar, phase, wait_limit(p))) {
+    tell(p);
+    on = false;
+    if (threadIdx.x == 0) lost.owed = 4 + 2 * (int)phase + par;
+  }
+  return on;
+}
+// After the last barrier of the cluster: what the others sent for the exchange that was given up has come.  (What they
+// sent for one that this CTA takes no part in came while they waited for it.)
+__device__ __forceinline__ void drain_exchange(const GP &p, uint64_t *bars, const Lost &lost) {
+  if (p.nc > 1 && threadIdx.x == 0 && lost.owed)
+    wait_cluster(&bars[lost.owed & 1], (uint32_t)(lost.owed >> 1) & 1, wait_limit(p));
 }
 // Before the first exchange: the barriers are there, and every CTA of the cluster runs.
-__device__ __forceinline__ void exchange_init(const GP &p, uint64_t *bars) {
+__device__ __forceinline__ void exchange_init(const GP &p, uint64_t *bars, Lost &lost, int rank) {
   if (p.nc == 1) return;
   if (threadIdx.x == 0) {
+    lost = {{0, 0}, p.inject && rank == 0, 0};
     tc::mbar_init(&bars[0], 1);
     tc::mbar_init(&bars[1], 1);
     tc::fence_mbar_init();
@@ -433,6 +462,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
   __shared__ Span spans[2][kWarps][kLanes], tiles[2][kCluster][kLanes];
   __shared__ int2 mark[2][kPacked ? kTile : 1];
   __shared__ uint64_t bars[2];
+  __shared__ Lost lost;
   const Place<V> at(p);
   const int me = threadIdx.x;
   const uint32_t row0 = (uint32_t)at.b * (uint32_t)p.T + (uint32_t)at.token();  // (B T is at most 2^30)
@@ -441,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
   f2 carry = !kPacked && p.h0 ? ldf<V>(p.h0 + (size_t)at.b * p.D + at.ch) : both(0.f);
   pass_through<V, kPacked>(p, at, p.h0, p.hT);
 
-  exchange_init(p, bars);
+  exchange_init(p, bars, lost, at.rank);
   int par = 0, tile0 = at.rank * kTile;
   uint32_t phase = 0;
   Inside inside;
@@ -489,7 +519,8 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
     const Span other = from_other_half(all);
     leave<false, kPacked>(spans[par], at.warp, at.lane, at.half, all, other);
     __syncthreads();
-    exchange<false, kPacked>(p, spans[par], tiles[par], &bars[par], phase, at.rank);
+    if (p.nc > 1 && !exchange<false, kPacked>(p, spans[par], tiles[par], bars, lost, !lost.gone, par, phase, at.rank))
+      lost.gone = 1;
     f2 in = fold<false, kPacked>(spans[par], tiles[par], at.lane, at.rank, p.nc, at.warp, carry);
     if (p.chunks && at.live && at.token() % kKeep == 0 && left > 0)
       stf<V>(p.chunks + ((size_t)at.b * nkept + (tile0 + at.token()) / kKeep) * p.D + at.ch, in);
@@ -520,6 +551,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
     __syncwarp();
   }
   if (p.nc > 1) tc::cluster_sync();  // (what this CTA sent has arrived)
+  drain_exchange(p, bars, lost);
 }
 
 // ---- forward for bf16 rows on 16 bytes: tiles by TMA.  As fwd_kernel, but a warp takes kTok tokens of 64
@@ -560,10 +592,11 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
   __shared__ Span spans[2][kWarps][32], tiles[2][kCluster][32];
   __shared__ int2 mark[2][kPacked ? kTileTma : 1];
   __shared__ uint64_t bars[2], full[2];
+  __shared__ Lost lost;
   const WidePlace at(p);
   const int round = p.nc * kTileTma, nkept = (p.T + kKeep - 1) / kKeep;
   auto fetch = [&](int t, int s) {  // by one thread
-    tc::mbar_expect_tx(&full[s], (uint32_t)sizeof(sm.in[s]));
+    tc::mbar_expect_tx(&full[s], (uint32_t)sizeof(sm.in[s]) + (p.inject && at.rank == 0 ? 16 : 0));
     tc::tma_load_3d(sm.in[s][0], &maps.r, at.strip, t, at.b, &full[s]);
     tc::tma_load_3d(sm.in[s][1], &maps.i, at.strip, t, at.b, &full[s]);
     tc::tma_load_3d(sm.in[s][2], &maps.x, at.strip, t, at.b, &full[s]);
@@ -574,6 +607,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
     tc::mbar_init(&full[1], 1);
     tc::mbar_init(&bars[0], 1);
     tc::mbar_init(&bars[1], 1);
+    lost = {{p.T, p.T}, 0, 0};
     tc::fence_mbar_init();
     for (int s = 0; s < 2; ++s)
       if (s * round < p.T) fetch(tile0 + s * round, s);
@@ -587,7 +621,8 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
   int par = 0;  // also the stage
   uint32_t phase = 0;
   Inside inside;
-  for (int base = 0; base < p.T; base += round, tile0 += round, phase ^= par, par ^= 1) {
+  int base = 0, end;
+  do {
     const int first = at.warp * kTok, left = p.T - tile0 - first;
     if (kPacked) inside.move(p, tile0);
     const bool marked = kPacked && !inside.plain(tile0, kTileTma);
@@ -595,7 +630,10 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
       mark_tile<kTileTma>(p, tile0, mark[par]);
       __syncthreads();
     }
-    if (!tc::mbar_wait(&full[par], phase) && p.status) atomicExch(p.status, (int)RDN_ERR_TIMEOUT);
+    if (!tc::mbar_wait(&full[par], phase, wait_limit(p))) {
+      tell(p);
+      lost.end[par] = 0;
+    }
     // (tokens past the row's end are zeros, which nothing that is kept follows)
     Span all = {both(1.f), both(0.f)}, kept[kTok];
 #pragma unroll
@@ -616,9 +654,11 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
     }
     spans[par][at.warp][at.lane] = all;
     __syncthreads();
-    if (threadIdx.x == 0 && base + 2 * round < p.T) fetch(tile0 + 2 * round, par);  // the stage has been read
+    end = lost.end[par];
+    if (threadIdx.x == 0 && base + 2 * round < end) fetch(tile0 + 2 * round, par);  // the stage has been read
     __syncwarp();
-    exchange<false, kPacked>(p, spans[par], tiles[par], &bars[par], phase, at.rank);
+    if (p.nc > 1 && !exchange<false, kPacked>(p, spans[par], tiles[par], bars, lost, true, par, phase, at.rank))
+      lost.end[par ^ 1] = 0;
     const f2 in = fold<false, kPacked>(spans[par], tiles[par], at.lane, at.rank, p.nc, at.warp, carry);
     if (p.chunks && at.live && at.warp == 0 && tile0 < p.T)
       stf<2>(p.chunks + ((size_t)at.b * nkept + tile0 / kKeep) * p.D + at.ch, in);
@@ -651,10 +691,19 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_tma_kernel(const GP p,
       }
     }
     __syncwarp();
-  }
+    base += round;
+    tile0 += round;
+    phase ^= par;
+    par ^= 1;
+  } while (base < end);
   if (at.lane == 0) tc::bulk_wait_all();
+  if (threadIdx.x == 0) {  // the last round's copies and, where the rounds were left, the next one's have come
+    tc::mbar_wait(&full[par ^ 1], phase ^ (uint32_t)(par ^ 1), wait_limit(p));
+    if (base < p.T) tc::mbar_wait(&full[par], phase, wait_limit(p));
+  }
   __syncwarp();
   if (p.nc > 1) tc::cluster_sync();  // (what this CTA sent has arrived)
+  drain_exchange(p, bars, lost);
 }
 
 // dlam = sigmoid(lam) / softplus(lam) times the sum of w, here of w / ln 2.
@@ -706,6 +755,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
   __shared__ int2 mark[2][kPacked ? kTile : 1];
   __shared__ f2 joined[kCluster][kLanes];
   __shared__ uint64_t bars[2];
+  __shared__ Lost lost;
   const Place<V> at(p);
   const int me = threadIdx.x;
   const uint32_t row0 = (uint32_t)at.b * (uint32_t)p.T + (uint32_t)at.token();  // (B T is at most 2^30)
@@ -715,7 +765,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
   f2 sum = both(0.f);
   pass_through<V, kPacked>(p, at, p.dhT, p.dh0);
 
-  exchange_init(p, bars);
+  exchange_init(p, bars, lost, at.rank);
   int par = 0;
   uint32_t phase = 0;
   Inside inside;
@@ -785,7 +835,8 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
     leave<false, kPacked>(fspans[par], at.warp, at.lane, at.half, fwd, fother);
     leave<true, kPacked>(spans[par], at.warp, at.lane, at.half, back, other);
     __syncthreads();
-    exchange<true, kPacked>(p, spans[par], tiles[par], &bars[par], phase, at.rank);
+    if (p.nc > 1 && !exchange<true, kPacked>(p, spans[par], tiles[par], bars, lost, !lost.gone, par, phase, at.rank))
+      lost.gone = 1;
     f2 q = fold<true, kPacked>(spans[par], tiles[par], at.lane, at.rank, p.nc, at.warp, carry);
     for (int w = 0; w < at.warp; ++w) h = over<kPacked>(fspans[par][w][at.lane], h);
     if (at.half) h = over<kPacked>(fother, h);
@@ -841,6 +892,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
     for (int w = 1; w < 2 * kWarps; ++w) sum = add2(sum, kept.u[0][w * kLanes + at.lane]);
   }
   leave_sum<V, kLanes>(p, at, lead, sum, joined);
+  drain_exchange(p, bars, lost);
 }
 
 // ---- backward for bf16 rows on 16 bytes: tiles by TMA, as fwd_tma_kernel.  The results take the inputs'
@@ -861,11 +913,12 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
   __shared__ int2 mark[2][kPacked ? kTileTma : 1];
   __shared__ f2 joined[kCluster][32];
   __shared__ uint64_t bars[2], full[2];
+  __shared__ Lost lost;
   const WidePlace at(p);
   const int me = threadIdx.x, first = at.warp * kTok;
   const int round = p.nc * kTileTma, nkept = (p.T + kKeep - 1) / kKeep;
   auto fetch = [&](int t, int s) {  // by one thread
-    tc::mbar_expect_tx(&full[s], (uint32_t)sizeof(sm.in[s]));
+    tc::mbar_expect_tx(&full[s], (uint32_t)sizeof(sm.in[s]) + (p.inject && at.rank == 0 ? 16 : 0));
     tc::tma_load_3d(sm.in[s][0], &maps.r, at.strip, t, at.b, &full[s]);
     tc::tma_load_3d(sm.in[s][1], &maps.i, at.strip, t, at.b, &full[s]);
     tc::tma_load_3d(sm.in[s][2], &maps.x, at.strip, t, at.b, &full[s]);
@@ -878,6 +931,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
     tc::mbar_init(&full[1], 1);
     tc::mbar_init(&bars[0], 1);
     tc::mbar_init(&bars[1], 1);
+    lost = {{0, 0}, 0, 0};
     tc::fence_mbar_init();
     fetch(tile0, 0);
   }
@@ -891,7 +945,8 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
   int par = 0;  // also the stage
   uint32_t phase = 0;
   Inside inside;
-  for (int base = last; base >= 0; base -= round, tile0 -= round, phase ^= par, par ^= 1) {
+  int base = last, end;
+  do {
     const int left = p.T - tile0 - first;
     f2 h = tile0 < p.T ? ldf<2>(p.chunks + ((size_t)at.b * nkept + tile0 / kKeep) * p.D + at.ch) : both(0.f);
     if (kPacked) inside.move(p, tile0);
@@ -900,7 +955,10 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
       mark_tile<kTileTma>(p, tile0, mark[par]);
       __syncthreads();
     }
-    if (!tc::mbar_wait(&full[par], phase) && p.status) atomicExch(p.status, (int)RDN_ERR_TIMEOUT);
+    if (!tc::mbar_wait(&full[par], phase, wait_limit(p))) {
+      tell(p);
+      lost.end[par] = INT_MAX;
+    }
     auto cell = [&](int which, int j) { return &sm.in[par][which][first + j][at.lane * 2]; };
     auto word = [&](int which, int j) -> uint32_t & { return *reinterpret_cast<uint32_t *>(cell(which, j)); };
     // this thread's span from a zero state, both ways
@@ -938,9 +996,11 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
     spans[par][at.warp][at.lane] = back;
     if (at.lane == 0) tc::bulk_wait_read();  // the round before has left the other stage
     __syncthreads();
+    end = lost.end[par];
     if (threadIdx.x == 0 && base >= round) fetch(tile0 - round, par ^ 1);
     __syncwarp();
-    exchange<true, kPacked>(p, spans[par], tiles[par], &bars[par], phase, at.rank);
+    if (p.nc > 1 && !exchange<true, kPacked>(p, spans[par], tiles[par], bars, lost, true, par, phase, at.rank))
+      lost.end[par ^ 1] = INT_MAX;
     f2 q = fold<true, kPacked>(spans[par], tiles[par], at.lane, at.rank, p.nc, at.warp, carry);
 #pragma unroll 1
     for (int w = 0; w < at.warp; ++w) h = over<kPacked>(fspans[par][w][at.lane], h);
@@ -979,8 +1039,16 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
     }
     if (!kPacked && p.dh0 && at.live && tile0 + first == 0) stf<2>(p.dh0 + (size_t)at.b * p.D + at.ch, q);
     __syncwarp();
-  }
+    base -= round;
+    tile0 -= round;
+    phase ^= par;
+    par ^= 1;
+  } while (base >= end);
   if (at.lane == 0) tc::bulk_wait_all();
+  if (threadIdx.x == 0) {  // the last round's copies and, where the rounds were left, the next one's have come
+    tc::mbar_wait(&full[par ^ 1], phase ^ (uint32_t)(par ^ 1), wait_limit(p));
+    if (base >= 0) tc::mbar_wait(&full[par], phase, wait_limit(p));
+  }
   // sum of w over this CTA's tokens, the warps in order
   __syncthreads();
   sm.si[0][me] = sum;
@@ -991,6 +1059,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_tma_kernel(const GP p,
     for (int w = 1; w < kWarps; ++w) sum = add2(sum, sm.si[0][w * 32 + at.lane]);
   }
   leave_sum<2, 32>(p, at, lead, sum, joined);
+  drain_exchange(p, bars, lost);
 }
 
 // dlam from the sums of the batch's rows, in order: 16 interleaved sums, joined in order.
@@ -1057,6 +1126,7 @@ GP params(const rdn_gscan_args &a, int V, bool bwd) {
   p.y = a.y; p.dx = a.dx; p.dr = a.dr; p.di = a.di;
   p.hT = a.hT; p.chunks = a.h_chunks; p.dh0 = a.dh0;
   p.status = status_word();
+  p.inject = fault_injection() == (bwd ? 4 : 3);
   return p;
 }
 

@@ -18,6 +18,8 @@ int *status_word();
 // skip one MMA completion signal, so that its bounded wait gives up
 // (RDN_ERR_TIMEOUT in the status word) and the kernel drains and exits;
 // "device_wait_bwd" (4) does the same in the tensor-core backward chain.
+// The gated linear recurrence takes both likewise (forward, backward): the
+// first wait in each strip's first CTA runs out.
 // 0 when unset or unrecognised.  Defined in api.cu.
 int fault_injection();
 }  // namespace rdn
