@@ -17,6 +17,7 @@
 //     dx = g m s,  di = g b (1 - s),  w_t = a g la (h_{t-1} - a b / (1 - a^2)),
 //     dr = (1 - sigmoid(r)) w,  dlam = sigmoid(lam) / softplus(lam) sum_t w_t
 // (la b / (1 - a^2) stays finite where la -> 0: it is la s x / m, and m ~ sqrt(-2 la)).
+#include <float.h>
 #include <limits.h>
 
 #include "launch.cuh"
@@ -201,7 +202,9 @@ __device__ __forceinline__ Gate gate(f2 r, f2 i, f2 k) {
 constexpr float kLn2 = 0.69314718f;
 template <int V>
 __device__ __forceinline__ f2 rate(const GP &p, int ch) {  // -c softplus(lam) log2(e)
-  const f2 k = mul2(pack2(softplusf(p.lam[ch]), V == 2 ? softplusf(p.lam[ch + V - 1]) : 0.f), both(-p.c * kLog2e));
+  // (finite factors: a softplus of 0 times the largest c is 0 too)
+  const float c = fmaxf(-p.c * kLog2e, -FLT_MAX);
+  const f2 k = mul2(pack2(softplusf(p.lam[ch]), V == 2 ? softplusf(p.lam[ch + V - 1]) : 0.f), both(c));
   return each(k, [](float v) { return max_nan(v, -1e30f); });  // (finite: a closed gate's 0 times it is 0)
 }
 
