@@ -630,7 +630,7 @@ def add_norm_q8(x, f=None, weight=None, eps=1e-6, out=None):
         scale = max|h| / 448,  q = h / scale rounded to float8_e4m3fn
     x, f [..., D] (bf16 or fp32, each its own); weight [D] fp32.  Returns
     (r, q, scale): r in x's type, scale [...] fp32; q and scale are the first
-    operand of linear_fwd.  out: (r, q, scale) to write into; r may be x.
+    operand of linear_fwd.  out: (r, q, scale) to write into, each a tensor or None; r may be x.
     Backward (straight through the rounding): block_norm_bwd(x=r,
     weight_next=weight, dr=dr, dh=dh)["dx"] is the gradient of x and of f."""
     dev, shape, ty = x.get_device(), x.shape, x.dtype
@@ -653,7 +653,7 @@ def add_norm_q8(x, f=None, weight=None, eps=1e-6, out=None):
         pq, ps = q.data_ptr(), s.data_ptr()
     else:
         r, q, s = out
-        if f is None:
+        if f is None and (r is None or r is x):
             r = x
         else:
             r = torch.empty(shape, dtype=ty, device=dev) if r is None else r
