@@ -768,6 +768,8 @@ def linear_bwd(x, w, dy, pre=None, act=None, bias=None, need_dx=True, need_dw=Tr
         res.pop("dw", None)
     if bias is not None:
         bt = _code(bias.dtype)
+        if bias.shape != (n,) or bias.get_device() != dev:
+            _bad("bias", bias, (n,), bias.dtype, dev)
         if res.get("dbias") is None:
             res["dbias"] = torch.empty(n, dtype=bias.dtype, device=dev)
         pdb = _whole("dbias", res["dbias"], (n,), bias.dtype, dev)
