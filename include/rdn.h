@@ -365,7 +365,8 @@ rdn_status_t rla_fwd_workspace_size(const rdn_fwd_args *args, size_t *bytes);
  * scan (bf16, Dk = 128), and with "device_wait_bwd" the tensor-core
  * backward chain, makes its first bounded wait give up, records
  * RDN_ERR_TIMEOUT here and drains its work in flight.  The gated linear
- * recurrence's forward and backward take the two likewise. */
+ * recurrence's and the matrix product's forward and backward take the two
+ * likewise. */
 rdn_status_t rdn_device_status(rdn_stream_t stream, int *status);
 
 /* Number of Dk x Dv blocks in each of S_chunks and R_chunks:

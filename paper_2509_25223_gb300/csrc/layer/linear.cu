@@ -204,6 +204,7 @@ cudaError_t launch_linear_fwd(const rdn_linear_args &a, cudaStream_t s) {
   p.e.pre = static_cast<__nv_bfloat16 *>(a.pre);
   p.e.res_ld = a.res_ld; p.e.y_ld = a.y_ld; p.e.pre_ld = a.N;
   p.e.act = a.act; p.e.bias_f32 = a.bias_dtype == RDN_F32; p.e.out_f32 = a.y_dtype == RDN_F32;
+  p.inject = fault_injection() == 3;
   return lin::run_product({a.x, a.M, a.K, a.x_ld, false}, {a.w, a.N, a.K, a.w_ld, false}, p, a.dtype == RDN_E4M3, s);
 }
 
@@ -224,6 +225,7 @@ cudaError_t launch_linear_bwd(const rdn_linear_args &a, cudaStream_t s) {
   d.part = a.dbias && !join ? reinterpret_cast<float *>(static_cast<char *>(a.workspace) + lin::dp_bytes(a)) : nullptr;
   d.dbias = a.dbias;
   d.bias_f32 = be == 4;
+  const int inject = fault_injection() == 4;
   const void *dp = a.dy;
   long long dp_ld = a.dy_ld;
   if ((a.act && d.dp) || a.dbias) {
@@ -242,6 +244,7 @@ cudaError_t launch_linear_bwd(const rdn_linear_args &a, cudaStream_t s) {
   if (a.dx) {
     lin::GemmP p{};
     p.M = a.M; p.N = a.K;
+    p.inject = inject;
     p.e.y = a.dx; p.e.y_ld = a.K;
     e = lin::run_product({dp, a.M, a.N, dp_ld, false}, {a.w, a.K, a.N, a.w_ld, true}, p, false, s);
     if (e != cudaSuccess) return e;
@@ -249,6 +252,7 @@ cudaError_t launch_linear_bwd(const rdn_linear_args &a, cudaStream_t s) {
   if (a.dw) {
     lin::GemmP p{};
     p.M = a.N; p.N = a.K;
+    p.inject = inject;
     p.e.y = a.dw; p.e.y_ld = a.K; p.e.out_f32 = we == 4;
     e = lin::run_product({dp, a.N, a.M, dp_ld, true}, {a.x, a.K, a.M, a.x_ld, true}, p, false, s);
   }

@@ -34,7 +34,10 @@ struct GemmP {
   int kblocks, tiles_m, tiles_n, splits;
   Epilogue e;
   int *status;
+  int inject;  // a test: the first tile's sums are not signalled
 };
+// A wait gives up after about a second, in a test sooner.
+__device__ __forceinline__ long long wait_limit(const GemmP &p) { return p.inject ? 10000000ll : 2000000000ll; }
 
 struct alignas(64) Map { unsigned char b[128]; };
 struct Maps { Map a, b; };
@@ -119,14 +122,14 @@ __host__ __device__ constexpr uint32_t idesc_of(int M, int N, bool a_mn, bool b_
   return (1u << 4) | (kFp8 ? 0u : (1u << 7) | (1u << 10)) | (a_mn ? tc::kAMajorMN : 0u) | (b_mn ? tc::kBMajorMN : 0u) |
          ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
-// Arrives on `bar` (of both CTAs of a pair) once this thread's products so far are done.
-template <bool kPair>
+// Arrives on `bar` (of a pair: of the CTAs in kTo) once this thread's products so far are done.
+template <bool kPair, int kTo = 3>
 __device__ __forceinline__ void commit(uint64_t *bar) {
   if constexpr (kPair)
     asm volatile(
         "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
             tc::smem_u32(bar)),
-        "h"((uint16_t)3)
+        "h"((uint16_t)kTo)
         : "memory");
   else
     tc::mma_commit(bar);

@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   using S = Smem<kBN>;
   constexpr int kStages = S::kStages, kTmem = kBN < 32 ? 32 : kBN;
   extern __shared__ unsigned char raw[];
-  __shared__ uint64_t full[kStages], empty[kStages], done;
+  __shared__ uint64_t full[kStages], empty[kStages], done, drained;
   __shared__ uint32_t slot;
   __shared__ int dead_;
   unsigned char *tiles = raw + ((1024 - (tc::smem_u32(raw) & 1023)) & 1023);
@@ -98,6 +98,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       tc::mbar_init(&empty[s], 1);
     }
     tc::mbar_init(&done, 1);
+    tc::mbar_init(&drained, 1);
     dead_ = 0;
     tc::fence_mbar_init();
     for (int n = 0; n < min(count, kStages); ++n) copy(n);  // ahead of everything else
@@ -109,6 +110,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   tc::fence_after_sync();
   const uint32_t tmem = slot;
   volatile int *dead = &dead_;
+  const long long limit = wait_limit(p);
   auto fail = [&] {
     *dead = 1;
     if (p.status) atomicExch(p.status, (int)RDN_ERR_TIMEOUT);
@@ -118,12 +120,12 @@ __global__ void __launch_bounds__(kThreads, 2)
     if (lane == 0) {
       int n = min(count, kStages);
       for (; n < count; ++n) {
-        if (!tc::mbar_wait(&empty[n % kStages], (uint32_t)(n / kStages + 1) & 1)) fail();
+        if (!tc::mbar_wait(&empty[n % kStages], (uint32_t)(n / kStages + 1) & 1, limit)) fail();
         if (*dead) break;
         copy(n);
       }
       for (int c = n > kStages ? n - kStages : 0; c < n; ++c)  // every copy has landed
-        if (!tc::mbar_wait(&full[c % kStages], (uint32_t)(c / kStages) & 1)) fail();
+        if (!tc::mbar_wait(&full[c % kStages], (uint32_t)(c / kStages) & 1, limit)) fail();
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -131,7 +133,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       constexpr uint32_t idesc = idesc_of<kFp8>(128, kBN, kAmn, kBmn);
       for (int n = 0; n < count; ++n) {
         const int s = n % kStages;
-        if (!tc::mbar_wait(&full[s], (uint32_t)(n / kStages) & 1)) fail();
+        if (!tc::mbar_wait(&full[s], (uint32_t)(n / kStages) & 1, limit)) fail();
         if (*dead) break;
         tc::fence_after_sync();
         const uint32_t at = tc::smem_u32(tiles + s * S::kStage);
@@ -141,8 +143,12 @@ __global__ void __launch_bounds__(kThreads, 2)
           mma_step<false, kFp8>(tmem, da + tile_step<kAmn>(j), db + tile_step<kBmn>(j), idesc, n + j > 0);
         tc::mma_commit(&empty[s]);
       }
-      tc::mma_commit(&done);
-      if (!tc::mbar_wait(&done, 0)) fail();
+      if (!p.inject) tc::mma_commit(&done);
+      if (!tc::mbar_wait(&done, 0, limit)) {
+        fail();
+        tc::mma_commit(&drained);  // (the products are done all the same, or never)
+        tc::mbar_wait(&drained, 0, limit);
+      }
     }
     __syncwarp();
   }

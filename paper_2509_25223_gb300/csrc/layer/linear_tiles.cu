@@ -266,6 +266,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const uint32_t tmem = b.tmem;
   volatile int *dead = &b.dead;
   const uint32_t full0 = tc::map_rank(&b.full[0], 0);
+  const long long limit = wait_limit(p);
   // A wait that gives up ends every role of the CTA at its next wait.
   auto fail = [&] {
     *dead = 1;
@@ -281,7 +282,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         tile_at(p, t, tm, tn);
         const int ra = tm * 256 + (int)rank * 128, rb = tn * kBN + (int)rank * (kBN / 2);
         for (int kb = 0; kb < p.kblocks; ++kb, at.next(), ++n) {
-          if (!tc::mbar_wait(&b.empty[at.s], at.phase ^ 1)) fail();
+          if (!tc::mbar_wait(&b.empty[at.s], at.phase ^ 1, limit)) fail();
           if (*dead) break;
           unsigned char *to = tiles + at.s * S::kStage;
           // both CTAs' copies complete on the first one's barrier
@@ -293,7 +294,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
       if (rank == 0)  // every copy has landed
         for (long long q = n > kStages ? n - kStages : 0; q < n; ++q)
-          if (!tc::mbar_wait(&b.full[q % kStages], (uint32_t)(q / kStages) & 1)) fail();
+          if (!tc::mbar_wait(&b.full[q % kStages], (uint32_t)(q / kStages) & 1, limit)) fail();
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -304,11 +305,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       int it = 0;
       for (int t = pair; t < ntiles && !*dead; t += pairs, ++it) {
         const int acc = it & 1;
-        if (!tc::mbar_wait_cluster(&b.taken[acc], (uint32_t)(it / 2 + 1) & 1, 2000000000ll)) fail();
+        if (!tc::mbar_wait_cluster(&b.taken[acc], (uint32_t)(it / 2 + 1) & 1, limit)) fail();
         if (*dead) break;
         tc::fence_after_sync();
         for (int kb = 0; kb < p.kblocks; ++kb, at.next()) {
-          if (!tc::mbar_wait(&b.full[at.s], at.phase)) {
+          if (!tc::mbar_wait(&b.full[at.s], at.phase, limit)) {
             fail();
             break;
           }
@@ -320,12 +321,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                                  kb + j > 0);
           commit<true>(&b.empty[at.s]);
         }
-        if (!*dead) commit<true>(&b.done[acc]);
+        if (!*dead && !(p.inject && it == 0)) commit<true>(&b.done[acc]);
       }
-      if (*dead) {
-        commit<true>(&b.drained);
-        tc::mbar_wait(&b.drained, 0);
-      }
+      // every product is done, whatever the others have given up meanwhile
+      commit<true, 1>(&b.drained);
+      if (!tc::mbar_wait(&b.drained, 0, limit)) fail();
     }
     __syncwarp();
   } else {
@@ -353,7 +353,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         rb.load(static_cast<const __nv_bfloat16 *>(p.e.res) + m * p.e.res_ld + n0, have, res_access);
       __syncwarp();
       bool ok = !*dead;
-      if (ok && !tc::mbar_wait(&b.done[acc], (uint32_t)(it / 2) & 1)) {
+      if (ok && !tc::mbar_wait(&b.done[acc], (uint32_t)(it / 2) & 1, limit)) {
         fail();
         ok = false;
       }

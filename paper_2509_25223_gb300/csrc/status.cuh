@@ -19,7 +19,8 @@ int *status_word();
 // (RDN_ERR_TIMEOUT in the status word) and the kernel drains and exits;
 // "device_wait_bwd" (4) does the same in the tensor-core backward chain.
 // The gated linear recurrence takes both likewise (forward, backward): the
-// first wait in each strip's first CTA runs out.
+// first wait on each strip's first CTA runs out; and the matrix products: the
+// first tile's sums are not signalled.
 // 0 when unset or unrecognised.  Defined in api.cu.
 int fault_injection();
 }  // namespace rdn
