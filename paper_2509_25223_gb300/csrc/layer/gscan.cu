@@ -561,7 +561,7 @@ __global__ void __launch_bounds__(kThreads, kFwdCtas) fwd_kernel(const GP p) {
 // channels, so that a tile is 64 tokens of 128 bytes, and the tiles come to shared memory a round ahead
 // (and go from there) as whole boxes: no addresses are worked out per row, which are a quarter of
 // fwd_kernel's instructions, and the spans of a thread's tokens stay in its registers.
-// 8 x 4096 tokens of 2048 channels: 129 us, 4.2 TB/s, 35 warp instructions for 32 elements (five of them special
+// 8 x 4096 tokens of 2048 channels: 129 us, 4.2 TB/s, 36 warp instructions for 32 elements (five of them special
 // functions); bound by issue and by the units' number (256 on 152 SMs leave 16 % of them idle).
 constexpr int kWide = 64, kTileTma = kKeep;  // channels and tokens of a box
 constexpr int kTmaUnits = 36;
@@ -900,7 +900,7 @@ __global__ void __launch_bounds__(kThreads, kBwdCtas) bwd_kernel(const GP p) {
 
 // ---- backward for bf16 rows on 16 bytes: tiles by TMA, as fwd_tma_kernel.  The results take the inputs'
 // places in the stage, from where they are copied out while the next round runs on the other.
-// 8 x 4096 tokens of 2048 channels: 228 us, 4.1 TB/s, 66 warp instructions for 32 elements; bound as the forward.
+// 8 x 4096 tokens of 2048 channels: 232 us, 4.0 TB/s, 67 warp instructions for 32 elements; bound as the forward.
 struct BwdMaps { TileMap x, r, i, dy, dx, dr, di; };
 struct BwdTiles {
   __nv_bfloat16 in[2][4][kTileTma][kWide];  // r, i, x, dy; then dr, di, dx
