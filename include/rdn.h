@@ -623,7 +623,8 @@ rdn_status_t rdn_gscan_step(const rdn_gscan_step_args *args, rdn_stream_t stream
  *                     r_out and q that share memory with x or f, or with one another, are refused else.
  * An element of h that is not finite has a NaN code; the other codes and the
  * scale of its row are unspecified.  The sum of a row's squares is fp32: of rows
- * whose sum passes 2^128 (elements near 1e19) the norm makes zeros.  Backward: straight through the rounding it is
+ * whose sum passes 2^128 (elements near 1e19) the norm makes zeros, and with
+ * eps = 0 of rows whose sum is below 2^-126 infinities.  Backward: straight through the rounding it is
  * that of the norm, rdn_norm_bwd with f = NULL, x = r_out and w_next = w. */
 typedef struct {
   long long rows;
